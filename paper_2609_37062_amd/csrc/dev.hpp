@@ -48,8 +48,12 @@ __device__ __forceinline__ f32x4 mfma_16x16x32(u32x4 a, u32x4 b, f32x4 c) {
 // this XCD's L2, so a workgroup on another XCD of the same launch reads it
 // once this wave's memory counter has drained.  Plain stores are only made
 // visible to other XCDs at the end of the kernel.
+// A store of more than 8 bytes takes its last registers one cycle late, and
+// the compiler, which keeps that cycle free behind its own stores, does not
+// look into an asm block: without the s_nop the next instruction overwrote the
+// fourth word in some lanes (seen as a wrong partial of one query head).
 __device__ __forceinline__ void store_wt(void* p, u32x4 v) {
-  asm volatile("global_store_dwordx4 %0, %1, off sc1" : : "v"(p), "v"(v) : "memory");
+  asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" : : "v"(p), "v"(v) : "memory");
 }
 __device__ __forceinline__ void store_wt(void* p, u32x2 v) {
   asm volatile("global_store_dwordx2 %0, %1, off sc1" : : "v"(p), "v"(v) : "memory");
