@@ -111,7 +111,8 @@ int vsk_weights_pack_head(vsk_handle* h, const void* embed_dev, const void* lm_h
  * The pool holds n_blocks blocks of 16 tokens for every layer, K and V.
  * Its internal layout is private to the library; use vsk_kv_write /
  * vsk_kv_read to move logical [n][n_kv_heads][head_dim] bf16 values.
- * Position p of a sequence lives at slot table[p/16]*16 + p%16. */
+ * Position p of a sequence lives at slot table[p/16]*16 + p%16 (after an
+ * eviction, its p-th cached token). */
 size_t vsk_kv_pool_bytes(const vsk_model_cfg* cfg, int32_t n_blocks);
 /* Bind a pool of n_blocks blocks.  pool_dev may be NULL, in which case only
  * the host allocator exists (device calls that need the pool return
@@ -152,7 +153,8 @@ int vsk_kv_read(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_t 
  * (Invariant 2).  For sequences seqs[0..n) with q_lens new rows each (the
  * rows are the last q_len resident positions, already reserved):
  *   block_table [n][max_blocks] int32 (unused entries -1)
- *   kv_len [n], cu_q [n+1], and per row r: row_seq[r], pos[r], slot[r].
+ *   kv_len [n], cu_q [n+1], and per row r: row_seq[r], pos[r] (its rotary
+ *   position: its place in the cache, and the tokens evicted before), slot[r].
  * Rows are numbered sequence by sequence.  vsk_batch_build validates and
  * keeps the host copy in the handle; vsk_batch_host_* reads it back. */
 int vsk_batch_build(vsk_handle* h, const int64_t* seqs_host, const int32_t* q_lens_host,
@@ -248,6 +250,68 @@ int vsk_prefill_chunk(vsk_handle* h, const int32_t* ids_dev, const int32_t* logi
  * size or an unknown dtype. */
 int vsk_argmax_sample(const void* logits_dev, int32_t dtype, int32_t rows, int32_t vocab,
                       int32_t* ids_dev, int32_t* no_value_dev, void* stream);
+
+/* ----------------------------------------------------------------- bounded cache
+ * Long-running sequences: attention over a part of the cache, what each cached
+ * token is worth, and shorter caches.
+ *
+ * A row at index p of its sequence's cache sees keys 0..p; with a window > 0
+ * only keys p - window + 1 .. p, and keys 0 .. sinks - 1, which stay visible
+ * (0 <= sinks; without a window it has no meaning).  Its attention weight of
+ * key t for query head h is w = exp(q_h . k_t / sqrt(head_dim)) over the sum
+ * of that over the keys it sees; its output is sum w v_t.  What a row does not
+ * see does not matter, NaN and infinities included; a value of a visible key
+ * that is not finite makes the outputs that it enters not finite. */
+
+/* Attention of the uploaded batch's rows (any q_lens) over one layer's cache,
+ * for queries of the caller's: q_dev bf16 [n_rows][n_q_heads][head_dim], after
+ * rotary; every row's own K, V in the cache already (vsk_kv_write or a pass).
+ * o_dev bf16 of the same shape.  mass_dev (nullable) float [n_seqs][mass_stride],
+ * rows in batch order: the weights that the sequence's rows gave key t, summed
+ * over rows and query heads in float32 in a fixed order, are stored to
+ * mass[t] (mass_add 0) or added to it (1), t < the cached length; entries
+ * behind stay as they are.  mass_stride >= the longest sequence.  q, o (both
+ * 16-byte aligned) and mass must not overlap.  Workspace as for the passes
+ * (the bound one; weights are not needed).  At most 16384 cached tokens a
+ * sequence.  Can be captured; a captured call keeps its batch buffer and
+ * workspace in use, and may not run beside another call with that workspace. */
+int vsk_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev, int32_t window, int32_t sinks,
+               float* mass_dev, int32_t mass_stride, int32_t mass_add, void* ws_dev, size_t ws_bytes, void* stream);
+/* The same for the passes: from now on their attention of `layer` (-1: every
+ * layer) sees that window and those sinks (0, 0: every key again, the state of
+ * a new handle).  The persistent step kernel has no windows
+ * (VSK_E_UNSUPPORTED).  A captured pass keeps what was set at its capture. */
+int vsk_set_span(vsk_handle* h, int32_t layer, int32_t window, int32_t sinks);
+/* Passes add every layer's weights to mass_dev float [n_seqs][stride], rows in
+ * batch order (NULL: no longer, the state of a new handle; a Project-Only row
+ * of a routed layer has no weights).  A pass over more sequences or longer ones
+ * than that is VSK_E_ARG; the persistent step kernel is VSK_E_UNSUPPORTED. */
+int vsk_set_mass(vsk_handle* h, float* mass_dev, int32_t n_seqs, int32_t stride);
+
+/* Shorter caches: for i < n, sequence dst[i] (created and empty, all
+ * different) takes keep[i] tokens of src[i] (1 .. its length, at most 16384):
+ * its first `sinks` and last `recent` ones (sinks + recent <= keep[i]) and, of
+ * those between, the ones of the largest mass_dev[i][t] (float [n][mass_stride];
+ * equal: lowest index; NaN below everything), in index order.  K, V of every
+ * layer are copied to fresh blocks (lowest free ids; VSK_E_NOMEM if there are
+ * too few), the sources stay: release them once they are not needed.  The
+ * copies are bit-exact, so the kept tokens keep their rotary positions, and
+ * dst[i] goes on at src[i]'s next position (vsk_batch_host_copy's pos; max_pos
+ * bounds positions, not cached tokens); from then on "index" above is the place
+ * in the shorter cache.  An evicted sequence cannot share a prefix
+ * (vsk_seq_share_prefix: VSK_E_STATE) and has no persistent step.
+ * kept_dev int32 [n][out_stride] receives the kept indexes, slots_dev
+ * (nullable, same shape) their new slots, mass_out_dev (nullable, same shape,
+ * float) their weights, followed by zeros up to out_stride; it may be mass_dev
+ * itself when the strides are equal.  The outputs must not overlap otherwise.
+ * meta_dev: device memory of at least vsk_kv_evict_bytes(), 256-byte aligned,
+ * left alone until the call's work has run.  Cannot be captured
+ * (VSK_E_STATE).  All or nothing. */
+size_t vsk_kv_evict_bytes(const vsk_handle* h, const int64_t* src_host, const int32_t* keep_host, int32_t n);
+int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host, const int32_t* keep_host, int32_t n,
+                 int32_t sinks, int32_t recent, const float* mass_dev, int32_t mass_stride, float* mass_out_dev,
+                 int32_t* kept_dev, int32_t* slots_dev, int32_t out_stride, void* meta_dev, size_t meta_bytes,
+                 void* stream);
 
 /* ----------------------------------------------------------------- routed mode
  * One routed layer per Algorithm 1 (Section 3.1, "Route-Guided Cohort

@@ -91,6 +91,10 @@ int BlockAllocator::seq_share_prefix(int64_t dst, int64_t src, int32_t n_tokens,
     err = "destination sequence not empty";
     return kErrState;
   }
+  if (s->second.dropped != 0) {
+    err = "sequence " + std::to_string(src) + " has evicted tokens: its first tokens are no prefix";
+    return kErrState;
+  }
   if (n_tokens < 0 || n_tokens % block_ != 0 || n_tokens > s->second.len) {
     err = "shared prefix must be block aligned and resident";
     return kErrArg;
@@ -148,6 +152,53 @@ int BlockAllocator::reserve(int64_t seq, int32_t n_new, int32_t* slots_out, std:
   return kOk;
 }
 
+int BlockAllocator::seq_evict(const int64_t* dst, const int64_t* src, const int32_t* keep, int32_t n,
+                              std::string& err) {
+  std::unordered_set<int64_t> seen;
+  int64_t need = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const SeqState* d = find(dst[i]);
+    const SeqState* s = find(src[i]);
+    if (!d || !s) {
+      err = "unknown sequence " + std::to_string(d ? src[i] : dst[i]);
+      return kErrState;
+    }
+    if (!d->blocks.empty() || d->len != 0) {
+      err = "destination sequence " + std::to_string(dst[i]) + " not empty";
+      return kErrState;
+    }
+    if (!seen.insert(dst[i]).second) {
+      err = "destination sequence " + std::to_string(dst[i]) + " listed twice";
+      return kErrArg;
+    }
+    if (keep[i] < 1 || keep[i] > s->len) {
+      err = "kept tokens must be 1..resident length";
+      return kErrArg;
+    }
+    need += (keep[i] + block_ - 1) / block_;
+  }
+  if (need > free_count_) {
+    err = "KV pool exhausted: need " + std::to_string(need) + " blocks, " + std::to_string(free_count_) + " free";
+    return kErrNomem;
+  }
+  for (int32_t i = 0; i < n; ++i) {
+    const SeqState& s = seqs_.at(src[i]);
+    const int32_t dropped = s.dropped + s.len - keep[i];
+    reserve(dst[i], keep[i], nullptr, err);  // (the blocks are there: cannot fail)
+    seqs_.at(dst[i]).dropped = dropped;
+  }
+  return kOk;
+}
+
+void BlockAllocator::seq_undo_evict(const int64_t* dst, int32_t n) {
+  for (int32_t i = 0; i < n; ++i) {
+    SeqState& d = seqs_.at(dst[i]);
+    for (int32_t b : d.blocks)
+      if (--ref_[b] == 0) ++free_count_;
+    d = SeqState{};
+  }
+}
+
 int build_batch(const BlockAllocator& a, const int64_t* seqs, const int32_t* q_lens, int32_t n,
                 BatchHost& out, std::string& err) {
   if (n <= 0 || !seqs || !q_lens) {
@@ -185,15 +236,19 @@ int build_batch(const BlockAllocator& a, const int64_t* seqs, const int32_t* q_l
   b.block_table.assign(static_cast<size_t>(n) * max_blocks, -1);
   b.row_seq.resize(b.n_rows);
   b.pos.resize(b.n_rows);
+  b.rot.resize(b.n_rows);
   b.slot.resize(b.n_rows);
   const int32_t bs = a.block();
   for (int32_t i = 0; i < n; ++i) {
     const SeqState* s = a.find(seqs[i]);
     std::copy(s->blocks.begin(), s->blocks.end(), b.block_table.begin() + static_cast<size_t>(i) * max_blocks);
+    b.max_position = std::max(b.max_position, s->len + s->dropped - 1);
+    b.evicted = b.evicted || s->dropped != 0;
     for (int32_t r = b.cu_q[i]; r < b.cu_q[i + 1]; ++r) {
       const int32_t p = s->len - (b.cu_q[i + 1] - r);
       b.row_seq[r] = i;
       b.pos[r] = p;
+      b.rot[r] = p + s->dropped;
       b.slot[r] = s->blocks[p / bs] * bs + p % bs;
     }
   }

@@ -28,6 +28,9 @@ enum Status : int {
 struct SeqState {
   std::vector<int32_t> blocks;
   int32_t len = 0;
+  // tokens that eviction dropped: the cached token at index i keeps the rotary
+  // position it had, and the next token's position is len + dropped
+  int32_t dropped = 0;
 };
 
 // Reference-counted block pool.  Free blocks are handed out lowest id first.
@@ -43,6 +46,11 @@ class BlockAllocator {
   int seq_set_blocks(int64_t seq, const int32_t* blocks, int32_t n, int32_t ctx_len, std::string& err);
   int seq_share_prefix(int64_t dst, int64_t src, int32_t n_tokens, std::string& err);
   int reserve(int64_t seq, int32_t n_new, int32_t* slots_out, std::string& err);
+  // dst[i] (empty, all different) takes keep[i] tokens of src[i], 1 .. its
+  // length, in fresh blocks, and continues at src's position.  The sources
+  // keep their blocks.  seq_undo_evict empties the destinations again.
+  int seq_evict(const int64_t* dst, const int64_t* src, const int32_t* keep, int32_t n, std::string& err);
+  void seq_undo_evict(const int64_t* dst, int32_t n);
 
   const SeqState* find(int64_t seq) const;
   int32_t n_blocks() const { return static_cast<int32_t>(ref_.size()); }
@@ -63,11 +71,14 @@ class BlockAllocator {
 // Host copy of one pass's metadata (see vsk_batch_build in vsk.h).
 struct BatchHost {
   int32_t n_seqs = 0, n_rows = 0, max_blocks = 0, max_kv_len = 0, max_q_len = 0;
+  int32_t max_position = 0;          // the largest rot
+  bool evicted = false;              // some sequence has dropped tokens (rot differs from pos)
   std::vector<int32_t> block_table;  // [n_seqs][max_blocks]
   std::vector<int32_t> kv_len;       // [n_seqs]
   std::vector<int32_t> cu_q;         // [n_seqs + 1]
   std::vector<int32_t> row_seq;      // [n_rows]
-  std::vector<int32_t> pos;          // [n_rows]
+  std::vector<int32_t> pos;          // [n_rows] index of the row's token in its sequence's cache
+  std::vector<int32_t> rot;          // [n_rows] its rotary position: pos and the tokens dropped before it
   std::vector<int32_t> slot;         // [n_rows]
   // Shared prefixes of a decode pass: groups of sequences whose tables start
   // with the same full blocks before each member's current token.

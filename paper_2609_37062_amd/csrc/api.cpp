@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "attn.hpp"
+#include "evict.hpp"
 #include "gemm.hpp"
 #include "internal.hpp"
 #include "misc.hpp"
@@ -314,7 +315,7 @@ int vsk_seq_share_prefix(vsk_handle* h, int64_t dst, int64_t src, int32_t n_toke
 int vsk_kv_reserve(vsk_handle* h, int64_t seq, int32_t n_new, int32_t* slots_host) {
   NEED_ALLOC(h);
   const SeqState* s = h->alloc.find(seq);
-  if (s && static_cast<int64_t>(s->len) + n_new > h->cfg.max_pos)
+  if (s && static_cast<int64_t>(s->len) + s->dropped + n_new > h->cfg.max_pos)
     return fail(h, VSK_E_RANGE, "positions would exceed max_pos");
   return h->alloc.reserve(seq, n_new, slots_host, h->err);
 }
@@ -393,7 +394,7 @@ int vsk_batch_host_copy(const vsk_handle* h, int32_t* block_table, int32_t* kv_l
   cp(kv_len, b.kv_len);
   cp(cu_q, b.cu_q);
   cp(row_seq, b.row_seq);
-  cp(pos, b.pos);
+  cp(pos, b.rot);
   cp(slot, b.slot);
   return VSK_OK;
 }
@@ -407,7 +408,7 @@ int vsk_batch_prefix_info(const vsk_handle* h, int32_t* pfx_blocks_host, int32_t
 
 static size_t meta_bytes(const BatchHost& b) {
   auto sz = [](const std::vector<int32_t>& v) { return align_up(std::max<size_t>(v.size(), 1) * 4); };
-  return sz(b.block_table) + sz(b.kv_len) + sz(b.cu_q) + sz(b.row_seq) + sz(b.pos) + sz(b.slot) +
+  return sz(b.block_table) + sz(b.kv_len) + sz(b.cu_q) + sz(b.row_seq) + sz(b.pos) + (b.evicted ? sz(b.rot) : 0) + sz(b.slot) +
          sz(b.pfx_blocks) + sz(b.pfx_splits) + sz(b.pfx_items) + sz(b.grp_rows) + sz(b.grp_info) + sz(b.pfx_tbl) +
          sz(b.pre_items) + sz(b.dec_rows);
 }
@@ -415,6 +416,39 @@ static size_t meta_bytes(const BatchHost& b) {
 size_t vsk_batch_device_bytes(const vsk_handle* h) {
   if (!h || !h->batch_built) return 0;
   return meta_bytes(h->bh);
+}
+
+// Copy `staging` to device memory from a pinned staging buffer: the transfer
+// runs asynchronously and the host returns at once, unless this buffer's
+// previous copy (issued two uploads ago) has not finished yet.
+static int stage_upload(vsk_handle* h, void* dev, const std::vector<uint8_t>& staging, hipStream_t s) {
+  Handle::Staging& st = h->stage[h->stage_next];
+  hipError_t e = hipSuccess;
+  if (st.pending) {
+    e = hipEventSynchronize(st.done);
+    if (e != hipSuccess) return hip_check(h, e, "metadata staging wait");
+    st.pending = false;
+  }
+  if (st.cap < staging.size()) {
+    if (st.host) (void)hipHostFree(st.host);
+    st.host = nullptr;
+    st.cap = 0;
+    const size_t cap = std::max<size_t>(align_up(staging.size(), 1 << 16), 1 << 16);
+    e = hipHostMalloc(&st.host, cap, hipHostMallocDefault);
+    if (e != hipSuccess) return hip_check(h, e, "metadata staging buffer");
+    st.cap = cap;
+  }
+  if (!st.done) {
+    e = hipEventCreateWithFlags(&st.done, hipEventDisableTiming);
+    if (e != hipSuccess) return hip_check(h, e, "metadata staging event");
+  }
+  std::memcpy(st.host, staging.data(), staging.size());
+  e = hipMemcpyAsync(dev, st.host, staging.size(), hipMemcpyHostToDevice, s);
+  if (e == hipSuccess) e = hipEventRecord(st.done, s);
+  if (e != hipSuccess) return hip_check(h, e, "metadata upload");
+  st.pending = true;
+  h->stage_next ^= 1;
+  return VSK_OK;
 }
 
 int vsk_batch_upload(vsk_handle* h, void* meta_dev, size_t bytes, void* stream) {
@@ -437,6 +471,8 @@ int vsk_batch_upload(vsk_handle* h, void* meta_dev, size_t bytes, void* stream) 
   put(b.cu_q, &d.cu_q);
   put(b.row_seq, &d.row_seq);
   put(b.pos, &d.pos);
+  d.rot = d.pos;
+  if (b.evicted) put(b.rot, &d.rot);  // (else the same numbers)
   put(b.slot, &d.slot);
   put(b.pfx_blocks, &d.pfx_blocks);
   put(b.pfx_splits, &d.pfx_splits);
@@ -450,41 +486,15 @@ int vsk_batch_upload(vsk_handle* h, void* meta_dev, size_t bytes, void* stream) 
   d.n_dec_rows = static_cast<int32_t>(b.dec_rows.size());
   d.n_pfx_items = b.n_pfx_items();
   d.max_pfx_splits = b.max_pfx_splits;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  // copy from a pinned staging buffer: the transfer runs asynchronously and
-  // the host returns at once, unless this buffer's previous copy (issued two
-  // uploads ago) has not finished yet
-  Handle::Staging& st = h->stage[h->stage_next];
-  hipError_t e = hipSuccess;
-  if (st.pending) {
-    e = hipEventSynchronize(st.done);
-    if (e != hipSuccess) return hip_check(h, e, "metadata staging wait");
-    st.pending = false;
-  }
-  if (st.cap < staging.size()) {
-    if (st.host) (void)hipHostFree(st.host);
-    st.host = nullptr;
-    st.cap = 0;
-    const size_t cap = std::max<size_t>(align_up(staging.size(), 1 << 16), 1 << 16);
-    e = hipHostMalloc(&st.host, cap, hipHostMallocDefault);
-    if (e != hipSuccess) return hip_check(h, e, "metadata staging buffer");
-    st.cap = cap;
-  }
-  if (!st.done) {
-    e = hipEventCreateWithFlags(&st.done, hipEventDisableTiming);
-    if (e != hipSuccess) return hip_check(h, e, "metadata staging event");
-  }
-  std::memcpy(st.host, staging.data(), staging.size());
-  e = hipMemcpyAsync(meta_dev, st.host, staging.size(), hipMemcpyHostToDevice, s);
-  if (e == hipSuccess) e = hipEventRecord(st.done, s);
-  if (e != hipSuccess) return hip_check(h, e, "metadata upload");
-  st.pending = true;
-  h->stage_next ^= 1;
+  const int st = stage_upload(h, meta_dev, staging, static_cast<hipStream_t>(stream));
+  if (st != VSK_OK) return st;
   d.n_seqs = b.n_seqs;
   d.n_rows = b.n_rows;
   d.max_blocks = b.max_blocks;
   d.max_kv_len = b.max_kv_len;
   d.max_q_len = b.max_q_len;
+  d.max_position = b.max_position;
+  d.evicted = b.evicted;
   h->bd = d;
   h->batch_uploaded = true;
   return VSK_OK;
@@ -511,6 +521,16 @@ int vsk_workspace_init(vsk_handle* h, void* ws_dev, size_t bytes, int32_t max_ro
   return VSK_OK;
 }
 
+// What every pass over the uploaded batch needs: positions within the model's,
+// and room for the weights per token, where the passes leave them.
+static int span_common(vsk_handle* h) {
+  const BatchDev& b = h->bd;
+  if (b.max_position >= h->cfg.max_pos) return fail(h, VSK_E_RANGE, "position beyond max_pos");
+  if (h->mass && (b.n_seqs > h->mass_seqs || b.max_kv_len > h->mass_stride))
+    return fail(h, VSK_E_ARG, "batch exceeds the bound weights per token (vsk_set_mass)");
+  return VSK_OK;
+}
+
 static int pass_common(vsk_handle* h, const int32_t* ids, void* logits, void* ws, size_t ws_bytes) {
   if (!h) return VSK_E_ARG;
   if (!h->packed) return fail(h, VSK_E_STATE, "no weights bound");
@@ -518,8 +538,9 @@ static int pass_common(vsk_handle* h, const int32_t* ids, void* logits, void* ws
   if (!h->batch_uploaded) return fail(h, VSK_E_STATE, "no batch uploaded");
   if (!ids || !logits || !ws) return fail(h, VSK_E_ARG, "null buffer");
   if (ws != h->ws || ws_bytes != h->ws_bytes) return fail(h, VSK_E_STATE, "workspace not initialised with this handle");
+  int st = span_common(h);
+  if (st != VSK_OK) return st;
   const BatchDev& b = h->bd;
-  if (b.max_kv_len > h->cfg.max_pos) return fail(h, VSK_E_RANGE, "position beyond max_pos");
   if (b.n_rows > h->wl.max_rows || b.n_seqs > h->wl.max_seqs || b.max_kv_len > h->wl.max_kv_len)
     return fail(h, VSK_E_ARG, "batch exceeds the workspace capacity");
   return VSK_OK;
@@ -584,7 +605,8 @@ int vsk_decode_step_scratch(vsk_handle* h, const int32_t* ids_dev, void* logits_
   if (!ids_dev || !logits_dev) return fail(h, VSK_E_ARG, "null buffer");
   const BatchDev& b = h->bd;
   if (b.max_q_len != 1) return fail(h, VSK_E_ARG, "decode_step needs one row per sequence");
-  if (b.max_kv_len > h->cfg.max_pos) return fail(h, VSK_E_RANGE, "position beyond max_pos");
+  int st = span_common(h);
+  if (st != VSK_OK) return st;
   // the workspace of exactly this batch, without the persistent kernel's region
   const WsLayout wl = ws_layout(h->cfg, b.n_rows, b.n_seqs, b.max_kv_len, false);
   if (wl.total > static_cast<size_t>(VSK_SCRATCH_BYTES))
@@ -731,6 +753,184 @@ int vsk_argmax_sample(const void* logits_dev, int32_t dtype, int32_t rows, int32
   hipError_t e =
       launch_argmax_logits(logits_dev, dtype, rows, vocab, ids_dev, no_value_dev, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? VSK_OK : VSK_E_HIP;
+}
+
+// ------------------------------------------------------------------ bounded cache
+static bool span_ok(int32_t window, int32_t sinks) { return window >= 0 && sinks >= 0; }
+
+// [a, a + an) and [b, b + bn) share bytes
+static bool overlap(const void* a, size_t an, const void* b, size_t bn) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + bn && y < x + an;
+}
+
+int vsk_set_span(vsk_handle* h, int32_t layer, int32_t window, int32_t sinks) {
+  if (!h) return VSK_E_ARG;
+  if (layer < -1 || layer >= h->cfg.n_layers) return fail(h, VSK_E_RANGE, "layer out of range");
+  if (!span_ok(window, sinks)) return fail(h, VSK_E_ARG, "window and sinks must not be negative");
+  // a window that holds every position a model can have is none
+  const Handle::Span v = window == 0 || window >= h->cfg.max_pos
+                             ? Handle::Span{}
+                             : Handle::Span{window, std::min(sinks, h->cfg.max_pos)};
+  std::vector<Handle::Span> all = h->spans;
+  if (all.empty()) all.resize(h->cfg.n_layers);
+  for (int32_t l = 0; l < h->cfg.n_layers; ++l)
+    if (layer < 0 || l == layer) all[l] = v;
+  const bool any = std::any_of(all.begin(), all.end(), [](const Handle::Span& x) { return x.window > 0; });
+  if (!any) all.clear();
+  h->spans.swap(all);
+  return VSK_OK;
+}
+
+int vsk_set_mass(vsk_handle* h, float* mass_dev, int32_t n_seqs, int32_t stride) {
+  if (!h) return VSK_E_ARG;
+  if (mass_dev && (n_seqs < 1 || stride < 1)) return fail(h, VSK_E_ARG, "weights per token need a positive size");
+  if (reinterpret_cast<uintptr_t>(mass_dev) % 4) return fail(h, VSK_E_ARG, "weights per token not 4-byte aligned");
+  h->mass = mass_dev;
+  h->mass_seqs = mass_dev ? n_seqs : 0;
+  h->mass_stride = mass_dev ? stride : 0;
+  return VSK_OK;
+}
+
+int vsk_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev, int32_t window, int32_t sinks,
+               float* mass_dev, int32_t mass_stride, int32_t mass_add, void* ws_dev, size_t ws_bytes, void* stream) {
+  if (!h) return VSK_E_ARG;
+  if (!h->pool) return fail(h, VSK_E_STATE, "no KV pool bound");
+  if (!h->batch_uploaded) return fail(h, VSK_E_STATE, "no batch uploaded");
+  if (layer < 0 || layer >= h->cfg.n_layers) return fail(h, VSK_E_RANGE, "layer out of range");
+  if (!q_dev || !o_dev || !ws_dev) return fail(h, VSK_E_ARG, "null buffer");
+  if (ws_dev != h->ws || ws_bytes != h->ws_bytes)
+    return fail(h, VSK_E_STATE, "workspace not initialised with this handle");
+  if (!span_ok(window, sinks)) return fail(h, VSK_E_ARG, "window and sinks must not be negative");
+  if (reinterpret_cast<uintptr_t>(q_dev) % 16 || reinterpret_cast<uintptr_t>(o_dev) % 16)
+    return fail(h, VSK_E_ARG, "q and o must be 16-byte aligned");
+  const BatchDev& b = h->bd;
+  if (b.max_kv_len > kMaxSpanBlocks * kBlock) return fail(h, VSK_E_RANGE, "sequence longer than 16384 cached tokens");
+  if (b.n_rows > h->wl.max_rows || b.n_seqs > h->wl.max_seqs || b.max_kv_len > h->wl.max_kv_len)
+    return fail(h, VSK_E_ARG, "batch exceeds the workspace capacity");
+  const size_t bytes = static_cast<size_t>(b.n_rows) * h->cfg.n_q_heads * h->cfg.head_dim * 2;
+  if (overlap(q_dev, bytes, o_dev, bytes)) return fail(h, VSK_E_ARG, "q and o overlap");
+  if (mass_dev) {
+    if (mass_stride < b.max_kv_len) return fail(h, VSK_E_ARG, "mass rows shorter than the longest sequence");
+    if (mass_add != 0 && mass_add != 1) return fail(h, VSK_E_ARG, "mass_add must be 0 or 1");
+    if (reinterpret_cast<uintptr_t>(mass_dev) % 4) return fail(h, VSK_E_ARG, "mass not 4-byte aligned");
+    const size_t mass_bytes = ((static_cast<size_t>(b.n_seqs) - 1) * mass_stride + b.max_kv_len) * 4;
+    if (overlap(mass_dev, mass_bytes, q_dev, bytes) || overlap(mass_dev, mass_bytes, o_dev, bytes))
+      return fail(h, VSK_E_ARG, "mass overlaps q or o");
+  }
+  if (window >= b.max_kv_len) window = 0;  // every row sees every key before it
+  sinks = window == 0 ? 0 : std::min(sinks, b.max_kv_len);
+  return hip_check(h, run_attend(*h, layer, static_cast<const uint16_t*>(q_dev), static_cast<uint16_t*>(o_dev), window,
+                                 sinks, mass_dev, mass_stride, mass_add != 0, static_cast<hipStream_t>(stream)),
+                   "attend");
+}
+
+// Device metadata of an eviction: [n][4] (length, kept, first source block,
+// first destination block), the sources' tables, the destinations'.
+static size_t evict_meta_ints(const vsk_handle* h, const int64_t* src, const int32_t* keep, int32_t n) {
+  size_t ints = 4 * static_cast<size_t>(n);
+  for (int32_t i = 0; i < n; ++i) {
+    const SeqState* s = h->alloc.find(src[i]);
+    if (!s || keep[i] < 1 || keep[i] > s->len) return 0;
+    ints += s->blocks.size() + (keep[i] + kBlock - 1) / kBlock;
+  }
+  return ints;
+}
+
+size_t vsk_kv_evict_bytes(const vsk_handle* h, const int64_t* src_host, const int32_t* keep_host, int32_t n) {
+  if (!h || !h->alloc_ready || !src_host || !keep_host || n < 1) return 0;
+  return align_up(evict_meta_ints(h, src_host, keep_host, n) * 4);
+}
+
+int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host, const int32_t* keep_host, int32_t n,
+                 int32_t sinks, int32_t recent, const float* mass_dev, int32_t mass_stride, float* mass_out_dev,
+                 int32_t* kept_dev, int32_t* slots_dev, int32_t out_stride, void* meta_dev, size_t meta_bytes_,
+                 void* stream) {
+  NEED_ALLOC(h);
+  if (!h->pool) return fail(h, VSK_E_STATE, "no KV pool bound");
+  if (!dst_host || !src_host || !keep_host || n < 1) return fail(h, VSK_E_ARG, "empty eviction");
+  if (n > 65535) return fail(h, VSK_E_ARG, "at most 65535 sequences a call");
+  if (!mass_dev || !kept_dev || !meta_dev) return fail(h, VSK_E_ARG, "null buffer");
+  if (sinks < 0 || recent < 0) return fail(h, VSK_E_ARG, "sinks and recent must not be negative");
+  int32_t max_keep = 0, max_len = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const SeqState* s = h->alloc.find(src_host[i]);
+    if (!s) return fail(h, VSK_E_STATE, "unknown sequence " + std::to_string(src_host[i]));
+    if (s->len > kEvictMaxLen) return fail(h, VSK_E_RANGE, "sequence longer than 16384 cached tokens");
+    if (keep_host[i] < 1 || keep_host[i] > s->len) return fail(h, VSK_E_ARG, "kept tokens must be 1..resident length");
+    if (static_cast<int64_t>(sinks) + recent > keep_host[i])
+      return fail(h, VSK_E_ARG, "sinks and recent tokens are more than the kept ones");
+    max_keep = std::max(max_keep, keep_host[i]);
+    max_len = std::max(max_len, s->len);
+  }
+  if (mass_stride < max_len) return fail(h, VSK_E_ARG, "mass rows shorter than the longest sequence");
+  if (out_stride < max_keep) return fail(h, VSK_E_ARG, "output rows shorter than the most kept tokens");
+  for (const void* p : {static_cast<const void*>(mass_dev), static_cast<const void*>(mass_out_dev),
+                        static_cast<const void*>(kept_dev), static_cast<const void*>(slots_dev)})
+    if (reinterpret_cast<uintptr_t>(p) % 4) return fail(h, VSK_E_ARG, "buffer not 4-byte aligned");
+  const size_t in_bytes = ((static_cast<size_t>(n) - 1) * mass_stride + max_len) * 4;
+  const size_t out_bytes = static_cast<size_t>(n) * out_stride * 4;
+  if (mass_out_dev && overlap(mass_dev, in_bytes, mass_out_dev, out_bytes) &&
+      !(mass_out_dev == mass_dev && out_stride == mass_stride))
+    return fail(h, VSK_E_ARG, "mass_out overlaps mass (in place: the same rows)");
+  if (overlap(kept_dev, out_bytes, mass_dev, in_bytes) ||
+      (mass_out_dev && overlap(kept_dev, out_bytes, mass_out_dev, out_bytes)) ||
+      (slots_dev && (overlap(slots_dev, out_bytes, mass_dev, in_bytes) || overlap(slots_dev, out_bytes, kept_dev, out_bytes) ||
+                     (mass_out_dev && overlap(slots_dev, out_bytes, mass_out_dev, out_bytes)))))
+    return fail(h, VSK_E_ARG, "outputs overlap");
+  const size_t ints = evict_meta_ints(h, src_host, keep_host, n);
+  if (meta_bytes_ < align_up(ints * 4)) return fail(h, VSK_E_ARG, "metadata buffer smaller than vsk_kv_evict_bytes()");
+  if (reinterpret_cast<uintptr_t>(meta_dev) % kAlign) return fail(h, VSK_E_ARG, "metadata buffer not aligned");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  int st = h->alloc.seq_evict(dst_host, src_host, keep_host, n, h->err);
+  if (st != VSK_OK) return st;
+  // a captured eviction would replay one moment's block tables
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  st = hip_check(h, hipStreamIsCapturing(s, &cap), "evict");
+  if (st == VSK_OK && cap != hipStreamCaptureStatusNone) st = fail(h, VSK_E_STATE, "an eviction cannot be captured");
+  if (st != VSK_OK) {
+    h->alloc.seq_undo_evict(dst_host, n);
+    return st;
+  }
+  std::vector<uint8_t> staging(align_up(ints * 4), 0);
+  int32_t* m = reinterpret_cast<int32_t*>(staging.data());
+  const int32_t info_ints = 4 * n;
+  int32_t at = 0, total_src = 0;
+  for (int32_t i = 0; i < n; ++i) total_src += static_cast<int32_t>(h->alloc.find(src_host[i])->blocks.size());
+  int32_t at_dst = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const SeqState* a = h->alloc.find(src_host[i]);
+    const SeqState* d = h->alloc.find(dst_host[i]);
+    m[4 * i] = a->len;
+    m[4 * i + 1] = keep_host[i];
+    m[4 * i + 2] = at;
+    m[4 * i + 3] = at_dst;
+    std::copy(a->blocks.begin(), a->blocks.end(), m + info_ints + at);
+    std::copy(d->blocks.begin(), d->blocks.end(), m + info_ints + total_src + at_dst);
+    at += static_cast<int32_t>(a->blocks.size());
+    at_dst += static_cast<int32_t>(d->blocks.size());
+  }
+  EvictArgs a{};
+  a.pool = h->pool;
+  a.n_layers = h->cfg.n_layers;
+  a.n_blocks = h->n_blocks;
+  a.Hkv = h->cfg.n_kv_heads;
+  a.hd = h->cfg.head_dim;
+  a.info = static_cast<const int32_t*>(meta_dev);
+  a.src_tbl = a.info + info_ints;
+  a.dst_tbl = a.src_tbl + total_src;
+  a.sinks = sinks;
+  a.recent = recent;
+  a.mass = mass_dev;
+  a.mass_stride = mass_stride;
+  a.mass_out = mass_out_dev;
+  a.kept = kept_dev;
+  a.slots = slots_dev;
+  a.out_stride = out_stride;
+  st = stage_upload(h, meta_dev, staging, s);
+  if (st == VSK_OK) st = hip_check(h, launch_evict(a, n, max_keep, s), "evict");
+  if (st != VSK_OK) h->alloc.seq_undo_evict(dst_host, n);
+  return st;
 }
 
 int vsk_stream_read(const void* src_dev, size_t bytes, uint32_t* out_dev, int32_t workgroups, void* stream) {
@@ -940,8 +1140,207 @@ static hipError_t run_step(Handle& h, const PassArgs& pa, int n_wgs, hipStream_t
 }
 
 bool step_eligible(Handle& h, const PassArgs& pa) {
+  // (it has no general walk, no weights per token and one position per row)
+  if (!h.spans.empty() || h.mass != nullptr || h.bd.evicted) return false;
   return h.exec_mode == 2 && pa.logit_rows == nullptr && h.bd.max_q_len == 1 && pa.wl.step &&
          h.bd.n_rows <= kStepMaxRows && step_workgroups(h) > 0;
+}
+
+// ------------------------------------------------------------------ attention of a batch
+// The launches of one layer's attention over the uploaded batch: shared
+// prefixes, prompt rows, decode rows, and (general walks) what they leave for
+// the weights per key.  Everything but the layer and its route mask.
+struct AttnPlan {
+  AttnArgs dec{};
+  AttnPrefixArgs pfx{};
+  AttnPrefillArgs pre{};
+  bool cascade = false, prefill = false, span = false;
+  int dec_splits = 1, pfx_fold = 0;
+};
+
+// out_Rg: the output as frags of that many row groups, 0 for row-major.
+// decode: a decode pass (every row one sequence's), whose shared prefixes are
+// read once.  Row r at index p sees keys 0..p, or with a window keys
+// p - window + 1 .. p and 0 .. sinks - 1.  general: the walk that takes
+// windows, row-major output and leaves (maximum, 1 / sum) per row and head.
+static AttnPlan plan_attn(Handle& h, const uint16_t* q, uint16_t* out, int out_Rg, uint8_t* ws, const WsLayout& wl,
+                          bool decode, int window, int sinks, bool general) {
+  const vsk_model_cfg& c = h.cfg;
+  const BatchDev& b = h.bd;
+  const int R = b.n_rows, d = c.head_dim, Nq = c.n_q_heads * d;
+  AttnPlan p;
+  p.span = general || window > 0 || out_Rg == 0;
+  // prefill rows: causal multi-row work items (keys staged per item in LDS)
+  p.prefill = h.prefill_attn != 0 && b.n_pre_items > 0 &&
+              b.max_kv_len <= (p.span ? kMaxSpanBlocks : kMaxPrefillBlocks) * kBlock;
+  AttnArgs& aa = p.dec;
+  aa.q = q;
+  aa.pool = h.pool;
+  aa.n_blocks = h.n_blocks;
+  aa.Hkv = c.n_kv_heads;
+  aa.hd = d;
+  aa.G = c.n_q_heads / c.n_kv_heads;
+  aa.Nq = Nq;
+  aa.block_table = b.block_table;
+  aa.max_blocks = b.max_blocks;
+  aa.row_seq = b.row_seq;
+  aa.pos = b.pos;
+  aa.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(d)));
+  // shared prefixes of a decode pass: read once per group by k_attn_prefix
+  const bool cascade = p.cascade = h.shared_prefix != 0 && b.n_pfx_items > 0 && decode && window == 0;
+  // the blocks each row of the decode kernel walks (after its shared prefix)
+  int blk_min = INT_MAX, blk_max = 0, n_dec = 0;
+  // and how many of those an earlier row of the launch reads too
+  int64_t blk_sum = 0, blk_again = 0;
+  {
+    const BatchHost& bh = h.bh;
+    auto row_blocks = [&](int r) {
+      const int nb = span_walk(bh.pos[r] + 1, bh.pos[r] + 1, window, sinks).nv - (cascade ? bh.pfx_blocks[r] : 0);
+      blk_min = std::min(blk_min, nb);
+      blk_max = std::max(blk_max, nb);
+      blk_sum += nb;
+      ++n_dec;
+    };
+    blk_again = cascade ? bh.reread_own : bh.reread_all;
+    if (p.prefill) {
+      for (int32_t r : bh.dec_rows) row_blocks(r);
+    } else {
+      for (int r = 0; r < R; ++r) {
+        row_blocks(r);
+        // a further row of a sequence walks the blocks of the row before it
+        if (r > 0 && bh.row_seq[r] == bh.row_seq[r - 1])
+          blk_again += span_walk(bh.pos[r - 1] + 1, bh.pos[r - 1] + 1, window, sinks).nv;
+      }
+    }
+  }
+  // KV that a launch reads once is loaded non-temporally, KV that its rows
+  // share with ordinary loads, which leave it in the caches for the next row.
+  // The line lies at half of the blocks.  Passes of two layers, non-temporal
+  // and ordinary: no block read again, 3B 200 rows of 1,000-3,000 tokens
+  // 1,603 and 1,769 us; a quarter, 64 rows behind one prefix (key 4 at 0) 336
+  // and 350; half, 319 and 311; three quarters, 291 and 251; nearly all, 256
+  // prompt rows behind 8,208 tokens 2,362 and 1,396.
+  aa.kv_once = 2 * blk_again < blk_sum ? 1 : 0;
+  aa.bps = h.attn_bps > 0 ? h.attn_bps : attn_auto_bps(R, c.n_kv_heads);
+  // 128..255 (row, KV head) pairs whose walks are within 20% of each other:
+  // one split per pair (no merge, and the items are balanced already); a
+  // wider spread keeps the split, the longest walk setting the time, and
+  // fewer pairs keep it for the parallelism.  Nor is any walk cut that is no
+  // longer than what each of the kAttnSlots workgroups in flight has to walk
+  // in all (8B, 100 rows of 1,500 to 2,500 tokens: 1,202 us for four layers at
+  // 96 blocks a split, 1,114 uncut).  Rows that a route tape makes Project-Only
+  // count too, the tape being on the device: with nine in ten of them uncut
+  // walks lose (128 rows of 4,000 to 7,900 tokens, two layers: 940 us uncut,
+  // 899 cut; with half of them 1,070 and 1,084).
+  const int pairs = n_dec * c.n_kv_heads;
+  if (h.attn_bps == 0 && n_dec > 0 && ((pairs >= 128 && pairs < 256 && 5 * blk_min >= 4 * blk_max) ||
+                                       blk_sum * c.n_kv_heads >= static_cast<int64_t>(kAttnSlots) * blk_max))
+    aa.bps = std::clamp((blk_max + 7) / 8 * 8, kAttnMinBps, kAttnMaxBps);
+  aa.max_splits = attn_splits(b.max_kv_len, aa.bps);
+  aa.part_o = reinterpret_cast<float*>(ws + wl.att_o);
+  aa.part_ml = reinterpret_cast<float2*>(ws + wl.att_ml);
+  aa.counter = reinterpret_cast<int*>(ws + wl.att_cnt);
+  aa.out = out;
+  aa.out_Rg = out_Rg;
+  aa.window = window;
+  aa.sinks = sinks;
+  aa.split_stride = aa.max_splits + (cascade ? b.max_pfx_splits : 0);
+  aa.pfx_blocks = cascade ? b.pfx_blocks : nullptr;
+  aa.pfx_splits = cascade ? b.pfx_splits : nullptr;
+  // decode work items launched per (row, KV head): the most splits any
+  // decode row has after its shared prefix (the rest would exit at once)
+  p.dec_splits = std::max(1, (blk_max + aa.bps - 1) / aa.bps);
+  p.pfx_fold = cascade ? b.max_pfx_splits : 0;
+  AttnPrefixArgs& ap = p.pfx;
+  ap.q = q;
+  ap.pool = h.pool;
+  ap.n_blocks = h.n_blocks;
+  ap.Hkv = c.n_kv_heads;
+  ap.G = aa.G;
+  ap.Nq = Nq;
+  ap.block_table = b.block_table;
+  ap.max_blocks = b.max_blocks;
+  ap.row_seq = b.row_seq;
+  ap.items = b.pfx_items;
+  ap.grp_rows = b.grp_rows;
+  ap.grp_info = b.grp_info;
+  ap.pfx_tbl = b.pfx_tbl;
+  ap.scale_log2 = aa.scale_log2;
+  ap.split_stride = aa.split_stride;
+  ap.part_o = aa.part_o;
+  ap.part_ml = aa.part_ml;
+  AttnPrefillArgs& pf = p.pre;
+  pf.q = q;
+  pf.pool = h.pool;
+  pf.n_blocks = h.n_blocks;
+  pf.Hkv = c.n_kv_heads;
+  pf.G = aa.G;
+  pf.Nq = Nq;
+  pf.block_table = b.block_table;
+  pf.max_blocks = b.max_blocks;
+  pf.kv_len = b.kv_len;
+  pf.pos = b.pos;
+  pf.items = b.pre_items;
+  pf.scale_log2 = aa.scale_log2;
+  pf.out = out;
+  pf.out_Rg = out_Rg;
+  pf.window = window;
+  pf.sinks = sinks;
+  // (maximum, 1 / sum) per row and head: in the space of the K-split products,
+  // which are added up before attention starts and written after it ends
+  // (8 bytes a head against at least 4 * head_dim)
+  if (general) aa.ml = pf.ml = reinterpret_cast<float2*>(ws + wl.ypart);
+  return p;
+}
+
+static hipError_t launch_attn(Handle& h, AttnPlan& p, int layer, const uint8_t* mask, LaunchEvents ev, hipStream_t s) {
+  const BatchDev& b = h.bd;
+  const int d = h.cfg.head_dim;
+  hipError_t e;
+  p.dec.layer = p.pfx.layer = p.pre.layer = layer;
+  p.dec.run_mask = p.pre.run_mask = mask;
+  if (p.cascade && (e = launch_attn_prefix(p.pfx, b.n_pfx_items, d, s)) != hipSuccess) return e;
+  if (p.prefill && (e = launch_attn_prefill(p.pre, b.n_pre_items, d, s, p.span)) != hipSuccess) return e;
+  int rows = b.n_dec_rows;
+  p.dec.rows = b.dec_rows;  // one-row sequences, longest walk first
+  if (!p.prefill && b.n_pre_items > 0) {
+    p.dec.rows = nullptr;  // every row a work item
+    rows = b.n_rows;
+  }
+  if (rows == 0) return hipSuccess;
+  return launch_attn_decode(p.dec, rows, p.dec_splits, p.pfx_fold, s, ev, p.span);
+}
+
+static hipError_t launch_mass(Handle& h, const AttnPlan& p, int layer, float* mass, int64_t stride, bool add,
+                              hipStream_t s) {
+  AttnMassArgs m{};
+  m.q = p.dec.q;
+  m.pool = p.dec.pool;
+  m.layer = layer;
+  m.n_blocks = p.dec.n_blocks;
+  m.Hkv = p.dec.Hkv;
+  m.G = p.dec.G;
+  m.Nq = p.dec.Nq;
+  m.block_table = p.dec.block_table;
+  m.max_blocks = p.dec.max_blocks;
+  m.kv_len = h.bd.kv_len;
+  m.cu_q = h.bd.cu_q;
+  m.scale_log2 = p.dec.scale_log2;
+  m.window = p.dec.window;
+  m.sinks = p.dec.sinks;
+  m.ml = p.dec.ml;
+  m.mass = mass;
+  m.stride = stride;
+  m.add = add ? 1 : 0;
+  return launch_attn_mass(m, h.bd.n_seqs, h.bd.max_kv_len, h.cfg.head_dim, s);
+}
+
+hipError_t run_attend(Handle& h, int layer, const uint16_t* q, uint16_t* out, int window, int sinks, float* mass,
+                      int64_t stride, bool add, hipStream_t s) {
+  AttnPlan p = plan_attn(h, q, out, 0, h.ws, h.wl, h.bd.max_q_len == 1, window, sinks, mass != nullptr);
+  hipError_t e = launch_attn(h, p, layer, nullptr, {}, s);
+  if (e == hipSuccess && mass != nullptr) e = launch_mass(h, p, layer, mass, stride, add, s);
+  return e;
 }
 
 hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
@@ -1003,122 +1402,16 @@ hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
   ga.Nq = Nq;
   ga.Nkv = Nkv;
   ga.slot = b.slot;
-  ga.pos = b.pos;
+  ga.pos = b.rot;
   ga.rope = reinterpret_cast<const float2*>(P + h.pl.rope);
   ga.x = x;
   ga.out_Rg = Rg;
   ga.xcd_remap = h.xcd_remap;
 
-  AttnArgs aa{};
-  aa.q = q;
-  aa.pool = h.pool;
-  aa.n_blocks = h.n_blocks;
-  aa.Hkv = c.n_kv_heads;
-  aa.hd = d;
-  aa.G = c.n_q_heads / c.n_kv_heads;
-  aa.Nq = Nq;
-  aa.block_table = b.block_table;
-  aa.max_blocks = b.max_blocks;
-  aa.row_seq = b.row_seq;
-  aa.pos = b.pos;
-  aa.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(d)));
-  // shared prefixes of a decode pass: read once per group by k_attn_prefix
-  const bool cascade = h.shared_prefix != 0 && b.n_pfx_items > 0 && pa.logit_rows == nullptr;
-  // the blocks each row of the decode kernel walks (after its shared prefix)
-  int blk_min = INT_MAX, blk_max = 0, n_dec = 0;
-  // and how many of those an earlier row of the launch reads too
-  int64_t blk_sum = 0, blk_again = 0;
-  {
-    const BatchHost& bh = h.bh;
-    auto row_blocks = [&](int r) {
-      const int nb = (bh.pos[r] + 1 + kBlock - 1) / kBlock - (cascade ? bh.pfx_blocks[r] : 0);
-      blk_min = std::min(blk_min, nb);
-      blk_max = std::max(blk_max, nb);
-      blk_sum += nb;
-      ++n_dec;
-    };
-    blk_again = cascade ? bh.reread_own : bh.reread_all;
-    if (h.prefill_attn != 0 && b.n_pre_items > 0 && b.max_kv_len <= kMaxPrefillBlocks * kBlock) {
-      for (int32_t r : bh.dec_rows) row_blocks(r);
-    } else {
-      for (int r = 0; r < R; ++r) {
-        row_blocks(r);
-        // a further row of a sequence walks the blocks of the row before it
-        if (r > 0 && bh.row_seq[r] == bh.row_seq[r - 1]) blk_again += bh.pos[r - 1] / kBlock + 1;
-      }
-    }
-  }
-  // KV that a launch reads once is loaded non-temporally, KV that its rows
-  // share with ordinary loads, which leave it in the caches for the next row.
-  // The line lies at half of the blocks.  Passes of two layers, non-temporal
-  // and ordinary: no block read again, 3B 200 rows of 1,000-3,000 tokens
-  // 1,603 and 1,769 us; a quarter, 64 rows behind one prefix (key 4 at 0) 336
-  // and 350; half, 319 and 311; three quarters, 291 and 251; nearly all, 256
-  // prompt rows behind 8,208 tokens 2,362 and 1,396.
-  aa.kv_once = 2 * blk_again < blk_sum ? 1 : 0;
-  aa.bps = h.attn_bps > 0 ? h.attn_bps : attn_auto_bps(R, c.n_kv_heads);
-  // 128..255 (row, KV head) pairs whose walks are within 20% of each other:
-  // one split per pair (no merge, and the items are balanced already); a
-  // wider spread keeps the split, the longest walk setting the time, and
-  // fewer pairs keep it for the parallelism.  Nor is any walk cut that is no
-  // longer than what each of the kAttnSlots workgroups in flight has to walk
-  // in all (8B, 100 rows of 1,500 to 2,500 tokens: 1,202 us for four layers at
-  // 96 blocks a split, 1,114 uncut).  Rows that a route tape makes Project-Only
-  // count too, the tape being on the device: with nine in ten of them uncut
-  // walks lose (128 rows of 4,000 to 7,900 tokens, two layers: 940 us uncut,
-  // 899 cut; with half of them 1,070 and 1,084).
-  const int pairs = n_dec * c.n_kv_heads;
-  if (h.attn_bps == 0 && n_dec > 0 && ((pairs >= 128 && pairs < 256 && 5 * blk_min >= 4 * blk_max) ||
-                                       blk_sum * c.n_kv_heads >= static_cast<int64_t>(kAttnSlots) * blk_max))
-    aa.bps = std::clamp((blk_max + 7) / 8 * 8, kAttnMinBps, kAttnMaxBps);
-  aa.max_splits = attn_splits(b.max_kv_len, aa.bps);
-  aa.part_o = reinterpret_cast<float*>(ws + wl.att_o);
-  aa.part_ml = reinterpret_cast<float2*>(ws + wl.att_ml);
-  aa.counter = reinterpret_cast<int*>(ws + wl.att_cnt);
-  aa.out = fa;
-  aa.out_Rg = Rg;
-  aa.split_stride = aa.max_splits + (cascade ? b.max_pfx_splits : 0);
-  aa.pfx_blocks = cascade ? b.pfx_blocks : nullptr;
-  aa.pfx_splits = cascade ? b.pfx_splits : nullptr;
-  // decode work items launched per (row, KV head): the most splits any
-  // decode row has after its shared prefix (the rest would exit at once)
-  const int dec_splits = std::max(1, (blk_max + aa.bps - 1) / aa.bps);
-  const int pfx_fold = cascade ? b.max_pfx_splits : 0;
-  AttnPrefixArgs ap{};
-  ap.q = q;
-  ap.pool = h.pool;
-  ap.n_blocks = h.n_blocks;
-  ap.Hkv = c.n_kv_heads;
-  ap.G = aa.G;
-  ap.Nq = Nq;
-  ap.block_table = b.block_table;
-  ap.max_blocks = b.max_blocks;
-  ap.row_seq = b.row_seq;
-  ap.items = b.pfx_items;
-  ap.grp_rows = b.grp_rows;
-  ap.grp_info = b.grp_info;
-  ap.pfx_tbl = b.pfx_tbl;
-  ap.scale_log2 = aa.scale_log2;
-  ap.split_stride = aa.split_stride;
-  ap.part_o = aa.part_o;
-  ap.part_ml = aa.part_ml;
-  // prefill rows: causal multi-row work items (keys staged per item in LDS)
-  const bool prefill = h.prefill_attn != 0 && b.n_pre_items > 0 && b.max_kv_len <= kMaxPrefillBlocks * kBlock;
-  AttnPrefillArgs pf{};
-  pf.q = q;
-  pf.pool = h.pool;
-  pf.n_blocks = h.n_blocks;
-  pf.Hkv = c.n_kv_heads;
-  pf.G = aa.G;
-  pf.Nq = Nq;
-  pf.block_table = b.block_table;
-  pf.max_blocks = b.max_blocks;
-  pf.kv_len = b.kv_len;
-  pf.pos = b.pos;
-  pf.items = b.pre_items;
-  pf.scale_log2 = aa.scale_log2;
-  pf.out = fa;
-  pf.out_Rg = Rg;
+  // attention of layers that see every key, planned once; layers with a window
+  // have a plan of their own (the last one is kept, layers come in runs)
+  AttnPlan attn = plan_attn(h, q, fa, Rg, ws, wl, pa.logit_rows == nullptr, 0, 0, h.mass != nullptr);
+  Handle::Span attn_span;
 
   const int rt = h.resid_target;  // -1 no split, 0 the layout's default, else the target
   const GemmPlan p_qkv = plan_gemm(Nq + 2 * Nkv, H, R, EPI_QKV, h.gemm_shape, 0, h.row_tile);
@@ -1190,8 +1483,6 @@ hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
     const bool routed = l >= first_routed;
     const int lr = l - first_routed;
     const uint8_t* mask = routed ? pa.tape_run + static_cast<size_t>(lr) * R : nullptr;
-    aa.run_mask = mask;
-    pf.run_mask = mask;
     // attention block
     if (!normed) TRY(norm(norm_gain(l, false), x, R, Rg, ssq, ssq_parts));
     ga.W = reinterpret_cast<const u4*>(L + h.pl.l.wqkv);
@@ -1209,24 +1500,13 @@ hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
     } else {
       TRY(probed(2, [&](LaunchEvents ev) { return launch_gemm(ga, p_qkv, EPI_QKV, s, ev); }));
     }
-    aa.layer = l;
-    if (cascade) {
-      ap.layer = l;
-      TRY(launch_attn_prefix(ap, b.n_pfx_items, d, s));
+    if (!h.spans.empty() && (h.spans[l].window != attn_span.window || h.spans[l].sinks != attn_span.sinks)) {
+      attn_span = h.spans[l];
+      attn = plan_attn(h, q, fa, Rg, ws, wl, pa.logit_rows == nullptr, attn_span.window, attn_span.sinks,
+                       h.mass != nullptr);
     }
-    if (prefill) {
-      pf.layer = l;
-      TRY(launch_attn_prefill(pf, b.n_pre_items, d, s));
-      aa.rows = b.dec_rows;
-      if (b.n_dec_rows > 0)
-        TRY(probed(4, [&](LaunchEvents ev) { return launch_attn_decode(aa, b.n_dec_rows, dec_splits, pfx_fold, s, ev); }));
-    } else if (b.n_pre_items == 0) {
-      aa.rows = b.dec_rows;  // every row, longest walk first
-      TRY(probed(4, [&](LaunchEvents ev) { return launch_attn_decode(aa, b.n_dec_rows, dec_splits, pfx_fold, s, ev); }));
-    } else {
-      aa.rows = nullptr;
-      TRY(probed(4, [&](LaunchEvents ev) { return launch_attn_decode(aa, R, dec_splits, pfx_fold, s, ev); }));
-    }
+    TRY(probed(4, [&](LaunchEvents ev) { return launch_attn(h, attn, l, mask, ev, s); }));
+    if (h.mass != nullptr) TRY(launch_mass(h, attn, l, h.mass, h.mass_stride, true, s));
     // O projection: x += o Wo^T, then the MLP's RMSNorm
     ga.W = reinterpret_cast<const u4*>(L + h.pl.l.wo);
     ga.X = reinterpret_cast<const u4*>(fa);
@@ -1326,7 +1606,7 @@ hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
   h.counters[0] += 1;
   h.counters[1] += 4 * n_run + 1;
   h.counters[2] += n_run;
-  h.counters[3] = aa.max_splits;
+  h.counters[3] = attn.dec.max_splits;
   h.counters[4] = p_d.n_groups;
   h.counters[5] = 0;
   return hipSuccess;

@@ -5,6 +5,27 @@
 
 namespace vsk {
 
+// The blocks that rows see through a window with sinks, as one list: the ns
+// blocks that hold the first `sinks` keys, then blocks wb .. of the window (up
+// to the last row's block).  With window 0, or where the two runs meet, ns
+// continues into wb and the list is the sequence's own blocks from its start.
+struct SpanWalk {
+  int lo;  // first key of the window of the first row (0: all of them)
+  int ns, wb;
+  int nv;  // blocks of the list
+  __host__ __device__ int block(int v) const { return v < ns ? v : v - ns + wb; }
+};
+// Rows with first_end .. last_end keys (position + 1).
+__host__ __device__ inline SpanWalk span_walk(int first_end, int last_end, int window, int sinks) {
+  SpanWalk g;
+  g.lo = window > 0 && first_end > window ? first_end - window : 0;
+  g.wb = g.lo / kBlock;
+  const int sb = (sinks + kBlock - 1) / kBlock;
+  g.ns = sb < g.wb ? sb : g.wb;
+  g.nv = g.ns + (last_end + kBlock - 1) / kBlock - g.wb;
+  return g;
+}
+
 struct AttnArgs {
   const uint16_t* q;  // [R][Nq] bf16
   const uint16_t* pool;
@@ -32,10 +53,17 @@ struct AttnArgs {
   // row reads no KV and its attention output is zero (Algorithm 1)
   const uint8_t* run_mask;
   int kv_once;  // 1: most KV blocks of the launch are read by one row only (non-temporal loads)
+  // general walk (launch_attn_decode with `span`): the row at position p sees
+  // keys p - window + 1 .. p (0: every key) and keys 0 .. sinks - 1;
+  // out_Rg 0 stores the output row-major ([R][Nq]); ml (nullable) receives
+  // each (row, query head)'s softmax maximum (base 2) and 1 / sum
+  int window, sinks;
+  float2* ml;  // [R][Nq / hd]
 };
 
 // Causal attention of prefill rows (see k_attn_prefill).
 constexpr int kMaxPrefillBlocks = 512;  // key blocks a prefill work item can stage (8192 positions)
+constexpr int kMaxSpanBlocks = 1024;    // a general one (16384 positions, the most a model can have)
 struct AttnPrefillArgs {
   const uint16_t* q;  // [R][Nq] bf16
   const uint16_t* pool;
@@ -49,6 +77,25 @@ struct AttnPrefillArgs {
   uint16_t* out;  // o frags (K = Nq)
   int out_Rg;
   const uint8_t* run_mask;  // routed layer (nullable): as in AttnArgs
+  int window, sinks;        // general walk: as in AttnArgs
+  float2* ml;
+};
+
+// Attention weight per key (see k_attn_mass).
+struct AttnMassArgs {
+  const uint16_t* q;  // [R][Nq] bf16
+  const uint16_t* pool;
+  int layer, n_blocks, Hkv, G, Nq;
+  const int32_t* block_table;  // [n_seqs][max_blocks]
+  int max_blocks;
+  const int32_t* kv_len;  // [n_seqs]
+  const int32_t* cu_q;    // [n_seqs + 1]
+  float scale_log2;
+  int window, sinks;
+  const float2* ml;  // [R][Nq / hd], as the attention of these rows left them
+  float* mass;       // [n_seqs][stride]
+  int64_t stride;
+  int add;  // 0: mass = the weights, 1: mass += them
 };
 
 // Shared-prefix attention: each work item reads a run of a group's prefix
@@ -73,9 +120,11 @@ struct AttnPrefixArgs {
 // grid_splits: split work items launched per (row, KV head), at least the
 // most any row has after its shared prefix and at most a.max_splits.
 // max_pfx_splits: the most prefix partials any row folds in.
+// span: the general walk (window, sinks, row-major output, ml).
 hipError_t launch_attn_decode(const AttnArgs& a, int n_rows, int grid_splits, int max_pfx_splits, hipStream_t s,
-                              LaunchEvents ev = {});
+                              LaunchEvents ev = {}, bool span = false);
 hipError_t launch_attn_prefix(const AttnPrefixArgs& a, int n_items, int head_dim, hipStream_t s);
-hipError_t launch_attn_prefill(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s);
+hipError_t launch_attn_prefill(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s, bool span = false);
+hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, int max_kv_len, int head_dim, hipStream_t s);
 
 }  // namespace vsk

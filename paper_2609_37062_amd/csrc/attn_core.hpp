@@ -80,9 +80,14 @@ __device__ __forceinline__ int pair_v_index(int lane) { return lane & 31; }
 // significant bits (each term is the bf16 rounding of what the previous
 // ones left over); the products of the terms are accumulated in float32.
 constexpr int kPTerms = 3;
-struct PTerms {
-  u32x4 t[kPTerms];
+// The general walks (windows, sinks, weights per token) take two: 16 bits of a
+// probability, where the output that they end in keeps 8.
+constexpr int kSpanPTerms = 2;
+template <int NT>
+struct PTermsOf {
+  u32x4 t[NT];
 };
+typedef PTermsOf<kPTerms> PTerms;
 
 // One step over the keys at positions t0 .. t0 + 31, in two phases so that a
 // caller streaming K and V through registers can reload K as soon as the
@@ -114,26 +119,23 @@ struct PTerms {
 // without fmas); the others, which wait for memory, never do (8B at 37 rows of
 // 100-6,000 tokens 845, 850 and 846).
 constexpr float kRoundedScores = 0x1p23f;
-template <int D, bool MASK, bool FULL>
-__device__ __forceinline__ void pair_scores(const u32x4 (&qf)[D / 32], const u32x4 (&kg)[2][D / 32], int t0,
-                                            int t_end, int lim, float sc, float& m, float& l, PTerms& pp,
-                                            float& alpha) {
+// S = K q of a step, the two groups of keys.
+template <int D>
+__device__ __forceinline__ void pair_qk(const u32x4 (&qf)[D / 32], const u32x4 (&kg)[2][D / 32], f32x4& s0, f32x4& s1) {
   constexpr int KC = D / 32;
-  f32x4 s0 = f32x4{0.f, 0.f, 0.f, 0.f}, s1 = s0;
+  s0 = f32x4{0.f, 0.f, 0.f, 0.f};
+  s1 = s0;
 #pragma unroll
   for (int c = 0; c < KC; ++c) s0 = mfma_16x16x32(kg[0][c], qf[c], s0);
 #pragma unroll
   for (int c = 0; c < KC; ++c) s1 = mfma_16x16x32(kg[1][c], qf[c], s1);
-  if constexpr (!FULL) {
-    // keys tv .. tv + 7 of this lane: those below `end` count
-    const int tv = t0 + 8 * ((threadIdx.x & 63) >> 4);
-    const int end = MASK ? min(t_end, lim + 1) : t_end;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      s0[r] = tv + r < end ? s0[r] : -INFINITY;
-      s1[r] = tv + 4 + r < end ? s1[r] : -INFINITY;
-    }
-  }
+}
+
+// The softmax step over a step's (masked) scores.  FMA: below kRoundedScores
+// the exponents are taken with fmas.
+template <bool FMA, int NT>
+__device__ __forceinline__ void pair_softmax(const f32x4& s0, const f32x4& s1, float sc, float& m, float& l,
+                                             PTermsOf<NT>& pp, float& alpha) {
   float mx = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
   mx = max_xor32(max_xor16(mx));
   const float m_new = fmaxf(m, mx * sc);
@@ -142,7 +144,7 @@ __device__ __forceinline__ void pair_scores(const u32x4 (&qf)[D / 32], const u32
   // below 2^-126 (flushed to 0) is negligible beside the maximum's 1
   alpha = __builtin_amdgcn_exp2f(m - mb);
   float p[8], ps[2] = {0.f, 0.f};
-  if (!MASK || __builtin_expect(__any(fabsf(mb) >= kRoundedScores), 0)) {
+  if (!FMA || __builtin_expect(__any(fabsf(mb) >= kRoundedScores), 0)) {
     // both sides of the difference rounded alike, so the maximum's is 0
 #pragma clang fp contract(off)
 #pragma unroll
@@ -169,7 +171,7 @@ __device__ __forceinline__ void pair_scores(const u32x4 (&qf)[D / 32], const u32
   for (int j = 0; j < 4; ++j) {
     float r0 = p[2 * j], r1 = p[2 * j + 1];
 #pragma unroll
-    for (int t = 0; t < kPTerms; ++t) {
+    for (int t = 0; t < NT; ++t) {
       pp.t[t][j] = pack_bf2(r0, r1);
       r0 -= bf2f(pp.t[t][j]);
       r1 -= __uint_as_float(pp.t[t][j] & 0xffff0000u);
@@ -177,8 +179,75 @@ __device__ __forceinline__ void pair_scores(const u32x4 (&qf)[D / 32], const u32
   }
 }
 
+template <int D, bool MASK, bool FULL>
+__device__ __forceinline__ void pair_scores(const u32x4 (&qf)[D / 32], const u32x4 (&kg)[2][D / 32], int t0,
+                                            int t_end, int lim, float sc, float& m, float& l, PTerms& pp,
+                                            float& alpha) {
+  f32x4 s0, s1;
+  pair_qk<D>(qf, kg, s0, s1);
+  if constexpr (!FULL) {
+    // keys tv .. tv + 7 of this lane: those below `end` count
+    const int tv = t0 + 8 * ((threadIdx.x & 63) >> 4);
+    const int end = MASK ? min(t_end, lim + 1) : t_end;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      s0[r] = tv + r < end ? s0[r] : -INFINITY;
+      s1[r] = tv + 4 + r < end ? s1[r] : -INFINITY;
+    }
+  }
+  pair_softmax<MASK>(s0, s1, sc, m, l, pp, alpha);
+}
+
+// Which of a lane's eight keys t .. t + 7 a row sees that has `end` keys and
+// whose window starts at key lo (bit i: key t + i).  The keys below `sinks`
+// stay visible.
+__device__ __forceinline__ uint32_t span_bits(int t, int end, int lo, int sinks) {
+  auto below = [&](int n) { return n <= t ? 0u : n - t >= 8 ? 0xffu : (1u << (n - t)) - 1u; };
+  return below(end) & (~below(lo) | below(sinks));
+}
+
+// The scores of a step of a general walk: keys whose bit is clear do not count.
+__device__ __forceinline__ void span_mask(uint32_t bits, f32x4& s0, f32x4& s1) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    s0[r] = bits >> r & 1u ? s0[r] : -INFINITY;
+    s1[r] = bits >> (4 + r) & 1u ? s1[r] : -INFINITY;
+  }
+}
+
+// V rows of the keys whose bit is clear become zero (a zero probability times
+// a NaN or an infinity there would be NaN).
+template <int D>
+__device__ __forceinline__ void span_zero_v(u32x4 (&vt)[D / 16], uint32_t bits) {
+  uint32_t mk[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    mk[j] = (bits >> (2 * j) & 1u ? 0x0000ffffu : 0u) | (bits >> (2 * j + 1) & 1u ? 0xffff0000u : 0u);
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vt[c][j] &= mk[j];
+}
+
 // The sum over a walk's keys from the four lanes of a column.
 __device__ __forceinline__ float walk_sum(float l) { return add_xor32(add_xor16(l)); }
+
+// O = alpha O + V^T P^T.  The lane holds O[column lane % 16][dim 16c + 4 (lane
+// / 16) + r]; the terms outermost: consecutive MFMAs then add into different
+// accumulators.
+template <int D, int NT>
+__device__ __forceinline__ void pair_pv_add(const u32x4 (&vt)[D / 16], const PTermsOf<NT>& pp, float alpha,
+                                            f32x4 (&o)[D / 16]) {
+  constexpr int VC = D / 16;
+  if (__any(alpha != 1.f)) {  // a column's maximum moved (x * 1 is x: skipping changes no bit)
+#pragma unroll
+    for (int c = 0; c < VC; ++c) o[c] *= alpha;
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int c = 0; c < VC; ++c) o[c] = mfma_16x16x32(vt[c], pp.t[t], o[c]);
+}
 
 // pair_pv: O = alpha O + V^T P^T from vt[c] (the V^T operands).  V rows of
 // keys at t >= t_end are zeroed first: a slot past the end of a sequence may
@@ -198,16 +267,7 @@ __device__ __forceinline__ void pair_pv(u32x4 (&vt)[D / 16], int t0, int t_end, 
 #pragma unroll
       for (int j = 0; j < 4; ++j) vt[c][j] &= mk[j];
   }
-  if (__any(alpha != 1.f)) {  // a column's maximum moved (x * 1 is x: skipping changes no bit)
-#pragma unroll
-    for (int c = 0; c < VC; ++c) o[c] *= alpha;
-  }
-  // lane holds O[column lane % 16][dim 16c + 4 (lane / 16) + r]; the terms
-  // outermost: consecutive MFMAs then add into different accumulators
-#pragma unroll
-  for (int t = 0; t < kPTerms; ++t)
-#pragma unroll
-    for (int c = 0; c < VC; ++c) o[c] = mfma_16x16x32(vt[c], pp.t[t], o[c]);
+  pair_pv_add<D>(vt, pp, alpha, o);
 }
 
 // WT: the attention output is stored write-through (sc1), so that other
@@ -215,7 +275,10 @@ __device__ __forceinline__ void pair_pv(u32x4 (&vt)[D / 16], int t0, int t_end, 
 // FOLD2: a wave loads two shared-prefix partials before folding either (one
 // round trip per two; 186 instead of 167 registers at head_dim 128), for
 // passes with more prefix partials per row than waves.
-template <int D, bool WT, int NW, bool FOLD2 = false, bool NTKV = true>
+// SPAN: the general walk (AttnArgs::window, sinks, ml, row-major output): the
+// wave's blocks are a run of the row's SpanWalk list, and a step is full
+// where both of its blocks are visible whole.
+template <int D, bool WT, int NW, bool FOLD2 = false, bool NTKV = true, bool SPAN = false>
 __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, int split, AttnLds<D, NW>& sm) {
   constexpr int KC = D / 32;  // K chunks (1 KiB) per block
   constexpr int VC = D / 16;  // V chunks (512 B) per block
@@ -224,15 +287,21 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   const int lane = tid & 63;
   const int w = tid >> 6;
   const int G = a.G;
+  auto out_index = [&](int col) {  // 4 consecutive columns of an output row are consecutive
+    if (SPAN && a.out_Rg == 0) return static_cast<size_t>(row) * a.Nq + col;
+    return frag_index(row, col, a.out_Rg);
+  };
   // routed layer: a Project-Only row reads no KV and emits zero (its own K,V
   // were written by the projection like every row's); split 0 stores it
   if (a.run_mask != nullptr && a.run_mask[row] == 0) {
     const int hz = lane & 15, qz = lane >> 4;
     if (split == 0 && w == 0 && hz < G) {
       const int col0 = (hk * G + hz) * D;
+      if constexpr (SPAN)  // (its weights are all zero: 2^(s - inf))
+        if (a.ml != nullptr && qz == 0) a.ml[static_cast<size_t>(row) * (a.Hkv * G) + hk * G + hz] = make_float2(INFINITY, 0.f);
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
-        const size_t i0 = frag_index(row, col0 + 16 * c + 4 * qz, a.out_Rg);
+        const size_t i0 = out_index(col0 + 16 * c + 4 * qz);
         const u32x2 zero = u32x2{0u, 0u};
         if constexpr (WT) store_wt(a.out + i0, zero);
         else *reinterpret_cast<u32x2*>(a.out + i0) = zero;
@@ -241,7 +310,9 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
     return;
   }
   const int kv_len = a.pos[row] + 1;
-  const int nb = (kv_len + kBlock - 1) / kBlock;
+  SpanWalk span{};
+  if constexpr (SPAN) span = span_walk(kv_len, kv_len, a.window, a.sinks);
+  const int nb = SPAN ? span.nv : (kv_len + kBlock - 1) / kBlock;
   // a shared prefix of P blocks is read by the prefix work items; this row's
   // splits cover blocks P.. and follow the prefix partials
   const int P = a.pfx_blocks != nullptr ? a.pfx_blocks[row] : 0;
@@ -253,7 +324,7 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   const int b_lo = P + split * a.bps;
   const int b_hi = min(nb, b_lo + a.bps);
   // the split's block-table entries, staged once for all waves
-  for (int i = tid; i < b_hi - b_lo; i += blockDim.x) sm.tbl[i] = table[b_lo + i];
+  for (int i = tid; i < b_hi - b_lo; i += blockDim.x) sm.tbl[i] = table[SPAN ? span.block(b_lo + i) : b_lo + i];
   const int h = lane & 15;       // query head within the group (valid if h < G)
   const int quad = lane >> 4;    // token quarter / k sub-range
   // q as the B operand of S = K q: lane holds q[h][32c + 8*quad .. +7]
@@ -367,14 +438,40 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   auto step = [&](u32x4 (&vc)[VC], u32x4 (&vn)[VC], int p, auto last_c) {
     constexpr bool LAST = decltype(last_c)::value;  // the range's last pair: its keys may end inside it
     const int t0 = t_first + 2 * kBlock * p;
-    PTerms pp;
     float alpha;
-    pair_scores<D, false, !LAST>(qf, kg, t0, t_end, 0, sc, m, l, pp, alpha);
-    if constexpr (!LAST) {
-      load_k(kg, p + 1, cnt, w_lo);
-      load_v(vn, p + 1, cnt, w_lo);
+    if constexpr (SPAN) {
+      const int va = __builtin_amdgcn_readfirstlane(b_lo + w_lo + 2 * p);
+      const int ba = span.block(va), bb = span.block(va + 1);
+      auto whole = [&](int b) {
+        return kBlock * (b + 1) <= kv_len && (kBlock * b >= span.lo || kBlock * (b + 1) <= a.sinks);
+      };
+      const bool full = 2 * p + 1 < cnt && whole(ba) && whole(bb);  // (uniform)
+      // the lane's keys are in the step's block quad / 2, which may lie past the wave's range
+      uint32_t bits = 0xffu;
+      if (!full)
+        bits = 2 * p + (quad >> 1) < cnt
+                   ? span_bits(kBlock * (quad >> 1 ? bb : ba) + 8 * (quad & 1), kv_len, span.lo, a.sinks)
+                   : 0u;
+      f32x4 s0, s1;
+      pair_qk<D>(qf, kg, s0, s1);
+      if (!full) span_mask(bits, s0, s1);
+      PTermsOf<kSpanPTerms> pp;
+      pair_softmax<false>(s0, s1, sc, m, l, pp, alpha);
+      if constexpr (!LAST) {
+        load_k(kg, p + 1, cnt, w_lo);
+        load_v(vn, p + 1, cnt, w_lo);
+      }
+      if (!full) span_zero_v<D>(vc, bits);
+      pair_pv_add<D>(vc, pp, alpha, o);
+    } else {
+      PTerms pp;
+      pair_scores<D, false, !LAST>(qf, kg, t0, t_end, 0, sc, m, l, pp, alpha);
+      if constexpr (!LAST) {
+        load_k(kg, p + 1, cnt, w_lo);
+        load_v(vn, p + 1, cnt, w_lo);
+      }
+      pair_pv<D, !LAST>(vc, t0, t_end, pp, alpha, o);
     }
-    pair_pv<D, !LAST>(vc, t0, t_end, pp, alpha, o);
   };
   constexpr auto kMore = std::false_type{};
   constexpr auto kLast = std::true_type{};
@@ -424,10 +521,12 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
     if (w == 0 && h < G) {
       const float inv = 1.f / l;
       const int col0 = (hk * G + h) * D;
+      if constexpr (SPAN)
+        if (a.ml != nullptr && quad == 0) a.ml[static_cast<size_t>(row) * (a.Hkv * G) + hk * G + h] = make_float2(m, inv);
 #pragma unroll
       for (int c = 0; c < VC; ++c) {
         const int e = 16 * c + 4 * quad;
-        const size_t i0 = frag_index(row, col0 + e, a.out_Rg);  // 4 consecutive dims, same 8-group
+        const size_t i0 = out_index(col0 + e);  // 4 consecutive dims, same 8-group
         u32x2 pk;
         pk[0] = pack_bf2(o[c][0] * inv, o[c][1] * inv);
         pk[1] = pack_bf2(o[c][2] * inv, o[c][3] * inv);
@@ -515,7 +614,10 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
     for (int u = 0; u < 2; ++u) {
       if (u == 1 && !two) break;
       const uint32_t ob = f2bf(acc[u] * (1.f / L[u]));
-      uint16_t* dst = a.out + frag_index(row, (hk * G + hh[u]) * D + ee[u], a.out_Rg);
+      uint16_t* dst = a.out + out_index((hk * G + hh[u]) * D + ee[u]);
+      if constexpr (SPAN)
+        if (a.ml != nullptr && ee[u] == 0)
+          a.ml[static_cast<size_t>(row) * (a.Hkv * G) + hk * G + hh[u]] = make_float2(M[u], 1.f / L[u]);
       if constexpr (WT) store_wt16(dst, ob);
       else *dst = static_cast<uint16_t>(ob);
     }

@@ -96,7 +96,10 @@ struct BatchDev {
   const int32_t* cu_q = nullptr;
   const int32_t* row_seq = nullptr;
   const int32_t* pos = nullptr;
+  const int32_t* rot = nullptr;
   const int32_t* slot = nullptr;
+  int32_t max_position = 0;
+  bool evicted = false;
   // shared prefixes (decode passes): see BatchHost
   const int32_t* pfx_blocks = nullptr;
   const int32_t* pfx_splits = nullptr;
@@ -193,6 +196,15 @@ struct Handle {
   int prefill_attn = 1;   // prefill rows through the causal multi-row kernel (0: one row per work item)
   int xcd_remap = 1;      // row-tiled projections: XCD-aware workgroup order (0: dispatch order)
   int row_tile = 0;       // row-tiled projections: 16-row groups per tile (0 auto; 6, 7, 8 or 11)
+  // what each layer's attention sees (vsk_set_span; empty: every key), and the
+  // weights per token that the passes leave (vsk_set_mass)
+  struct Span {
+    int32_t window = 0, sinks = 0;
+  };
+  std::vector<Span> spans;  // [n_layers] or empty
+  float* mass = nullptr;
+  int32_t mass_seqs = 0;
+  int64_t mass_stride = 0;
   int step_wgs = -1;   // workgroups of a persistent launch on this device (0: not runnable; -1: not queried)
   uint64_t* step_trace = nullptr;  // measurement: timestamp buffer of the persistent kernel
   size_t step_trace_cap = 0;       // its capacity in uint64
@@ -250,6 +262,10 @@ struct PassArgs {
   bool clear_counters = false;
 };
 hipError_t run_pass(Handle& h, const PassArgs& a, hipStream_t s);
+// One layer's attention of the uploaded batch for given queries, row-major, with
+// the bound workspace (mass nullable).
+hipError_t run_attend(Handle& h, int layer, const uint16_t* q, uint16_t* out, int window, int sinks, float* mass,
+                      int64_t stride, bool add, hipStream_t s);
 // True when run_pass would take the persistent step kernel for this pass.
 bool step_eligible(Handle& h, const PassArgs& a);
 

@@ -86,6 +86,12 @@ SIGNATURES = [
     ("vsk_decode_step_scratch", C.c_int, [_VP, _VP, _VP, _VP, _VP]),
     ("vsk_prefill_chunk", C.c_int, [_VP, _VP, _VP, _I32, _VP, _VP, _VP, _SZ, _VP]),
     ("vsk_argmax_sample", C.c_int, [_VP, _I32, _I32, _I32, _VP, _VP, _VP]),
+    ("vsk_attend", C.c_int, [_VP, _I32, _VP, _VP, _I32, _I32, _VP, _I32, _I32, _VP, _SZ, _VP]),
+    ("vsk_set_span", C.c_int, [_VP, _I32, _I32, _I32]),
+    ("vsk_set_mass", C.c_int, [_VP, _VP, _I32, _I32]),
+    ("vsk_kv_evict_bytes", _SZ, [_VP, _PI64, _PI32, _I32]),
+    ("vsk_kv_evict", C.c_int, [_VP, _PI64, _PI64, _PI32, _I32, _I32, _I32, _VP, _I32, _VP, _VP, _VP, _I32, _VP, _SZ,
+                               _VP]),
     ("vsk_set_tuning", C.c_int, [_VP, _I32, _I32]),
     ("vsk_residual_copy", C.c_int, [_VP, _VP, _I32, _VP]),
     ("vsk_routed_weight_bytes", _SZ, [C.POINTER(ModelCfg), _I32, _I32]),
@@ -337,6 +343,38 @@ class Engine:
                       stream=None):
         self._ck(lib().vsk_prefill_chunk(self.h, ids_ptr, logit_rows_ptr, n_logit_rows, logits_ptr, next_ids_ptr,
                                          ws_ptr, ws_bytes, stream), "prefill_chunk")
+
+    # -- bounded cache
+    def attend(self, layer, q_ptr, o_ptr, ws_ptr, ws_bytes, window=0, sinks=0, mass_ptr=None, mass_stride=0,
+               mass_add=False, stream=None):
+        """Attention of the batch's rows over one layer's cache; mass_ptr: the weight of each cached token."""
+        self._ck(lib().vsk_attend(self.h, layer, q_ptr, o_ptr, window, sinks, mass_ptr, mass_stride, int(mass_add),
+                                  ws_ptr, ws_bytes, stream), "attend")
+
+    def set_span(self, layer, window, sinks=0):
+        """Window and sinks of a layer's attention in the passes (layer -1: every layer; window 0: every key)."""
+        self._ck(lib().vsk_set_span(self.h, layer, window, sinks), "set_span")
+
+    def set_mass(self, mass_ptr, n_seqs=0, stride=0):
+        """Passes add the attention weight of each cached token to [n_seqs][stride] floats (None: no longer)."""
+        self._ck(lib().vsk_set_mass(self.h, mass_ptr, n_seqs, stride), "set_mass")
+
+    def kv_evict_bytes(self, src, keep):
+        s = np.ascontiguousarray(src, np.int64)
+        k = np.ascontiguousarray(keep, np.int32)
+        return lib().vsk_kv_evict_bytes(self.h, _p64(s), _p32(k), len(s))
+
+    def kv_evict(self, dst, src, keep, sinks, recent, mass_ptr, mass_stride, meta_ptr, meta_bytes, mass_out_ptr=None,
+                 kept_ptr=None, slots_ptr=None, out_stride=0, stream=None):
+        """Sequences dst take the keep[i] most attended tokens of sequences src."""
+        d = np.ascontiguousarray(dst, np.int64)
+        s = np.ascontiguousarray(src, np.int64)
+        k = np.ascontiguousarray(keep, np.int32)
+        if not len(d) == len(s) == len(k):
+            raise VskError(-1, "kv_evict: dst, src and keep differ in length")
+        self._ck(lib().vsk_kv_evict(self.h, _p64(d), _p64(s), _p32(k), len(s), sinks, recent, mass_ptr, mass_stride,
+                                    mass_out_ptr, kept_ptr, slots_ptr, out_stride, meta_ptr, meta_bytes, stream),
+                 "kv_evict")
 
     # -- routed mode
     def routed_weight_bytes(self, first_routed, proj_ffn):

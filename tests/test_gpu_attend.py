@@ -1,0 +1,236 @@
+"""vsk_attend on the device against float64: single tokens and prompt rows, full
+and windowed, one split and several, every head layout, values that are not
+finite where a row does not see them, and the weight per cached token."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from cache_case import BLOCK, Cache, attend_ref, check, visible  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+SPANS = [(0, 0), (1, 0), (1, 5), (16, 4), (17, 16), (40, 33), (256, 4), (1000, 100)]
+
+
+@pytest.mark.parametrize("kv,group,hd", [(1, 1, 64), (2, 16, 64), (4, 3, 128), (8, 4, 128), (3, 7, 128), (1, 16, 128)])
+@pytest.mark.parametrize("window,sinks", SPANS)
+def test_single_tokens(kv, group, hd, window, sinks):
+    print(f"[gpu] attend decode kv={kv} group={group} hd={hd} window={window} sinks={sinks}", flush=True)
+    c = Cache(kv, group, hd, [1, 2, 15, 16, 17, 31, 32, 33, 48, 63, 129, 300, 777], seed=kv * 100 + group)
+    c.batch(range(13), [1] * 13)
+    c.attend(window=window, sinks=sinks)
+    check(c, window, sinks)
+    c.close()
+
+
+@pytest.mark.parametrize("bps", [0, 8, 16, 512])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 4), (1500, 130)])
+def test_single_tokens_split_and_joined(bps, window, sinks):
+    print(f"[gpu] attend splits bps={bps} window={window} sinks={sinks}", flush=True)
+    c = Cache(2, 4, 128, [2000, 5, 1023, 1537, 4099], seed=3)
+    c.eng.set_tuning(0, bps)
+    c.batch(range(5), [1] * 5)
+    for _ in range(2):  # the second call finds the arrival counters at zero again
+        c.o.fill_(-7.0)
+        c.attend(window=window, sinks=sinks)
+        check(c, window, sinks)
+    c.close()
+
+
+@pytest.mark.parametrize("kv,group,hd", [(1, 1, 64), (2, 16, 64), (2, 3, 128), (4, 4, 128), (1, 7, 128)])
+@pytest.mark.parametrize("window,sinks", SPANS)
+def test_prompt_rows(kv, group, hd, window, sinks):
+    print(f"[gpu] attend prompt kv={kv} group={group} hd={hd} window={window} sinks={sinks}", flush=True)
+    c = Cache(kv, group, hd, [2, 16, 37, 130, 411, 290], seed=kv * 10 + group)
+    c.batch(range(6), [2, 16, 37, 33, 200, 1])  # fresh, later chunks, and one decode row
+    c.attend(window=window, sinks=sinks)
+    check(c, window, sinks)
+    c.close()
+
+
+def test_prompt_rows_one_work_item_a_row():
+    c = Cache(2, 4, 128, [70, 300], seed=5)
+    c.eng.set_tuning(6, 0)
+    c.batch([0, 1], [70, 3])
+    for window, sinks in [(0, 0), (20, 3)]:
+        c.attend(window=window, sinks=sinks)
+        check(c, window, sinks)
+    c.close()
+
+
+def test_long_cache():
+    """16384 cached tokens: 1024 blocks, single tokens and a prompt's last rows."""
+    c = Cache(1, 2, 64, [16384, 16383], seed=6)
+    for q_lens in ([1, 1], [3, 40]):
+        c.batch([0, 1], q_lens)
+        for window, sinks in [(0, 0), (9000, 70)]:
+            c.attend(window=window, sinks=sinks)
+            check(c, window, sinks)
+    c.close()
+
+
+def test_a_shared_prefix_is_the_same_attention():
+    """Sequences whose tables start with the same blocks, decoding."""
+    c = Cache(2, 4, 128, [200, 150, 170], seed=7, tables=None, spare=64)
+    # sequences 3, 4 hold sequence 0's first 9 blocks and own blocks behind them
+    free = [b for b in range(c.n_blocks) if all(b not in t for t in c.blocks)]
+    for i, n in ((3, 160), (4, 149)):
+        own = -(-(n - 144) // BLOCK)
+        c.eng.seq_create(i)
+        c.eng.seq_set_blocks(i, np.concatenate([c.blocks[0][:9], free[:own]]).astype(np.int32), n)
+        free = free[own:]
+        k = np.concatenate([c.K[0][0][:144], c.K[0][1][:n - 144]])
+        v = np.concatenate([c.V[0][0][:144], c.V[0][1][:n - 144]])
+        c.K[0].append(k)
+        c.V[0].append(v)
+        c.write(0, i, 144)
+    c.batch([0, 1, 3, 2, 4], [1] * 5)
+    assert c.eng.batch_prefix_info()[1] == 1
+    mass = torch.zeros((5, 256), device="cuda")
+    for window, sinks in [(0, 0), (30, 5)]:
+        c.attend(window=window, sinks=sinks, mass=mass)
+        check(c, window, sinks, mass=mass)
+    c.close()
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("prompt", [False, True])
+def test_what_a_row_does_not_see_does_not_matter(bad, prompt):
+    """K and V that are not finite: hidden by the window, or only visible to
+    later rows, whose outputs are then not finite."""
+    print(f"[gpu] attend bad={bad} prompt={prompt}", flush=True)
+    window, sinks = 40, 5
+    c = Cache(2, 4, 128, [300, 97], seed=8)
+    ql = [60, 50] if prompt else [1, 1]
+    c.batch([0, 1], ql)
+    c.attend(window=window, sinks=sinks)
+    good = c.out()
+    mass = torch.zeros((2, 300), device="cuda")
+    # hidden from every row: behind the sinks, before the first row's window
+    for s in (0, 1):
+        n = len(c.K[0][s])
+        lo = n - ql[s] - window
+        if lo > 8:
+            c.K[0][s][5:lo] = bad
+            c.V[0][s][5:lo] = bad
+            c.write(0, s)
+    c.attend(window=window, sinks=sinks, mass=mass)
+    np.testing.assert_array_equal(c.out(), good)
+    m = mass.cpu().numpy()
+    assert np.isfinite(m).all() and (m[0, 5:300 - ql[0] - window] == 0).all()
+    if prompt:
+        # one key of the chunk itself: rows before it, and rows whose window has
+        # left it behind, do not see it
+        key = 300 - 60 + 7
+        for which in (c.V, c.K):
+            keep = which[0][0][key].copy()
+            which[0][0][key] = bad
+            c.write(0, 0)
+            c.attend(window=window, sinks=sinks)
+            o = c.out()
+            for r in range(60):
+                p = 240 + r
+                if not visible(p, 300, window, sinks)[key]:
+                    np.testing.assert_array_equal(o[r], good[r], err_msg=str(r))
+                elif which is c.V:
+                    assert not np.isfinite(o[r]).any(), r
+            which[0][0][key] = keep
+            c.write(0, 0)
+    c.close()
+
+
+@pytest.mark.parametrize("q_lens", [[1, 1, 1, 1], [1, 40, 17, 2], [300, 33, 200, 1]])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (20, 3), (100, 40)])
+def test_weights_per_token(q_lens, window, sinks):
+    print(f"[gpu] attend mass q_lens={q_lens} window={window} sinks={sinks}", flush=True)
+    c = Cache(4, 3, 64, [300, 40, 217, 33], seed=9)
+    c.batch(range(4), q_lens)
+    mass = torch.full((4, 333), 0.5, device="cuda")
+    c.attend(window=window, sinks=sinks, mass=mass)
+    ref = check(c, window, sinks, mass=mass)
+    m = mass.cpu().numpy()
+    for i, n in enumerate(c.lens):
+        assert (m[i, n:] == 0.5).all(), "entries behind the sequence"
+        assert abs(m[i, :n].sum() - q_lens[i] * 12) < 1e-3 * q_lens[i] * 12  # every row and head gives 1
+        assert ref[i][1].shape == (n,)
+    base = mass.cpu().numpy().astype(np.float64)
+    c.attend(window=window, sinks=sinks, mass=mass, add=True)
+    check(c, window, sinks, mass=mass, base=base)
+    again = torch.zeros_like(mass)
+    c.attend(window=window, sinks=sinks, mass=again)
+    third = torch.zeros_like(mass)
+    c.attend(window=window, sinks=sinks, mass=third)
+    assert torch.equal(again, third), "the same sums on every call"
+    c.close()
+
+
+def test_large_scores_stay_finite():
+    """Scores of 2^26: one key takes all the weight."""
+    c = Cache(2, 4, 128, [200, 90], seed=10, scale=2.0 ** 24)
+    c.batch([0, 1], [40, 1])
+    mass = torch.zeros((2, 200), device="cuda")
+    for window, sinks in [(0, 0), (30, 2)]:
+        c.attend(window=window, sinks=sinks, mass=mass)
+        o = c.out()
+        assert np.isfinite(o).all()
+        r0 = 0
+        for i, ql in enumerate(c.q_lens):
+            n = c.lens[i]
+            q = c.q[r0:r0 + ql].double().numpy()
+            for r in range(ql):
+                see = np.flatnonzero(visible(n - ql + r, n, window, sinks))
+                for h in range(8):
+                    s = c.K[0][i][see, h // 4].astype(np.float64) @ q[r, h]
+                    top = np.sort(s)[-2:] if len(see) > 1 else np.array([-np.inf, s[0]])
+                    if top[1] - top[0] < 2.0 ** 14:  # (float32 sums tell these apart)
+                        continue
+                    np.testing.assert_array_equal(o[r0 + r, h], c.V[0][i][see[s.argmax()], h // 4])
+            m = mass[i, :n].cpu().numpy()
+            assert np.isfinite(m).all() and abs(m.sum() - ql * 8) < 1e-3 * ql * 8
+            r0 += ql
+    c.close()
+
+
+def test_layers_streams_and_replays():
+    """Each layer reads its own cache; a call on another stream, and one in a
+    captured graph, replayed with eager work between, give the same bits."""
+    c = Cache(2, 4, 128, [1500, 700, 90], layers=3, seed=11)
+    c.batch(range(3), [1, 30, 1])
+    eager = []
+    for l in range(3):
+        c.attend(layer=l, window=333, sinks=4)
+        check(c, 333, 4, layer=l)
+        eager.append(c.out())
+    side = torch.cuda.Stream()
+    mass = torch.zeros((3, 1500), device="cuda")
+    with torch.cuda.stream(side):
+        c.attend(layer=1, window=333, sinks=4, mass=mass, stream=side.cuda_stream)
+    np.testing.assert_array_equal(c.out(), eager[1])
+    want = mass.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.attend(layer=1, window=333, sinks=4, mass=mass, stream=torch.cuda.current_stream().cuda_stream)
+    for _ in range(3):
+        c.attend(layer=2, window=333, sinks=4)
+        np.testing.assert_array_equal(c.out(), eager[2])
+        mass.fill_(9.0)
+        g.replay()
+        np.testing.assert_array_equal(c.out(), eager[1])
+        for i, n in enumerate(c.lens):
+            assert torch.equal(mass[i, :n], want[i, :n]) and bool((mass[i, n:] == 9.0).all())
+    c.close()
+
+
+def test_heads_of_one_query_each_and_odd_rows():
+    """A single row of a single head against the formula written out."""
+    c = Cache(1, 1, 128, [50], seed=12)
+    c.batch([0], [1])
+    c.attend(window=9, sinks=2)
+    o, ob, _, _ = attend_ref(c.q.float().numpy(), c.K[0][0], c.V[0][0], 49, 9, 2)
+    assert (np.abs(c.out() - o) <= ob).all()
+    see = [0, 1] + list(range(41, 50))
+    s = c.K[0][0][see, 0].astype(np.float64) @ c.q[0, 0].double().numpy() / np.sqrt(128)
+    w = np.exp(s) / np.exp(s).sum()
+    np.testing.assert_allclose(o[0, 0], w @ c.V[0][0][see, 0], rtol=1e-12, atol=1e-12)
+    c.close()

@@ -1,0 +1,207 @@
+"""vsk_kv_evict on the device: which tokens stay (against a sort on the host), their
+K, V bit for bit, weights and slots, the sources as they were, positions
+afterwards, and calls that must change nothing."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from cache_case import BLOCK, Cache, check  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def evict(c, dst, src, keep, sinks, recent, mass, stride=None, in_place=False, slots=True):
+    """The call and its outputs on the host: kept, slots, mass_out."""
+    from paper_2609_37062_amd.runner import _dev_buffer
+    n = len(src)
+    stride = stride or max(keep) + 3
+    if in_place:
+        stride = mass.shape[1]
+    for d in dst:
+        c.eng.seq_create(d)
+    kept = torch.full((n, stride), -5, dtype=torch.int32, device="cuda")
+    sl = torch.full((n, stride), -5, dtype=torch.int32, device="cuda")
+    out = mass if in_place else torch.full((n, stride), 77.0, device="cuda")
+    nb = c.eng.kv_evict_bytes(src, keep)
+    t, meta = _dev_buffer(nb, "cuda")
+    c.eng.kv_evict(dst, src, keep, sinks, recent, mass.data_ptr(), mass.shape[1], meta, nb, mass_out_ptr=out.data_ptr(),
+                   kept_ptr=kept.data_ptr(), slots_ptr=sl.data_ptr() if slots else None, out_stride=stride, stream=c.sp)
+    torch.cuda.synchronize()
+    return kept.cpu().numpy(), sl.cpu().numpy(), out.cpu().numpy()
+
+
+def kept_ref(m, n, keep, sinks, recent):
+    """Largest weight first, equal ones by index, NaN behind everything."""
+    mid = np.arange(sinks, n - recent)
+    w = m[mid].astype(np.float64)
+    order = mid[np.lexsort((mid, -np.where(np.isnan(w), 0, w), np.isnan(w)))]
+    return np.sort(np.concatenate([np.arange(sinks), order[:keep - sinks - recent], np.arange(n - recent, n)]))
+
+
+def check_evicted(c, dst, src, keep, sinks, recent, m, got):
+    kept, sl, out = got
+    for i, (d, s, k) in enumerate(zip(dst, src, keep)):
+        n = len(c.K[0][s])
+        ref = kept_ref(m[i], n, k, sinks, recent)
+        np.testing.assert_array_equal(kept[i, :k], ref)
+        assert (kept[i, k:] == -5).all() and (sl[i, k:] == -5).all()
+        np.testing.assert_array_equal(out[i, :k], m[i, ref])
+        assert (out[i, k:] == 0).all()
+        assert c.eng.seq_info(d)[0] == k and len(c.eng.seq_info(d)[1]) == -(-k // BLOCK)
+        np.testing.assert_array_equal(sl[i, :k], c.slots(d, k))
+        for l in range(c.layers):
+            K, V = c.read(l, d)
+            np.testing.assert_array_equal(K, c.K[l][s][ref])
+            np.testing.assert_array_equal(V, c.V[l][s][ref])
+            K, V = c.read(l, s)
+            np.testing.assert_array_equal(K, c.K[l][s])
+            np.testing.assert_array_equal(V, c.V[l][s])
+
+
+CASES = [
+    # kv, hd, layers, lens, keep, sinks, recent
+    (1, 64, 1, [1], [1], 0, 0),
+    (1, 64, 1, [2, 17, 16], [1, 1, 1], 0, 1),
+    (2, 128, 2, [50, 33, 16], [20, 17, 16], 4, 5),
+    (4, 64, 3, [300, 299, 18], [100, 1, 18], 0, 0),
+    (2, 128, 1, [4099, 2000], [1000, 1999], 16, 256),
+    (8, 128, 2, [1030, 700, 65], [64, 64, 64], 4, 60),  # nothing chosen by weight
+    (3, 64, 1, [16384, 9001], [5000, 33], 4, 8),
+]
+
+
+@pytest.mark.parametrize("kv,hd,layers,lens,keep,sinks,recent", CASES)
+@pytest.mark.parametrize("weights", ["spread", "zeros", "ties"])
+def test_kept_tokens(kv, hd, layers, lens, keep, sinks, recent, weights):
+    print(f"[gpu] evict kv={kv} hd={hd} lens={lens} keep={keep} {weights}", flush=True)
+    c = Cache(kv, 1, hd, lens, layers=layers, seed=len(lens), spare=1200)
+    n = len(lens)
+    m = np.exp(3 * c.rng.standard_normal((n, max(lens) + 2))).astype(np.float32)
+    if weights == "zeros":
+        m[:] = 0
+    if weights == "ties":
+        m = np.floor(c.rng.random(m.shape) * 4).astype(np.float32)
+    free = c.eng.free_blocks()
+    dst = list(range(n, 2 * n))
+    got = evict(c, dst, list(range(n)), keep, sinks, recent, torch.from_numpy(m).cuda())
+    check_evicted(c, dst, range(n), keep, sinks, recent, m, got)
+    assert c.eng.free_blocks() == free - sum(-(-k // BLOCK) for k in keep)
+    for s in range(n):
+        c.eng.seq_release(s)
+    c.close()
+
+
+def test_weights_of_every_kind():
+    """Signed zeros are equal, infinities order, NaN comes last, negative weights count."""
+    c = Cache(1, 1, 64, [40, 40], seed=3, spare=40)
+    m = np.zeros((2, 40), np.float32)
+    m[0, 3:20] = [np.nan, np.inf, -np.inf, 0.0, -0.0, 0.0, -0.0, 1.0, -1.0, np.nan, 2.0, 2.0, -np.nan, 1e-45, 0.0, np.inf, -2.0]
+    m[0, 20:] = np.nan
+    m[1] = -np.inf
+    m[1, 7] = np.nan
+    for k in (1, 2, 5, 8, 12, 15, 20, 39, 40):
+        dst = [100 + k, 200 + k]
+        got = evict(c, dst, [0, 1], [k, k], 0, 1, torch.from_numpy(m).cuda())
+        check_evicted(c, dst, [0, 1], [k, k], 0, 1, m, got)
+        for d in dst:
+            c.eng.seq_release(d)
+    c.close()
+
+
+def test_in_place_weights_and_no_slots():
+    c = Cache(2, 1, 128, [500, 77, 300], seed=4, spare=60)
+    m = np.abs(c.rng.standard_normal((3, 512))).astype(np.float32)
+    md = torch.from_numpy(m).cuda()
+    kept, sl, out = evict(c, [5, 6, 7], [0, 1, 2], [200, 40, 299], 4, 30, md, in_place=True, slots=False)
+    assert (sl == -5).all()
+    for i, k in enumerate([200, 40, 299]):
+        ref = kept_ref(m[i], [500, 77, 300][i], k, 4, 30)
+        np.testing.assert_array_equal(kept[i, :k], ref)
+        np.testing.assert_array_equal(out[i, :k], m[i, ref])
+        assert (out[i, k:] == 0).all()
+    c.close()
+
+
+def test_one_source_twice_and_shared_blocks():
+    """Two destinations of one source, whose first blocks another sequence shares."""
+    c = Cache(2, 1, 64, [100], seed=5, spare=40)
+    c.eng.seq_create(50)
+    c.eng.seq_share_prefix(50, 0, 96)
+    m = np.abs(c.rng.standard_normal((2, 100))).astype(np.float32)
+    got = evict(c, [1, 2], [0, 0], [30, 60], 2, 8, torch.from_numpy(m).cuda())
+    check_evicted(c, [1, 2], [0, 0], [30, 60], 2, 8, m, got)
+    K, _ = c.read(0, 50)
+    np.testing.assert_array_equal(K, c.K[0][0][:96])
+    c.close()
+
+
+def test_positions_go_on_and_prefixes_are_refused():
+    c = Cache(1, 2, 64, [100, 60], seed=6, spare=40, max_pos=128)
+    m = torch.rand((1, 100), device="cuda")
+    evict(c, [7], [0], [40], 4, 10, m)
+    e = c.eng
+    e.seq_release(0)
+    e.reserve(7, 3)
+    e.batch_build([7, 1], [3, 1])
+    b = e.batch_host()
+    np.testing.assert_array_equal(b["pos"], [100, 101, 102, 59])
+    np.testing.assert_array_equal(b["kv_len"], [43, 60])
+    np.testing.assert_array_equal(b["slot"][:3], c.slots(7, 43)[40:])
+    e.seq_create(8)
+    with pytest.raises(c.vsk.VskError) as x:
+        e.seq_share_prefix(8, 7, 16)
+    assert x.value.code == "STATE"
+    # again, from the shorter cache: what was dropped adds up
+    m2 = torch.rand((1, 43), device="cuda")
+    evict(c, [9], [7], [20], 4, 10, m2)
+    e.reserve(9, 1)
+    e.batch_build([9], [1])
+    assert e.batch_host()["pos"].tolist() == [103]
+    # max_pos bounds positions, not what is cached
+    with pytest.raises(c.vsk.VskError) as x:
+        e.reserve(9, 25)
+    assert x.value.code == "RANGE"
+    e.reserve(9, 24)
+    c.close()
+
+
+def test_attention_over_an_evicted_cache():
+    c = Cache(2, 4, 128, [900, 333], seed=7, spare=80)
+    m = np.abs(c.rng.standard_normal((2, 900))).astype(np.float32)
+    kept, _, _ = evict(c, [2, 3], [0, 1], [201, 100], 4, 64, torch.from_numpy(m).cuda())
+    for i, k in enumerate((201, 100)):
+        c.K[0].append(c.K[0][i][kept[i, :k]])
+        c.V[0].append(c.V[0][i][kept[i, :k]])
+    c.batch([2, 1, 3], [1, 1, 5])
+    for window, sinks in [(0, 0), (50, 4)]:
+        c.attend(window=window, sinks=sinks)
+        check(c, window, sinks)
+    c.close()
+
+
+def test_refused_evictions_change_nothing():
+    c = Cache(1, 1, 64, [100, 20], seed=8, spare=2)
+    m = torch.rand((2, 100), device="cuda")
+    e = c.eng
+    free = e.free_blocks()
+    with pytest.raises(c.vsk.VskError) as x:
+        evict(c, [5, 6], [0, 1], [33, 1], 0, 0, m)  # 4 blocks of 2
+    assert x.value.code == "NOMEM"
+    assert e.free_blocks() == free and e.seq_info(5) == (0, []) and e.seq_info(6) == (0, [])
+    g = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    kept = torch.zeros((1, 32), dtype=torch.int32, device="cuda")
+    nb = e.kv_evict_bytes([0], [16])
+    _t, meta = c.buf(nb, "cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=side):
+        with pytest.raises(c.vsk.VskError) as x:
+            e.kv_evict([5], [0], [16], 0, 0, m.data_ptr(), 100, meta, nb, kept_ptr=kept.data_ptr(), out_stride=32,
+                       stream=torch.cuda.current_stream().cuda_stream)
+        kept.add_(1)
+    assert x.value.code == "STATE" and e.free_blocks() == free and e.seq_info(5) == (0, [])
+    e.kv_evict([5], [0], [16], 0, 0, m.data_ptr(), 100, meta, nb, kept_ptr=kept.data_ptr(), out_stride=32, stream=c.sp)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(kept.cpu().numpy()[0, :16], kept_ref(m[0].cpu().numpy(), 100, 16, 0, 0))
+    c.close()
