@@ -826,20 +826,27 @@ int vsk_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev, int
 }
 
 // Device metadata of an eviction: [n][4] (length, kept, first source block,
-// first destination block), the sources' tables, the destinations'.
-static size_t evict_meta_ints(const vsk_handle* h, const int64_t* src, const int32_t* keep, int32_t n) {
+// first destination block), the sources' tables, the destinations'; and, not
+// uploaded (`blocks` destination blocks' worth), the kept tokens' source slots.
+static size_t evict_meta_ints(const vsk_handle* h, const int64_t* src, const int32_t* keep, int32_t n,
+                              size_t* blocks) {
   size_t ints = 4 * static_cast<size_t>(n);
+  *blocks = 0;
   for (int32_t i = 0; i < n; ++i) {
     const SeqState* s = h->alloc.find(src[i]);
     if (!s || keep[i] < 1 || keep[i] > s->len) return 0;
-    ints += s->blocks.size() + (keep[i] + kBlock - 1) / kBlock;
+    *blocks += (keep[i] + kBlock - 1) / kBlock;
+    ints += s->blocks.size();
   }
-  return ints;
+  return ints + *blocks;
 }
+static size_t evict_meta_bytes(size_t ints, size_t blocks) { return align_up(ints * 4) + align_up(blocks * kBlock * 4); }
 
 size_t vsk_kv_evict_bytes(const vsk_handle* h, const int64_t* src_host, const int32_t* keep_host, int32_t n) {
   if (!h || !h->alloc_ready || !src_host || !keep_host || n < 1) return 0;
-  return align_up(evict_meta_ints(h, src_host, keep_host, n) * 4);
+  size_t blocks = 0;
+  const size_t ints = evict_meta_ints(h, src_host, keep_host, n, &blocks);
+  return ints == 0 ? 0 : evict_meta_bytes(ints, blocks);
 }
 
 int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host, const int32_t* keep_host, int32_t n,
@@ -878,8 +885,9 @@ int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host
       (slots_dev && (overlap(slots_dev, out_bytes, mass_dev, in_bytes) || overlap(slots_dev, out_bytes, kept_dev, out_bytes) ||
                      (mass_out_dev && overlap(slots_dev, out_bytes, mass_out_dev, out_bytes)))))
     return fail(h, VSK_E_ARG, "outputs overlap");
-  const size_t ints = evict_meta_ints(h, src_host, keep_host, n);
-  if (meta_bytes_ < align_up(ints * 4)) return fail(h, VSK_E_ARG, "metadata buffer smaller than vsk_kv_evict_bytes()");
+  size_t blocks = 0;
+  const size_t ints = evict_meta_ints(h, src_host, keep_host, n, &blocks);
+  if (meta_bytes_ < evict_meta_bytes(ints, blocks)) return fail(h, VSK_E_ARG, "metadata buffer smaller than vsk_kv_evict_bytes()");
   if (reinterpret_cast<uintptr_t>(meta_dev) % kAlign) return fail(h, VSK_E_ARG, "metadata buffer not aligned");
   hipStream_t s = static_cast<hipStream_t>(stream);
   int st = h->alloc.seq_evict(dst_host, src_host, keep_host, n, h->err);
@@ -919,6 +927,7 @@ int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host
   a.info = static_cast<const int32_t*>(meta_dev);
   a.src_tbl = a.info + info_ints;
   a.dst_tbl = a.src_tbl + total_src;
+  a.from = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(meta_dev) + align_up(ints * 4));
   a.sinks = sinks;
   a.recent = recent;
   a.mass = mass_dev;
@@ -928,7 +937,7 @@ int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host
   a.slots = slots_dev;
   a.out_stride = out_stride;
   st = stage_upload(h, meta_dev, staging, s);
-  if (st == VSK_OK) st = hip_check(h, launch_evict(a, n, max_keep, s), "evict");
+  if (st == VSK_OK) st = hip_check(h, launch_evict(a, n, max_len, max_keep, s), "evict");
   if (st != VSK_OK) h->alloc.seq_undo_evict(dst_host, n);
   return st;
 }

@@ -11,9 +11,11 @@ struct EvictArgs {
   uint16_t* pool;
   int n_layers, n_blocks, Hkv, hd;
   // per sequence of the call: [n][4]: cached tokens, tokens kept, first entry in src_tbl and in dst_tbl
+  // (a destination block has 16 entries in from)
   const int32_t* info;
   const int32_t* src_tbl;
   const int32_t* dst_tbl;
+  int32_t* from;  // written by the selection: the source slot of each kept token
   int sinks, recent;
   const float* mass;
   int64_t mass_stride;
@@ -22,6 +24,6 @@ struct EvictArgs {
   int32_t* slots;      // nullable
   int64_t out_stride;
 };
-hipError_t launch_evict(const EvictArgs& a, int n, int max_keep, hipStream_t s);
+hipError_t launch_evict(const EvictArgs& a, int n, int max_len, int max_keep, hipStream_t s);
 
 }  // namespace vsk

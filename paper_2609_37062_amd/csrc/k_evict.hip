@@ -15,10 +15,6 @@
 
 namespace vsk {
 
-constexpr int kSelThreads = 1024;
-constexpr int kSelWaves = kSelThreads / 64;
-constexpr int kSelPer = kEvictMaxLen / kSelThreads;  // tokens of a thread
-
 // Larger weight, larger key; -0 and 0 alike; NaN 0 (below -infinity).
 __device__ __forceinline__ uint32_t mass_key(float v) {
   const uint32_t u = __float_as_uint(v == 0.f ? 0.f : v);
@@ -42,142 +38,191 @@ __device__ __forceinline__ int block_before(int v, int* s_w) {
   return before;
 }
 
-__global__ __launch_bounds__(kSelThreads) void k_evict_select(EvictArgs a) {
-  __shared__ int s_hist[kSelWaves][256];
-  __shared__ int s_w[kSelWaves];
+// Exclusive prefix sum, in place, over N <= 256 counts in LDS, by every thread's call.
+template <int N>
+__device__ __forceinline__ void scan_counts(int* s) {
+  constexpr int E = (N + 63) / 64;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    int c[E], sum = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      c[e] = lane * E + e < N ? s[lane * E + e] : 0;
+      sum += c[e];
+    }
+    int x = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(x, d, 64);
+      if (lane >= d) x += y;
+    }
+    x -= sum;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (lane * E + e < N) s[lane * E + e] = x;
+      x += c[e];
+    }
+  }
+  __syncthreads();
+}
+
+// Token i = j T + thread is the thread's j-th: loads and stores then run along
+// the tokens.  (Runs of tokens a thread: 34 us at 16,000 tokens, most of it
+// 4-byte stores to 64 lines an instruction; this order 26.)
+template <int T, int PER>
+__global__ __launch_bounds__(T) void k_evict_select(EvictArgs a) {
+  constexpr int W = T / 64;
+  __shared__ int s_hist[2048];
+  __shared__ int s_w[W];
+  __shared__ int s_tie[PER * W], s_stay[PER * W];  // counts of 64 tokens each, in index order
   __shared__ uint32_t s_digit;
   __shared__ int s_left;
-  const int seq = blockIdx.x, tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
+  const int seq = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int32_t* info = a.info + 4 * seq;
   const int len = info[0], keep = info[1];
+  const int32_t* src_tbl = a.src_tbl + info[2];
   const int32_t* dst_tbl = a.dst_tbl + info[3];
+  int32_t* from = a.from + static_cast<int64_t>(info[3]) * kBlock;
   const float* mass = a.mass + seq * a.mass_stride;
-  const int per = (len + kSelThreads - 1) / kSelThreads;  // tokens tid * per .. of this thread
-  const int i0 = tid * per;
   const int lo = a.sinks, hi = len - a.recent;  // the tokens that compete
-  float v[kSelPer];
-  uint32_t key[kSelPer];
+  float v[PER];
+  uint32_t key[PER];
 #pragma unroll
-  for (int j = 0; j < kSelPer; ++j) {
-    const int i = i0 + j;
-    v[j] = j < per && i < len ? mass[i] : 0.f;
+  for (int j = 0; j < PER; ++j) {
+    const int i = j * T + tid;
+    v[j] = i < len ? mass[i] : 0.f;
     key[j] = mass_key(v[j]);
   }
-  auto competes = [&](int j) { return j < per && i0 + j >= lo && i0 + j < hi; };
-  int left = keep - a.sinks - a.recent;  // how many of them stay
-  uint32_t top = 0;                      // the digits of the smallest kept key, as found so far
-  const bool all = left >= hi - lo;      // (uniform)
-  if (left > 0 && !all) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < kSelWaves * 256; i += kSelThreads) (&s_hist[0][0])[i] = 0;
+  auto competes = [&](int j) { return j * T + tid >= lo && j * T + tid < hi; };
+  const int left0 = keep - a.sinks - a.recent;  // how many of them stay
+  int left = left0;                             // and of those whose key starts with `top`
+  uint32_t top = 0;                             // the smallest kept key, as far as it is known
+  const bool all = left0 >= hi - lo;            // (uniform)
+  if (left0 > 0 && !all) {
+#pragma unroll
+    for (int d = 0; d < 3; ++d) {
+      constexpr int kShift[3] = {21, 10, 0}, kBits[3] = {11, 11, 10};
+      const int shift = kShift[d], bins = 1 << kBits[d];
+      for (int b = tid; b < bins; b += T) s_hist[b] = 0;
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < kSelPer; ++j) {
-        const bool in = competes(j) && (shift == 24 || key[j] >> (shift + 8) == top >> (shift + 8));
-        if (in) atomicAdd(&s_hist[w][key[j] >> shift & 255u], 1);
+      for (int j = 0; j < PER; ++j) {
+        // equal keys (zeros, above all) would queue at one counter: the lanes
+        // that agree with the first one are counted together
+        const bool in = competes(j) && (d == 0 || key[j] >> (shift + kBits[d]) == top >> (shift + kBits[d]));
+        const uint64_t ins = __ballot(in);
+        if (ins == 0) continue;
+        const uint32_t first = __builtin_amdgcn_readlane(key[j], __builtin_ctzll(ins));
+        const uint64_t same = __ballot(in && key[j] == first);
+        if (lane == 0) atomicAdd(&s_hist[first >> shift & (bins - 1)], static_cast<int>(__popcll(same)));
+        if (in && key[j] != first) atomicAdd(&s_hist[key[j] >> shift & (bins - 1)], 1);
       }
       __syncthreads();
-      if (w == 0) {  // digits 4 lane .. 4 lane + 3, from the largest digit down
-        int c[4], sum = 0;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          c[d] = 0;
-          for (int x = 0; x < kSelWaves; ++x) c[d] += s_hist[x][4 * lane + d];
-          sum += c[d];
-        }
-        int above = sum;  // keys of this lane's digits and those of higher lanes
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const int y = __shfl_down(above, d, 64);
-          if (lane + d < 64) above += y;
-        }
-        above -= sum;
-#pragma unroll
-        for (int d = 3; d >= 0; --d) {
-          if (above < left && above + c[d] >= left) {
-            s_digit = 4 * lane + d;
-            s_left = left - above;
-          }
-          above += c[d];
-        }
+      // bins from the largest down, `own` of them a thread
+      const int own = bins / T;
+      int sum = 0;
+      for (int b = 0; b < own; ++b) sum += s_hist[bins - 1 - (tid * own + b)];
+      int above = block_before(sum, s_w);
+      if (above < left && above + sum >= left) {
+        int b = bins - 1 - tid * own;
+        while (above + s_hist[b] < left) above += s_hist[b--];
+        s_digit = b;
+        s_left = left - above;
       }
       __syncthreads();
       top |= s_digit << shift;
       left = s_left;
-      __syncthreads();
     }
   }
   // above `top` every token stays, of those at `top` the first `left`
-  int n_tie = 0;
+  const uint64_t before = (1ull << lane) - 1ull;
 #pragma unroll
-  for (int j = 0; j < kSelPer; ++j) n_tie += competes(j) && key[j] == top;
-  int tie = block_before(n_tie, s_w);
-  uint32_t stays = 0;
-  int n_stay = 0;
-#pragma unroll
-  for (int j = 0; j < kSelPer; ++j) {
-    const int i = i0 + j;
-    if (j >= per || i >= len) continue;
-    bool s = i < lo || i >= hi || all;
-    if (!s && keep > a.sinks + a.recent) {
-      s = key[j] > top || (key[j] == top && tie < left);
-      tie += key[j] == top;
-    }
-    stays |= static_cast<uint32_t>(s) << j;
-    n_stay += s;
+  for (int j = 0; j < PER; ++j) {
+    const int n = __popcll(__ballot(competes(j) && key[j] == top));
+    if (lane == 0) s_tie[j * W + w] = n;
   }
-  int at = block_before(n_stay, s_w);
-  int32_t* kept = a.kept + seq * a.out_stride;
-  // (mass_out may be mass itself: every weight has been read above, the two
-  // prefix sums' barriers since)
+  scan_counts<PER * W>(s_tie);
+  uint32_t stays = 0;
 #pragma unroll
-  for (int j = 0; j < kSelPer; ++j) {
-    if (!(stays >> j & 1u)) continue;
-    kept[at] = i0 + j;
+  for (int j = 0; j < PER; ++j) {
+    const int i = j * T + tid;
+    const uint64_t ties = __ballot(competes(j) && key[j] == top);
+    bool s = i < len && (i < lo || i >= hi || all);
+    if (left0 > 0 && competes(j))
+      s = s || key[j] > top || (key[j] == top && s_tie[j * W + w] + __popcll(ties & before) < left);
+    stays |= static_cast<uint32_t>(s) << j;
+    const int n = __popcll(__ballot(s));
+    if (lane == 0) s_stay[j * W + w] = n;
+  }
+  scan_counts<PER * W>(s_stay);
+  int32_t* kept = a.kept + seq * a.out_stride;
+  // (mass_out may be mass itself: every weight has been read above, the scans'
+  // barriers since)
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const bool s = stays >> j & 1u;
+    const int at = s_stay[j * W + w] + __popcll(__ballot(s) & before);
+    if (!s) continue;
+    const int i = j * T + tid;
+    kept[at] = i;
+    from[at] = src_tbl[i / kBlock] * kBlock + i % kBlock;
     if (a.slots != nullptr) a.slots[seq * a.out_stride + at] = dst_tbl[at / kBlock] * kBlock + at % kBlock;
     if (a.mass_out != nullptr) a.mass_out[seq * a.out_stride + at] = v[j];
-    ++at;
   }
   if (a.mass_out != nullptr)
-    for (int64_t i = keep + tid; i < a.out_stride; i += kSelThreads) a.mass_out[seq * a.out_stride + i] = 0.f;
+    for (int64_t i = keep + tid; i < a.out_stride; i += T) a.mass_out[seq * a.out_stride + i] = 0.f;
 }
 
-// One thread per 16-byte piece of the destination: 8 dims of a token of K, 8
-// tokens of a dim of V.
+// One workgroup per destination block of a layer and KV head, one thread per
+// 16-byte piece: 8 dims of a token of K, 8 tokens of a dim of V.  Lanes run
+// along what is contiguous in the pool: the tokens of K pieces, the dims of V
+// pieces.  A line of the pool holds eight tokens of K, or eight tokens of
+// eight dims of V, so where few tokens stay the lines read are more than the
+// bytes moved: with one in five kept, 85% of the source.
 __global__ __launch_bounds__(256) void k_evict_move(EvictArgs a) {
   const int seq = blockIdx.z, layer = blockIdx.y / a.Hkv, hk = blockIdx.y % a.Hkv;
   const int32_t* info = a.info + 4 * seq;
-  const int keep = info[1];
-  const int hd = a.hd;
+  const int keep = info[1], hd = a.hd;
   const int blk = blockIdx.x;  // destination block
   if (blk * kBlock >= keep) return;
-  const int32_t* src_tbl = a.src_tbl + info[2];
-  const int32_t* kept = a.kept + seq * a.out_stride + blk * kBlock;
+  const int32_t* from = a.from + (static_cast<int64_t>(info[3]) + blk) * kBlock;
   const int n = min(kBlock, keep - blk * kBlock);
   const size_t head = static_cast<size_t>(kBlock) * hd, stride = head * a.Hkv;
-  const uint16_t* kp = a.pool + static_cast<size_t>(layer) * 2 * a.n_blocks * stride + hk * head;
-  const uint16_t* vp = kp + static_cast<size_t>(a.n_blocks) * stride;
+  uint16_t* kp = a.pool + static_cast<size_t>(layer) * 2 * a.n_blocks * stride + hk * head;
+  uint16_t* vp = kp + static_cast<size_t>(a.n_blocks) * stride;
   const size_t to = static_cast<size_t>(a.dst_tbl[info[3] + blk]) * stride;
-  for (int i = threadIdx.x; i < n * (hd / 8); i += blockDim.x) {
-    const int t = i / (hd / 8), e = i % (hd / 8) * 8;
-    const int s = kept[t];
-    const size_t from = static_cast<size_t>(src_tbl[s / kBlock]) * stride;
-    *reinterpret_cast<u32x4*>(const_cast<uint16_t*>(kp) + to + kv_k_index(t, e)) =
-        *reinterpret_cast<const u32x4*>(kp + from + kv_k_index(s % kBlock, e));
-  }
-  for (int i = threadIdx.x; i < n * hd; i += blockDim.x) {
-    const int t = i / hd, e = i % hd;
-    const int s = kept[t];
-    const size_t from = static_cast<size_t>(src_tbl[s / kBlock]) * stride;
-    const_cast<uint16_t*>(vp)[to + kv_v_index(t, e)] = vp[from + kv_v_index(s % kBlock, e)];
-  }
+  const int i = threadIdx.x;  // < 2 hd
+  // K: the piece at place i of the block's 2 hd (its token's bits 2 and 3 are swapped, see kv_k_index)
+  const int p = i % kBlock, tk = (p & 3) | ((p & 4) << 1) | ((p & 8) >> 1), e = i / kBlock * 8;
+  const int sk = from[min(tk, n - 1)];
+  // V: dim and half of the piece at place i
+  const int ev = i / 32 * 16 + i % 16, t0 = i % 32 / 16 * 8;
+  int sv[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sv[j] = from[min(t0 + j, n - 1)];
+  const u32x4 x = *reinterpret_cast<const u32x4*>(kp + (sk >> 4) * stride + kv_k_index(sk & 15, e));
+  uint32_t y[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) y[j] = vp[(sv[j] >> 4) * stride + kv_v_index(sv[j] & 15, ev)];
+  // (the block is the sequence's own: its slots behind the last token may hold anything)
+  *reinterpret_cast<u32x4*>(kp + to + i * 8) = x;
+  *reinterpret_cast<u32x4*>(vp + to + i * 8) =
+      u32x4{y[0] | y[1] << 16, y[2] | y[3] << 16, y[4] | y[5] << 16, y[6] | y[7] << 16};
 }
 
-hipError_t launch_evict(const EvictArgs& a, int n, int max_keep, hipStream_t s) {
-  hipLaunchKernelGGL(k_evict_select, dim3(n), dim3(kSelThreads), 0, s, a);
+// Few tokens take few waves (cheaper rounds), and never more registers than tokens need.
+static void launch_select(const EvictArgs& a, int n, int max_len, hipStream_t s) {
+  if (max_len <= 1024) hipLaunchKernelGGL((k_evict_select<256, 4>), dim3(n), dim3(256), 0, s, a);
+  else if (max_len <= 4096) hipLaunchKernelGGL((k_evict_select<1024, 4>), dim3(n), dim3(1024), 0, s, a);
+  else hipLaunchKernelGGL((k_evict_select<1024, kEvictMaxLen / 1024>), dim3(n), dim3(1024), 0, s, a);
+}
+
+hipError_t launch_evict(const EvictArgs& a, int n, int max_len, int max_keep, hipStream_t s) {
+  launch_select(a, n, max_len, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_evict_move, dim3((max_keep + kBlock - 1) / kBlock, a.n_layers * a.Hkv, n), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(k_evict_move, dim3((max_keep + kBlock - 1) / kBlock, a.n_layers * a.Hkv, n), dim3(2 * a.hd), 0, s, a);
   return hipGetLastError();
 }
 

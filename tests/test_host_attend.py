@@ -95,8 +95,8 @@ def test_evict_refusals():
 
 def test_evict_bytes():
     e = _engine()
-    # [n][4] numbers, 7 + 3 source blocks, 2 + 1 destination blocks
-    assert e.kv_evict_bytes([0, 1], [20, 3]) == (8 + 10 + 3) * 4 // 256 * 256 + 256
+    # [n][4] numbers, 7 + 3 source blocks, 2 + 1 destination blocks; 3 blocks of kept slots
+    assert e.kv_evict_bytes([0, 1], [20, 3]) == 256 + 256
     for src, keep in (([5], [1]), ([0], [0]), ([0], [101])):
         assert e.kv_evict_bytes(src, keep) == 0
     e.close()
