@@ -1309,7 +1309,10 @@ static hipError_t launch_attn(Handle& h, AttnPlan& p, int layer, const uint8_t* 
   p.dec.layer = p.pfx.layer = p.pre.layer = layer;
   p.dec.run_mask = p.pre.run_mask = mask;
   if (p.cascade && (e = launch_attn_prefix(p.pfx, b.n_pfx_items, d, s)) != hipSuccess) return e;
-  if (p.prefill && (e = launch_attn_prefill(p.pre, b.n_pre_items, d, s, p.span)) != hipSuccess) return e;
+  if (p.prefill) {
+    e = p.span ? launch_attn_rows(p.pre, b.n_pre_items, d, s) : launch_attn_prefill(p.pre, b.n_pre_items, d, s);
+    if (e != hipSuccess) return e;
+  }
   int rows = b.n_dec_rows;
   p.dec.rows = b.dec_rows;  // one-row sequences, longest walk first
   if (!p.prefill && b.n_pre_items > 0) {

@@ -77,7 +77,7 @@ struct AttnPrefillArgs {
   uint16_t* out;  // o frags (K = Nq)
   int out_Rg;
   const uint8_t* run_mask;  // routed layer (nullable): as in AttnArgs
-  int window, sinks;        // general walk: as in AttnArgs
+  int window, sinks;        // general walk (launch_attn_rows): as in AttnArgs, as are out_Rg 0 and ml
   float2* ml;
 };
 
@@ -124,7 +124,9 @@ struct AttnPrefixArgs {
 hipError_t launch_attn_decode(const AttnArgs& a, int n_rows, int grid_splits, int max_pfx_splits, hipStream_t s,
                               LaunchEvents ev = {}, bool span = false);
 hipError_t launch_attn_prefix(const AttnPrefixArgs& a, int n_items, int head_dim, hipStream_t s);
-hipError_t launch_attn_prefill(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s, bool span = false);
+hipError_t launch_attn_prefill(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s);
+// the general one of prompt rows (k_rows.hip)
+hipError_t launch_attn_rows(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s);
 hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, int max_kv_len, int head_dim, hipStream_t s);
 
 }  // namespace vsk

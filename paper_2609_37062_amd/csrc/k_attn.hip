@@ -94,9 +94,7 @@ hipError_t launch_attn_decode(const AttnArgs& a, int n_rows, int grid_splits, in
 // t >= t_end do not count (their V is zeroed: stale slots may hold NaN
 // patterns); with MASK a key also needs t <= lim.  Keys below full_end (the
 // same for the whole wave) count for every column.  Returns true on the waves
-// that hold a tile's result (half 0).  With SPAN (MASK only) tbl lists the
-// blocks of ws.span, and ws says what the wave's columns and the lane's own
-// column see of them.
+// that hold a tile's result (half 0).
 constexpr int kWalkLead = 2;
 constexpr int kWalkSlots = kWalkLead + 1;
 template <int D, int NH>
@@ -105,56 +103,11 @@ struct WalkLds {
   u32x4 ring[kWalkSlots][NH][2][D / 16][64];
 };
 
-struct WalkSpan {
-  SpanWalk span;
-  int sinks;
-  int lo;       // first key of the lane's column's window
-  int full_lo;  // of the wave's last row's (uniform): from there on a key counts for every column
-  int from;     // the wave's first block of the list but for those of the sinks (uniform)
-};
-
-// P V of a step of which some keys count for some columns only, where V holds
-// values that are not finite: each column on its own, from V (read again: chunk
-// c at vp[32 c]) with the keys that it does not see set to zero (0 x NaN is
-// NaN).  Rare, so slow is fine.
-template <int D, int NT>
-__device__ __forceinline__ void span_pv_columns(const u32x4* vp, const PTermsOf<NT>& pp, uint32_t bits, float alpha,
-                                                f32x4 (&o)[D / 16]) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int c = 0; c < D / 16; ++c) {
-    o[c] *= alpha;
-#pragma unroll 1
-    for (int h = 0; h < 16; ++h) {
-      u32x4 v[1] = {vp[32 * c]};
-      span_zero_v<16>(v, __shfl(bits, h + (lane & 48), 64));
-      f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int t = 0; t < NT; ++t) y = mfma_16x16x32(v[0], pp.t[t], y);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) o[c][r] = (lane & 15) == h ? o[c][r] + y[r] : o[c][r];
-    }
-  }
-}
-
-// Some value of V (of any lane of the wave) is an infinity or a NaN.
-template <int D>
-__device__ __forceinline__ bool v_not_finite(const u32x4 (&vt)[D / 16]) {
-  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-  u16x2 top = u16x2{0, 0};
-#pragma unroll
-  for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vt[c][j] & 0x7fff7fffu));
-  return __any(top[0] >= 0x7f80 || top[1] >= 0x7f80);
-}
-
-template <int D, int NCT, int NH, bool MASK, bool SPAN = false>
+template <int D, int NCT, int NH, bool MASK>
 __device__ __forceinline__ bool mq_walk(const u32x4 (&qf)[D / 32], const uint16_t* kbase, const uint16_t* vbase,
                                         size_t kv_stride, const int32_t* tbl, int cnt, int my_cnt, int b0, int lim,
                                         int t_end, int full_end, float sc, float& m, float& l,
-                                        f32x4 (&o)[D / 16], WalkLds<D, NH>& sm, const WalkSpan& ws = {}) {
+                                        f32x4 (&o)[D / 16], WalkLds<D, NH>& sm) {
   constexpr int KC = D / 32;   // K chunks (1 KiB) per block
   constexpr int VC = D / 16;   // V chunks (512 B) per block
   constexpr int NCH = 2 * KC;  // 1 KiB chunks per block
@@ -206,7 +159,7 @@ __device__ __forceinline__ bool mq_walk(const u32x4 (&qf)[D / 32], const uint16_
       for (int st = 0; st < n_steps; ++st) {
         barrier_after_lds_reads();
         const int p = st * NH + hh;
-        if (p < my_pairs && (!SPAN || 2 * kBlock * p < ws.sinks || 2 * p + 1 >= ws.from)) {
+        if (p < my_pairs) {
           const u32x4* kp = &sm.ring[st % kWalkSlots][hh][kb][0][0];
           const u32x4* vp = &sm.ring[st % kWalkSlots][hh][vb][KC][0] + vi;
           u32x4 kg[2][KC];
@@ -218,36 +171,6 @@ __device__ __forceinline__ bool mq_walk(const u32x4 (&qf)[D / 32], const uint16_
           }
 #pragma unroll
           for (int c = 0; c < VC; ++c) vt[c] = vp[c * 32];
-          if constexpr (SPAN) {
-            const int quad = lane >> 4;
-            const int ba = ws.span.block(2 * p), bb = ws.span.block(2 * p + 1);
-            auto whole = [&](int b) {
-              return kBlock * (b + 1) <= full_end && (kBlock * b >= ws.full_lo || kBlock * (b + 1) <= ws.sinks);
-            };
-            const bool full = 2 * p + 1 < cnt && whole(ba) && whole(bb);  // (uniform)
-            f32x4 s0, s1;
-            pair_qk<D>(qf, kg, s0, s1);
-            uint32_t bits = 0xffu, held = 0xffu;  // keys that the column sees, that the sequence has
-            if (!full) {
-              const int t = kBlock * (quad >> 1 ? bb : ba) + 8 * (quad & 1);
-              const bool in = 2 * p + (quad >> 1) < cnt;
-              bits = in ? span_bits(t, min(t_end, lim + 1), ws.lo, ws.sinks) : 0u;
-              held = in ? span_bits(t, t_end, 0, 0) : 0u;
-              span_mask(bits, s0, s1);
-            }
-            PTermsOf<kSpanPTerms> pp;
-            float alpha;
-            pair_softmax<true>(s0, s1, sc, m, l, pp, alpha);
-            if (!full) {
-              span_zero_v<D>(vt, held);
-              if (__builtin_expect(v_not_finite<D>(vt), 0)) {
-                span_pv_columns<D>(vp, pp, bits, alpha, o);
-                continue;
-              }
-            }
-            pair_pv_add<D>(vt, pp, alpha, o);
-            continue;
-          }
           const int t0 = kBlock * (b0 + 2 * p);
           PTerms pp;
           float alpha;
@@ -367,13 +290,11 @@ __global__ __launch_bounds__(64 * (kPfxWaves + 1)) void k_attn_prefix(AttnPrefix
 // wave walks the blocks up to its last row's position; each lane masks the
 // keys past its own row.  The output is normalised and stored as the O
 // projection's input frags.
-// SPAN: the general walk (window, sinks, ml, row-major output); the item's
-// blocks are the SpanWalk list of its rows.
-template <int D, bool SPAN>
+template <int D>
 __global__ __launch_bounds__(64 * (kPreTiles + 1)) void k_attn_prefill(AttnPrefillArgs a) {
   constexpr int KC = D / 32;
   constexpr int VC = D / 16;
-  __shared__ int32_t tbl[SPAN ? kMaxSpanBlocks : kMaxPrefillBlocks];
+  __shared__ int32_t tbl[kMaxPrefillBlocks];
   __shared__ WalkLds<D, 1> ring;
 
   // one-dimensional grid, an item's KV heads consecutive (items come
@@ -388,11 +309,9 @@ __global__ __launch_bounds__(64 * (kPreTiles + 1)) void k_attn_prefill(AttnPrefi
   const int h = lane & 15, quad = lane >> 4;
   const int kv_end = a.kv_len[seq];
   const int p_last = a.pos[row0 + n_rows - 1];
-  SpanWalk span{};
-  if constexpr (SPAN) span = span_walk(a.pos[row0] + 1, p_last + 1, a.window, a.sinks);
-  const int nb = SPAN ? span.nv : p_last / kBlock + 1;  // blocks any row of the item reads
+  const int nb = p_last / kBlock + 1;  // blocks any row of the item reads
   const int32_t* table = a.block_table + static_cast<size_t>(seq) * a.max_blocks;
-  for (int i = tid; i < nb; i += blockDim.x) tbl[i] = table[SPAN ? span.block(i) : i];
+  for (int i = tid; i < nb; i += blockDim.x) tbl[i] = table[i];
 
   const int c = 16 * w + h;
   const bool cvalid = w < kPreTiles && c < n_cols;  // (wave kPreTiles only loads blocks)
@@ -419,38 +338,19 @@ __global__ __launch_bounds__(64 * (kPreTiles + 1)) void k_attn_prefill(AttnPrefi
   __syncthreads();  // tbl
   // the workgroup walks the blocks of its last row; each wave computes up to
   // its own last column's block (none if it has no column)
-  const bool has = w < kPreTiles && 16 * w < n_cols;
   const int c_last = min(16 * w + 15, n_cols - 1);
-  const int p0 = has ? a.pos[row0 + 16 * w / G] : -1, p1 = has ? a.pos[row0 + c_last / G] : -1;  // the wave's rows
+  const int w_blocks = w < kPreTiles && 16 * w < n_cols ? a.pos[row0 + c_last / G] / kBlock + 1 : 0;
   // keys up to the wave's first row's position count for all its columns
-  const int w_full = __builtin_amdgcn_readfirstlane(p0 + 1);
-  if constexpr (SPAN) {
-    auto first = [&](int p) { return a.window > 0 && p + 1 > a.window ? p + 1 - a.window : 0; };
-    auto list = [&](int b) { return b - span.wb + span.ns; };  // place of block b of the window
-    WalkSpan ws;
-    ws.span = span;
-    ws.sinks = a.sinks;
-    ws.lo = first(lim);
-    ws.full_lo = __builtin_amdgcn_readfirstlane(first(p1));
-    ws.from = __builtin_amdgcn_readfirstlane(list(first(p0) / kBlock));
-    const int w_blocks = __builtin_amdgcn_readfirstlane(has ? list(p1 / kBlock) + 1 : 0);
-    mq_walk<D, kPreTiles, 1, true, true>(qf, kbase, vbase, kv_stride, tbl, nb, w_blocks, 0, lim, kv_end,
-                                         min(kv_end, w_full), a.scale_log2, m, l, o, ring, ws);
-  } else {
-    const int w_blocks = has ? p1 / kBlock + 1 : 0;
-    mq_walk<D, kPreTiles, 1, true>(qf, kbase, vbase, kv_stride, tbl, nb, w_blocks, 0, lim, min(kv_end, kBlock * nb),
-                                   min(kv_end, w_full), a.scale_log2, m, l, o, ring);
-  }
-  if (!has) return;
+  const int w_full = __builtin_amdgcn_readfirstlane(w_blocks > 0 ? a.pos[row0 + 16 * w / G] + 1 : 0);
+  mq_walk<D, kPreTiles, 1, true>(qf, kbase, vbase, kv_stride, tbl, nb, w_blocks, 0, lim, min(kv_end, kBlock * nb),
+                                 min(kv_end, w_full), a.scale_log2, m, l, o, ring);
+  if (!(w < kPreTiles && 16 * w < n_cols)) return;
 
   if (cvalid) {
     // a Project-Only row of a routed layer emits zero
     const bool po = a.run_mask != nullptr && a.run_mask[row] == 0;
     const float inv = 1.f / l;
     const int col0 = (hk * G + qh) * D;
-    if constexpr (SPAN)
-      if (a.ml != nullptr && quad == 0)
-        a.ml[static_cast<size_t>(row) * (a.Hkv * G) + hk * G + qh] = po ? make_float2(INFINITY, 0.f) : make_float2(m, inv);
 #pragma unroll
     for (int k = 0; k < VC; ++k) {
       const int e = 16 * k + 4 * quad;
@@ -459,25 +359,21 @@ __global__ __launch_bounds__(64 * (kPreTiles + 1)) void k_attn_prefill(AttnPrefi
         pk[0] = pack_bf2(o[k][0] * inv, o[k][1] * inv);
         pk[1] = pack_bf2(o[k][2] * inv, o[k][3] * inv);
       }
-      const size_t i0 = SPAN && a.out_Rg == 0 ? static_cast<size_t>(row) * a.Nq + col0 + e
-                                              : frag_index(row, col0 + e, a.out_Rg);
-      *reinterpret_cast<u32x2*>(a.out + i0) = pk;
+      *reinterpret_cast<u32x2*>(a.out + frag_index(row, col0 + e, a.out_Rg)) = pk;
     }
   }
 }
 
-template <int D>
-static void launch_prefill_d(const AttnPrefillArgs& a, dim3 grid, bool span, hipStream_t s) {
-  if (span) hipLaunchKernelGGL((k_attn_prefill<D, true>), grid, dim3(64 * (kPreTiles + 1)), 0, s, a);
-  else hipLaunchKernelGGL((k_attn_prefill<D, false>), grid, dim3(64 * (kPreTiles + 1)), 0, s, a);
-}
-
-hipError_t launch_attn_prefill(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s, bool span) {
+hipError_t launch_attn_prefill(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s) {
   if (n_items <= 0) return hipSuccess;
   dim3 grid(n_items * a.Hkv);
-  if (head_dim == 128) launch_prefill_d<128>(a, grid, span, s);
-  else if (head_dim == 64) launch_prefill_d<64>(a, grid, span, s);
-  else return hipErrorInvalidValue;
+  if (head_dim == 128) {
+    hipLaunchKernelGGL((k_attn_prefill<128>), grid, dim3(64 * (kPreTiles + 1)), 0, s, a);
+  } else if (head_dim == 64) {
+    hipLaunchKernelGGL((k_attn_prefill<64>), grid, dim3(64 * (kPreTiles + 1)), 0, s, a);
+  } else {
+    return hipErrorInvalidValue;
+  }
   return hipGetLastError();
 }
 

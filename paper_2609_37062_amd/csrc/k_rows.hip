@@ -1,0 +1,315 @@
+// General attention of prompt rows: a sliding window with sinks, or every key,
+// over the paged cache.
+//
+// One work item per (run of a sequence's consecutive new rows, KV head); its
+// columns are the run's (row, query head) pairs, up to 128, 32 a wave.  Scores
+// and outputs are taken transposed on v_mfma_f32_32x32x16_bf16: S^T = K q^T of
+// 32 keys (two blocks) x 32 columns, O^T += V^T P^T.  A lane then holds 16
+// scores of one column, and as the cache keeps K's tokens with bits 2 and 3
+// swapped, these are tokens 8 h .. 8 h + 7 (h = lane / 32) of either block: what
+// P^T's operand asks of that lane, with no exchange between lanes.
+//
+// Why 32 columns a wave: every wave reads the step's K and V from LDS, 16 KiB
+// at head_dim 128.  With 16 columns (the passes' walk) eight waves read 128 KiB
+// a step, at 128 bytes a cycle longer than the step's MFMAs take; with 32 a
+// byte feeds twice the work.
+//
+// K and V go through registers into two LDS slots: the loads of step i + 2 are
+// issued and those of step i + 1 stored before step i is computed, with one
+// barrier a step.  NH halves of a workgroup walk alternate pairs of blocks and
+// are joined at the end: with few work items two halves keep two waves on each
+// SIMD, with many one half and two workgroups do.
+#include "attn_core.hpp"
+
+namespace vsk {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16 mfma_32x32x16(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
+                                                 0, 0);
+}
+
+constexpr int kRowTiles = 4;               // 32-column tiles of a work item
+static_assert(kRowTiles * 32 == kPreCols, "a work item's columns");
+// A running maximum may lag by this (base 2) before the sums are rescaled: the
+// weights are then up to 2^8, the float32 sums as exact as before.
+constexpr float kRowsLag = 8.f;
+
+// Some value of V (of any lane of the wave) is an infinity or a NaN.
+template <int N>
+__device__ __forceinline__ bool not_finite(const u32x4 (&v)[N]) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  u16x2 top = u16x2{0, 0};
+#pragma unroll
+  for (int c = 0; c < N; ++c)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[c][j] & 0x7fff7fffu));
+  return __any(top[0] >= 0x7f80 || top[1] >= 0x7f80);
+}
+
+// Eight bf16 values of which those with a clear bit become zero.
+__device__ __forceinline__ u32x4 keep_bits(u32x4 v, uint32_t bits) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    v[j] &= (bits >> (2 * j) & 1u ? 0x0000ffffu : 0u) | (bits >> (2 * j + 1) & 1u ? 0xffff0000u : 0u);
+  return v;
+}
+
+template <int D, int NH>
+struct RowsLds {
+  u32x4 kv[2][NH][2][2][2 * D];  // [slot][half][K, V][block][16-byte piece]
+  int32_t tbl[kMaxSpanBlocks];
+  float m[kRowTiles][64], l[kRowTiles][64];  // the second half's, when the halves join
+};
+
+template <int D, int NH>
+__global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
+  constexpr int T = 256 * NH;
+  constexpr int QC = D / 16;  // q and K operands of a step
+  constexpr int OC = D / 32;  // tiles of 32 dims
+  constexpr int LD = D / 32;  // 16-byte loads a thread and step
+  __shared__ RowsLds<D, NH> sm;
+
+  // an item's KV heads are consecutive (items come longest walk first)
+  const int hk = blockIdx.x % a.Hkv;
+  const int32_t* it = a.items + static_cast<size_t>(blockIdx.x / a.Hkv) * 3;
+  const int seq = it[0], row0 = it[1], n_rows = it[2];
+  const int G = a.G, n_cols = n_rows * G;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ct = w % kRowTiles, hh = w / kRowTiles;
+  const int lc = lane & 31, hi = lane >> 5;
+  const int kv_end = a.kv_len[seq];
+  const int pos0 = a.pos[row0];  // (a run's rows are consecutive positions)
+  const SpanWalk span = span_walk(pos0 + 1, pos0 + n_rows, a.window, a.sinks);
+  const int32_t* table = a.block_table + static_cast<size_t>(seq) * a.max_blocks;
+  for (int i = tid; i < span.nv; i += T) sm.tbl[i] = table[span.block(i)];
+
+  // this lane's column and what it sees: keys lo .. p and below sinks
+  const int c = 32 * ct + lc;
+  const bool on = c < n_cols;
+  const int row = on ? c / G : 0, qh = on ? c % G : 0;
+  const int end = on ? min(kv_end, pos0 + row + 1) : 0;
+  auto first_key = [&](int n) { return a.window > 0 && n > a.window ? n - a.window : 0; };  // of a row with n keys
+  const int lo = first_key(pos0 + row + 1);
+  u32x4 qf[QC];
+  {
+    const uint16_t* qrow = a.q + static_cast<size_t>(row0 + row) * a.Nq + static_cast<size_t>(hk * G + qh) * D + 8 * hi;
+#pragma unroll
+    for (int s = 0; s < QC; ++s)
+      qf[s] = on ? *reinterpret_cast<const u32x4*>(qrow + 16 * s) : u32x4{0u, 0u, 0u, 0u};
+  }
+  // the wave's part of the list (none without a column), and from where to
+  // where a key counts for all its columns
+  const bool has = 32 * ct < n_cols;
+  const int ra = 32 * ct / G, rb = min(32 * ct + 31, n_cols - 1) / G;  // its first and last row
+  const int w_from = first_key(pos0 + ra + 1) / kBlock - span.wb + span.ns;
+  const int w_to = has ? (pos0 + rb) / kBlock - span.wb + span.ns + 1 : 0;
+  const int full_end = min(kv_end, pos0 + ra + 1), full_lo = first_key(pos0 + rb + 1);
+
+  const size_t head = static_cast<size_t>(kBlock) * D, stride = head * a.Hkv;
+  const uint16_t* kbase = a.pool + static_cast<size_t>(a.layer) * 2 * a.n_blocks * stride + hk * head;
+  const uint16_t* vbase = kbase + static_cast<size_t>(a.n_blocks) * stride;
+  const int n_pairs = (span.nv + 1) / 2, n_steps = (n_pairs + NH - 1) / NH;
+  u32x4 st[LD];
+  // piece tid + j T of a step's NH x {K, V} x two blocks x 2 D pieces; blocks
+  // past the list: its last one again (nobody counts its keys)
+  auto load = [&](int step) {
+#pragma unroll
+    for (int j = 0; j < LD; ++j) {
+      const int x = tid + j * T, piece = x % (2 * D), part = x / (2 * D);  // part: half, K or V, block
+      const int v = min(2 * (step * NH + part / 4) + part % 2, span.nv - 1);
+      const uint16_t* base = part & 2 ? vbase : kbase;
+      st[j] = *reinterpret_cast<const u32x4*>(base + static_cast<size_t>(sm.tbl[v]) * stride + piece * 8);
+    }
+  };
+  auto store = [&](int slot) {
+#pragma unroll
+    for (int j = 0; j < LD; ++j) (&sm.kv[slot][0][0][0][0])[tid + j * T] = st[j];
+  };
+  float m = -INFINITY, l = 0.f;
+  f32x16 o[OC];
+#pragma unroll
+  for (int i = 0; i < OC; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+  const float sc = a.scale_log2;
+
+  __syncthreads();  // tbl
+  load(0);
+  store(0);
+  if (n_steps > 1) load(1);
+  for (int step = 0; step < n_steps; ++step) {
+    barrier_after_lds_reads();  // step's slot is whole, the other one free
+    if (step + 1 < n_steps) store((step + 1) & 1);
+    if (step + 2 < n_steps) load(step + 2);
+    const int v = 2 * (step * NH + hh);  // the pair's first block of the list
+    if (v >= w_to || (v + 1 < w_from && kBlock * v >= a.sinks)) continue;
+    const int ba = span.block(v), bb = span.block(v + 1);
+    auto whole = [&](int b) {
+      return kBlock * (b + 1) <= full_end && (kBlock * b >= full_lo || kBlock * (b + 1) <= a.sinks);
+    };
+    const bool full = v + 1 < span.nv && whole(ba) && whole(bb);  // (uniform)
+    const u32x4* kp = &sm.kv[step & 1][hh][0][lc >> 4][(lane & 15) + 16 * hi];
+    f32x16 s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < QC; ++i) s = mfma_32x32x16(kp[32 * i], qf[i], s);
+    // s[r]: key 8 hi + r of block A (r < 8), 8 hi + r - 8 of block B
+    uint32_t bits[2] = {0xffu, 0xffu};
+    if (!full) {
+      bits[0] = span_bits(kBlock * ba + 8 * hi, end, lo, a.sinks);
+      bits[1] = v + 1 < span.nv ? span_bits(kBlock * bb + 8 * hi, end, lo, a.sinks) : 0u;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = bits[r / 8] >> (r % 8) & 1u ? s[r] : -INFINITY;
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    mx = max_xor32(mx) * sc;
+    if (__any(mx > m + kRowsLag)) {  // (-inf + 8 is -inf: a column's first keys always do)
+      const float mn = fmaxf(m, mx);
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < OC; ++i) o[i] *= f;
+    }
+    const float mb = m == -INFINITY ? 0.f : m;
+    float p[16];
+    if (__builtin_expect(__any(fabsf(mb) >= kRoundedScores), 0)) {
+      // both sides of the difference rounded alike (see pair_softmax)
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = s[r] * sc;
+        p[r] = __builtin_amdgcn_exp2f(x - mb);
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc, -mb));
+    }
+    float ps[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ps[j] = (p[j] + p[j + 4]) + (p[j + 8] + p[j + 12]);
+    l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+    u32x4 pt[2][kSpanPTerms];  // [block][term]
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float r0 = p[8 * b + 2 * j], r1 = p[8 * b + 2 * j + 1];
+#pragma unroll
+        for (int t = 0; t < kSpanPTerms; ++t) {
+          pt[b][t][j] = pack_bf2(r0, r1);
+          r0 -= bf2f(pt[b][t][j]);
+          r1 -= __uint_as_float(pt[b][t][j] & 0xffff0000u);
+        }
+      }
+    const u32x4* vp = &sm.kv[step & 1][hh][1][0][32 * (lc >> 4) + (lane & 15) + 16 * hi];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      u32x4 vt[OC];
+#pragma unroll
+      for (int i = 0; i < OC; ++i) vt[i] = vp[2 * D * b + 64 * i];
+      if (!full) {
+        // slots past the sequence's end may hold a NaN, and 0 x NaN is NaN
+        const uint32_t held = v + b < span.nv ? span_bits(kBlock * (b ? bb : ba) + 8 * hi, kv_end, 0, 0) : 0u;
+#pragma unroll
+        for (int i = 0; i < OC; ++i) vt[i] = keep_bits(vt[i], held);
+        if (__builtin_expect(not_finite(vt), 0)) {
+          // so may keys that some columns see and others do not: each column
+          // on its own, the keys that it does not see set to zero (rare, slow)
+#pragma unroll 1
+          for (int h = 0; h < 32; ++h) {
+            const uint32_t sees = __shfl(bits[b], h + (lane & 32), 64) & held;
+#pragma unroll
+            for (int i = 0; i < OC; ++i) {
+              f32x16 y;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) y[r] = 0.f;
+              const u32x4 vz = keep_bits(vp[2 * D * b + 64 * i], sees);
+#pragma unroll
+              for (int t = 0; t < kSpanPTerms; ++t) y = mfma_32x32x16(vz, pt[b][t], y);
+#pragma unroll
+              for (int r = 0; r < 16; ++r) o[i][r] = lc == h ? o[i][r] + y[r] : o[i][r];
+            }
+          }
+          continue;
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < kSpanPTerms; ++t)
+#pragma unroll
+        for (int i = 0; i < OC; ++i) o[i] = mfma_32x32x16(vt[i], pt[b][t], o[i]);
+    }
+  }
+  l = add_xor32(l);
+
+  if constexpr (NH == 2) {  // the second half's sums join the first's
+    static_assert(sizeof(sm.kv) >= kRowTiles * OC * 16 * 64 * 4, "space for a half's sums");
+    float* so = reinterpret_cast<float*>(&sm.kv[0][0][0][0][0]) + ct * OC * 16 * 64 + lane;
+    __syncthreads();
+    if (hh == 1) {
+#pragma unroll
+      for (int i = 0; i < OC; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) so[(i * 16 + r) * 64] = o[i][r];
+      sm.m[ct][lane] = m;
+      sm.l[ct][lane] = l;
+    }
+    __syncthreads();
+    if (hh == 1) return;
+    const float m2 = sm.m[ct][lane], l2 = sm.l[ct][lane];
+    const float M = fmaxf(m, m2);
+    const float f0 = m == -INFINITY ? 0.f : exp2f(m - M), f1 = m2 == -INFINITY ? 0.f : exp2f(m2 - M);
+    m = M;
+    l = l * f0 + l2 * f1;
+#pragma unroll
+    for (int i = 0; i < OC; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[i][r] = o[i][r] * f0 + so[(i * 16 + r) * 64] * f1;
+  }
+  if (!has) return;
+  // a Project-Only row of a routed layer emits zero
+  const int grow = row0 + row;
+  const bool po = a.run_mask != nullptr && on && a.run_mask[grow] == 0;
+  const float inv = po ? 0.f : 1.f / l;
+  if (a.ml != nullptr && on && hi == 0)
+    a.ml[static_cast<size_t>(grow) * (a.Hkv * G) + hk * G + qh] = po ? make_float2(INFINITY, 0.f) : make_float2(m, inv);
+  // the lane holds dims 32 i + 8 g + 4 hi + r of o[i][4 g + r]; two groups'
+  // halves change places so that it stores eight consecutive dims
+#pragma unroll
+  for (int i = 0; i < OC; ++i)
+#pragma unroll
+    for (int g = 0; g < 4; g += 2) {
+      uint32_t x[2], y[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        x[r] = po ? 0u : pack_bf2(o[i][4 * g + 2 * r] * inv, o[i][4 * g + 2 * r + 1] * inv);
+        y[r] = po ? 0u : pack_bf2(o[i][4 * g + 4 + 2 * r] * inv, o[i][4 * g + 5 + 2 * r] * inv);
+        const auto z = __builtin_amdgcn_permlane32_swap(x[r], y[r], false, false);
+        x[r] = z[0];
+        y[r] = z[1];
+      }
+      const int col = (hk * G + qh) * D + 32 * i + 8 * (g + hi);
+      const size_t at = a.out_Rg == 0 ? static_cast<size_t>(grow) * a.Nq + col : frag_index(grow, col, a.out_Rg);
+      if (on) *reinterpret_cast<u32x4*>(a.out + at) = u32x4{x[0], x[1], y[0], y[1]};
+    }
+}
+
+template <int D>
+static void launch_rows_d(const AttnPrefillArgs& a, int wgs, hipStream_t s) {
+  if (wgs <= 256) hipLaunchKernelGGL((k_attn_rows<D, 2>), dim3(wgs), dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((k_attn_rows<D, 1>), dim3(wgs), dim3(256), 0, s, a);
+}
+
+hipError_t launch_attn_rows(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s) {
+  if (n_items <= 0) return hipSuccess;
+  if (head_dim == 128) launch_rows_d<128>(a, n_items * a.Hkv, s);
+  else if (head_dim == 64) launch_rows_d<64>(a, n_items * a.Hkv, s);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+}  // namespace vsk
