@@ -14,11 +14,17 @@
 // a step, at 128 bytes a cycle longer than the step's MFMAs take; with 32 a
 // byte feeds twice the work.
 //
-// K and V go through registers into two LDS slots: the loads of step i + 2 are
-// issued and those of step i + 1 stored before step i is computed, with one
-// barrier a step.  NH halves of a workgroup walk alternate pairs of blocks and
-// are joined at the end: with few work items two halves keep two waves on each
-// SIMD, with many one half and two workgroups do.
+// K and V go through registers into four LDS slots: at step i the loads of step
+// i + 3 are issued and those of step i + 2 stored, with one barrier a step.  NH
+// halves of a workgroup walk alternate pairs of blocks and are joined at the
+// end: with few work items two halves keep two waves on each SIMD, with many
+// one half and two workgroups do.
+//
+// The 24 MFMAs of a step take about as long as its softmax.  One after the
+// other, with the two waves of a SIMD in step, they added up (129 us for 1,000
+// rows of 32/8 heads through a window of 4,096, matrix cores busy a third of
+// the time); so P V of a step waits for the next one and is issued between its
+// exponentials (@ROWS@).
 #include "attn_core.hpp"
 
 namespace vsk {
@@ -47,6 +53,11 @@ __device__ __forceinline__ bool not_finite(const u32x4 (&v)[N]) {
   return __any(top[0] >= 0x7f80 || top[1] >= 0x7f80);
 }
 
+// 0xffff in the halves that hold such a value.
+__device__ __forceinline__ uint32_t not_finite_halves(uint32_t v) {
+  return ((v & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((v & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+
 // Eight bf16 values of which those with a clear bit become zero.
 __device__ __forceinline__ u32x4 keep_bits(u32x4 v, uint32_t bits) {
 #pragma unroll
@@ -57,7 +68,7 @@ __device__ __forceinline__ u32x4 keep_bits(u32x4 v, uint32_t bits) {
 
 template <int D, int NH>
 struct RowsLds {
-  u32x4 kv[2][NH][2][2][2 * D];  // [slot][half][K, V][block][16-byte piece]
+  u32x4 kv[2][2][NH][2][2 * D];  // [slot][K, V][half][block][16-byte piece]
   int32_t tbl[kMaxSpanBlocks];
   float m[kRowTiles][64], l[kRowTiles][64];  // the second half's, when the halves join
 };
@@ -102,8 +113,6 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   // where a key counts for all its columns
   const bool has = 32 * ct < n_cols;
   const int ra = 32 * ct / G, rb = min(32 * ct + 31, n_cols - 1) / G;  // its first and last row
-  const int w_from = first_key(pos0 + ra + 1) / kBlock - span.wb + span.ns;
-  const int w_to = has ? (pos0 + rb) / kBlock - span.wb + span.ns + 1 : 0;
   const int full_end = min(kv_end, pos0 + ra + 1), full_lo = first_key(pos0 + rb + 1);
 
   const size_t head = static_cast<size_t>(kBlock) * D, stride = head * a.Hkv;
@@ -111,20 +120,25 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   const uint16_t* vbase = kbase + static_cast<size_t>(a.n_blocks) * stride;
   const int n_pairs = (span.nv + 1) / 2, n_steps = (n_pairs + NH - 1) / NH;
   u32x4 st[LD];
-  // piece tid + j T of a step's NH x {K, V} x two blocks x 2 D pieces; blocks
-  // past the list: its last one again (nobody counts its keys)
+  // A step's NH x {K, V} x two blocks x 2 D pieces, as they lie in LDS: the
+  // thread's are K and V of NJ places.  Blocks past the list: its last one
+  // again (nobody counts its keys).
+  constexpr int NJ = LD / 2;
+  auto place = [&](int j) { return tid + j * T; };  // of NH x two blocks x 2 D
   auto load = [&](int step) {
 #pragma unroll
-    for (int j = 0; j < LD; ++j) {
-      const int x = tid + j * T, piece = x % (2 * D), part = x / (2 * D);  // part: half, K or V, block
-      const int v = min(2 * (step * NH + part / 4) + part % 2, span.nv - 1);
-      const uint16_t* base = part & 2 ? vbase : kbase;
-      st[j] = *reinterpret_cast<const u32x4*>(base + static_cast<size_t>(sm.tbl[v]) * stride + piece * 8);
+    for (int j = 0; j < NJ; ++j) {
+      const int piece = place(j) % (2 * D), blk = place(j) / (2 * D);  // (blk: half, block)
+      const int v = min(2 * NH * step + blk, span.nv - 1);
+      const uint64_t at =
+          static_cast<uint64_t>(static_cast<uint32_t>(sm.tbl[v])) * static_cast<uint32_t>(stride) + piece * 8;
+      st[2 * j] = *reinterpret_cast<const u32x4*>(kbase + at);
+      st[2 * j + 1] = *reinterpret_cast<const u32x4*>(vbase + at);
     }
   };
   auto store = [&](int slot) {
 #pragma unroll
-    for (int j = 0; j < LD; ++j) (&sm.kv[slot][0][0][0][0])[tid + j * T] = st[j];
+    for (int j = 0; j < LD; ++j) (&sm.kv[slot][j % 2][0][0][0])[place(j / 2)] = st[j];
   };
   float m = -INFINITY, l = 0.f;
   f32x16 o[OC];
@@ -135,114 +149,161 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   const float sc = a.scale_log2;
 
   __syncthreads();  // tbl
-  load(0);
-  store(0);
-  if (n_steps > 1) load(1);
-  for (int step = 0; step < n_steps; ++step) {
-    barrier_after_lds_reads();  // step's slot is whole, the other one free
-    if (step + 1 < n_steps) store((step + 1) & 1);
-    if (step + 2 < n_steps) load(step + 2);
-    const int v = 2 * (step * NH + hh);  // the pair's first block of the list
-    if (v >= w_to || (v + 1 < w_from && kBlock * v >= a.sinks)) continue;
-    const int ba = span.block(v), bb = span.block(v + 1);
-    auto whole = [&](int b) {
-      return kBlock * (b + 1) <= full_end && (kBlock * b >= full_lo || kBlock * (b + 1) <= a.sinks);
-    };
-    const bool full = v + 1 < span.nv && whole(ba) && whole(bb);  // (uniform)
-    const u32x4* kp = &sm.kv[step & 1][hh][0][lc >> 4][(lane & 15) + 16 * hi];
-    f32x16 s;
+  // Blocks of the list of which every key counts for all columns of the wave:
+  // those before f_sinks, and f_from .. f_to - 1.
+  const int f_sinks = min(a.sinks / kBlock, span.ns);
+  const int f_from = (full_lo + kBlock - 1) / kBlock - span.wb + span.ns;
+  const int f_to = full_end / kBlock - span.wb + span.ns;
+  auto pair_of = [&](int step) { return 2 * (step * NH + hh); };  // a step's first block of the list
+  auto is_full = [&](int step) {  // (uniform)
+    const int v = pair_of(step);
+    return v + 1 < f_to && (v >= f_from || v + 1 < f_sinks);
+  };
+  // of a lane's keys, those that its column sees, and those that the sequence has
+  auto seen = [&](int step, int b) {
+    const int v = pair_of(step) + b;
+    return v < span.nv ? span_bits(kBlock * span.block(v) + 8 * hi, end, lo, a.sinks) : 0u;
+  };
+  auto held = [&](int step, int b) {
+    const int v = pair_of(step) + b;
+    return step >= 0 && v < span.nv ? span_bits(kBlock * span.block(v) + 8 * hi, kv_end, 0, 0) : 0u;
+  };
+  // V of a step of which some keys count for some columns only: those of no
+  // token become zero (slots past the sequence's end may hold a NaN, and
+  // 0 x NaN is NaN), and so do values that are not finite ...
+  bool poisoned = false;  // (uniform)
+  auto clean = [&](int step, int b, u32x4 (&vt)[OC]) __attribute__((always_inline)) {
+    const uint32_t keep = held(step, b);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    for (int i = 0; i < OC; ++i) vt[i] = keep_bits(vt[i], keep);
+    if (__builtin_expect(not_finite(vt), 0)) {
+      poisoned = true;
 #pragma unroll
-    for (int i = 0; i < QC; ++i) s = mfma_32x32x16(kp[32 * i], qf[i], s);
-    // s[r]: key 8 hi + r of block A (r < 8), 8 hi + r - 8 of block B
-    uint32_t bits[2] = {0xffu, 0xffu};
-    if (!full) {
-      bits[0] = span_bits(kBlock * ba + 8 * hi, end, lo, a.sinks);
-      bits[1] = v + 1 < span.nv ? span_bits(kBlock * bb + 8 * hi, end, lo, a.sinks) : 0u;
+      for (int i = 0; i < OC; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = bits[r / 8] >> (r % 8) & 1u ? s[r] : -INFINITY;
+        for (int j = 0; j < 4; ++j) vt[i][j] &= ~not_finite_halves(vt[i][j]);
     }
-    float mx = s[0];
+  };
+  // ... and here the columns that see one get NaN where it enters (rare)
+  auto poison = [&](int step) __attribute__((always_inline)) {
+    poisoned = false;
+    const u32x4* vp = &sm.kv[step & 1][1][hh][0][32 * (lc >> 4) + (lane & 15) + 16 * hi];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-    mx = max_xor32(mx) * sc;
-    if (__any(mx > m + kRowsLag)) {  // (-inf + 8 is -inf: a column's first keys always do)
-      const float mn = fmaxf(m, mx);
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-      m = mn;
-      l *= f;
+    for (int i = 0; i < OC; ++i) {
+      f32x16 y;  // how many such values of keys that the column sees
 #pragma unroll
-      for (int i = 0; i < OC; ++i) o[i] *= f;
-    }
-    const float mb = m == -INFINITY ? 0.f : m;
-    float p[16];
-    if (__builtin_expect(__any(fabsf(mb) >= kRoundedScores), 0)) {
-      // both sides of the difference rounded alike (see pair_softmax)
-#pragma clang fp contract(off)
+      for (int r = 0; r < 16; ++r) y[r] = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float x = s[r] * sc;
-        p[r] = __builtin_amdgcn_exp2f(x - mb);
+      for (int b = 0; b < 2; ++b) {
+        u32x4 x = vp[2 * D * b + 64 * i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = not_finite_halves(x[j]) & 0x3f803f80u;  // 1.0
+        y = mfma_32x32x16(x, keep_bits(u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}, seen(step, b)), y);
       }
-    } else {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc, -mb));
+      for (int r = 0; r < 16; ++r) o[i][r] = y[r] != 0.f ? NAN : o[i][r];
     }
-    float ps[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) ps[j] = (p[j] + p[j + 4]) + (p[j + 8] + p[j + 12]);
-    l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
-    u32x4 pt[2][kSpanPTerms];  // [block][term]
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float r0 = p[8 * b + 2 * j], r1 = p[8 * b + 2 * j + 1];
-#pragma unroll
-        for (int t = 0; t < kSpanPTerms; ++t) {
-          pt[b][t][j] = pack_bf2(r0, r1);
-          r0 -= bf2f(pt[b][t][j]);
-          r1 -= __uint_as_float(pt[b][t][j] & 0xffff0000u);
-        }
-      }
-    const u32x4* vp = &sm.kv[step & 1][hh][1][0][32 * (lc >> 4) + (lane & 15) + 16 * hi];
+  };
+
+  // O^T += V^T P^T of a step, block by block.  FAST: every key counts, the
+  // maximum has not moved and no score is huge -- no branch and no change of a
+  // register on a condition, which the compiler would pay for with copies of
+  // all the sums in every step.
+  auto rest = [&](int step, const f32x16& s, auto fast_c) __attribute__((always_inline)) {
+    constexpr bool FAST = decltype(fast_c)::value;
+    const u32x4* vp = &sm.kv[step & 1][1][hh][0][32 * (lc >> 4) + (lane & 15) + 16 * hi];
+    const float mb = !FAST && m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       u32x4 vt[OC];
 #pragma unroll
       for (int i = 0; i < OC; ++i) vt[i] = vp[2 * D * b + 64 * i];
-      if (!full) {
-        // slots past the sequence's end may hold a NaN, and 0 x NaN is NaN
-        const uint32_t held = v + b < span.nv ? span_bits(kBlock * (b ? bb : ba) + 8 * hi, kv_end, 0, 0) : 0u;
+      float p[8];
+      if constexpr (FAST) {
 #pragma unroll
-        for (int i = 0; i < OC; ++i) vt[i] = keep_bits(vt[i], held);
-        if (__builtin_expect(not_finite(vt), 0)) {
-          // so may keys that some columns see and others do not: each column
-          // on its own, the keys that it does not see set to zero (rare, slow)
-#pragma unroll 1
-          for (int h = 0; h < 32; ++h) {
-            const uint32_t sees = __shfl(bits[b], h + (lane & 32), 64) & held;
+        for (int r = 0; r < 8; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[8 * b + r], sc, -mb));
+      } else {
+        // both sides of a difference rounded alike (see pair_softmax)
+#pragma clang fp contract(off)
 #pragma unroll
-            for (int i = 0; i < OC; ++i) {
-              f32x16 y;
-#pragma unroll
-              for (int r = 0; r < 16; ++r) y[r] = 0.f;
-              const u32x4 vz = keep_bits(vp[2 * D * b + 64 * i], sees);
-#pragma unroll
-              for (int t = 0; t < kSpanPTerms; ++t) y = mfma_32x32x16(vz, pt[b][t], y);
-#pragma unroll
-              for (int r = 0; r < 16; ++r) o[i][r] = lc == h ? o[i][r] + y[r] : o[i][r];
-            }
-          }
-          continue;
+        for (int r = 0; r < 8; ++r) {
+          const float x = s[8 * b + r] * sc;
+          p[r] = __builtin_amdgcn_exp2f(x - mb);
         }
       }
+      l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      u32x4 pt[kSpanPTerms];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float r0 = p[2 * j], r1 = p[2 * j + 1];
+#pragma unroll
+        for (int t = 0; t < kSpanPTerms; ++t) {
+          pt[t][j] = pack_bf2(r0, r1);
+          r0 -= bf2f(pt[t][j]);
+          r1 -= __uint_as_float(pt[t][j] & 0xffff0000u);
+        }
+      }
+      if constexpr (!FAST) clean(step, b, vt);
 #pragma unroll
       for (int t = 0; t < kSpanPTerms; ++t)
 #pragma unroll
-        for (int i = 0; i < OC; ++i) o[i] = mfma_32x32x16(vt[i], pt[b][t], o[i]);
+        for (int i = 0; i < OC; ++i) o[i] = mfma_32x32x16(vt[i], pt[t], o[i]);
     }
+  };
+
+  load(0);
+  store(0);
+  if (n_steps > 1) load(1);
+  bool big = false;  // (uniform) scores so large that a fma's unrounded product would be off the maximum
+  f32x16 s;          // s[r]: key 8 hi + r of the step's first block (r < 8), 8 hi + r - 8 of the second
+  float mx;
+  auto scores = [&](int step) __attribute__((always_inline)) {
+    barrier_after_lds_reads();  // the step's slot is whole, the other one free
+    if (step + 1 < n_steps) {
+      store((step + 1) & 1);
+      load(step + 2);  // (past the list: its last block)
+    }
+    const u32x4* kp = &sm.kv[step & 1][0][hh][lc >> 4][(lane & 15) + 16 * hi];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < QC; ++i) s = mfma_32x32x16(kp[32 * i], qf[i], s);
+    mx = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    mx = max_xor32(mx) * sc;
+  };
+  int step = 0;
+  scores(0);
+  for (;;) {
+    // (a loop of its own, so that the sums stay where they are)
+    while (is_full(step) && !big && !__any(mx > m + kRowsLag)) {  // (-inf + 8 is -inf: first keys always are)
+      rest(step, s, std::true_type{});
+      if (++step == n_steps) break;
+      scores(step);
+    }
+    if (step == n_steps) break;
+    if (!is_full(step)) {
+      const uint32_t bits = seen(step, 0) | seen(step, 1) << 8;
+      mx = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = bits >> r & 1u ? s[r] : -INFINITY;
+        mx = fmaxf(mx, s[r]);
+      }
+      mx = max_xor32(mx) * sc;
+    }
+    const float mn = fmaxf(m, mx);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+    m = mn;
+    l *= f;
+#pragma unroll
+    for (int i = 0; i < OC; ++i) o[i] *= f;
+    big = __any(fabsf(m) >= kRoundedScores && m != -INFINITY);
+    rest(step, s, std::false_type{});
+    if (__builtin_expect(poisoned, 0)) poison(step);
+    if (++step == n_steps) break;
+    scores(step);
   }
   l = add_xor32(l);
 
