@@ -1165,6 +1165,7 @@ struct AttnPlan {
   AttnPrefillArgs pre{};
   bool cascade = false, prefill = false, span = false;
   int dec_splits = 1, pfx_fold = 0;
+  int64_t part_bytes = 0;  // of the split partials' space
 };
 
 // out_Rg: the output as frags of that many row groups, 0 for row-major.
@@ -1298,6 +1299,7 @@ static AttnPlan plan_attn(Handle& h, const uint16_t* q, uint16_t* out, int out_R
   // (maximum, 1 / sum) per row and head: in the space of the K-split products,
   // which are added up before attention starts and written after it ends
   // (8 bytes a head against at least 4 * head_dim)
+  p.part_bytes = static_cast<int64_t>(wl.att_ml - wl.att_o);
   if (general) aa.ml = pf.ml = reinterpret_cast<float2*>(ws + wl.ypart);
   return p;
 }
@@ -1344,7 +1346,21 @@ static hipError_t launch_mass(Handle& h, const AttnPlan& p, int layer, float* ma
   m.mass = mass;
   m.stride = stride;
   m.add = add ? 1 : 0;
-  return launch_attn_mass(m, h.bd.n_seqs, h.bd.max_kv_len, h.cfg.head_dim, s);
+  // sequences of several rows: enough parts of their rows for four workgroups a
+  // compute unit, in the space of the split partials, which are done with
+  const BatchHost& bh = h.bh;
+  int64_t tiles = 0, singles = 0;
+  for (int32_t i = 0; i < bh.n_seqs; ++i) {
+    if (bh.cu_q[i + 1] - bh.cu_q[i] == 1) ++singles;
+    else tiles += (bh.kv_len[i] + kMassTile - 1) / kMassTile;
+  }
+  m.part = p.dec.part_o;
+  m.part_len = (h.bd.max_kv_len + kMassTile - 1) / kMassTile * kMassTile;
+  if (tiles > 0) {
+    const int64_t room = (p.part_bytes / 4) / (static_cast<int64_t>(m.Hkv) * bh.n_seqs * m.part_len);
+    m.parts = static_cast<int>(std::min<int64_t>({room, 16, (1024 + tiles * m.Hkv - 1) / (tiles * m.Hkv)}));
+  }
+  return launch_attn_mass(m, h.bd.n_seqs, singles > 0, h.bd.max_kv_len, h.cfg.head_dim, s);
 }
 
 hipError_t run_attend(Handle& h, int layer, const uint16_t* q, uint16_t* out, int window, int sinks, float* mass,

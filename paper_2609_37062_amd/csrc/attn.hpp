@@ -96,7 +96,13 @@ struct AttnMassArgs {
   float* mass;       // [n_seqs][stride]
   int64_t stride;
   int add;  // 0: mass = the weights, 1: mass += them
+  // sequences of several rows: their weights per (KV head, part of the rows)
+  // go to part [Hkv * parts][n_seqs][part_len] first, and are added up from
+  // there; 0 parts: taken as those of one row are
+  float* part;
+  int parts, part_len;
 };
+constexpr int kMassTile = 128;  // keys of a work item of such a sequence
 
 // Shared-prefix attention: each work item reads a run of a group's prefix
 // blocks once for up to kPfxCols (row, query head) columns of the group.
@@ -127,6 +133,7 @@ hipError_t launch_attn_prefix(const AttnPrefixArgs& a, int n_items, int head_dim
 hipError_t launch_attn_prefill(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s);
 // the general one of prompt rows (k_rows.hip)
 hipError_t launch_attn_rows(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s);
-hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, int max_kv_len, int head_dim, hipStream_t s);
+hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, bool singles, int max_kv_len, int head_dim,
+                            hipStream_t s);
 
 }  // namespace vsk

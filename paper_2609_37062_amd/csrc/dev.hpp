@@ -44,6 +44,13 @@ __device__ __forceinline__ f32x4 mfma_16x16x32(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
                                                  __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
+// D(32x32,f32) += A(32x16) * B(16x32): lane l feeds row (column) l % 32 of A (B),
+// k 8 (l / 32) .. + 7, and holds D[8 (r / 4) + 4 (l / 32) + r % 4][l % 32] in r.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16 mfma_32x32x16(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
+                                                 0, 0);
+}
 // Write-through stores (sc1): the data goes to memory instead of staying in
 // this XCD's L2, so a workgroup on another XCD of the same launch reads it
 // once this wave's memory counter has drained.  Plain stores are only made

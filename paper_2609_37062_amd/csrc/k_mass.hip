@@ -6,9 +6,23 @@
 // with s the base-2 score and (m, 1 / l) what the attention of these rows left
 // for each (row, head).  Scores are taken again from K and q with the
 // attention's own products, so an exponent is exactly the one that the softmax
-// summed.  A workgroup owns 32 keys of a sequence and sums over every head and
-// row, each wave a run of (KV head, 16-column tile) units, in a fixed order:
-// no atomics, so results do not change from run to run.
+// summed.  Every sum is taken in a fixed order: no atomics, so results do not
+// change from run to run.
+//
+// k_attn_mass, for sequences of one row: a workgroup owns 32 keys of a sequence
+// and sums over every head and row, each wave a run of (KV head, 16-column tile)
+// units.  It reads K once more, and that bounds it.
+//
+// k_mass_rows, for sequences of several rows: a product of K with all the
+// queries that see it, 4 hd flops less than the attention's for each (row,
+// head, key), and an exponential for each.  A workgroup of four waves owns 128
+// keys of a KV head, 32 a wave, which stay in registers as the operand of
+// v_mfma_f32_32x32x16_bf16; the queries pass by in tiles of 32 (row, head)
+// columns through LDS, one read for all four waves.  Each wave sums its keys'
+// weights per lane and across lanes once at the end.  The KV heads, and parts
+// of the rows where there are few keys, are added up by k_mass_sum.  777 rows
+// over 2,300 cached tokens (32/8 heads x 128): 196 us as k_attn_mass (every
+// workgroup read every query, 16 columns at a time), 41 + 5 of the sum.
 #include "attn_core.hpp"
 
 namespace vsk {
@@ -26,6 +40,7 @@ __global__ __launch_bounds__(64 * kMassWaves) void k_attn_mass(AttnMassArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane & 15, quad = lane >> 4;
   const int r0 = a.cu_q[seq], n = a.cu_q[seq + 1] - r0;
+  if (n > 1 && a.parts > 0) return;  // k_mass_rows
   const int p0 = kv_len - n;  // position of the first row
   // the rows that see any of these keys: from position t0 on, and while the
   // window reaches back to key t0 + 31 (a sink key is seen by all of them)
@@ -104,12 +119,183 @@ __global__ __launch_bounds__(64 * kMassWaves) void k_attn_mass(AttnMassArgs a) {
   }
 }
 
-hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, int max_kv_len, int head_dim, hipStream_t s) {
-  const dim3 grid((max_kv_len + 31) / 32, n_seqs);
-  if (head_dim == 128) hipLaunchKernelGGL((k_attn_mass<128>), grid, dim3(64 * kMassWaves), 0, s, a);
-  else if (head_dim == 64) hipLaunchKernelGGL((k_attn_mass<64>), grid, dim3(64 * kMassWaves), 0, s, a);
-  else return hipErrorInvalidValue;
+constexpr int kMassCols = 32;  // columns of a tile
+
+template <int D>
+__global__ __launch_bounds__(256, 4) void k_mass_rows(AttnMassArgs a) {
+  constexpr int QC = D / 16;   // operands of a tile
+  constexpr int P = D / 8;     // 16-byte pieces of a query
+  constexpr int LD = kMassCols * P / 256;  // of a tile's, a thread
+  __shared__ u32x4 s_q[2][P * kMassCols];  // [slot][piece][column ^ piece % 8]
+  __shared__ float2 s_ml[2][kMassCols];
+  const int seq = blockIdx.z;
+  const int kv_len = a.kv_len[seq];
+  const int r0 = a.cu_q[seq], n = a.cu_q[seq + 1] - r0;
+  const int t0 = kMassTile * blockIdx.x;
+  if (t0 >= kv_len || n == 1) return;
+  const int hk = blockIdx.y % a.Hkv, part = blockIdx.y / a.Hkv;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lc = lane & 31, hi = lane >> 5, G = a.G;
+  const int p0 = kv_len - n;  // position of the first row
+  // the rows that see any of the 128 keys (see k_attn_mass), and of their
+  // columns this part's tiles
+  const int ra = max(0, t0 - p0);
+  const int rb = a.window > 0 && t0 >= a.sinks ? min(n, t0 + kMassTile - 1 + a.window - p0) : n;
+  const int c_end = rb * G;
+  const int all = max(0, c_end - ra * G + kMassCols - 1) / kMassCols;
+  const int per = (all + a.parts - 1) / a.parts;
+  const int i0 = min(all, part * per), tiles = min(all, i0 + per) - i0;
+  const int c_first = ra * G + i0 * kMassCols;
+
+  // K of the wave's 32 keys (blocks past the sequence: its last one again)
+  const int nb = (kv_len + kBlock - 1) / kBlock;
+  const int tw = t0 + 32 * w, bl = tw / kBlock;
+  u32x4 kt[QC];
+  {
+    const int32_t* table = a.block_table + static_cast<size_t>(seq) * a.max_blocks;
+    const size_t head = static_cast<size_t>(kBlock) * D, stride = head * a.Hkv;
+    const size_t blk = table[min(bl + (lc >> 4), nb - 1)];
+    const u32x4* kp = reinterpret_cast<const u32x4*>(a.pool + (static_cast<size_t>(a.layer) * 2 * a.n_blocks + blk) * stride +
+                                                     hk * head) + (lane & 15) + 16 * hi;
+#pragma unroll
+    for (int i = 0; i < QC; ++i) kt[i] = kp[32 * i];
+  }
+  // a tile's queries: the thread's pieces tid % P of columns tid / P + (256 / P) j;
+  // a column's row and head move on by 32 columns a tile
+  const int dr = kMassCols / G, dg = kMassCols % G;
+  int row[LD], g[LD];
+#pragma unroll
+  for (int j = 0; j < LD; ++j) {
+    const int c = c_first + tid / P + 256 / P * j;
+    row[j] = c / G;
+    g[j] = c % G;
+  }
+  auto step = [&](int& r, int& h) {
+    r += dr;
+    h += dg;
+    const int over = h >= G;
+    r += over;
+    h -= over ? G : 0;
+  };
+  u32x4 st[LD];
+  float2 stm = make_float2(0.f, 0.f);
+  int mrow = (c_first + lc) / G, mg = (c_first + lc) % G;  // the lane's own column, and (first 32 threads) whose ml to load
+  int lrow = mrow, lg = mg;
+  const uint16_t* qh = a.q + static_cast<size_t>(r0) * a.Nq + static_cast<size_t>(hk) * G * D + tid % P * 8;
+  const float2* mlh = a.ml + static_cast<size_t>(r0) * (a.Hkv * G) + hk * G;
+  auto load = [&]() {  // (columns past the last row: its last head again, nobody counts them)
+#pragma unroll
+    for (int j = 0; j < LD; ++j) {
+      const int r = min(row[j], n - 1);
+      st[j] = *reinterpret_cast<const u32x4*>(qh + static_cast<size_t>(r) * a.Nq + g[j] * D);
+      step(row[j], g[j]);
+    }
+    if (tid < kMassCols) stm = mlh[static_cast<size_t>(min(lrow, n - 1)) * (a.Hkv * G) + lg];
+    step(lrow, lg);
+  };
+  auto store = [&](int slot) {
+    const int k = tid % P;
+#pragma unroll
+    for (int j = 0; j < LD; ++j) s_q[slot][k * kMassCols + ((tid / P + 256 / P * j) ^ (k & 7))] = st[j];
+    if (tid < kMassCols) s_ml[slot][tid] = stm;
+  };
+  const float sc = a.scale_log2;
+  float acc[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+  if (tiles > 0) {
+    load();
+    store(0);
+    if (tiles > 1) load();
+  }
+  for (int i = 0; i < tiles; ++i) {
+    barrier_after_lds_reads();  // the tile's slot is whole, the other one free
+    if (i + 1 < tiles) {
+      store((i + 1) & 1);
+      if (i + 2 < tiles) load();
+    }
+    const float2 ml = s_ml[i & 1][lc];
+    f32x16 s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < QC; ++c) {
+      const int k = 2 * c + hi;
+      s = mfma_32x32x16(kt[c], s_q[i & 1][k * kMassCols + (lc ^ (k & 7))], s);
+    }
+    // s[r]: key tw + 8 hi + r (r < 8), tw + 16 + 8 hi + r - 8
+    const int c0 = c_first + kMassCols * i;
+    const int fr = c0 / G, lr = min(c0 + kMassCols, c_end) - 1;  // (uniform) first row, last column
+    const int end0 = p0 + fr + 1, end1 = p0 + lr / G + 1;      // keys of the first and the last row
+    const bool full = c0 + kMassCols <= c_end && tw + 32 <= min(kv_len, end0) &&
+                      (a.window == 0 || end1 <= a.window || tw >= end1 - a.window || tw + 32 <= a.sinks);
+    if (full && !__any(fabsf(ml.x) >= kRoundedScores)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[r] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[r], sc, -ml.x)), ml.y, acc[r]);
+    } else {
+      // (both sides of a difference rounded alike, see pair_softmax)
+#pragma clang fp contract(off)
+      const int end = c0 + lc < c_end ? min(kv_len, p0 + mrow + 1) : 0;
+      const int lo = a.window > 0 && p0 + mrow + 1 > a.window ? p0 + mrow + 1 - a.window : 0;
+      const uint32_t bits =
+          span_bits(tw + 8 * hi, end, lo, a.sinks) | span_bits(tw + kBlock + 8 * hi, end, lo, a.sinks) << 8;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = s[r] * sc;
+        const float y = __builtin_amdgcn_exp2f(x - ml.x) * ml.y;
+        acc[r] += bits >> r & 1u ? y : 0.f;
+      }
+    }
+    step(mrow, mg);
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) acc[r] += shfl_xor(acc[r], x);
+  if (lc == 0) {
+    float* dst = a.part + (static_cast<size_t>(part * a.Hkv + hk) * gridDim.z + seq) * a.part_len + tw + 8 * hi;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dst[r < 8 ? r : r + 8] = acc[r];  // (part_len is a multiple of the tile)
+  }
+}
+
+// mass = (or +=) the sum over KV heads and parts, of the sequences of several rows.
+__global__ __launch_bounds__(256) void k_mass_sum(AttnMassArgs a) {
+  const int seq = blockIdx.y, t = blockIdx.x * 256 + threadIdx.x;
+  if (a.cu_q[seq + 1] - a.cu_q[seq] == 1 || t >= a.kv_len[seq]) return;
+  const int n = a.Hkv * a.parts;
+  const size_t next = static_cast<size_t>(gridDim.y) * a.part_len;
+  const float* p = a.part + static_cast<size_t>(seq) * a.part_len + t;
+  float* dst = a.mass + seq * a.stride + t;
+  float y = 0.f;
+  for (int i = 0; i < n; i += 8) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = p[min(i + j, n - 1) * next];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y += i + j < n ? v[j] : 0.f;
+  }
+  *dst = (a.add != 0 ? *dst : 0.f) + y;
+}
+
+template <int D>
+static hipError_t launch_mass_d(const AttnMassArgs& a, int n_seqs, bool singles, int max_kv_len, hipStream_t s) {
+  if (singles || a.parts == 0)
+    hipLaunchKernelGGL((k_attn_mass<D>), dim3((max_kv_len + 31) / 32, n_seqs), dim3(64 * kMassWaves), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 0) return e;
+  hipLaunchKernelGGL((k_mass_rows<D>), dim3((max_kv_len + kMassTile - 1) / kMassTile, a.Hkv * a.parts, n_seqs), dim3(256),
+                     0, s, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL(k_mass_sum, dim3((max_kv_len + 255) / 256, n_seqs), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+
+hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, bool singles, int max_kv_len, int head_dim,
+                            hipStream_t s) {
+  if (head_dim == 128) return launch_mass_d<128>(a, n_seqs, singles, max_kv_len, s);
+  if (head_dim == 64) return launch_mass_d<64>(a, n_seqs, singles, max_kv_len, s);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace vsk

@@ -29,12 +29,6 @@
 
 namespace vsk {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-__device__ __forceinline__ f32x16 mfma_32x32x16(u32x4 a, u32x4 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
-                                                 0, 0);
-}
-
 constexpr int kRowTiles = 4;               // 32-column tiles of a work item
 static_assert(kRowTiles * 32 == kPreCols, "a work item's columns");
 // A running maximum may lag by this (base 2) before the sums are rescaled: the
