@@ -1300,6 +1300,16 @@ static AttnPlan plan_attn(Handle& h, const uint16_t* q, uint16_t* out, int out_R
   // which are added up before attention starts and written after it ends
   // (8 bytes a head against at least 4 * head_dim)
   p.part_bytes = static_cast<int64_t>(wl.att_ml - wl.att_o);
+  // the scores of one-row sequences for their weights per key, where they fit
+  // behind the split partials (which are sized for splits of 8 blocks)
+  if (general && !cascade && b.n_dec_rows > 0 && (p.prefill || b.n_pre_items == 0)) {
+    const int64_t used = static_cast<int64_t>(R) * c.n_kv_heads * aa.split_stride * aa.G * d * 4;
+    const int64_t len = static_cast<int64_t>(blk_max + 1) / 2 * 32;
+    if (used + len * b.n_dec_rows * c.n_q_heads * 4 <= p.part_bytes) {
+      aa.scores = aa.part_o + used / 4;
+      aa.scores_len = len;
+    }
+  }
   if (general) aa.ml = pf.ml = reinterpret_cast<float2*>(ws + wl.ypart);
   return p;
 }
@@ -1354,13 +1364,19 @@ static hipError_t launch_mass(Handle& h, const AttnPlan& p, int layer, float* ma
     if (bh.cu_q[i + 1] - bh.cu_q[i] == 1) ++singles;
     else tiles += (bh.kv_len[i] + kMassTile - 1) / kMassTile;
   }
+  m.scores = p.dec.scores;
+  m.scores_len = p.dec.scores_len;
+  m.rows = h.bd.dec_rows;
+  m.n_rows = h.bd.n_dec_rows;
+  m.row_seq = h.bd.row_seq;
+  m.hd = h.cfg.head_dim;
   m.part = p.dec.part_o;
   m.part_len = (h.bd.max_kv_len + kMassTile - 1) / kMassTile * kMassTile;
   if (tiles > 0) {
     const int64_t room = (p.part_bytes / 4) / (static_cast<int64_t>(m.Hkv) * bh.n_seqs * m.part_len);
     m.parts = static_cast<int>(std::min<int64_t>({room, 16, (1024 + tiles * m.Hkv - 1) / (tiles * m.Hkv)}));
   }
-  return launch_attn_mass(m, h.bd.n_seqs, singles > 0, h.bd.max_kv_len, h.cfg.head_dim, s);
+  return launch_attn_mass(m, h.bd.n_seqs, singles > 0, tiles > 0, h.bd.max_kv_len, h.cfg.head_dim, s);
 }
 
 hipError_t run_attend(Handle& h, int layer, const uint16_t* q, uint16_t* out, int window, int sinks, float* mass,

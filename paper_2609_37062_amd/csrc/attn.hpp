@@ -59,6 +59,10 @@ struct AttnArgs {
   // each (row, query head)'s softmax maximum (base 2) and 1 / sum
   int window, sinks;
   float2* ml;  // [R][Nq / hd]
+  // nullable: the scores too, [rows of the launch][Nq / hd][scores_len], key by
+  // key of the row's SpanWalk list, -inf where the row does not see it
+  float* scores;
+  int64_t scores_len;
 };
 
 // Causal attention of prefill rows (see k_attn_prefill).
@@ -85,7 +89,7 @@ struct AttnPrefillArgs {
 struct AttnMassArgs {
   const uint16_t* q;  // [R][Nq] bf16
   const uint16_t* pool;
-  int layer, n_blocks, Hkv, G, Nq;
+  int layer, n_blocks, Hkv, hd, G, Nq;
   const int32_t* block_table;  // [n_seqs][max_blocks]
   int max_blocks;
   const int32_t* kv_len;  // [n_seqs]
@@ -101,6 +105,13 @@ struct AttnMassArgs {
   // there; 0 parts: taken as those of one row are
   float* part;
   int parts, part_len;
+  // sequences of one row: their scores, as the attention left them (nullable:
+  // taken again), and the rows of that launch
+  const float* scores;
+  int64_t scores_len;
+  const int32_t* rows;
+  int n_rows;
+  const int32_t* row_seq;
 };
 constexpr int kMassTile = 128;  // keys of a work item of such a sequence
 
@@ -133,7 +144,8 @@ hipError_t launch_attn_prefix(const AttnPrefixArgs& a, int n_items, int head_dim
 hipError_t launch_attn_prefill(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s);
 // the general one of prompt rows (k_rows.hip)
 hipError_t launch_attn_rows(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s);
-hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, bool singles, int max_kv_len, int head_dim,
+// singles, several: the batch has sequences of one row, of several
+hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, bool singles, bool several, int max_kv_len, int head_dim,
                             hipStream_t s);
 
 }  // namespace vsk

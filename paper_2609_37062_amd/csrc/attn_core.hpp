@@ -278,8 +278,10 @@ __device__ __forceinline__ void pair_pv(u32x4 (&vt)[D / 16], int t0, int t_end, 
 // SPAN: the general walk (AttnArgs::window, sinks, ml, row-major output): the
 // wave's blocks are a run of the row's SpanWalk list, and a step is full
 // where both of its blocks are visible whole.
+// launch_row: the row's place in the launch, for its scores.
 template <int D, bool WT, int NW, bool FOLD2 = false, bool NTKV = true, bool SPAN = false>
-__device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, int split, AttnLds<D, NW>& sm) {
+__device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, int split, AttnLds<D, NW>& sm,
+                                          int launch_row = 0) {
   constexpr int KC = D / 32;  // K chunks (1 KiB) per block
   constexpr int VC = D / 16;  // V chunks (512 B) per block
 
@@ -455,6 +457,12 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
       f32x4 s0, s1;
       pair_qk<D>(qf, kg, s0, s1);
       if (!full) span_mask(bits, s0, s1);
+      if (a.scores != nullptr && h < G && 2 * p + (quad >> 1) < cnt) {  // (16 bytes to 4 floats each)
+        float* dst = a.scores +
+                     ((static_cast<int64_t>(launch_row) * a.Hkv + hk) * G + h) * a.scores_len + kBlock * va + 8 * quad;
+        *reinterpret_cast<f32x4*>(dst) = s0;
+        *reinterpret_cast<f32x4*>(dst + 4) = s1;
+      }
       PTermsOf<kSpanPTerms> pp;
       pair_softmax<false>(s0, s1, sc, m, l, pp, alpha);
       if constexpr (!LAST) {

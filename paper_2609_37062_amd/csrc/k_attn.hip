@@ -39,7 +39,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn_decode(AttnArgs a) {
   __shared__ AttnLds<D, kAttnWaves> sm;
   const int split = (blockIdx.y + blockIdx.z) % gridDim.y;
   attn_unit<D, false, kAttnWaves, FOLD2, NTKV, SPAN>(
-      a, a.rows != nullptr ? a.rows[blockIdx.z] : static_cast<int>(blockIdx.z), blockIdx.x, split, sm);
+      a, a.rows != nullptr ? a.rows[blockIdx.z] : static_cast<int>(blockIdx.z), blockIdx.x, split, sm, blockIdx.z);
 }
 
 template <int D, bool FOLD2, bool NTKV, bool SPAN>

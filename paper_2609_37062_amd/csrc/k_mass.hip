@@ -11,7 +11,12 @@
 //
 // k_attn_mass, for sequences of one row: a workgroup owns 32 keys of a sequence
 // and sums over every head and row, each wave a run of (KV head, 16-column tile)
-// units.  It reads K once more, and that bounds it.
+// units.  It reads K once more, and that bounds it.  So the attention of such
+// rows leaves its scores where the workspace has room for them, 4 bytes a (head,
+// key) beside 4 hd of K and V a (KV head, key), and k_mass_scores sums over
+// those instead: 32 sequences of 1,000-4,000 tokens (32/8 heads x 128) 32 us,
+// of its own; with the scores the
+// attention takes 60 instead of 54 and their sum 5.
 //
 // k_mass_rows, for sequences of several rows: a product of K with all the
 // queries that see it, 4 hd flops less than the attention's for each (row,
@@ -40,7 +45,7 @@ __global__ __launch_bounds__(64 * kMassWaves) void k_attn_mass(AttnMassArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane & 15, quad = lane >> 4;
   const int r0 = a.cu_q[seq], n = a.cu_q[seq + 1] - r0;
-  if (n > 1 && a.parts > 0) return;  // k_mass_rows
+  if (n > 1 ? a.parts > 0 : a.scores != nullptr) return;  // k_mass_rows, k_mass_scores
   const int p0 = kv_len - n;  // position of the first row
   // the rows that see any of these keys: from position t0 on, and while the
   // window reaches back to key t0 + 31 (a sink key is seen by all of them)
@@ -117,6 +122,63 @@ __global__ __launch_bounds__(64 * kMassWaves) void k_attn_mass(AttnMassArgs a) {
     for (int i = 1; i < kMassWaves; ++i) y += s_sum[i][tid];
     *dst = s + y;
   }
+}
+
+// One workgroup per 256 keys of a sequence, four keys a lane, its four waves
+// sharing the heads; the waves' sums are added in order.
+__global__ __launch_bounds__(256) void k_mass_scores(AttnMassArgs a) {
+  __shared__ float4 s_sum[4][64];
+  const int row = a.rows[blockIdx.y], seq = a.row_seq[row];
+  const int kv_len = a.kv_len[seq];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t0 = 256 * blockIdx.x;
+  if (t0 >= kv_len) return;
+  const int t = t0 + 4 * lane, b = t / kBlock;
+  const SpanWalk span = span_walk(kv_len, kv_len, a.window, a.sinks);
+  const bool in = t < kv_len && (b < span.ns || b >= span.wb);
+  const int v = (b < span.ns ? b : b - span.wb + span.ns) * kBlock + t % kBlock;  // its place in the list
+  const int heads = a.Nq / a.hd;
+  const float* sp = a.scores + static_cast<int64_t>(blockIdx.y) * heads * a.scores_len + (in ? v : 0);
+  const float2* mlp = a.ml + static_cast<int64_t>(row) * heads;
+  float y[4] = {0.f, 0.f, 0.f, 0.f};
+  constexpr int kU = 4;  // heads in flight
+  for (int h0 = w; h0 < heads; h0 += 4 * kU) {
+    float4 s[kU];
+    float2 ml[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int h = min(h0 + 4 * u, heads - 1);
+      s[u] = *reinterpret_cast<const float4*>(sp + static_cast<int64_t>(h) * a.scores_len);
+      ml[u] = mlp[h];
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      // (both sides of a difference rounded alike, see pair_softmax; a
+      // Project-Only row has no scores, and nothing to sum)
+#pragma clang fp contract(off)
+      const bool on = h0 + 4 * u < heads && ml[u].y != 0.f;
+      const float x[4] = {s[u].x, s[u].y, s[u].z, s[u].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float z = x[j] * a.scale_log2;
+        const float e = __builtin_amdgcn_exp2f(z - ml[u].x) * ml[u].y;
+        y[j] += on ? e : 0.f;
+      }
+    }
+  }
+  s_sum[w][lane] = make_float4(y[0], y[1], y[2], y[3]);
+  __syncthreads();
+  if (w != 0) return;
+  float z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 x = s_sum[i][lane];
+    z[0] += x.x; z[1] += x.y; z[2] += x.z; z[3] += x.w;
+  }
+  float* dst = a.mass + seq * a.stride + t;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (t + j < kv_len) dst[j] = (a.add != 0 ? dst[j] : 0.f) + (in ? z[j] : 0.f);
 }
 
 constexpr int kMassCols = 32;  // columns of a tile
@@ -279,8 +341,12 @@ __global__ __launch_bounds__(256) void k_mass_sum(AttnMassArgs a) {
 }
 
 template <int D>
-static hipError_t launch_mass_d(const AttnMassArgs& a, int n_seqs, bool singles, int max_kv_len, hipStream_t s) {
-  if (singles || a.parts == 0)
+static hipError_t launch_mass_d(const AttnMassArgs& a, int n_seqs, bool singles, bool several, int max_kv_len,
+                                hipStream_t s) {
+  // (sequences of one row first: the scores lie where the others' parts go)
+  if (singles && a.scores != nullptr)
+    hipLaunchKernelGGL(k_mass_scores, dim3((max_kv_len + 255) / 256, a.n_rows), dim3(256), 0, s, a);
+  if ((singles && a.scores == nullptr) || (several && a.parts == 0))
     hipLaunchKernelGGL((k_attn_mass<D>), dim3((max_kv_len + 31) / 32, n_seqs), dim3(64 * kMassWaves), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 0) return e;
@@ -291,10 +357,10 @@ static hipError_t launch_mass_d(const AttnMassArgs& a, int n_seqs, bool singles,
   return hipGetLastError();
 }
 
-hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, bool singles, int max_kv_len, int head_dim,
+hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, bool singles, bool several, int max_kv_len, int head_dim,
                             hipStream_t s) {
-  if (head_dim == 128) return launch_mass_d<128>(a, n_seqs, singles, max_kv_len, s);
-  if (head_dim == 64) return launch_mass_d<64>(a, n_seqs, singles, max_kv_len, s);
+  if (head_dim == 128) return launch_mass_d<128>(a, n_seqs, singles, several, max_kv_len, s);
+  if (head_dim == 64) return launch_mass_d<64>(a, n_seqs, singles, several, max_kv_len, s);
   return hipErrorInvalidValue;
 }
 

@@ -165,6 +165,18 @@ def test_weights_per_token(q_lens, window, sinks):
     c.close()
 
 
+def test_weights_without_room_for_scores_or_parts():
+    """So long and so few rows that the workspace holds neither the scores nor
+    the parts of the weights: they are taken as 32 keys a workgroup."""
+    c = Cache(1, 1, 64, [16001, 15000, 16384, 16383], seed=13)
+    c.batch(range(4), [2, 1, 1, 1])
+    mass = torch.zeros((4, 16384), device="cuda")
+    for window, sinks in [(0, 0), (5000, 33)]:
+        c.attend(window=window, sinks=sinks, mass=mass)
+        check(c, window, sinks, mass=mass)
+    c.close()
+
+
 def test_large_scores_stay_finite():
     """Scores of 2^26: one key takes all the weight."""
     c = Cache(2, 4, 128, [200, 90], seed=10, scale=2.0 ** 24)
