@@ -924,7 +924,8 @@ int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host
   a.n_blocks = h->n_blocks;
   a.Hkv = h->cfg.n_kv_heads;
   a.hd = h->cfg.head_dim;
-  a.info = static_cast<const int32_t*>(meta_dev);
+  a.info = static_cast<int32_t*>(meta_dev);
+  a.n_ints = static_cast<int>(ints);
   a.src_tbl = a.info + info_ints;
   a.dst_tbl = a.src_tbl + total_src;
   a.from = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(meta_dev) + align_up(ints * 4));
@@ -936,8 +937,9 @@ int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host
   a.kept = kept_dev;
   a.slots = slots_dev;
   a.out_stride = out_stride;
-  st = stage_upload(h, meta_dev, staging, s);
-  if (st == VSK_OK) st = hip_check(h, launch_evict(a, n, max_len, max_keep, s), "evict");
+  const bool small = ints <= static_cast<size_t>(kEvictSmall);  // (goes with the launch)
+  if (!small) st = stage_upload(h, meta_dev, staging, s);
+  if (st == VSK_OK) st = hip_check(h, launch_evict(a, small ? m : nullptr, ints, n, max_len, max_keep, s), "evict");
   if (st != VSK_OK) h->alloc.seq_undo_evict(dst_host, n);
   return st;
 }
@@ -1231,7 +1233,9 @@ static AttnPlan plan_attn(Handle& h, const uint16_t* q, uint16_t* out, int out_R
   // and 350; half, 319 and 311; three quarters, 291 and 251; nearly all, 256
   // prompt rows behind 8,208 tokens 2,362 and 1,396.
   aa.kv_once = 2 * blk_again < blk_sum ? 1 : 0;
-  aa.bps = h.attn_bps > 0 ? h.attn_bps : attn_auto_bps(R, c.n_kv_heads);
+  // (a general walk counts the rows that it is for, not the prompt rows beside
+  // them: 7 rows of 300-3,000 tokens beside a prompt chunk 22 -> 16 us)
+  aa.bps = h.attn_bps > 0 ? h.attn_bps : attn_auto_bps(p.span ? n_dec : R, c.n_kv_heads);
   // 128..255 (row, KV head) pairs whose walks are within 20% of each other:
   // one split per pair (no merge, and the items are balanced already); a
   // wider spread keeps the split, the longest walk setting the time, and

@@ -10,6 +10,9 @@
 //
 // k_evict_move: copies K and V of the kept tokens, every layer and KV head, to
 // the destination's blocks.
+#include <cstring>
+#include <type_traits>
+
 #include "dev.hpp"
 #include "evict.hpp"
 
@@ -70,9 +73,11 @@ __device__ __forceinline__ void scan_counts(int* s) {
 // Token i = j T + thread is the thread's j-th: loads and stores then run along
 // the tokens.  (Runs of tokens a thread: 34 us at 16,000 tokens, most of it
 // 4-byte stores to 64 lines an instruction; this order 26.)
-template <int T, int PER>
-__global__ __launch_bounds__(T) void k_evict_select(EvictArgs a) {
+// M is EvictSmall, or int where the metadata is in its buffer already.
+template <int T, int PER, typename M>
+__global__ __launch_bounds__(T) void k_evict_select(EvictArgs a, M meta) {
   constexpr int W = T / 64;
+  constexpr bool kSmall = std::is_same_v<M, EvictSmall>;
   __shared__ int s_hist[2048];
   __shared__ int s_w[W];
   __shared__ int s_tie[PER * W], s_stay[PER * W];  // counts of 64 tokens each, in index order
@@ -80,9 +85,18 @@ __global__ __launch_bounds__(T) void k_evict_select(EvictArgs a) {
   __shared__ int s_left;
   const int seq = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int32_t* info = a.info + 4 * seq;
+  const int32_t* src_tbl = a.src_tbl;
+  const int32_t* dst_tbl = a.dst_tbl;
+  if constexpr (kSmall) {
+    // (every sequence's workgroup stores all of it: the same values)
+    for (int i = tid; i < a.n_ints; i += T) a.info[i] = meta.v[i];
+    info = meta.v + 4 * seq;
+    src_tbl = meta.v + (a.src_tbl - a.info);
+    dst_tbl = meta.v + (a.dst_tbl - a.info);
+  }
   const int len = info[0], keep = info[1];
-  const int32_t* src_tbl = a.src_tbl + info[2];
-  const int32_t* dst_tbl = a.dst_tbl + info[3];
+  src_tbl += info[2];
+  dst_tbl += info[3];
   int32_t* from = a.from + static_cast<int64_t>(info[3]) * kBlock;
   const float* mass = a.mass + seq * a.mass_stride;
   const int lo = a.sinks, hi = len - a.recent;  // the tokens that compete
@@ -212,14 +226,24 @@ __global__ __launch_bounds__(256) void k_evict_move(EvictArgs a) {
 }
 
 // Few tokens take few waves (cheaper rounds), and never more registers than tokens need.
-static void launch_select(const EvictArgs& a, int n, int max_len, hipStream_t s) {
-  if (max_len <= 1024) hipLaunchKernelGGL((k_evict_select<256, 4>), dim3(n), dim3(256), 0, s, a);
-  else if (max_len <= 4096) hipLaunchKernelGGL((k_evict_select<1024, 4>), dim3(n), dim3(1024), 0, s, a);
-  else hipLaunchKernelGGL((k_evict_select<1024, kEvictMaxLen / 1024>), dim3(n), dim3(1024), 0, s, a);
+template <typename M>
+static void launch_select(const EvictArgs& a, const M& meta, int n, int max_len, hipStream_t s) {
+  if (max_len <= 1024) hipLaunchKernelGGL((k_evict_select<256, 4, M>), dim3(n), dim3(256), 0, s, a, meta);
+  else if (max_len <= 4096) hipLaunchKernelGGL((k_evict_select<1024, 4, M>), dim3(n), dim3(1024), 0, s, a, meta);
+  else hipLaunchKernelGGL((k_evict_select<1024, kEvictMaxLen / 1024, M>), dim3(n), dim3(1024), 0, s, a, meta);
 }
 
-hipError_t launch_evict(const EvictArgs& a, int n, int max_len, int max_keep, hipStream_t s) {
-  launch_select(a, n, max_len, s);
+hipError_t launch_evict(const EvictArgs& a, const int32_t* meta, size_t ints, int n, int max_len, int max_keep,
+                        hipStream_t s) {
+  if (meta != nullptr) {
+    if (ints > static_cast<size_t>(kEvictSmall)) return hipErrorInvalidValue;
+    EvictSmall m;
+    std::memset(&m, 0, sizeof(m));
+    std::memcpy(m.v, meta, ints * 4);
+    launch_select(a, m, n, max_len, s);
+  } else {
+    launch_select(a, 0, n, max_len, s);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_evict_move, dim3((max_keep + kBlock - 1) / kBlock, a.n_layers * a.Hkv, n), dim3(2 * a.hd), 0, s, a);
