@@ -34,6 +34,7 @@ static_assert(kRowTiles * 32 == kPreCols, "a work item's columns");
 // A running maximum may lag by this (base 2) before the sums are rescaled: the
 // weights are then up to 2^8, the float32 sums as exact as before.
 constexpr float kRowsLag = 8.f;
+constexpr int kRowSlots = 4;
 
 // Some value of V (of any lane of the wave) is an infinity or a NaN.
 template <int N>
@@ -62,7 +63,7 @@ __device__ __forceinline__ u32x4 keep_bits(u32x4 v, uint32_t bits) {
 
 template <int D, int NH>
 struct RowsLds {
-  u32x4 kv[2][2][NH][2][2 * D];  // [slot][K, V][half][block][16-byte piece]
+  u32x4 kv[kRowSlots][2][NH][2][2 * D];  // [slot][K, V][half][block][16-byte piece]
   int32_t tbl[kMaxSpanBlocks];
   float m[kRowTiles][64], l[kRowTiles][64];  // the second half's, when the halves join
 };
@@ -181,7 +182,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   // ... and here the columns that see one get NaN where it enters (rare)
   auto poison = [&](int step) __attribute__((always_inline)) {
     poisoned = false;
-    const u32x4* vp = &sm.kv[step & 1][1][hh][0][32 * (lc >> 4) + (lane & 15) + 16 * hi];
+    const u32x4* vp = &sm.kv[step % kRowSlots][1][hh][0][32 * (lc >> 4) + (lane & 15) + 16 * hi];
 #pragma unroll
     for (int i = 0; i < OC; ++i) {
       f32x16 y;  // how many such values of keys that the column sees
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   // all the sums in every step.
   auto rest = [&](int step, const f32x16& s, auto fast_c) __attribute__((always_inline)) {
     constexpr bool FAST = decltype(fast_c)::value;
-    const u32x4* vp = &sm.kv[step & 1][1][hh][0][32 * (lc >> 4) + (lane & 15) + 16 * hi];
+    const u32x4* vp = &sm.kv[step % kRowSlots][1][hh][0][32 * (lc >> 4) + (lane & 15) + 16 * hi];
     const float mb = !FAST && m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -247,34 +248,44 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
 
   load(0);
   store(0);
-  if (n_steps > 1) load(1);
+  load(1);  // (past the list: its last block)
+  store(1);
+  load(2);
   bool big = false;  // (uniform) scores so large that a fma's unrounded product would be off the maximum
   f32x16 s;          // s[r]: key 8 hi + r of the step's first block (r < 8), 8 hi + r - 8 of the second
   float mx;
-  auto scores = [&](int step) __attribute__((always_inline)) {
-    barrier_after_lds_reads();  // the step's slot is whole, the other one free
-    if (step + 1 < n_steps) {
-      store((step + 1) & 1);
-      load(step + 2);  // (past the list: its last block)
-    }
-    const u32x4* kp = &sm.kv[step & 1][0][hh][lc >> 4][(lane & 15) + 16 * hi];
+  auto next = [&](int step) __attribute__((always_inline)) {
+    barrier_after_lds_reads();  // the next step's slot is whole, the one of two steps ago free
+    store((step + 2) % kRowSlots);
+    load(step + 3);
+  };
+  auto qk = [&](int step, f32x16& s) __attribute__((always_inline)) {
+    const u32x4* kp = &sm.kv[step % kRowSlots][0][hh][lc >> 4][(lane & 15) + 16 * hi];
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
     for (int i = 0; i < QC; ++i) s = mfma_32x32x16(kp[32 * i], qf[i], s);
-    mx = s[0];
+  };
+  auto top = [&](const f32x16& s) __attribute__((always_inline)) {
+    float x = s[0];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-    mx = max_xor32(mx) * sc;
+    for (int r = 1; r < 16; ++r) x = fmaxf(x, s[r]);
+    return max_xor32(x) * sc;
   };
   int step = 0;
-  scores(0);
+  __syncthreads();
+  qk(0, s);
+  mx = top(s);
   for (;;) {
     // (a loop of its own, so that the sums stay where they are)
     while (is_full(step) && !big && !__any(mx > m + kRowsLag)) {  // (-inf + 8 is -inf: first keys always are)
+      next(step);
+      f32x16 sn;
+      qk(step + 1, sn);
       rest(step, s, std::true_type{});
+      s = sn;
+      mx = top(s);
       if (++step == n_steps) break;
-      scores(step);
     }
     if (step == n_steps) break;
     if (!is_full(step)) {
@@ -294,10 +305,12 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
 #pragma unroll
     for (int i = 0; i < OC; ++i) o[i] *= f;
     big = __any(fabsf(m) >= kRoundedScores && m != -INFINITY);
+    next(step);
     rest(step, s, std::false_type{});
     if (__builtin_expect(poisoned, 0)) poison(step);
     if (++step == n_steps) break;
-    scores(step);
+    qk(step, s);
+    mx = top(s);
   }
   l = add_xor32(l);
 
