@@ -206,12 +206,17 @@ __device__ __forceinline__ uint32_t span_bits(int t, int end, int lo, int sinks)
   return below(end) & (~below(lo) | below(sinks));
 }
 
+// x where bit r is set, else -inf (a bit field and an insert: no condition code).
+__device__ __forceinline__ float bit_or_neg_inf(float x, uint32_t bits, int r) {
+  const uint32_t mk = static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - r)) >> 31);
+  return __uint_as_float((__float_as_uint(x) & mk) | (0xff800000u & ~mk));
+}
 // The scores of a step of a general walk: keys whose bit is clear do not count.
 __device__ __forceinline__ void span_mask(uint32_t bits, f32x4& s0, f32x4& s1) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    s0[r] = bits >> r & 1u ? s0[r] : -INFINITY;
-    s1[r] = bits >> (4 + r) & 1u ? s1[r] : -INFINITY;
+    s0[r] = bit_or_neg_inf(s0[r], bits, r);
+    s1[r] = bit_or_neg_inf(s1[r], bits, 4 + r);
   }
 }
 

@@ -163,20 +163,21 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     const int v = pair_of(step) + b;
     return step >= 0 && v < span.nv ? span_bits(kBlock * span.block(v) + 8 * hi, kv_end, 0, 0) : 0u;
   };
-  // V of a step of which some keys count for some columns only: those of no
-  // token become zero (slots past the sequence's end may hold a NaN, and
-  // 0 x NaN is NaN), and so do values that are not finite ...
+  // V of a step of which some keys count for some columns only.  Where all of it
+  // is finite, weights of zero leave the others out.  Otherwise keys of no token
+  // become zero (slots past the sequence's end may hold a NaN, and 0 x NaN is
+  // NaN), and so do values that are not finite ...
   bool poisoned = false;  // (uniform)
   auto clean = [&](int step, int b, u32x4 (&vt)[OC]) __attribute__((always_inline)) {
-    const uint32_t keep = held(step, b);
-#pragma unroll
-    for (int i = 0; i < OC; ++i) vt[i] = keep_bits(vt[i], keep);
     if (__builtin_expect(not_finite(vt), 0)) {
+      const uint32_t keep = held(step, b);
       poisoned = true;
 #pragma unroll
-      for (int i = 0; i < OC; ++i)
+      for (int i = 0; i < OC; ++i) {
+        vt[i] = keep_bits(vt[i], keep);
 #pragma unroll
         for (int j = 0; j < 4; ++j) vt[i][j] &= ~not_finite_halves(vt[i][j]);
+      }
     }
   };
   // ... and here the columns that see one get NaN where it enters (rare)
@@ -293,18 +294,20 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
       mx = -INFINITY;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[r] = bits >> r & 1u ? s[r] : -INFINITY;
+        s[r] = bit_or_neg_inf(s[r], bits, r);
         mx = fmaxf(mx, s[r]);
       }
       mx = max_xor32(mx) * sc;
     }
-    const float mn = fmaxf(m, mx);
-    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-    m = mn;
-    l *= f;
+    if (__any(mx > m + kRowsLag)) {
+      const float mn = fmaxf(m, mx);
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
 #pragma unroll
-    for (int i = 0; i < OC; ++i) o[i] *= f;
-    big = __any(fabsf(m) >= kRoundedScores && m != -INFINITY);
+      for (int i = 0; i < OC; ++i) o[i] *= f;
+      big = __any(fabsf(m) >= kRoundedScores && m != -INFINITY);
+    }
     next(step);
     rest(step, s, std::false_type{});
     if (__builtin_expect(poisoned, 0)) poison(step);
