@@ -1300,6 +1300,23 @@ static AttnPlan plan_attn(Handle& h, const uint16_t* q, uint16_t* out, int out_R
   pf.out_Rg = out_Rg;
   pf.window = window;
   pf.sinks = sinks;
+  // few work items with long walks are cut, so that they fill the compute units
+  // once, into splits of four steps of 64 keys at least, and joined: 64 rows of
+  // 32/8 heads after 8,000 tokens 155 us as 16 work items, 31 as 256; 333 rows
+  // 171 us as 88, 105 as 176 (and 104 as 440, in two rounds)
+  pf.splits = 1;
+  pf.part_o = aa.part_o;
+  pf.part_ml = aa.part_ml;
+  const int items = p.prefill && p.span ? b.n_pre_items * c.n_kv_heads : 0;
+  if (items > 0 && items <= 256) {
+    const BatchHost& bh = h.bh;
+    int nv = 0;
+    for (int32_t i = 0; i < bh.n_pre_items(); ++i) {
+      const int32_t r0 = bh.pre_items[3 * i + 1], r1 = r0 + bh.pre_items[3 * i + 2] - 1;
+      nv = std::max(nv, span_walk(bh.pos[r0] + 1, bh.pos[r1] + 1, window, sinks).nv);
+    }
+    pf.splits = std::max(1, std::min({256 / items, nv / 16, static_cast<int>(wl.max_splits)}));
+  }
   // (maximum, 1 / sum) per row and head: in the space of the K-split products,
   // which are added up before attention starts and written after it ends
   // (8 bytes a head against at least 4 * head_dim)

@@ -83,6 +83,11 @@ struct AttnPrefillArgs {
   const uint8_t* run_mask;  // routed layer (nullable): as in AttnArgs
   int window, sinks;        // general walk (launch_attn_rows): as in AttnArgs, as are out_Rg 0 and ml
   float2* ml;
+  // general walk: an item's walk cut into `splits` work items, whose sums meet
+  // in part_o [R][Hkv][splits][G][hd] and part_ml [R][Hkv][splits][G]
+  int splits;
+  float* part_o;
+  float2* part_ml;
 };
 
 // Attention weight per key (see k_attn_mass).

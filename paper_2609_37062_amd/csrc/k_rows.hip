@@ -76,9 +76,9 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   constexpr int LD = D / 32;  // 16-byte loads a thread and step
   __shared__ RowsLds<D, NH> sm;
 
-  // an item's KV heads are consecutive (items come longest walk first)
-  const int hk = blockIdx.x % a.Hkv;
-  const int32_t* it = a.items + static_cast<size_t>(blockIdx.x / a.Hkv) * 3;
+  // an item's KV heads are consecutive, then its splits (items come longest walk first)
+  const int hk = blockIdx.x % a.Hkv, split = static_cast<int>(blockIdx.x / a.Hkv) % a.splits;
+  const int32_t* it = a.items + static_cast<size_t>(blockIdx.x / a.Hkv / a.splits) * 3;
   const int seq = it[0], row0 = it[1], n_rows = it[2];
   const int G = a.G, n_cols = n_rows * G;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -113,7 +113,9 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   const size_t head = static_cast<size_t>(kBlock) * D, stride = head * a.Hkv;
   const uint16_t* kbase = a.pool + static_cast<size_t>(a.layer) * 2 * a.n_blocks * stride + hk * head;
   const uint16_t* vbase = kbase + static_cast<size_t>(a.n_blocks) * stride;
-  const int n_pairs = (span.nv + 1) / 2, n_steps = (n_pairs + NH - 1) / NH;
+  const int n_pairs = (span.nv + 1) / 2, all_steps = (n_pairs + NH - 1) / NH;
+  const int per = (all_steps + a.splits - 1) / a.splits;
+  const int first = min(all_steps, split * per), n_steps = min(all_steps, first + per);  // the split's: first .. n_steps - 1
   u32x4 st[LD];
   // A step's NH x {K, V} x two blocks x 2 D pieces, as they lie in LDS: the
   // thread's are K and V of NJ places.  Blocks past the list: its last one
@@ -247,11 +249,11 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     }
   };
 
-  load(0);
-  store(0);
-  load(1);  // (past the list: its last block)
-  store(1);
-  load(2);
+  load(first);
+  store(first % kRowSlots);
+  load(first + 1);  // (past the list: its last block)
+  store((first + 1) % kRowSlots);
+  load(first + 2);
   bool big = false;  // (uniform) scores so large that a fma's unrounded product would be off the maximum
   f32x16 s;          // s[r]: key 8 hi + r of the step's first block (r < 8), 8 hi + r - 8 of the second
   float mx;
@@ -273,11 +275,11 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     for (int r = 1; r < 16; ++r) x = fmaxf(x, s[r]);
     return max_xor32(x) * sc;
   };
-  int step = 0;
+  int step = first;
   __syncthreads();
-  qk(0, s);
+  qk(step, s);
   mx = top(s);
-  for (;;) {
+  while (step < n_steps) {
     // (a loop of its own, so that the sums stay where they are)
     while (is_full(step) && !big && !__any(mx > m + kRowsLag)) {  // (-inf + 8 is -inf: first keys always are)
       next(step);
@@ -345,6 +347,18 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   // a Project-Only row of a routed layer emits zero
   const int grow = row0 + row;
   const bool po = a.run_mask != nullptr && on && a.run_mask[grow] == 0;
+  if (a.splits > 1) {
+    const size_t at = ((static_cast<size_t>(grow) * a.Hkv + hk) * a.splits + split) * G + qh;
+    if (!on) return;
+    if (hi == 0) a.part_ml[at] = make_float2(m, l);
+#pragma unroll
+    for (int i = 0; i < OC; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(a.part_o + at * D + 32 * i + 8 * g + 4 * hi) =
+            f32x4{o[i][4 * g], o[i][4 * g + 1], o[i][4 * g + 2], o[i][4 * g + 3]};
+    return;
+  }
   const float inv = po ? 0.f : 1.f / l;
   if (a.ml != nullptr && on && hi == 0)
     a.ml[static_cast<size_t>(grow) * (a.Hkv * G) + hk * G + qh] = po ? make_float2(INFINITY, 0.f) : make_float2(m, inv);
@@ -369,16 +383,66 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     }
 }
 
+// The splits of the items' rows joined, in split order: four dims a thread.
 template <int D>
-static void launch_rows_d(const AttnPrefillArgs& a, int wgs, hipStream_t s) {
-  if (wgs <= 256) hipLaunchKernelGGL((k_attn_rows<D, 2>), dim3(wgs), dim3(512), 0, s, a);
+__global__ __launch_bounds__(256) void k_rows_join(AttnPrefillArgs a) {
+  constexpr int kT = D / 4;  // threads of a column
+  const int hk = blockIdx.x % a.Hkv;
+  const int32_t* it = a.items + static_cast<size_t>(blockIdx.x / a.Hkv) * 3;
+  const int c = blockIdx.y * (256 / kT) + threadIdx.x / kT, e = threadIdx.x % kT * 4;
+  if (c >= it[2] * a.G) return;
+  const int row = it[1] + c / a.G, qh = c % a.G;
+  const bool po = a.run_mask != nullptr && a.run_mask[row] == 0;  // a Project-Only row emits zero
+  const size_t at = (static_cast<size_t>(row) * a.Hkv + hk) * a.splits * a.G + qh;
+  float M = -INFINITY, L = 0.f;
+  f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+  constexpr int kU = 4;  // splits in flight
+  for (int s0 = 0; s0 < a.splits; s0 += kU) {
+    float2 ml[kU];
+    f32x4 x[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const size_t i = at + static_cast<size_t>(min(s0 + u, a.splits - 1)) * a.G;
+      ml[u] = a.part_ml[i];
+      x[u] = *reinterpret_cast<const f32x4*>(a.part_o + i * D + e);
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      if (s0 + u >= a.splits || ml[u].x == -INFINITY) continue;  // (a split of which the row sees nothing)
+      const float mn = fmaxf(M, ml[u].x);
+      const float f0 = M == -INFINITY ? 0.f : exp2f(M - mn), f1 = exp2f(ml[u].x - mn);
+      L = L * f0 + ml[u].y * f1;
+      y = y * f0 + x[u] * f1;
+      M = mn;
+    }
+  }
+  const float inv = po ? 0.f : 1.f / L;
+  if (a.ml != nullptr && e == 0)
+    a.ml[static_cast<size_t>(row) * (a.Hkv * a.G) + hk * a.G + qh] = po ? make_float2(INFINITY, 0.f) : make_float2(M, inv);
+  const int col = (hk * a.G + qh) * D + e;
+  const size_t to = a.out_Rg == 0 ? static_cast<size_t>(row) * a.Nq + col : frag_index(row, col, a.out_Rg);
+  u32x2 pk = u32x2{0u, 0u};
+  if (!po) pk = u32x2{pack_bf2(y[0] * inv, y[1] * inv), pack_bf2(y[2] * inv, y[3] * inv)};
+  *reinterpret_cast<u32x2*>(a.out + to) = pk;
+}
+
+// Up to one work item a compute unit, eight waves each; beyond that two of four
+// waves, which wait for each other less often (2 x 2,000 fresh rows of 32/8
+// heads 133 and 120 us, 4 x 1,037 of 24/8 through a window of 256 58 and 41,
+// 3 x 1,500 of 8/8 42 and 49; 1,000 rows through 4,096 in 256 work items 117
+// and, one wave a SIMD, about twice that).
+template <int D>
+static void launch_rows_d(const AttnPrefillArgs& a, int n_items, hipStream_t s) {
+  const int wgs = n_items * a.Hkv * a.splits;
+  if (n_items * a.Hkv <= 256) hipLaunchKernelGGL((k_attn_rows<D, 2>), dim3(wgs), dim3(512), 0, s, a);
   else hipLaunchKernelGGL((k_attn_rows<D, 1>), dim3(wgs), dim3(256), 0, s, a);
+  if (a.splits > 1) hipLaunchKernelGGL((k_rows_join<D>), dim3(n_items * a.Hkv, kPreCols * D / 1024), dim3(256), 0, s, a);
 }
 
 hipError_t launch_attn_rows(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s) {
   if (n_items <= 0) return hipSuccess;
-  if (head_dim == 128) launch_rows_d<128>(a, n_items * a.Hkv, s);
-  else if (head_dim == 64) launch_rows_d<64>(a, n_items * a.Hkv, s);
+  if (head_dim == 128) launch_rows_d<128>(a, n_items, s);
+  else if (head_dim == 64) launch_rows_d<64>(a, n_items, s);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
