@@ -1395,7 +1395,7 @@ static hipError_t launch_mass(Handle& h, const AttnPlan& p, int layer, float* ma
   m.part_len = (h.bd.max_kv_len + kMassTile - 1) / kMassTile * kMassTile;
   if (tiles > 0) {
     const int64_t room = (p.part_bytes / 4) / (static_cast<int64_t>(m.Hkv) * bh.n_seqs * m.part_len);
-    m.parts = static_cast<int>(std::min<int64_t>({room, 16, (1024 + tiles * m.Hkv - 1) / (tiles * m.Hkv)}));
+    m.parts = static_cast<int>(std::min<int64_t>({room, 16, std::max<int64_t>(1, 1024 / (tiles * m.Hkv))}));
   }
   return launch_attn_mass(m, h.bd.n_seqs, singles > 0, tiles > 0, h.bd.max_kv_len, h.cfg.head_dim, s);
 }
@@ -1565,8 +1565,10 @@ hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
     } else {
       TRY(probed(2, [&](LaunchEvents ev) { return launch_gemm(ga, p_qkv, EPI_QKV, s, ev); }));
     }
-    if (!h.spans.empty() && (h.spans[l].window != attn_span.window || h.spans[l].sinks != attn_span.sinks)) {
-      attn_span = h.spans[l];
+    // (a window that no row reaches the end of is none)
+    const Handle::Span span = h.spans.empty() || h.spans[l].window >= b.max_kv_len ? Handle::Span{} : h.spans[l];
+    if (span.window != attn_span.window || span.sinks != attn_span.sinks) {
+      attn_span = span;
       attn = plan_attn(h, q, fa, Rg, ws, wl, pa.logit_rows == nullptr, attn_span.window, attn_span.sinks,
                        h.mass != nullptr);
     }

@@ -14,8 +14,8 @@
 // units.  It reads K once more, and that bounds it.  So the attention of such
 // rows leaves its scores where the workspace has room for them, 4 bytes a (head,
 // key) beside 4 hd of K and V a (KV head, key), and k_mass_scores sums over
-// those instead: 32 sequences of 1,000-4,000 tokens (32/8 heads x 128) 32 us,
-// of its own; with the scores the
+// those instead: 32 sequences of 1,000-4,000 tokens (32/8 heads x 128) 32 us of
+// its own; with the scores the
 // attention takes 60 instead of 54 and their sum 5.
 //
 // k_mass_rows, for sequences of several rows: a product of K with all the
@@ -27,7 +27,12 @@
 // weights per lane and across lanes once at the end.  The KV heads, and parts
 // of the rows where there are few keys, are added up by k_mass_sum.  777 rows
 // over 2,300 cached tokens (32/8 heads x 128): 196 us as k_attn_mass (every
-// workgroup read every query, 16 columns at a time), 41 + 5 of the sum.
+// workgroup read every query, 16 columns at a time), 38 + 5 of the sum.  Loads,
+// products and exponentials each take 7 to 11 of the 38 where they are left out:
+// a wave goes through them one after the other, and three waves a SIMD hide part
+// of that.
+#include <climits>
+
 #include "attn_core.hpp"
 
 namespace vsk {
@@ -184,7 +189,7 @@ __global__ __launch_bounds__(256) void k_mass_scores(AttnMassArgs a) {
 constexpr int kMassCols = 32;  // columns of a tile
 
 template <int D>
-__global__ __launch_bounds__(256, 4) void k_mass_rows(AttnMassArgs a) {
+__global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
   constexpr int QC = D / 16;   // operands of a tile
   constexpr int P = D / 8;     // 16-byte pieces of a query
   constexpr int LD = kMassCols * P / 256;  // of a tile's, a thread
@@ -193,9 +198,9 @@ __global__ __launch_bounds__(256, 4) void k_mass_rows(AttnMassArgs a) {
   const int seq = blockIdx.z;
   const int kv_len = a.kv_len[seq];
   const int r0 = a.cu_q[seq], n = a.cu_q[seq + 1] - r0;
-  const int t0 = kMassTile * blockIdx.x;
+  // KV heads fastest: an XCD then keeps few heads' queries in its L2
+  const int hk = blockIdx.x % a.Hkv, t0 = kMassTile * static_cast<int>(blockIdx.x / a.Hkv), part = blockIdx.y;
   if (t0 >= kv_len || n == 1) return;
-  const int hk = blockIdx.y % a.Hkv, part = blockIdx.y / a.Hkv;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lc = lane & 31, hi = lane >> 5, G = a.G;
   const int p0 = kv_len - n;  // position of the first row
@@ -241,8 +246,7 @@ __global__ __launch_bounds__(256, 4) void k_mass_rows(AttnMassArgs a) {
   };
   u32x4 st[LD];
   float2 stm = make_float2(0.f, 0.f);
-  int mrow = (c_first + lc) / G, mg = (c_first + lc) % G;  // the lane's own column, and (first 32 threads) whose ml to load
-  int lrow = mrow, lg = mg;
+  int lrow = (c_first + lc) / G, lg = (c_first + lc) % G;  // (first 32 threads) whose ml to load
   const uint16_t* qh = a.q + static_cast<size_t>(r0) * a.Nq + static_cast<size_t>(hk) * G * D + tid % P * 8;
   const float2* mlh = a.ml + static_cast<size_t>(r0) * (a.Hkv * G) + hk * G;
   auto load = [&]() {  // (columns past the last row: its last head again, nobody counts them)
@@ -261,23 +265,23 @@ __global__ __launch_bounds__(256, 4) void k_mass_rows(AttnMassArgs a) {
     for (int j = 0; j < LD; ++j) s_q[slot][k * kMassCols + ((tid / P + 256 / P * j) ^ (k & 7))] = st[j];
     if (tid < kMassCols) s_ml[slot][tid] = stm;
   };
+  // tiles from which every column sees all 32 keys start at columns f_from ..
+  // f_to: their first row is at key tw + 31 or behind it, and the window of
+  // their last one reaches back to key tw
+  const int f_from = tw + 32 <= kv_len ? (tw + 31 - p0) * G : INT_MAX;
+  const int f_to = min(c_end, a.window == 0 || tw + 32 <= a.sinks ? INT_MAX : (tw + a.window - p0) * G) - kMassCols;
   const float sc = a.scale_log2;
   float acc[16];
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-  if (tiles > 0) {
-    load();
-    store(0);
-    if (tiles > 1) load();
-  }
-  for (int i = 0; i < tiles; ++i) {
+  // a tile's scores: s[r] is key tw + 8 hi + r (r < 8), tw + 16 + 8 hi + r - 8
+  f32x16 s;
+  float2 ml;
+  auto scores = [&](int i) __attribute__((always_inline)) {
     barrier_after_lds_reads();  // the tile's slot is whole, the other one free
-    if (i + 1 < tiles) {
-      store((i + 1) & 1);
-      if (i + 2 < tiles) load();
-    }
-    const float2 ml = s_ml[i & 1][lc];
-    f32x16 s;
+    store((i + 1) & 1);         // (past the last tile: columns of the last row again)
+    load();
+    ml = s_ml[i & 1][lc];
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
@@ -285,30 +289,40 @@ __global__ __launch_bounds__(256, 4) void k_mass_rows(AttnMassArgs a) {
       const int k = 2 * c + hi;
       s = mfma_32x32x16(kt[c], s_q[i & 1][k * kMassCols + (lc ^ (k & 7))], s);
     }
-    // s[r]: key tw + 8 hi + r (r < 8), tw + 16 + 8 hi + r - 8
-    const int c0 = c_first + kMassCols * i;
-    const int fr = c0 / G, lr = min(c0 + kMassCols, c_end) - 1;  // (uniform) first row, last column
-    const int end0 = p0 + fr + 1, end1 = p0 + lr / G + 1;      // keys of the first and the last row
-    const bool full = c0 + kMassCols <= c_end && tw + 32 <= min(kv_len, end0) &&
-                      (a.window == 0 || end1 <= a.window || tw >= end1 - a.window || tw + 32 <= a.sinks);
-    if (full && !__any(fabsf(ml.x) >= kRoundedScores)) {
+  };
+  if (tiles > 0) {
+    load();
+    store(0);
+    load();
+    int i = 0;
+    scores(0);
+    while (i < tiles) {
+      // (a loop of its own, so that the sums stay where they are)
+      while (c_first + kMassCols * i >= f_from && c_first + kMassCols * i <= f_to && !__any(fabsf(ml.x) >= kRoundedScores)) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[r] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[r], sc, -ml.x)), ml.y, acc[r]);
-    } else {
-      // (both sides of a difference rounded alike, see pair_softmax)
-#pragma clang fp contract(off)
-      const int end = c0 + lc < c_end ? min(kv_len, p0 + mrow + 1) : 0;
-      const int lo = a.window > 0 && p0 + mrow + 1 > a.window ? p0 + mrow + 1 - a.window : 0;
-      const uint32_t bits =
-          span_bits(tw + 8 * hi, end, lo, a.sinks) | span_bits(tw + kBlock + 8 * hi, end, lo, a.sinks) << 8;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float x = s[r] * sc;
-        const float y = __builtin_amdgcn_exp2f(x - ml.x) * ml.y;
-        acc[r] += bits >> r & 1u ? y : 0.f;
+        for (int r = 0; r < 16; ++r) acc[r] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[r], sc, -ml.x)), ml.y, acc[r]);
+        if (++i == tiles) break;
+        scores(i);
       }
+      if (i == tiles) break;
+      {
+        // (both sides of a difference rounded alike, see pair_softmax)
+#pragma clang fp contract(off)
+        const int c = c_first + kMassCols * i + lc, p = p0 + c / G;
+        const int end = c < c_end ? min(kv_len, p + 1) : 0;
+        const int lo = a.window > 0 && p + 1 > a.window ? p + 1 - a.window : 0;
+        const uint32_t bits =
+            span_bits(tw + 8 * hi, end, lo, a.sinks) | span_bits(tw + kBlock + 8 * hi, end, lo, a.sinks) << 8;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float x = s[r] * sc;
+          const float y = __builtin_amdgcn_exp2f(x - ml.x) * ml.y;
+          acc[r] += bits >> r & 1u ? y : 0.f;
+        }
+      }
+      if (++i == tiles) break;
+      scores(i);
     }
-    step(mrow, mg);
   }
 #pragma unroll
   for (int r = 0; r < 16; ++r)
@@ -350,7 +364,7 @@ static hipError_t launch_mass_d(const AttnMassArgs& a, int n_seqs, bool singles,
     hipLaunchKernelGGL((k_attn_mass<D>), dim3((max_kv_len + 31) / 32, n_seqs), dim3(64 * kMassWaves), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 0) return e;
-  hipLaunchKernelGGL((k_mass_rows<D>), dim3((max_kv_len + kMassTile - 1) / kMassTile, a.Hkv * a.parts, n_seqs), dim3(256),
+  hipLaunchKernelGGL((k_mass_rows<D>), dim3((max_kv_len + kMassTile - 1) / kMassTile * a.Hkv, a.parts, n_seqs), dim3(256),
                      0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(k_mass_sum, dim3((max_kv_len + 255) / 256, n_seqs), dim3(256), 0, s, a);
