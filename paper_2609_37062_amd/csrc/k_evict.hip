@@ -4,8 +4,8 @@
 // the last `recent` tokens and, of those between, the ones of the largest
 // weights (equal weights: lowest index; NaN below everything), listed in
 // index order.  The smallest kept weight is found by radix select over the
-// weights' order-preserving 32-bit keys, four digits of 8 bits, the keys held
-// in registers; ranks come from block-wide prefix sums.  Everything is whole
+// weights' order-preserving 32-bit keys, digits of 11, 11 and 10 bits, the keys
+// held in registers; ranks come from block-wide prefix sums.  Everything is whole
 // numbers, so nothing depends on an order of arrival.
 //
 // k_evict_move: copies K and V of the kept tokens, every layer and KV head, to

@@ -18,13 +18,21 @@
 // i + 3 are issued and those of step i + 2 stored, with one barrier a step.  NH
 // halves of a workgroup walk alternate pairs of blocks and are joined at the
 // end: with few work items two halves keep two waves on each SIMD, with many
-// one half and two workgroups do.
+// one half and two workgroups do.  Fewer work items than compute units with
+// long walks are cut into splits, which k_rows_join adds up in their order.
 //
-// The 24 MFMAs of a step take about as long as its softmax.  One after the
-// other, with the two waves of a SIMD in step, they added up (129 us for 1,000
-// rows of 32/8 heads through a window of 4,096, matrix cores busy a third of
-// the time); so P V of a step waits for the next one and is issued between its
-// exponentials (@ROWS@).
+// What bounds it: at head_dim 128 a step of a wave is 24 MFMAs (8 of the scores,
+// 16 of the outputs: a weight goes in as the sum of two bf16 terms) and a softmax
+// of about the same time on the vector ALUs.  So steps whose keys all count are a
+// loop of their own, without a register that changes on a condition, in which the
+// next step's scores are issued between this step's exponentials.  1,000 rows of
+// 32/8 heads x 128 through a window of 4,096 took
+// 184 us on 16-column tiles, 129 on these, 116 with that loop, 112 with the next
+// step's scores in it; 777 rows after 2,300 tokens 92, 84 with the loop, 79;
+// 4 x 1,037 rows of 24/8 through a window of 256, whose steps are mostly cut by
+// a mask, 60, 45, 41, and 39 with masks as bit inserts and finite V left as it is.
+// The matrix cores are then busy 44% of the time, at the 2.0 GHz that they hold.
+// One bf16 term a weight would take 89 us of the 112, at errors of 2^-9 a weight.
 #include "attn_core.hpp"
 
 namespace vsk {

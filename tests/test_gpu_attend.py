@@ -246,3 +246,97 @@ def test_heads_of_one_query_each_and_odd_rows():
     w = np.exp(s) / np.exp(s).sum()
     np.testing.assert_allclose(o[0, 0], w @ c.V[0][0][see, 0], rtol=1e-12, atol=1e-12)
     c.close()
+
+
+@pytest.mark.parametrize("kv,group,hd", [(2, 4, 128), (1, 7, 128), (2, 16, 64)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1000, 200), (70, 33)])
+def test_few_prompt_rows_behind_long_caches(kv, group, hd, window, sinks):
+    """Walks that are cut into splits and joined, beside short ones and a decode
+    row, with their weights; and keys behind the chunk that only some rows see."""
+    c = Cache(kv, group, hd, [3000, 1700, 901, 40], seed=14)
+    c.batch(range(4), [7, 33, 1, 20])
+    mass = torch.zeros((4, 3000), device="cuda")
+    c.attend(window=window, sinks=sinks, mass=mass)
+    check(c, window, sinks, mass=mass)
+    good = c.out()
+    if window:
+        lo, hi = sinks, 3000 - 7 - window  # no row of the first sequence sees these
+        if lo < hi:
+            for x in (c.K, c.V):
+                x[0][0][lo:hi] = np.nan
+            c.write(0, 0)
+            c.attend(window=window, sinks=sinks, mass=mass)
+            np.testing.assert_array_equal(c.out(), good)
+            assert bool(torch.isfinite(mass).all()) and bool((mass[0, lo:hi] == 0).all())
+    c.V[0][0][2996] = np.inf  # rows 0..2 do not see it
+    c.write(0, 0)
+    c.attend(window=window, sinks=sinks)
+    o = c.out()
+    np.testing.assert_array_equal(o[:3], good[:3])
+    np.testing.assert_array_equal(o[7:], good[7:])
+    assert not np.isfinite(o[3:7]).any()
+    c.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_many_short_prompts(hd):
+    """More work items than compute units."""
+    lens = [2 + 7 * i % 121 + i for i in range(34)]
+    c = Cache(8, 2, hd, lens, seed=15)
+    c.batch(range(34), [min(n, 2 + i % 4) for i, n in enumerate(lens)])
+    mass = torch.zeros((34, max(lens)), device="cuda")
+    for window, sinks in [(0, 0), (18, 3)]:
+        c.attend(window=window, sinks=sinks, mass=mass)
+        check(c, window, sinks, mass=mass)
+    c.close()
+
+
+def test_two_engines_on_two_streams():
+    """Calls of different engines, side by side, are what each is alone."""
+    cs = [Cache(2, 4, 128, [900, 333], seed=16), Cache(4, 2, 64, [500, 70, 5], seed=17)]
+    for c, ql in zip(cs, ([40, 1], [1, 70, 2])):
+        c.batch(range(len(c.lens)), ql)
+    masses = [torch.zeros((len(c.lens), 900), device="cuda") for c in cs]
+    alone = []
+    for c, m in zip(cs, masses):
+        c.attend(window=100, sinks=9, mass=m)
+        alone.append((c.out(), m.clone()))
+        m.zero_()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for c, m, s in zip(cs, masses, streams):
+            c.attend(window=100, sinks=9, mass=m, stream=s.cuda_stream)
+    for c, m, (o, am) in zip(cs, masses, alone):
+        np.testing.assert_array_equal(c.out(), o)
+        assert torch.equal(m, am)
+        c.close()
+
+
+@pytest.mark.parametrize("kv,hd", [(1, 64), (3, 128)])
+def test_reading_slots_of_any_order(kv, hd):
+    """kv_read: runs of a block and none, the same slot twice, slots outside the
+    pool (their rows stay as they are), outputs 2 bytes off, list lengths around 16."""
+    c = Cache(kv, 1, hd, [100, 33], seed=18)
+    own = np.concatenate([c.slots(0, 100), c.slots(1, 33)])
+    K = np.concatenate(c.K[0])
+    V = np.concatenate(c.V[0])
+    rng = np.random.default_rng(3)
+    for order in (np.arange(133), np.arange(5, 133), rng.permutation(133), rng.integers(0, 133, 200), np.arange(16),
+                  np.arange(8, 25), np.array([7])):
+        for off in (0, 1):
+            n = len(order)
+            sl = own[order].astype(np.int32)
+            skip = rng.random(n) < 0.1
+            sl[skip] = rng.choice([-1, c.n_blocks * BLOCK, 2 ** 31 - 1], skip.sum())
+            s = torch.from_numpy(sl).cuda()
+            k = torch.full((n * kv * hd + 9,), -3.0, dtype=torch.bfloat16, device="cuda")
+            v = torch.full_like(k, -3.0)
+            c.eng.kv_read(0, s.data_ptr(), n, k.data_ptr() + 2 * off, v.data_ptr() + 2 * off, c.sp)
+            torch.cuda.synchronize()
+            for got, src in ((k, K), (v, V)):
+                want = np.full(n * kv * hd + 9, -3.0, np.float32)
+                x = want[off:off + n * kv * hd].reshape(n, kv, hd)
+                x[~skip] = src[order[~skip]]
+                np.testing.assert_array_equal(got.float().cpu().numpy(), want)
+    c.close()
