@@ -84,6 +84,35 @@ __device__ __forceinline__ void lds_load16(const u32x4* g, u32x4* lds) {
   __builtin_amdgcn_global_load_lds(g, (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
 
+// The same from base + voff (bytes), into LDS at lds + 16 (4) * lane, as
+// instructions that the compiler does not wait for by itself: the wave waits
+// for its copies with s_waitcnt vmcnt.  (M0, which takes the LDS address, is a
+// register the compiler never allocates and uses for nothing else here.)
+template <bool NT>
+__device__ __forceinline__ void lds_copy16(const void* base, uint32_t voff, uint32_t lds) {
+  if constexpr (NT)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+                 :
+                 : "v"(voff), "s"(base), "s"(lds)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(voff), "s"(base), "s"(lds)
+                 : "memory");
+}
+__device__ __forceinline__ void lds_copy4(const void* base, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+               :
+               : "v"(voff), "s"(base), "s"(lds)
+               : "memory");
+}
+// The LDS address of p, which is the same for the whole wave.
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return __builtin_amdgcn_readfirstlane(
+      static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char*)p)));
+}
+
 // Workgroup barrier without a memory fence, for rings filled by
 // global-to-LDS loads.  __syncthreads() also fences, and before the fence the
 // compiler waits for every outstanding load into LDS, which would drain the

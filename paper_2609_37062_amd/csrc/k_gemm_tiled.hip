@@ -40,23 +40,6 @@
 
 namespace vsk {
 
-// 16 bytes per lane from base + voff (bytes) into LDS at lds + 16 * lane.  (M0,
-// which takes the LDS address, is a register the compiler never allocates and
-// uses for nothing else here.)
-template <bool NT>
-__device__ __forceinline__ void lds_copy16(const void* base, uint32_t voff, uint32_t lds) {
-  if constexpr (NT)
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
-                 :
-                 : "v"(voff), "s"(base), "s"(lds)
-                 : "memory");
-  else
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-                 :
-                 : "v"(voff), "s"(base), "s"(lds)
-                 : "memory");
-}
-
 constexpr int kChunk = 2;  // K steps per chunk (every K here is a multiple of 64)
 // Chunks of a tile's fragments held in LDS: at most 144 KiB, at most four
 constexpr int tiled_buffers(int mg, int tn) {

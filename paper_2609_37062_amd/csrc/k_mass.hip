@@ -187,14 +187,20 @@ __global__ __launch_bounds__(256) void k_mass_scores(AttnMassArgs a) {
 }
 
 constexpr int kMassCols = 32;  // columns of a tile
+constexpr int kMassSlots = 4;  // tiles in LDS
+constexpr int kMassLead = 3;   // of them under way
 
 template <int D>
 __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
   constexpr int QC = D / 16;   // operands of a tile
   constexpr int P = D / 8;     // 16-byte pieces of a query
   constexpr int LD = kMassCols * P / 256;  // of a tile's, a thread
-  __shared__ u32x4 s_q[2][P * kMassCols];  // [slot][piece][column ^ piece % 8]
-  __shared__ float2 s_ml[2][kMassCols];
+  // a column's pieces lie in groups of four, [group][column][four]; the four in
+  // an order by column, so that 16 lanes that read the same piece of as many
+  // columns take 16 different 16-byte bank groups
+  __shared__ u32x4 s_q[kMassSlots][P / 4][kMassCols][4];
+  __shared__ float2 s_ml[kMassSlots][4][kMassCols];  // (every wave its own)
+  auto order = [](int c) { return c >> 2 & 3; };
   const int seq = blockIdx.z;
   const int kv_len = a.kv_len[seq];
   const int r0 = a.cu_q[seq], n = a.cu_q[seq + 1] - r0;
@@ -204,15 +210,15 @@ __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lc = lane & 31, hi = lane >> 5, G = a.G;
   const int p0 = kv_len - n;  // position of the first row
-  // the rows that see any of the 128 keys (see k_attn_mass), and of their
-  // columns this part's tiles
+  // the rows that see any of the 128 keys (see k_attn_mass), and of them this
+  // part's tiles, of as many whole rows as fit
   const int ra = max(0, t0 - p0);
   const int rb = a.window > 0 && t0 >= a.sinks ? min(n, t0 + kMassTile - 1 + a.window - p0) : n;
-  const int c_end = rb * G;
-  const int all = max(0, c_end - ra * G + kMassCols - 1) / kMassCols;
+  const int Rt = kMassCols / G;
+  const int all = max(0, rb - ra + Rt - 1) / Rt;
   const int per = (all + a.parts - 1) / a.parts;
   const int i0 = min(all, part * per), tiles = min(all, i0 + per) - i0;
-  const int c_first = ra * G + i0 * kMassCols;
+  const int r_first = ra + i0 * Rt;
 
   // K of the wave's 32 keys (blocks past the sequence: its last one again)
   const int nb = (kv_len + kBlock - 1) / kBlock;
@@ -227,49 +233,41 @@ __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
 #pragma unroll
     for (int i = 0; i < QC; ++i) kt[i] = kp[32 * i];
   }
-  // a tile's queries: the thread's pieces tid % P of columns tid / P + (256 / P) j;
-  // a column's row and head move on by 32 columns a tile
-  const int dr = kMassCols / G, dg = kMassCols % G;
-  int row[LD], g[LD];
+  // a tile's queries: the wave's 64 LD pieces from 64 LD w on, LD a lane, at the
+  // same places of every tile
+  const int row_bytes = 2 * a.Nq, ml_bytes = 8 * a.Hkv * G;
+  int qr[LD], qo[LD];  // row in the tile, byte in the row
 #pragma unroll
   for (int j = 0; j < LD; ++j) {
-    const int c = c_first + tid / P + 256 / P * j;
-    row[j] = c / G;
-    g[j] = c % G;
+    const int x = 64 * (LD * w + j) + lane, c = min(x / 4 % kMassCols, Rt * G - 1);
+    qr[j] = c / G;
+    qo[j] = 2 * (c % G * D + 8 * (x / 128 * 4 + (x % 4 ^ order(x / 4 % kMassCols))));
   }
-  auto step = [&](int& r, int& h) {
-    r += dr;
-    h += dg;
-    const int over = h >= G;
-    r += over;
-    h -= over ? G : 0;
-  };
-  u32x4 st[LD];
-  float2 stm = make_float2(0.f, 0.f);
-  int lrow = (c_first + lc) / G, lg = (c_first + lc) % G;  // (first 32 threads) whose ml to load
-  const uint16_t* qh = a.q + static_cast<size_t>(r0) * a.Nq + static_cast<size_t>(hk) * G * D + tid % P * 8;
-  const float2* mlh = a.ml + static_cast<size_t>(r0) * (a.Hkv * G) + hk * G;
-  auto load = [&]() {  // (columns past the last row: its last head again, nobody counts them)
+  const int mc = min(lane / 2, Rt * G - 1);  // the column whose (m, 1 / l) the lane copies half of
+  const int mr = mc / G, mo = 8 * (mc % G) + 4 * (lane % 2);
+  const char* qh = reinterpret_cast<const char*>(a.q + static_cast<size_t>(r0) * a.Nq + static_cast<size_t>(hk) * G * D);
+  const char* mlh = reinterpret_cast<const char*>(a.ml + static_cast<size_t>(r0) * (a.Hkv * G) + hk * G);
+  const uint32_t q_lds = lds_address(&s_q[0][0][0][0]) + 1024 * LD * w, ml_lds = lds_address(&s_ml[0][w][0]);
+  constexpr int kTileLoads = LD + 1;
+  // tile i's copies into its slot (rows past the last one: it again, nobody
+  // counts them)
+  auto copy = [&](int i) __attribute__((always_inline)) {
+    const int first = min(r_first + Rt * i, n - 1), last = n - 1 - first, slot = i % kMassSlots;
+    const char* q0 = qh + static_cast<size_t>(first) * row_bytes;
+    const char* m0 = mlh + static_cast<size_t>(first) * ml_bytes;
 #pragma unroll
-    for (int j = 0; j < LD; ++j) {
-      const int r = min(row[j], n - 1);
-      st[j] = *reinterpret_cast<const u32x4*>(qh + static_cast<size_t>(r) * a.Nq + g[j] * D);
-      step(row[j], g[j]);
-    }
-    if (tid < kMassCols) stm = mlh[static_cast<size_t>(min(lrow, n - 1)) * (a.Hkv * G) + lg];
-    step(lrow, lg);
+    for (int j = 0; j < LD; ++j)
+      lds_copy16<false>(q0, __umul24(min(qr[j], last), row_bytes) + qo[j],
+                        q_lds + static_cast<uint32_t>(slot * sizeof(s_q[0]) + 1024 * j));
+    lds_copy4(m0, __umul24(min(mr, last), ml_bytes) + mo, ml_lds + static_cast<uint32_t>(slot * sizeof(s_ml[0])));
   };
-  auto store = [&](int slot) {
-    const int k = tid % P;
-#pragma unroll
-    for (int j = 0; j < LD; ++j) s_q[slot][k * kMassCols + ((tid / P + 256 / P * j) ^ (k & 7))] = st[j];
-    if (tid < kMassCols) s_ml[slot][tid] = stm;
-  };
-  // tiles from which every column sees all 32 keys start at columns f_from ..
-  // f_to: their first row is at key tw + 31 or behind it, and the window of
-  // their last one reaches back to key tw
-  const int f_from = tw + 32 <= kv_len ? (tw + 31 - p0) * G : INT_MAX;
-  const int f_to = min(c_end, a.window == 0 || tw + 32 <= a.sinks ? INT_MAX : (tw + a.window - p0) * G) - kMassCols;
+  // tiles of whose rows all see the wave's 32 keys start at rows f_from .. f_to:
+  // the first one is at key tw + 31 or behind it, and the window of the last
+  // one reaches back to key tw
+  const int f_from = tw + 32 <= kv_len ? tw + 31 - p0 : INT_MAX;
+  const int f_to = min(rb, a.window == 0 || tw + 32 <= a.sinks ? INT_MAX : tw + a.window - p0) - Rt;
+  const int cr = lc / G;  // the lane's column's row in its tile (Rt: none)
+  const bool c_on = lc < Rt * G;  // (else its weights are times zero)
   const float sc = a.scale_log2;
   float acc[16];
 #pragma unroll
@@ -278,27 +276,29 @@ __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
   f32x16 s;
   float2 ml;
   auto scores = [&](int i) __attribute__((always_inline)) {
-    barrier_after_lds_reads();  // the tile's slot is whole, the other one free
-    store((i + 1) & 1);         // (past the last tile: columns of the last row again)
-    load();
-    ml = s_ml[i & 1][lc];
+    // the tile's copies have landed once at most those of the kMassLead - 1
+    // tiles behind it are under way; the barrier publishes them and frees the
+    // slot of the tile before
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kMassLead - 1) * kTileLoads) : "memory");
+    barrier_after_lds_reads();
+    copy(i + kMassLead);
+    ml = s_ml[i % kMassSlots][w][lc];
+    ml.y = c_on ? ml.y : 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
     for (int c = 0; c < QC; ++c) {
-      const int k = 2 * c + hi;
-      s = mfma_32x32x16(kt[c], s_q[i & 1][k * kMassCols + (lc ^ (k & 7))], s);
+      s = mfma_32x32x16(kt[c], s_q[i % kMassSlots][c / 2][lc][(2 * (c % 2) + hi) ^ order(lc)], s);
     }
   };
   if (tiles > 0) {
-    load();
-    store(0);
-    load();
+#pragma unroll
+    for (int j = 0; j < kMassLead; ++j) copy(j);
     int i = 0;
     scores(0);
     while (i < tiles) {
       // (a loop of its own, so that the sums stay where they are)
-      while (c_first + kMassCols * i >= f_from && c_first + kMassCols * i <= f_to && !__any(fabsf(ml.x) >= kRoundedScores)) {
+      while (r_first + Rt * i >= f_from && r_first + Rt * i <= f_to && !__any(fabsf(ml.x) >= kRoundedScores)) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[r] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[r], sc, -ml.x)), ml.y, acc[r]);
         if (++i == tiles) break;
@@ -308,8 +308,8 @@ __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
       {
         // (both sides of a difference rounded alike, see pair_softmax)
 #pragma clang fp contract(off)
-        const int c = c_first + kMassCols * i + lc, p = p0 + c / G;
-        const int end = c < c_end ? min(kv_len, p + 1) : 0;
+        const int row = r_first + Rt * i + cr, p = p0 + row;
+        const int end = row < rb ? min(kv_len, p + 1) : 0;
         const int lo = a.window > 0 && p + 1 > a.window ? p + 1 - a.window : 0;
         const uint32_t bits =
             span_bits(tw + 8 * hi, end, lo, a.sinks) | span_bits(tw + kBlock + 8 * hi, end, lo, a.sinks) << 8;
@@ -323,16 +323,27 @@ __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
       if (++i == tiles) break;
       scores(i);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the copies past the last tile)
+  }
+  // The sums over the 32 columns: lanes trade halves of their keys, so that 16
+  // sums of 16 lanes become one each of 2
+  float y[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    const auto z = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[r]), __float_as_uint(acc[r + 8]), false, false);
+    y[r] = __uint_as_float(z[0]) + __uint_as_float(z[1]);  // lanes 16 .. 31 of 32: key r + 8's
   }
 #pragma unroll
-  for (int r = 0; r < 16; ++r)
+  for (int x = 8; x > 1; x >>= 1)
 #pragma unroll
-    for (int x = 1; x < 32; x <<= 1) acc[r] += shfl_xor(acc[r], x);
-  if (lc == 0) {
-    float* dst = a.part + (static_cast<size_t>(part * a.Hkv + hk) * gridDim.z + seq) * a.part_len + tw + 8 * hi;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dst[r < 8 ? r : r + 8] = acc[r];  // (part_len is a multiple of the tile)
-  }
+    for (int r = 0; r < x / 2; ++r) {
+      const float mine = lane & x ? y[r + x / 2] : y[r], theirs = lane & x ? y[r] : y[r + x / 2];
+      y[r] = mine + shfl_xor(theirs, x);
+    }
+  y[0] += shfl_xor(y[0], 1);
+  if ((lane & 1) == 0)  // (part_len is a multiple of the tile)
+    a.part[(static_cast<size_t>(part * a.Hkv + hk) * gridDim.z + seq) * a.part_len + tw + 8 * hi + 16 * (lc >> 4) +
+           (lane >> 1 & 7)] = y[0];
 }
 
 // mass = (or +=) the sum over KV heads and parts, of the sequences of several rows.

@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   constexpr int T = 256 * NH;
   constexpr int QC = D / 16;  // q and K operands of a step
   constexpr int OC = D / 32;  // tiles of 32 dims
-  constexpr int LD = D / 32;  // 16-byte loads a thread and step
+  constexpr int kCopies = D / 32;  // 1 KiB copies of a wave's piece of a step
   __shared__ RowsLds<D, NH> sm;
 
   // an item's KV heads are consecutive, then its splits (items come longest walk first)
@@ -124,26 +124,22 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   const int n_pairs = (span.nv + 1) / 2, all_steps = (n_pairs + NH - 1) / NH;
   const int per = (all_steps + a.splits - 1) / a.splits;
   const int first = min(all_steps, split * per), n_steps = min(all_steps, first + per);  // the split's: first .. n_steps - 1
-  u32x4 st[LD];
-  // A step's NH x {K, V} x two blocks x 2 D pieces, as they lie in LDS: the
-  // thread's are K and V of NJ places.  Blocks past the list: its last one
-  // again (nobody counts its keys).
-  constexpr int NJ = LD / 2;
-  auto place = [&](int j) { return tid + j * T; };  // of NH x two blocks x 2 D
-  auto load = [&](int step) {
+  // A step's NH x two blocks x {K, V} are one each for a wave to copy into LDS.
+  // Blocks past the list: its last one again (nobody counts their keys).
+  const int my_blk = w >> 1;  // of the step's 2 NH
+  const uint16_t* my_base = w & 1 ? vbase : kbase;
+  const uint32_t my_lds = lds_address(&sm.kv[0][w & 1][w >> 2][w >> 1 & 1][0]);
+  const uint32_t lane16 = 16 * lane;
+  auto copy = [&](int step) __attribute__((always_inline)) {
+    const uint32_t blk = __builtin_amdgcn_readfirstlane(sm.tbl[min(2 * NH * step + my_blk, span.nv - 1)]);
+    const uint16_t* src = my_base + static_cast<uint64_t>(blk) * static_cast<uint32_t>(stride);
+    const uint32_t dst = my_lds + static_cast<uint32_t>(step % kRowSlots * sizeof(sm.kv[0]));
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int piece = place(j) % (2 * D), blk = place(j) / (2 * D);  // (blk: half, block)
-      const int v = min(2 * NH * step + blk, span.nv - 1);
-      const uint64_t at =
-          static_cast<uint64_t>(static_cast<uint32_t>(sm.tbl[v])) * static_cast<uint32_t>(stride) + piece * 8;
-      st[2 * j] = *reinterpret_cast<const u32x4*>(kbase + at);
-      st[2 * j + 1] = *reinterpret_cast<const u32x4*>(vbase + at);
-    }
+    for (int j = 0; j < kCopies; ++j) lds_copy16<false>(src + 512 * j, lane16, dst + 1024 * j);
   };
-  auto store = [&](int slot) {
-#pragma unroll
-    for (int j = 0; j < LD; ++j) (&sm.kv[slot][j % 2][0][0][0])[place(j / 2)] = st[j];
+  // until all but the newest `steps` steps' copies of this wave have landed
+  auto landed = [&](auto steps) __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(steps)::value * kCopies) : "memory");
   };
   float m = -INFINITY, l = 0.f;
   f32x16 o[OC];
@@ -257,18 +253,15 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     }
   };
 
-  load(first);
-  store(first % kRowSlots);
-  load(first + 1);  // (past the list: its last block)
-  store((first + 1) % kRowSlots);
-  load(first + 2);
+#pragma unroll
+  for (int j = 0; j < 3; ++j) copy(first + j);
   bool big = false;  // (uniform) scores so large that a fma's unrounded product would be off the maximum
   f32x16 s;          // s[r]: key 8 hi + r of the step's first block (r < 8), 8 hi + r - 8 of the second
   float mx;
   auto next = [&](int step) __attribute__((always_inline)) {
-    barrier_after_lds_reads();  // the next step's slot is whole, the one of two steps ago free
-    store((step + 2) % kRowSlots);
-    load(step + 3);
+    landed(std::integral_constant<int, 1>{});
+    barrier_after_lds_reads();  // the next step's slot is whole, the one of the last step free
+    copy(step + 3);
   };
   auto qk = [&](int step, f32x16& s) __attribute__((always_inline)) {
     const u32x4* kp = &sm.kv[step % kRowSlots][0][hh][lc >> 4][(lane & 15) + 16 * hi];
@@ -284,7 +277,8 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     return max_xor32(x) * sc;
   };
   int step = first;
-  __syncthreads();
+  landed(std::integral_constant<int, 2>{});
+  barrier_after_lds_reads();
   qk(step, s);
   mx = top(s);
   while (step < n_steps) {
@@ -326,6 +320,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     mx = top(s);
   }
   l = add_xor32(l);
+  landed(std::integral_constant<int, 0>{});  // (the steps past the list: before LDS is used again or ends)
 
   if constexpr (NH == 2) {  // the second half's sums join the first's
     static_assert(sizeof(sm.kv) >= kRowTiles * OC * 16 * 64 * 4, "space for a half's sums");
