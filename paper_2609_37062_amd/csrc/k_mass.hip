@@ -15,22 +15,23 @@
 // rows leaves its scores where the workspace has room for them, 4 bytes a (head,
 // key) beside 4 hd of K and V a (KV head, key), and k_mass_scores sums over
 // those instead: 32 sequences of 1,000-4,000 tokens (32/8 heads x 128) 32 us of
-// its own; with the scores the
-// attention takes 60 instead of 54 and their sum 5.
+// its own; with the scores the attention takes 60 instead of 54 and their sum 5.
 //
 // k_mass_rows, for sequences of several rows: a product of K with all the
-// queries that see it, 4 hd flops less than the attention's for each (row,
-// head, key), and an exponential for each.  A workgroup of four waves owns 128
-// keys of a KV head, 32 a wave, which stay in registers as the operand of
-// v_mfma_f32_32x32x16_bf16; the queries pass by in tiles of 32 (row, head)
-// columns through LDS, one read for all four waves.  Each wave sums its keys'
-// weights per lane and across lanes once at the end.  The KV heads, and parts
-// of the rows where there are few keys, are added up by k_mass_sum.  777 rows
-// over 2,300 cached tokens (32/8 heads x 128): 196 us as k_attn_mass (every
-// workgroup read every query, 16 columns at a time), 38 + 5 of the sum.  Loads,
-// products and exponentials each take 7 to 11 of the 38 where they are left out:
-// a wave goes through them one after the other, and three waves a SIMD hide part
-// of that.
+// queries that see it, 2 hd flops for each (row, head, key) where the attention
+// has 4, and an exponential.  A workgroup of four waves owns 128 keys of a KV
+// head, 32 a wave, which stay in registers as the operand of
+// v_mfma_f32_32x32x16_bf16; the queries pass by in tiles of as many whole rows
+// as have 32 (row, head) columns, copied straight into LDS three tiles ahead,
+// one read for all four waves.  (Whole rows: what a lane copies then lies at a
+// constant offset from the tile's first row.)  Each wave sums its keys' weights
+// per lane and across lanes once at the end.  The KV heads, and parts of the rows
+// where there are few keys, are added up by k_mass_sum.  777 rows over 2,300
+// cached tokens (32/8 heads x 128): 196 us as k_attn_mass (every workgroup read
+// every query, 16 columns at a time), 41 with loads through registers and columns
+// that ran on over rows (139 vector operations a tile of 32 x 32, 48 of them the
+// exponentials), 33 so, and 4.5 for the sum.  64 keys a wave, which halve the
+// reads of LDS, took 36: two waves a SIMD hide less.
 #include <climits>
 
 #include "attn_core.hpp"
@@ -189,6 +190,7 @@ __global__ __launch_bounds__(256) void k_mass_scores(AttnMassArgs a) {
 constexpr int kMassCols = 32;  // columns of a tile
 constexpr int kMassSlots = 4;  // tiles in LDS
 constexpr int kMassLead = 3;   // of them under way
+static_assert(kMassLead < kMassSlots, "a slot for the tile that is read");
 
 template <int D>
 __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {

@@ -14,25 +14,28 @@
 // a step, at 128 bytes a cycle longer than the step's MFMAs take; with 32 a
 // byte feeds twice the work.
 //
-// K and V go through registers into four LDS slots: at step i the loads of step
-// i + 3 are issued and those of step i + 2 stored, with one barrier a step.  NH
-// halves of a workgroup walk alternate pairs of blocks and are joined at the
-// end: with few work items two halves keep two waves on each SIMD, with many
-// one half and two workgroups do.  Fewer work items than compute units with
-// long walks are cut into splits, which k_rows_join adds up in their order.
+// K and V are copied straight into four LDS slots, a wave one of a step's K or V
+// blocks: at step i the copies of step i + 3 are issued and those of step i + 1
+// waited for, with one barrier a step.  NH halves of a workgroup walk alternate
+// pairs of blocks and are joined at the end: with few work items two halves keep
+// two waves on each SIMD, with many one half and two workgroups do.  Fewer work
+// items than compute units with long walks are cut into splits, which
+// k_rows_join adds up in their order.
 //
 // What bounds it: at head_dim 128 a step of a wave is 24 MFMAs (8 of the scores,
 // 16 of the outputs: a weight goes in as the sum of two bf16 terms) and a softmax
-// of about the same time on the vector ALUs.  So steps whose keys all count are a
-// loop of their own, without a register that changes on a condition, in which the
-// next step's scores are issued between this step's exponentials.  1,000 rows of
-// 32/8 heads x 128 through a window of 4,096 took
-// 184 us on 16-column tiles, 129 on these, 116 with that loop, 112 with the next
-// step's scores in it; 777 rows after 2,300 tokens 92, 84 with the loop, 79;
-// 4 x 1,037 rows of 24/8 through a window of 256, whose steps are mostly cut by
-// a mask, 60, 45, 41, and 39 with masks as bit inserts and finite V left as it is.
-// The matrix cores are then busy 44% of the time, at the 2.0 GHz that they hold.
-// One bf16 term a weight would take 89 us of the 112, at errors of 2^-9 a weight.
+// of 108 vector operations and 16 exponentials.  So steps whose keys all count
+// are a loop of their own, without a register that changes on a condition, in
+// which the next step's scores are issued between this step's exponentials.
+// 1,000 rows of 32/8 heads x 128 through a window of 4,096 took 184 us on
+// 16-column tiles, 129 on these, 116 with that loop, 112 with the next step's
+// scores in it, 103 with copies into LDS instead of loads and stores; 777 rows
+// after 2,300 tokens 92, 84 with the loop, 79, 72; 4 x 1,037 rows of 24/8 through
+// a window of 256, whose steps are mostly cut by a mask, 60, 45, 41, and 38 with
+// masks as bit inserts and finite V left as it is.  These MFMAs with the same
+// vector operations between them and nothing else, no memory, would take 82 of
+// the 103: with all of them busy the chip runs 1.45 PFLOP/s.  One bf16 term a
+// weight would be a fifth faster, at errors of 2^-9 a weight.
 #include "attn_core.hpp"
 
 namespace vsk {
@@ -43,6 +46,7 @@ static_assert(kRowTiles * 32 == kPreCols, "a work item's columns");
 // weights are then up to 2^8, the float32 sums as exact as before.
 constexpr float kRowsLag = 8.f;
 constexpr int kRowSlots = 4;
+static_assert(kRowSlots == 4, "three steps of copies ahead of the one that is read");
 
 // Some value of V (of any lane of the wave) is an infinity or a NaN.
 template <int N>
