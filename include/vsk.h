@@ -305,7 +305,7 @@ int vsk_set_mass(vsk_handle* h, float* mass_dev, int32_t n_seqs, int32_t stride)
  * float) their weights, followed by zeros up to out_stride; it may be mass_dev
  * itself when the strides are equal.  The outputs must not overlap otherwise.
  * meta_dev: device memory of at least vsk_kv_evict_bytes(), 256-byte aligned,
- * left alone until the call's work has run.  Cannot be captured
+ * beside the others, left alone until the call's work has run.  Cannot be captured
  * (VSK_E_STATE).  All or nothing. */
 size_t vsk_kv_evict_bytes(const vsk_handle* h, const int64_t* src_host, const int32_t* keep_host, int32_t n);
 int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host, const int32_t* keep_host, int32_t n,

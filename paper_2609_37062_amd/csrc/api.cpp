@@ -889,6 +889,11 @@ int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host
   const size_t ints = evict_meta_ints(h, src_host, keep_host, n, &blocks);
   if (meta_bytes_ < evict_meta_bytes(ints, blocks)) return fail(h, VSK_E_ARG, "metadata buffer smaller than vsk_kv_evict_bytes()");
   if (reinterpret_cast<uintptr_t>(meta_dev) % kAlign) return fail(h, VSK_E_ARG, "metadata buffer not aligned");
+  const size_t used = evict_meta_bytes(ints, blocks);
+  if (overlap(meta_dev, used, mass_dev, in_bytes) || overlap(meta_dev, used, kept_dev, out_bytes) ||
+      (mass_out_dev && overlap(meta_dev, used, mass_out_dev, out_bytes)) ||
+      (slots_dev && overlap(meta_dev, used, slots_dev, out_bytes)))
+    return fail(h, VSK_E_ARG, "metadata buffer overlaps mass or outputs");
   hipStream_t s = static_cast<hipStream_t>(stream);
   int st = h->alloc.seq_evict(dst_host, src_host, keep_host, n, h->err);
   if (st != VSK_OK) return st;

@@ -248,3 +248,62 @@ def test_a_conversation_in_a_bounded_cache(spans, monkeypatch):
     b = d.eng.batch_host()
     np.testing.assert_array_equal(b["pos"], [sp.ctx + sp.q_len + drop - 1 for sp in w.seqs])
     d.release()
+
+
+@pytest.mark.parametrize("kind", ["decode", "mixed"])
+def test_replayed_passes_add_weights(kind):
+    """A captured pass over a windowed layer and a full one: every replay, with eager
+    passes between, gives the eager pass's bits and adds the same weights."""
+    if kind == "decode":
+        w = decode_workload(MID, [7, 16, 90, 500], seed=27, name="replay-decode")
+    else:
+        w = mixed_workload(MID, 1, 45, [3, 300], seed=28, name="replay-mixed")
+    d = _run(w)
+    n = max(s.ctx + s.q_len for s in w.seqs)
+    mass = torch.zeros((w.n_seqs, n), device="cuda")
+    d.eng.set_span(0, 30, 4)
+    d.eng.set_mass(mass.data_ptr(), w.n_seqs, n)
+    d.step()
+    lg, ids = d.results()
+    once = mass.clone()
+    assert float(once.sum()) > 0
+    d.step()
+    torch.cuda.synchronize()
+    twice = mass.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        d.step(torch.cuda.current_stream().cuda_stream)
+    for _ in range(4):
+        mass.zero_()
+        d.logits.zero_()
+        g.replay()
+        a, b = d.results()
+        np.testing.assert_array_equal(a, lg)
+        np.testing.assert_array_equal(b, ids)
+        assert torch.equal(mass, once)
+        d.step()
+        torch.cuda.synchronize()
+        assert torch.equal(mass, twice)
+    d.release()
+
+
+def test_the_scratch_entry_sees_windows_and_leaves_weights():
+    w = decode_workload(MID, [7, 16, 90, 500], seed=27, name="scratch-decode")
+    d = _run(w)
+    mass = torch.zeros((2, 4, 501), device="cuda")
+    d.eng.set_span(1, 30, 4)
+    d.eng.set_mass(mass[0].data_ptr(), 4, 501)
+    d.step()
+    a = d.results()
+    d.logits.zero_()
+    d.eng.set_mass(mass[1].data_ptr(), 4, 501)
+    d.eng.decode_step_scratch(d.ids.data_ptr(), d.logits.data_ptr(), d.next_ids.data_ptr(), d.sp)
+    b = d.results()
+    np.testing.assert_array_equal(a[0], b[0])
+    np.testing.assert_array_equal(a[1], b[1])
+    assert torch.equal(mass[0], mass[1]) and float(mass[0].sum()) > 0
+    d.eng.set_mass(mass[1].data_ptr(), 3, 501)
+    with pytest.raises(Exception) as x:
+        d.eng.decode_step_scratch(d.ids.data_ptr(), d.logits.data_ptr(), d.next_ids.data_ptr(), d.sp)
+    assert x.value.code == "ARG"
+    d.release()

@@ -205,3 +205,42 @@ def test_refused_evictions_change_nothing():
     torch.cuda.synchronize()
     np.testing.assert_array_equal(kept.cpu().numpy()[0, :16], kept_ref(m[0].cpu().numpy(), 100, 16, 0, 0))
     c.close()
+
+
+def test_evictions_in_a_row_share_a_metadata_buffer():
+    """Calls one after the other on another stream, with one buffer: metadata that
+    goes with the launch and metadata that is uploaded, a source that the call
+    before wrote."""
+    from paper_2609_37062_amd.runner import _dev_buffer
+    lens = [16384, 500, 300]
+    c = Cache(1, 1, 64, lens, layers=2, seed=9, spare=1500)
+    m = np.abs(c.rng.standard_normal((3, 16384))).astype(np.float32)
+    md = torch.from_numpy(m).cuda()
+    calls = [([10], [0], [9000]), ([11, 12], [1, 2], [200, 299]), ([13], [10], [2000]), ([14, 15], [13, 12], [77, 16])]
+    nb = 1 << 18
+    _t, meta = _dev_buffer(nb, "cuda")
+    side = torch.cuda.Stream()
+    outs = []
+    torch.cuda.synchronize()
+    for dst, src, keep in calls:
+        kept = torch.zeros((len(dst), 9000), dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+        for d in dst:
+            c.eng.seq_create(d)
+        assert c.eng.kv_evict_bytes(src, keep) <= nb
+        c.eng.kv_evict(dst, src, keep, 4, 8, md.data_ptr(), 16384, meta, nb, kept_ptr=kept.data_ptr(), out_stride=9000,
+                       stream=side.cuda_stream)
+        outs.append(kept)
+    torch.cuda.synchronize()
+    at = {i: np.arange(n) for i, n in enumerate(lens)}  # logical tokens of each sequence, and whose
+    root = {i: i for i in range(3)}
+    for (dst, src, keep), kept in zip(calls, outs):
+        for i, (d, s, k) in enumerate(zip(dst, src, keep)):
+            ref = kept_ref(m[i], len(at[s]), k, 4, 8)
+            np.testing.assert_array_equal(kept[i, :k].cpu().numpy(), ref)
+            at[d], root[d] = at[s][ref], root[s]
+            for l in range(2):
+                K, V = c.read(l, d)
+                np.testing.assert_array_equal(K, c.K[l][root[d]][at[d]])
+                np.testing.assert_array_equal(V, c.V[l][root[d]][at[d]])
+    c.close()

@@ -113,3 +113,14 @@ def test_positions_and_prefixes_without_eviction_are_unchanged():
     e.seq_share_prefix(9, 0, 96)
     assert e.seq_info(9)[0] == 96
     e.close()
+
+
+def test_evict_refuses_metadata_among_its_buffers():
+    e = _engine()
+    e.seq_create(7)
+    free = e.free_blocks()
+    for bad in (dict(meta=FAKE), dict(mass=8 * FAKE + 256), dict(kept=8 * FAKE + 508), dict(mass_out=8 * FAKE),
+                dict(slots=8 * FAKE + 128)):
+        assert _code(_evict, e, **bad) == "ARG", bad
+    assert e.free_blocks() == free and e.seq_info(7) == (0, [])
+    e.close()
