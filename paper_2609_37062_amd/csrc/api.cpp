@@ -1209,10 +1209,12 @@ static AttnPlan plan_attn(Handle& h, const uint16_t* q, uint16_t* out, int out_R
   int blk_min = INT_MAX, blk_max = 0, n_dec = 0;
   // and how many of those an earlier row of the launch reads too
   int64_t blk_sum = 0, blk_again = 0;
+  int32_t walks[kPackedRows];  // of up to so many rows
   {
     const BatchHost& bh = h.bh;
     auto row_blocks = [&](int r) {
       const int nb = span_walk(bh.pos[r] + 1, bh.pos[r] + 1, window, sinks).nv - (cascade ? bh.pfx_blocks[r] : 0);
+      if (n_dec < kPackedRows) walks[n_dec] = nb;
       blk_min = std::min(blk_min, nb);
       blk_max = std::max(blk_max, nb);
       blk_sum += nb;
@@ -1241,6 +1243,10 @@ static AttnPlan plan_attn(Handle& h, const uint16_t* q, uint16_t* out, int out_R
   // (a general walk counts the rows that it is for, not the prompt rows beside
   // them: 7 rows of 300-3,000 tokens beside a prompt chunk 22 -> 16 us)
   aa.bps = h.attn_bps > 0 ? h.attn_bps : attn_auto_bps(p.span ? n_dec : R, c.n_kv_heads);
+  // (the even splits of general walks like 128 blocks once there are enough
+  // pairs: 48 rows of 300-16,000 tokens 260 -> 255 us, 64 of 2,000-12,000 293 ->
+  // 286, 100 of 1,000-4,000 166 -> 162; 32 of 1,000-4,000 72 -> 77)
+  if (p.span && h.attn_bps == 0 && n_dec * c.n_kv_heads >= 384) aa.bps = 128;
   // 128..255 (row, KV head) pairs whose walks are within 20% of each other:
   // one split per pair (no merge, and the items are balanced already); a
   // wider spread keeps the split, the longest walk setting the time, and
@@ -1255,6 +1261,37 @@ static AttnPlan plan_attn(Handle& h, const uint16_t* q, uint16_t* out, int out_R
   if (h.attn_bps == 0 && n_dec > 0 && ((pairs >= 128 && pairs < 256 && 5 * blk_min >= 4 * blk_max) ||
                                        blk_sum * c.n_kv_heads >= static_cast<int64_t>(kAttnSlots) * blk_max))
     aa.bps = std::clamp((blk_max + 7) / 8 * 8, kAttnMinBps, kAttnMaxBps);
+  if (p.span && n_dec <= kPackedRows) {
+    auto items = [&](int bps) {
+      int64_t n = 0;
+      for (int i = 0; i < n_dec; ++i) {
+        const int e = even_split(walks[i], bps);
+        n += (walks[i] + e - 1) / e;
+      }
+      return n * c.n_kv_heads;
+    };
+    // few general walks: the shortest splits that give every compute unit one
+    // work item at most, unless the longest is then half as long again as an
+    // even share.  (One more than compute units, and a unit has two while others
+    // run dry: 4 rows of 8,000-16,000 tokens, 8 heads x 128, 768 work items 40 us,
+    // 264 44, 200 33; 2 of 15,000-16,000 496 28, 248 24; 8 of 8,000 1,024 46, 256 42.)
+    const int share = static_cast<int>(blk_sum * c.n_kv_heads / kAttnUnits);
+    if (h.attn_bps == 0 && share >= kAttnMinBps)
+      for (int bps = std::max(32, (share + 7) / 8 * 8); bps <= std::min(kAttnMaxBps, share * 3 / 2); bps += 8)
+        if (items(bps) <= kAttnUnits) {
+          aa.bps = bps;
+          break;
+        }
+    // so many work items, but a grid of rows x most splits would be more than
+    // the units: packed (0.9 us of every work item; 8 rows of 3,000-16,000 tokens
+    // 63 us in 224 of a grid of 384, 52 packed)
+    const int64_t n = items(aa.bps);
+    const int64_t most = (blk_max + aa.bps - 1) / aa.bps;
+    if (n <= kAttnUnits && n_dec * most * c.n_kv_heads > kAttnUnits) {
+      aa.packed = n_dec;
+      aa.packed_items = static_cast<int>(n / c.n_kv_heads);
+    }
+  }
   aa.max_splits = attn_splits(b.max_kv_len, aa.bps);
   aa.part_o = reinterpret_cast<float*>(ws + wl.att_o);
   aa.part_ml = reinterpret_cast<float2*>(ws + wl.att_ml);

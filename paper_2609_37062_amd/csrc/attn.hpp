@@ -26,6 +26,14 @@ __host__ __device__ inline SpanWalk span_walk(int first_end, int last_end, int w
   return g;
 }
 
+// Blocks of a split where `bps` of them at most cut a walk of nb: even splits, of
+// whole steps of a work item's four waves.
+__host__ __device__ inline int even_split(int nb, int bps) {
+  const int n = (nb + bps - 1) / bps;
+  return n > 1 ? ((nb + n - 1) / n + 7) / 8 * 8 : bps;
+}
+constexpr int kPackedRows = 64;  // rows of a launch whose splits a wave can count
+
 struct AttnArgs {
   const uint16_t* q;  // [R][Nq] bf16
   const uint16_t* pool;
@@ -58,6 +66,9 @@ struct AttnArgs {
   // out_Rg 0 stores the output row-major ([R][Nq]); ml (nullable) receives
   // each (row, query head)'s softmax maximum (base 2) and 1 / sum
   int window, sinks;
+  // of at most kPackedRows rows: their number (else 0), and their splits, which
+  // are the launch's work items with none between that has nothing to do
+  int packed, packed_items;
   float2* ml;  // [R][Nq / hd]
   // nullable: the scores too, [rows of the launch][Nq / hd][scores_len], key by
   // key of the row's SpanWalk list, -inf where the row does not see it

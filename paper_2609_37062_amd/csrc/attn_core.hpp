@@ -324,12 +324,13 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   // splits cover blocks P.. and follow the prefix partials
   const int P = a.pfx_blocks != nullptr ? a.pfx_blocks[row] : 0;
   const int n_ps = P > 0 ? a.pfx_splits[row] : 0;
-  const int n_splits = (nb - P + a.bps - 1) / a.bps;
+  const int bps = SPAN ? even_split(nb - P, a.bps) : a.bps;
+  const int n_splits = (nb - P + bps - 1) / bps;
   if (split >= n_splits) return;
   const int seq = a.row_seq[row];
   const int32_t* table = a.block_table + static_cast<size_t>(seq) * a.max_blocks;
-  const int b_lo = P + split * a.bps;
-  const int b_hi = min(nb, b_lo + a.bps);
+  const int b_lo = P + split * bps;
+  const int b_hi = min(nb, b_lo + bps);
   // the split's block-table entries, staged once for all waves
   for (int i = tid; i < b_hi - b_lo; i += blockDim.x) sm.tbl[i] = table[SPAN ? span.block(b_lo + i) : b_lo + i];
   const int h = lane & 15;       // query head within the group (valid if h < G)

@@ -154,6 +154,7 @@ inline int attn_splits(int kv_len, int bps) {
 inline int attn_auto_bps(int n_rows, int n_kv_heads) { return n_rows * n_kv_heads >= 256 ? 96 : 32; }
 
 constexpr int kAttnSlots = 512;  // decode work items in flight: two per compute unit
+constexpr int kAttnUnits = 256;  // compute units
 
 struct Handle {
   vsk_model_cfg cfg{};

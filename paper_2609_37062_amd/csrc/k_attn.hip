@@ -34,12 +34,41 @@ constexpr int kPreTiles = kPreCols / 16;   // 16-column tiles (one wave each) of
 // two layers of hidden 3072, split not turned and turned: 2 KV heads, 37 rows
 // of 100 to 6,000 tokens 216 -> 203, 16 of 2,000 to 4,000 168 -> 161; 4 heads,
 // 37 rows 264 -> 256, 100 rows of 1,500 to 2,500 396 -> 375.
+//
+// General walks: grid (KV head, row, split), longest row first, with a row's
+// splits even; where all of them are at most one a compute unit, and the grid
+// would be more (rows of different lengths), packed: (KV head, split of any row).
 template <int D, bool FOLD2, bool NTKV, bool SPAN>
 __global__ __launch_bounds__(64 * kAttnWaves) void k_attn_decode(AttnArgs a) {
   __shared__ AttnLds<D, kAttnWaves> sm;
-  const int split = (blockIdx.y + blockIdx.z) % gridDim.y;
-  attn_unit<D, false, kAttnWaves, FOLD2, NTKV, SPAN>(
-      a, a.rows != nullptr ? a.rows[blockIdx.z] : static_cast<int>(blockIdx.z), blockIdx.x, split, sm, blockIdx.z);
+  if constexpr (!SPAN) {
+    const int split = (blockIdx.y + blockIdx.z) % gridDim.y;
+    attn_unit<D, false, kAttnWaves, FOLD2, NTKV, SPAN>(
+        a, a.rows != nullptr ? a.rows[blockIdx.z] : static_cast<int>(blockIdx.z), blockIdx.x, split, sm, blockIdx.z);
+  } else {
+    int r = blockIdx.y, split = blockIdx.z;
+    if (a.packed > 0) {  // work item blockIdx.y of all the rows' splits, row by row
+      const int lane = threadIdx.x & 63;
+      int n = 0;
+      if (lane < a.packed) {
+        const int row = a.rows != nullptr ? a.rows[lane] : lane, kv_len = a.pos[row] + 1;
+        const int nb = span_walk(kv_len, kv_len, a.window, a.sinks).nv - (a.pfx_blocks != nullptr ? a.pfx_blocks[row] : 0);
+        const int bps = even_split(nb, a.bps);
+        n = (nb + bps - 1) / bps;
+      }
+      int end = n;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int x = __shfl_up(end, d, 64);
+        if (lane >= d) end += x;
+      }
+      const uint64_t behind = __ballot(end > static_cast<int>(blockIdx.y));
+      if (behind == 0) return;
+      r = __builtin_ctzll(behind);
+      split = blockIdx.y - __builtin_amdgcn_readlane(end - n, r);
+    }
+    attn_unit<D, false, kAttnWaves, FOLD2, NTKV, SPAN>(a, a.rows != nullptr ? a.rows[r] : r, blockIdx.x, split, sm, r);
+  }
 }
 
 template <int D, bool FOLD2, bool NTKV, bool SPAN>
@@ -67,7 +96,9 @@ static void launch_decode_d(const AttnArgs& a, dim3 grid, bool fold2, bool span,
 hipError_t launch_attn_decode(const AttnArgs& a, int n_rows, int grid_splits, int max_pfx_splits, hipStream_t s,
                               LaunchEvents ev, bool span) {
   if (grid_splits < 1 || grid_splits > a.max_splits) return hipErrorInvalidValue;
-  dim3 grid(a.Hkv, grid_splits, n_rows);
+  const dim3 grid = !span          ? dim3(a.Hkv, grid_splits, n_rows)
+                    : a.packed > 0 ? dim3(a.Hkv, a.packed_items)
+                                   : dim3(a.Hkv, n_rows, grid_splits);
   const bool fold2 = a.pfx_splits != nullptr && max_pfx_splits > kAttnWaves;
   if (a.hd == 128) launch_decode_d<128>(a, grid, fold2, span, s, ev);
   else if (a.hd == 64) launch_decode_d<64>(a, grid, fold2, span, s, ev);

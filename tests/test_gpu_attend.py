@@ -340,3 +340,51 @@ def test_reading_slots_of_any_order(kv, hd):
                 x[~skip] = src[order[~skip]]
                 np.testing.assert_array_equal(got.float().cpu().numpy(), want)
     c.close()
+
+
+@pytest.mark.parametrize("hd,group", [(64, 2), (128, 1)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (3000, 40)])
+def test_single_tokens_of_uneven_long_caches(hd, group, window, sinks):
+    """Rows of which some have one split and some many, all of them in one round."""
+    c = Cache(8, group, hd, [8000, 300, 5000, 2500, 1200, 40, 1], seed=19)
+    c.batch(range(7), [1] * 7)
+    mass = torch.zeros((7, 8000), device="cuda")
+    c.attend(window=window, sinks=sinks)
+    check(c, window, sinks)
+    c.attend(window=window, sinks=sinks, mass=mass)
+    check(c, window, sinks, mass=mass)
+    c.close()
+
+
+def test_uneven_caches_behind_a_shared_prefix():
+    c = Cache(8, 1, 64, [6000], seed=20, spare=600)
+    free = [b for b in range(c.n_blocks) if b not in set(c.blocks[0].tolist())]
+    rng = np.random.default_rng(4)
+    for i, n in enumerate((4000, 500, 900, 2000), start=1):
+        own = -(-(n - 320) // BLOCK)
+        c.eng.seq_create(i)
+        c.eng.seq_set_blocks(i, np.concatenate([c.blocks[0][:20], free[:own]]).astype(np.int32), n)
+        free = free[own:]
+        perm = 320 + rng.permutation(6000 - 320)[:n - 320]
+        c.K[0].append(np.concatenate([c.K[0][0][:320], c.K[0][0][perm]]))
+        c.V[0].append(np.concatenate([c.V[0][0][:320], c.V[0][0][perm]]))
+        c.write(0, i, 320)
+    c.batch(range(5), [1] * 5)
+    assert c.eng.batch_prefix_info()[1] == 1
+    mass = torch.zeros((5, 6000), device="cuda")
+    for window, sinks in [(0, 0), (2500, 16)]:
+        c.attend(window=window, sinks=sinks, mass=mass)
+        check(c, window, sinks, mass=mass)
+    c.close()
+
+
+def test_many_single_tokens():
+    """More rows than a wave counts, and splits of 128 blocks."""
+    lens = [1 + 37 * i % 700 + (2500 if i % 23 == 5 else 0) for i in range(97)]
+    c = Cache(4, 1, 64, lens, seed=21)
+    c.batch(range(97), [1] * 97)
+    mass = torch.zeros((97, max(lens)), device="cuda")
+    for window, sinks in [(0, 0), (400, 7)]:
+        c.attend(window=window, sinks=sinks, mass=mass)
+        check(c, window, sinks, mass=mass)
+    c.close()
