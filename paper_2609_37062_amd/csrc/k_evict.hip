@@ -10,6 +10,8 @@
 //
 // k_evict_move: copies K and V of the kept tokens, every layer and KV head, to
 // the destination's blocks.
+//
+// k_evict_small: both, for a few short sequences.
 #include <cstring>
 #include <type_traits>
 
@@ -188,29 +190,15 @@ __global__ __launch_bounds__(T) void k_evict_select(EvictArgs a, M meta) {
     for (int64_t i = keep + tid; i < a.out_stride; i += T) a.mass_out[seq * a.out_stride + i] = 0.f;
 }
 
-// One workgroup per destination block of a layer and KV head, one thread per
-// 16-byte piece: 8 dims of a token of K, 8 tokens of a dim of V.  Lanes run
-// along what is contiguous in the pool: the tokens of K pieces, the dims of V
-// pieces.  A line of the pool holds eight tokens of K, or eight tokens of
-// eight dims of V, so where few tokens stay the lines read are more than the
-// bytes moved: with one in five kept, 85% of the source.
-__global__ __launch_bounds__(256) void k_evict_move(EvictArgs a) {
-  const int seq = blockIdx.z, layer = blockIdx.y / a.Hkv, hk = blockIdx.y % a.Hkv;
-  const int32_t* info = a.info + 4 * seq;
-  const int keep = info[1], hd = a.hd;
-  const int blk = blockIdx.x;  // destination block
-  if (blk * kBlock >= keep) return;
-  const int32_t* from = a.from + (static_cast<int64_t>(info[3]) + blk) * kBlock;
-  const int n = min(kBlock, keep - blk * kBlock);
-  const size_t head = static_cast<size_t>(kBlock) * hd, stride = head * a.Hkv;
-  uint16_t* kp = a.pool + static_cast<size_t>(layer) * 2 * a.n_blocks * stride + hk * head;
-  uint16_t* vp = kp + static_cast<size_t>(a.n_blocks) * stride;
-  const size_t to = static_cast<size_t>(a.dst_tbl[info[3] + blk]) * stride;
-  const int i = threadIdx.x;  // < 2 hd
-  // K: the piece at place i of the block's 2 hd (its token's bits 2 and 3 are swapped, see kv_k_index)
+// The 16-byte piece at place i of a destination block's K and V (2 hd places): 8
+// dims of a token of K, 8 tokens of a dim of V, from the slots `from` of the
+// block's n tokens.
+__device__ __forceinline__ void move_piece(uint16_t* kp, uint16_t* vp, size_t stride, size_t to, const int32_t* from,
+                                           int n, int i) {
+  // K: its token's bits 2 and 3 are swapped, see kv_k_index
   const int p = i % kBlock, tk = (p & 3) | ((p & 4) << 1) | ((p & 8) >> 1), e = i / kBlock * 8;
   const int sk = from[min(tk, n - 1)];
-  // V: dim and half of the piece at place i
+  // V: dim and half
   const int ev = i / 32 * 16 + i % 16, t0 = i % 32 / 16 * 8;
   int sv[8];
 #pragma unroll
@@ -223,6 +211,120 @@ __global__ __launch_bounds__(256) void k_evict_move(EvictArgs a) {
   *reinterpret_cast<u32x4*>(kp + to + i * 8) = x;
   *reinterpret_cast<u32x4*>(vp + to + i * 8) =
       u32x4{y[0] | y[1] << 16, y[2] | y[3] << 16, y[4] | y[5] << 16, y[6] | y[7] << 16};
+}
+
+// One workgroup per destination block of a layer and KV head, one thread per
+// piece.  Lanes run along what is contiguous in the pool: the tokens of K
+// pieces, the dims of V pieces.  A line of the pool holds eight tokens of K, or
+// eight tokens of eight dims of V, so where few tokens stay the lines read are
+// more than the bytes moved: with one in five kept, 85% of the source.
+__global__ __launch_bounds__(256) void k_evict_move(EvictArgs a) {
+  const int seq = blockIdx.z, layer = blockIdx.y / a.Hkv, hk = blockIdx.y % a.Hkv;
+  const int32_t* info = a.info + 4 * seq;
+  const int keep = info[1], hd = a.hd;
+  const int blk = blockIdx.x;  // destination block
+  if (blk * kBlock >= keep) return;
+  const size_t head = static_cast<size_t>(kBlock) * hd, stride = head * a.Hkv;
+  uint16_t* kp = a.pool + static_cast<size_t>(layer) * 2 * a.n_blocks * stride + hk * head;
+  uint16_t* vp = kp + static_cast<size_t>(a.n_blocks) * stride;
+  const size_t to = static_cast<size_t>(a.dst_tbl[info[3] + blk]) * stride;
+  move_piece(kp, vp, stride, to, a.from + (static_cast<int64_t>(info[3]) + blk) * kBlock,
+             min(kBlock, keep - blk * kBlock), threadIdx.x);
+}
+
+// Both at once for short sequences: every workgroup (a KV head's run of
+// kSmallRun destination blocks of a layer and sequence) makes the selection for
+// itself, a wave alone -- the smallest kept key bit by bit, counted by ballots --
+// and moves its blocks.  One launch instead of two that depend on each other:
+// 96 of 201 tokens, one layer of 4 heads x 64, 6.5 us instead of 6.7 and 3.3.
+// With many workgroups the selections made again cost more than the launch (calls
+// with the cache read back, 400 of 512 tokens of 8 heads x 128: 4 layers, 224
+// workgroups, 36 us and 47-53 apart; 16 layers, 896, 127 and 125; 8 sequences,
+// 2,048, 160 and 151).
+constexpr int kSmallLen = 512;  // tokens
+constexpr int kSmallRun = 4;
+constexpr int kSmallWgs = 512;
+__global__ __launch_bounds__(256) void k_evict_small(EvictArgs a, EvictSmall meta) {
+  constexpr int PER = kSmallLen / 64;
+  __shared__ int32_t s_from[kSmallRun * kBlock];
+  const int seq = blockIdx.z, layer = blockIdx.y, hk = blockIdx.x % a.Hkv, run = blockIdx.x / a.Hkv;
+  const int32_t* info = meta.v + 4 * seq;
+  const int len = info[0], keep = info[1];
+  const int first = run * kSmallRun * kBlock;  // of the run's kept tokens
+  if (first >= keep) return;
+  const int32_t* src_tbl = meta.v + (a.src_tbl - a.info) + info[2];
+  const int32_t* dst_tbl = meta.v + (a.dst_tbl - a.info) + info[3];
+  const int tid = threadIdx.x, lane = tid & 63;
+  if (tid < 64) {
+    const float* mass = a.mass + seq * a.mass_stride;
+    const int lo = a.sinks, hi = len - a.recent;  // the tokens that compete
+    const int left0 = keep - a.sinks - a.recent;  // how many of them stay
+    // token 64 q + lane; `in` the ones that compete
+    float v[PER];
+    uint32_t key[PER];
+    uint64_t in[PER];
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      const int i = 64 * q + lane;
+      v[q] = i < len ? mass[i] : 0.f;
+      key[q] = mass_key(v[q]);
+      in[q] = __ballot(i >= lo && i < hi);
+    }
+    auto at_least = [&](uint32_t k) {
+      int n = 0;
+#pragma unroll
+      for (int q = 0; q < PER; ++q) n += __popcll(__ballot(key[q] >= k) & in[q]);
+      return n;
+    };
+    uint32_t top = 0;  // at least left0 keys are as large
+    int n = max(0, hi - lo);
+    for (uint32_t bit = 1u << 31; bit != 0 && n != left0; bit >>= 1) {
+      const int m = at_least(top | bit);
+      if (m >= left0) {
+        top |= bit;
+        n = m;
+      }
+    }
+    // n of them: where that is more, the ones equal to `top` stay by index
+    int ties = left0 - (n == left0 ? 0 : at_least(top + 1));  // (top + 1 is at most NaN's ~0)
+    const bool cut = n != left0;
+    int at0 = 0;
+    const uint64_t before = (1ull << lane) - 1ull;
+    const bool writes = layer == 0 && hk == 0 && run == 0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      const int i = 64 * q + lane;
+      uint64_t chosen = __ballot(left0 > 0 && key[q] >= top) & in[q];
+      if (cut) {
+        const uint64_t equal = __ballot(key[q] == top) & in[q];
+        const int mine = __popcll(equal & before);
+        chosen &= ~(equal & __ballot(mine >= ties));
+        ties = max(0, ties - static_cast<int>(__popcll(equal)));
+      }
+      const uint64_t stay = chosen | __ballot(i < len && (i < lo || i >= hi));
+      const int at = at0 + __popcll(stay & before);
+      at0 += __popcll(stay);
+      if (!(stay >> lane & 1u)) continue;
+      if (at >= first && at < first + kSmallRun * kBlock) s_from[at - first] = src_tbl[i / kBlock] * kBlock + i % kBlock;
+      if (!writes) continue;
+      a.kept[seq * a.out_stride + at] = i;
+      if (a.slots != nullptr) a.slots[seq * a.out_stride + at] = dst_tbl[at / kBlock] * kBlock + at % kBlock;
+      if (a.mass_out != nullptr) a.mass_out[seq * a.out_stride + at] = v[q];
+    }
+    if (writes && a.mass_out != nullptr)
+      for (int64_t i = keep + lane; i < a.out_stride; i += 64) a.mass_out[seq * a.out_stride + i] = 0.f;
+  }
+  __syncthreads();
+  const int hd = a.hd;
+  const size_t head = static_cast<size_t>(kBlock) * hd, stride = head * a.Hkv;
+  uint16_t* kp = a.pool + static_cast<size_t>(layer) * 2 * a.n_blocks * stride + hk * head;
+  uint16_t* vp = kp + static_cast<size_t>(a.n_blocks) * stride;
+  for (int x = tid; x < kSmallRun * 2 * hd; x += 256) {
+    const int b = x / (2 * hd), n = min(kBlock, keep - first - b * kBlock);
+    if (n > 0)
+      move_piece(kp, vp, stride, static_cast<size_t>(dst_tbl[first / kBlock + b]) * stride, s_from + b * kBlock, n,
+                 x % (2 * hd));
+  }
 }
 
 // Few tokens take few waves (cheaper rounds), and never more registers than tokens need.
@@ -240,6 +342,13 @@ hipError_t launch_evict(const EvictArgs& a, const int32_t* meta, size_t ints, in
     EvictSmall m;
     std::memset(&m, 0, sizeof(m));
     std::memcpy(m.v, meta, ints * 4);
+    // (in place, another workgroup would read weights that one has replaced)
+    const int runs = (max_keep + kSmallRun * kBlock - 1) / (kSmallRun * kBlock);
+    if (max_len <= kSmallLen && a.mass_out != a.mass &&
+        static_cast<int64_t>(runs) * a.Hkv * a.n_layers * n <= kSmallWgs) {
+      hipLaunchKernelGGL(k_evict_small, dim3(runs * a.Hkv, a.n_layers, n), dim3(256), 0, s, a, m);
+      return hipGetLastError();
+    }
     launch_select(a, m, n, max_len, s);
   } else {
     launch_select(a, 0, n, max_len, s);

@@ -244,3 +244,30 @@ def test_evictions_in_a_row_share_a_metadata_buffer():
                 np.testing.assert_array_equal(K, c.K[l][root[d]][at[d]])
                 np.testing.assert_array_equal(V, c.V[l][root[d]][at[d]])
     c.close()
+
+
+@pytest.mark.parametrize("kv,hd,layers", [(1, 64, 1), (3, 128, 2), (8, 64, 4)])
+@pytest.mark.parametrize("weights", ["spread", "zeros", "ties", "strange"])
+def test_kept_tokens_of_short_sequences(kv, hd, layers, weights):
+    """Lengths around 64, 256 and 512, in one launch or two, with and without room
+    for weights and slots; and the same in place."""
+    for lens, keep, sinks, recent in [([1], [1], 0, 0), ([512], [129], 4, 8), ([511], [511], 0, 3), ([513], [129], 4, 8),
+                                      ([64, 65, 300], [64, 9, 64], 4, 5), ([257, 256], [1, 255], 0, 0),
+                                      ([500], [65], 65, 0), ([500], [65], 0, 65), ([130, 90], [70, 70], 10, 10)]:
+        c = Cache(kv, 1, hd, lens, layers=layers, seed=len(lens), spare=150)
+        n = len(lens)
+        m = np.exp(3 * c.rng.standard_normal((n, max(lens) + 2))).astype(np.float32)
+        if weights == "zeros":
+            m[:] = 0
+        if weights == "ties":
+            m = np.floor(c.rng.random(m.shape) * 3).astype(np.float32)
+        if weights == "strange":
+            m = c.rng.choice(np.array([np.nan, np.inf, -np.inf, 0.0, -0.0, -1.0, 1e-45, 3e38], np.float32), m.shape)
+        dst = list(range(n, 2 * n))
+        got = evict(c, dst, list(range(n)), keep, sinks, recent, torch.from_numpy(m).cuda())
+        check_evicted(c, dst, range(n), keep, sinks, recent, m, got)
+        again = evict(c, [d + n for d in dst], list(range(n)), keep, sinks, recent, torch.from_numpy(m).cuda(), in_place=True)
+        for i, k in enumerate(keep):
+            np.testing.assert_array_equal(again[0][i, :k], got[0][i, :k])
+            np.testing.assert_array_equal(again[2][i, :k], got[2][i, :k])
+        c.close()
