@@ -388,3 +388,14 @@ def test_many_single_tokens():
         c.attend(window=window, sinks=sinks, mass=mass)
         check(c, window, sinks, mass=mass)
     c.close()
+
+
+def test_weights_of_prompt_rows_one_work_item_a_row():
+    c = Cache(2, 3, 64, [70, 300, 33], seed=22)
+    c.eng.set_tuning(6, 0)
+    c.batch([0, 1, 2], [70, 5, 1])
+    mass = torch.zeros((3, 300), device="cuda")
+    for window, sinks in [(0, 0), (20, 3)]:
+        c.attend(window=window, sinks=sinks, mass=mass)
+        check(c, window, sinks, mass=mass)
+    c.close()
