@@ -56,7 +56,7 @@ struct AttnArgs {
   // 0..pfx_splits[row]-1 and its first split starts from them
   const int32_t* pfx_blocks;  // [R]
   const int32_t* pfx_splits;  // [R]
-  const int32_t* rows;        // nullable: the rows of the launch (grid z indexes it), else all rows
+  const int32_t* rows;        // nullable: the rows of the launch (k_attn_decode indexes it), else all rows
   // routed layer (nullable): per row 1 RUN, 0 Project-Only; a Project-Only
   // row reads no KV and its attention output is zero (Algorithm 1)
   const uint8_t* run_mask;

@@ -73,10 +73,6 @@ __device__ __forceinline__ void store_wt16(void* p, uint32_t v) {
   asm volatile("global_store_short %0, %1, off sc1" : : "v"(p), "v"(v) : "memory");
 }
 
-// threadIdx.x through an opaque move: values derived from it inside a
-// phase of a persistent kernel are then computed in that phase instead of
-// being hoisted out of the surrounding loop and held in registers across
-// every other phase.
 // 16 bytes per lane from global memory straight into LDS: lane l's bytes land
 // at lds + 16 l (the LDS address must be the same for the whole wave).  The
 // load counts in the wave's vector-memory counter until its bytes are in LDS.
@@ -132,6 +128,10 @@ __device__ __forceinline__ void barrier_no_fence() {
   asm volatile("" ::: "memory");
 }
 
+// threadIdx.x through an opaque move: values derived from it inside a
+// phase of a persistent kernel are then computed in that phase instead of
+// being hoisted out of the surrounding loop and held in registers across
+// every other phase.
 __device__ __forceinline__ int opaque_tid() {
   int t;
   asm volatile("v_mov_b32 %0, %1" : "=v"(t) : "v"(static_cast<int>(threadIdx.x)));
