@@ -269,7 +269,7 @@ __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
   const int f_from = tw + 32 <= kv_len ? tw + 31 - p0 : INT_MAX;
   const int f_to = min(rb, a.window == 0 || tw + 32 <= a.sinks ? INT_MAX : tw + a.window - p0) - Rt;
   const int cr = lc / G;  // the lane's column's row in its tile (Rt: none)
-  const bool c_on = lc < Rt * G;  // (else its weights are times zero)
+  const bool c_on = lc < Rt * G;  // (else it counts nowhere: no bits, and times zero in full tiles)
   const float sc = a.scale_log2;
   float acc[16];
 #pragma unroll
@@ -311,7 +311,10 @@ __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
         // (both sides of a difference rounded alike, see pair_softmax)
 #pragma clang fp contract(off)
         const int row = r_first + Rt * i + cr, p = p0 + row;
-        const int end = row < rb ? min(kv_len, p + 1) : 0;
+        // (a column behind the tile's rows is a copy of its last one, under the
+        // next row's index: that row's own key may be far above the copy's
+        // maximum, and 0 x infinity is NaN)
+        const int end = c_on && row < rb ? min(kv_len, p + 1) : 0;
         const int lo = a.window > 0 && p + 1 > a.window ? p + 1 - a.window : 0;
         const uint32_t bits =
             span_bits(tw + 8 * hi, end, lo, a.sinks) | span_bits(tw + kBlock + 8 * hi, end, lo, a.sinks) << 8;

@@ -399,3 +399,45 @@ def test_weights_of_prompt_rows_one_work_item_a_row():
         c.attend(window=window, sinks=sinks, mass=mass)
         check(c, window, sinks, mass=mass)
     c.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("group", [3, 5, 7, 12])
+@pytest.mark.parametrize("scale", [60.0, 2.0 ** 24])
+def test_weights_of_large_scores_where_groups_leave_columns_over(group, hd, scale):
+    """32 columns hold 10, 6, 4, 2 whole rows of these groups.  A row's own key
+    may score far above all that the row before it sees; every weight is finite,
+    and a row's weights come to 1 a head."""
+    for seed in range(3):
+        print(f"[gpu] large scores group={group} hd={hd} scale={scale} seed={seed}", flush=True)
+        c = Cache(1, group, hd, [40, 33], seed=100 + seed, scale=scale)
+        c.batch([0, 1], [40, 33])
+        mass = torch.zeros((2, 40), device="cuda")
+        for window, sinks in [(0, 0), (1, 0), (30, 2)]:
+            c.attend(window=window, sinks=sinks, mass=mass)
+            if scale < 2.0 ** 20:
+                check(c, window, sinks, mass=mass)
+            assert np.isfinite(c.out()).all()
+            for i, n in enumerate(c.lens):
+                m = mass[i, :n].cpu().numpy()
+                assert np.isfinite(m).all(), (window, np.flatnonzero(~np.isfinite(m)))
+                assert abs(m.sum() - n * group) < 1e-3 * n * group
+        c.close()
+
+
+@pytest.mark.parametrize("group", [3, 4, 7, 12])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
+def test_a_query_that_is_not_a_number_stays_with_the_keys_it_sees(group, window, sinks):
+    c = Cache(1, group, 64, [60], seed=23)
+    c.batch([0], [45])
+    mass = torch.zeros((1, 60), device="cuda")
+    q = c.qd.clone()
+    for r in range(45):
+        c.qd.copy_(q)
+        c.qd[r] = float("nan")
+        c.attend(window=window, sinks=sinks, mass=mass)
+        m = mass[0].cpu().numpy()
+        see = visible(15 + r, 60, window, sinks)
+        assert np.isfinite(m[~see]).all(), (r, np.flatnonzero(~np.isfinite(m) & ~see))
+        assert np.isnan(m[see]).all(), r
+    c.close()
