@@ -96,8 +96,9 @@ __global__ __launch_bounds__(64 * kMassWaves) void k_attn_mass(AttnMassArgs a) {
     f32x4 s0, s1;
     pair_qk<D>(qf, kg, s0, s1);
     const int end = min(kv_len, p0 + row + 1);
+    // (1 / l is 0 for a Project-Only row, which has no weights: 0 x NaN would be one)
     const uint32_t bits =
-        on ? span_bits(t0 + 8 * quad, end, a.window > 0 && end > a.window ? end - a.window : 0, a.sinks) : 0u;
+        on && ml.y != 0.f ? span_bits(t0 + 8 * quad, end, a.window > 0 && end > a.window ? end - a.window : 0, a.sinks) : 0u;
     {
       // (both sides of the difference rounded alike, as in pair_softmax)
 #pragma clang fp contract(off)
@@ -311,10 +312,11 @@ __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
         // (both sides of a difference rounded alike, see pair_softmax)
 #pragma clang fp contract(off)
         const int row = r_first + Rt * i + cr, p = p0 + row;
-        // (a column behind the tile's rows is a copy of its last one, under the
-        // next row's index: that row's own key may be far above the copy's
-        // maximum, and 0 x infinity is NaN)
-        const int end = c_on && row < rb ? min(kv_len, p + 1) : 0;
+        // (1 / l is 0 for columns without weights.  Behind the tile's rows they are
+        // copies of its last one, under the next row's index: that row's own key
+        // may be far above the copy's maximum, and 0 x infinity is NaN.  A
+        // Project-Only row's keys may hold anything)
+        const int end = ml.y != 0.f && row < rb ? min(kv_len, p + 1) : 0;
         const int lo = a.window > 0 && p + 1 > a.window ? p + 1 - a.window : 0;
         const uint32_t bits =
             span_bits(tw + 8 * hi, end, lo, a.sinks) | span_bits(tw + kBlock + 8 * hi, end, lo, a.sinks) << 8;

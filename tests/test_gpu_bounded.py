@@ -307,3 +307,47 @@ def test_the_scratch_entry_sees_windows_and_leaves_weights():
         d.eng.decode_step_scratch(d.ids.data_ptr(), d.logits.data_ptr(), d.next_ids.data_ptr(), d.sp)
     assert x.value.code == "ARG"
     d.release()
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("kind", ["chunk", "one item a row", "prefix"])
+def test_project_only_rows_leave_no_weights_on_keys_that_are_not_finite(kind, bad):
+    """A layer whose rows are all Project-Only reads no K and V: what these hold changes no bit."""
+    import dataclasses
+    from workloads.configs import SeqSpec, prefix_groups_workload
+    if kind == "prefix":
+        w = prefix_groups_workload(MID, [(96, 3)], [10, 21, 5, 40], seed=29, name="po-prefix")
+    else:
+        w = mixed_workload(MID, 1, 19, [60, 33, 5], seed=30, name="po-chunk")
+        s = w.seqs[1]
+        seqs = [w.seqs[0], SeqSpec(60, 21, s.blocks, s.content, logits=True)] + w.seqs[2:]
+        tokens = np.random.default_rng(31).integers(0, MID.vocab, 19 + 21 + 2).astype(np.int32)
+        w = dataclasses.replace(w, seqs=seqs, tokens=tokens, n_pool_blocks=w.n_pool_blocks + 4)
+    d = _run(w, routed=True)
+    assert MID.n_routed == 1
+    if kind == "one item a row":
+        d.eng.set_tuning(6, 0)
+    d.set_route(np.zeros((1, w.n_rows), bool), np.ones((1, w.n_rows), np.float32))
+    n = max(s.ctx + s.q_len for s in w.seqs)
+    mass = torch.zeros((w.n_seqs, n), device="cuda")
+    d.eng.set_mass(mass.data_ptr(), w.n_seqs, n)
+    want = {}
+    for spans in ((0, 0), (40, 2)):
+        d.eng.set_span(-1, *spans)
+        mass.zero_()
+        d.step_routed()
+        want[spans] = (d.results()[0], mass.clone())
+        assert float(mass.sum()) > 0
+    for i, s in enumerate(w.seqs):
+        if s.ctx:
+            sl = torch.from_numpy(d.seq_slots(i, 0, s.ctx)).cuda()
+            x = torch.full((s.ctx, MID.n_kv_heads, MID.head_dim), bad, dtype=torch.bfloat16, device="cuda")
+            d.eng.kv_write(1, sl.data_ptr(), s.ctx, x.data_ptr(), x.data_ptr(), d.sp)
+            torch.cuda.synchronize()
+    for spans, (lg, m) in want.items():
+        d.eng.set_span(-1, *spans)
+        mass.zero_()
+        d.step_routed()
+        np.testing.assert_array_equal(d.results()[0], lg)
+        assert torch.equal(mass, m), (spans, torch.nonzero(mass != m)[:5].tolist())
+    d.release()
