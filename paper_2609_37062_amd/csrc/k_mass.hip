@@ -182,10 +182,14 @@ __global__ __launch_bounds__(256) void k_mass_scores(AttnMassArgs a) {
     const float4 x = s_sum[i][lane];
     z[0] += x.x; z[1] += x.y; z[2] += x.z; z[3] += x.w;
   }
+  // (what the row does not see has no weight from it, also where the row's sum
+  // is not finite and 2^-infinity times it would be NaN)
   float* dst = a.mass + seq * a.stride + t;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (t + j < kv_len) dst[j] = (a.add != 0 ? dst[j] : 0.f) + (in ? z[j] : 0.f);
+  for (int j = 0; j < 4; ++j) {
+    const bool seen = t + j >= span.lo || t + j < a.sinks;
+    if (t + j < kv_len) dst[j] = (a.add != 0 ? dst[j] : 0.f) + (seen ? z[j] : 0.f);
+  }
 }
 
 constexpr int kMassCols = 32;  // columns of a tile

@@ -441,3 +441,26 @@ def test_a_query_that_is_not_a_number_stays_with_the_keys_it_sees(group, window,
         assert np.isfinite(m[~see]).all(), (r, np.flatnonzero(~np.isfinite(m) & ~see))
         assert np.isnan(m[see]).all(), r
     c.close()
+
+
+@pytest.mark.parametrize("window,sinks", [(40, 3), (17, 0), (5, 21)])
+@pytest.mark.parametrize("which", ["q", "K"])
+def test_single_tokens_whose_weights_are_not_numbers_leave_other_keys_alone(which, window, sinks):
+    """A query, or a key that it sees, is NaN: keys of the same blocks that the row does not see keep what they had."""
+    c = Cache(2, 3, 64, [97, 300, 16], seed=24)
+    c.batch(range(3), [1, 1, 1])
+    mass = torch.full((3, 300), 0.25, device="cuda")
+    if which == "q":
+        c.qd[:] = float("nan")
+    else:
+        for i, n in enumerate(c.lens):
+            c.K[0][i][n - 1] = np.nan
+            c.write(0, i)
+    for add in (True, False):
+        c.attend(window=window, sinks=sinks, mass=mass, add=add)
+        m = mass.cpu().numpy()
+        for i, n in enumerate(c.lens):
+            see = visible(n - 1, n, window, sinks)
+            assert (m[i, :n][~see] == (0.25 if add else 0.0)).all(), (i, np.flatnonzero(m[i, :n] != 0.25))
+            assert np.isnan(m[i, :n][see]).all() and (m[i, n:] == 0.25).all()
+    c.close()
