@@ -1377,7 +1377,19 @@ static AttnPlan plan_attn(Handle& h, const uint16_t* q, uint16_t* out, int out_R
   return p;
 }
 
-static hipError_t launch_attn(Handle& h, AttnPlan& p, int layer, const uint8_t* mask, LaunchEvents ev, hipStream_t s) {
+// The next pair of class `cls`'s probe events, while some remain (vsk_set_probe).
+static LaunchEvents next_probe(Handle& h, int cls) {
+  LaunchEvents ev;
+  if (h.probe_i[cls] < h.probe_b[cls].size()) {
+    ev.start = h.probe_b[cls][h.probe_i[cls]];
+    ev.stop = h.probe_e[cls][h.probe_i[cls]];
+    ++h.probe_i[cls];
+  }
+  return ev;
+}
+
+// probed: of a pass, whose decode attention is a class of the timing probes.
+static hipError_t launch_attn(Handle& h, AttnPlan& p, int layer, const uint8_t* mask, bool probed, hipStream_t s) {
   const BatchDev& b = h.bd;
   const int d = h.cfg.head_dim;
   hipError_t e;
@@ -1395,7 +1407,7 @@ static hipError_t launch_attn(Handle& h, AttnPlan& p, int layer, const uint8_t* 
     rows = b.n_rows;
   }
   if (rows == 0) return hipSuccess;
-  return launch_attn_decode(p.dec, rows, p.dec_splits, p.pfx_fold, s, ev, p.span);
+  return launch_attn_decode(p.dec, rows, p.dec_splits, p.pfx_fold, s, probed ? next_probe(h, 4) : LaunchEvents{}, p.span);
 }
 
 static hipError_t launch_mass(Handle& h, const AttnPlan& p, int layer, float* mass, int64_t stride, bool add,
@@ -1447,7 +1459,7 @@ static hipError_t launch_mass(Handle& h, const AttnPlan& p, int layer, float* ma
 hipError_t run_attend(Handle& h, int layer, const uint16_t* q, uint16_t* out, int window, int sinks, float* mass,
                       int64_t stride, bool add, hipStream_t s) {
   AttnPlan p = plan_attn(h, q, out, 0, h.ws, h.wl, h.bd.max_q_len == 1, window, sinks, mass != nullptr);
-  hipError_t e = launch_attn(h, p, layer, nullptr, {}, s);
+  hipError_t e = launch_attn(h, p, layer, nullptr, false, s);
   if (e == hipSuccess && mass != nullptr) e = launch_mass(h, p, layer, mass, stride, add, s);
   return e;
 }
@@ -1485,15 +1497,7 @@ hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
   // probed launch of kernel class `cls`: while probe events remain, the
   // launch takes the next pair, bound to its dispatch (the kernel's own start
   // and end times)
-  auto probed = [&](int cls, auto&& launch) -> hipError_t {
-    LaunchEvents ev;
-    if (h.probe_i[cls] < h.probe_b[cls].size()) {
-      ev.start = h.probe_b[cls][h.probe_i[cls]];
-      ev.stop = h.probe_e[cls][h.probe_i[cls]];
-      ++h.probe_i[cls];
-    }
-    return launch(ev);
-  };
+  auto probed = [&](int cls, auto&& launch) -> hipError_t { return launch(next_probe(h, cls)); };
 
   TRY(launch_embed_norm(reinterpret_cast<const uint16_t*>(P + h.pl.embed), pa.ids, R, H, c.vocab, x,
                         norm_gain(0, false), c.rms_eps, fb, Rg,
@@ -1616,7 +1620,7 @@ hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
       attn = plan_attn(h, q, fa, Rg, ws, wl, pa.logit_rows == nullptr, attn_span.window, attn_span.sinks,
                        h.mass != nullptr);
     }
-    TRY(probed(4, [&](LaunchEvents ev) { return launch_attn(h, attn, l, mask, ev, s); }));
+    TRY(launch_attn(h, attn, l, mask, true, s));
     if (h.mass != nullptr) TRY(launch_mass(h, attn, l, h.mass, h.mass_stride, true, s));
     // O projection: x += o Wo^T, then the MLP's RMSNorm
     ga.W = reinterpret_cast<const u4*>(L + h.pl.l.wo);

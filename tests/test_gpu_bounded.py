@@ -351,3 +351,25 @@ def test_project_only_rows_leave_no_weights_on_keys_that_are_not_finite(kind, ba
         np.testing.assert_array_equal(d.results()[0], lg)
         assert torch.equal(mass, m), (spans, torch.nonzero(mass != m)[:5].tolist())
     d.release()
+
+
+@pytest.mark.parametrize("window", [0, 9])
+def test_probes_of_decode_attention_wait_for_a_decode_kernel(window):
+    """A pass of prompt rows alone launches no decode attention: the next decode pass takes the pairs."""
+    from bench import HipEvents
+    w = mixed_workload(MID, 1, 33, [], seed=32, name="probe-prompt")
+    d = _run(w, pool_blocks=8, max_kv_len=64)
+    d.eng.set_span(-1, window, 0)
+    ev = HipEvents()
+    b, e = ev.create(3), ev.create(3)
+    d.eng.set_probe(4, b, e)
+    d.step()
+    d.eng.reserve(0, 1)
+    d.rebatch([0])
+    d.step()
+    torch.cuda.synchronize()
+    for l in range(MID.n_layers):
+        assert 0 < ev.elapsed_ms(b[l], e[l]) < 1000
+    d.eng.set_probe(4, [], [])
+    ev.destroy(b + e)
+    d.release()
