@@ -517,7 +517,9 @@ int vsk_residual_copy(vsk_handle* h, void* dst_dev, int32_t n_rows, void* stream
  * for attestation in tests and benchmarks.  Writes up to cap int64 values:
  * [0] passes run, [1] projection phases, [2] attention phases, [3] attention
  * splits (max per row), [4] workgroups per 16-column tile of the last down
- * projection, [5] 1 if the last pass ran as the persistent kernel, else 0. */
+ * projection, [5] 1 if the last pass ran as the persistent kernel, else 0,
+ * [6] workgroups that the weights per token of the last layer, or vsk_attend,
+ * that took them were launched as. */
 int vsk_exec_counters(const vsk_handle* h, int64_t* out, int32_t cap);
 
 /* Measurement: while buf_dev is set (NULL clears it), each persistent pass

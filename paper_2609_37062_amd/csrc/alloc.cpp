@@ -288,12 +288,19 @@ void plan_prefix_items(BatchHost& b, int32_t group_size, int32_t n_kv_heads, int
 void plan_prefill_items(BatchHost& b, int32_t group_size, int32_t block) {
   b.pre_items.clear();
   b.dec_rows.clear();
+  b.mass_tiles.clear();
+  b.max_single_len = 0;
   const int32_t per = std::max(1, kPreCols / group_size);
   for (int32_t i = 0; i < b.n_seqs; ++i) {
     const int32_t r0 = b.cu_q[i], r1 = b.cu_q[i + 1];
     if (r1 - r0 == 1) {
       b.dec_rows.push_back(r0);
+      b.max_single_len = std::max(b.max_single_len, b.kv_len[i]);
       continue;
+    }
+    for (int32_t t = 0; t < b.kv_len[i]; t += kMassTile) {
+      b.mass_tiles.push_back(i);
+      b.mass_tiles.push_back(t);
     }
     for (int32_t r = r0; r < r1; r += per) {
       const int32_t it[3] = {i, r, std::min(per, r1 - r)};

@@ -98,6 +98,10 @@ struct BatchHost {
   // blocks of the dec_rows' walks that an earlier one of them reads too: of
   // walks after the shared prefix, and of whole walks (count_reread_blocks)
   int64_t reread_own = 0, reread_all = 0;
+  // Keys of sequences of several rows, for the weights per token (plan_prefill_items)
+  std::vector<int32_t> mass_tiles;   // [n][2]: sequence, first key of a run of kMassTile
+  int32_t max_single_len = 0;        // the longest sequence of one row
+  int32_t n_mass_tiles() const { return static_cast<int32_t>(mass_tiles.size() / 2); }
   int32_t n_pre_items() const { return static_cast<int32_t>(pre_items.size() / 3); }
 };
 
@@ -107,7 +111,8 @@ struct BatchHost {
 // row of a decode pass) are listed for the decode attention, ordered by the
 // blocks each reads after its shared prefix, most first (ties in row order):
 // the decode grid dispatches its rows in that order, so the longest walks
-// start first instead of finishing last.
+// start first instead of finishing last.  The keys of the other sequences are
+// listed in runs of kMassTile.
 void plan_prefill_items(BatchHost& b, int32_t group_size, int32_t block);
 
 // Count the blocks that the walks of one-row sequences read again
@@ -119,6 +124,8 @@ void count_reread_blocks(const BlockAllocator& a, BatchHost& b);
 // each walked by two waves; of one prefill work item: 8 tiles of 16.
 constexpr int32_t kPfxCols = 64;
 constexpr int32_t kPreCols = 128;
+// Keys of a work item of the weights per token of a sequence of several rows.
+constexpr int32_t kMassTile = 128;
 // Most prefix splits of one group, and the largest split (blocks).
 constexpr int32_t kMaxPfxSplits = 16;
 constexpr int32_t kMaxPfxBps = 512;

@@ -410,7 +410,7 @@ static size_t meta_bytes(const BatchHost& b) {
   auto sz = [](const std::vector<int32_t>& v) { return align_up(std::max<size_t>(v.size(), 1) * 4); };
   return sz(b.block_table) + sz(b.kv_len) + sz(b.cu_q) + sz(b.row_seq) + sz(b.pos) + (b.evicted ? sz(b.rot) : 0) + sz(b.slot) +
          sz(b.pfx_blocks) + sz(b.pfx_splits) + sz(b.pfx_items) + sz(b.grp_rows) + sz(b.grp_info) + sz(b.pfx_tbl) +
-         sz(b.pre_items) + sz(b.dec_rows);
+         sz(b.pre_items) + sz(b.dec_rows) + (b.mass_tiles.empty() ? 0 : sz(b.mass_tiles));
 }
 
 size_t vsk_batch_device_bytes(const vsk_handle* h) {
@@ -482,6 +482,7 @@ int vsk_batch_upload(vsk_handle* h, void* meta_dev, size_t bytes, void* stream) 
   put(b.pfx_tbl, &d.pfx_tbl);
   put(b.pre_items, &d.pre_items);
   put(b.dec_rows, &d.dec_rows);
+  if (!b.mass_tiles.empty()) put(b.mass_tiles, &d.mass_tiles);
   d.n_pre_items = b.n_pre_items();
   d.n_dec_rows = static_cast<int32_t>(b.dec_rows.size());
   d.n_pfx_items = b.n_pfx_items();
@@ -1431,29 +1432,31 @@ static hipError_t launch_mass(Handle& h, const AttnPlan& p, int layer, float* ma
   m.mass = mass;
   m.stride = stride;
   m.add = add ? 1 : 0;
-  // sequences of several rows: their rows in so many parts that there are up to
-  // four workgroups a compute unit (777 rows over 2,300 tokens in 3, 4, 5, 7, 10
-  // parts of 200 workgroups each: 37, 34, 33, 35, 35 us, and the sum 4.5 to 6.7),
-  // in the space of the split partials, which are done with
   const BatchHost& bh = h.bh;
-  int64_t tiles = 0, singles = 0;
-  for (int32_t i = 0; i < bh.n_seqs; ++i) {
-    if (bh.cu_q[i + 1] - bh.cu_q[i] == 1) ++singles;
-    else tiles += (bh.kv_len[i] + kMassTile - 1) / kMassTile;
-  }
   m.scores = p.dec.scores;
   m.scores_len = p.dec.scores_len;
   m.rows = h.bd.dec_rows;
   m.n_rows = h.bd.n_dec_rows;
+  m.max_len = bh.max_single_len;
   m.row_seq = h.bd.row_seq;
   m.hd = h.cfg.head_dim;
+  // sequences of several rows: their rows in so many parts that there are up to
+  // four workgroups a compute unit (777 rows over 2,300 tokens in 3, 4, 5, 7, 10
+  // parts of 200 workgroups each: 37, 34, 33, 35, 35 us, and the sum 4.5 to 6.7),
+  // and none without a row, in the space of the split partials, which are done
+  // with and always hold one part: of a sequence of two rows at least, for 128
+  // keys each, head_dim floats a (row, query head)
+  m.tiles = h.bd.mass_tiles;
+  m.n_tiles = bh.n_mass_tiles();
   m.part = p.dec.part_o;
-  m.part_len = (h.bd.max_kv_len + kMassTile - 1) / kMassTile * kMassTile;
-  if (tiles > 0) {
-    const int64_t room = (p.part_bytes / 4) / (static_cast<int64_t>(m.Hkv) * bh.n_seqs * m.part_len);
-    m.parts = static_cast<int>(std::min<int64_t>({room, 16, std::max<int64_t>(1, 1024 / (tiles * m.Hkv))}));
+  if (m.n_tiles > 0) {
+    const int64_t wgs = static_cast<int64_t>(m.n_tiles) * m.Hkv;
+    const int64_t room = (p.part_bytes / 4) / (wgs * kMassTile);
+    const int row_tile = 32 / m.G;
+    m.parts = static_cast<int>(std::min<int64_t>(
+        {room, 16, std::max<int64_t>(1, 1024 / wgs), (h.bd.max_q_len + row_tile - 1) / row_tile}));
   }
-  return launch_attn_mass(m, h.bd.n_seqs, singles > 0, tiles > 0, h.bd.max_kv_len, h.cfg.head_dim, s);
+  return launch_attn_mass(m, h.cfg.head_dim, &h.counters[6], s);
 }
 
 hipError_t run_attend(Handle& h, int layer, const uint16_t* q, uint16_t* out, int window, int sinks, float* mass,

@@ -116,20 +116,22 @@ struct AttnMassArgs {
   float* mass;       // [n_seqs][stride]
   int64_t stride;
   int add;  // 0: mass = the weights, 1: mass += them
-  // sequences of several rows: their weights per (KV head, part of the rows)
-  // go to part [Hkv * parts][n_seqs][part_len] first, and are added up from
-  // there; 0 parts: taken as those of one row are
+  // sequences of several rows, in runs of kMassTile keys [n_tiles][2] (sequence,
+  // first key): their weights per (KV head, part of the rows) go to part
+  // [Hkv * parts][n_tiles][kMassTile] first, and are added up from there; 0
+  // parts: taken as those of one row are
+  const int32_t* tiles;
+  int n_tiles;
   float* part;
-  int parts, part_len;
+  int parts;
   // sequences of one row: their scores, as the attention left them (nullable:
-  // taken again), and the rows of that launch
+  // taken again), their rows, and the longest of them
   const float* scores;
   int64_t scores_len;
   const int32_t* rows;
-  int n_rows;
+  int n_rows, max_len;
   const int32_t* row_seq;
 };
-constexpr int kMassTile = 128;  // keys of a work item of such a sequence
 
 // Shared-prefix attention: each work item reads a run of a group's prefix
 // blocks once for up to kPfxCols (row, query head) columns of the group.
@@ -160,8 +162,7 @@ hipError_t launch_attn_prefix(const AttnPrefixArgs& a, int n_items, int head_dim
 hipError_t launch_attn_prefill(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s);
 // the general one of prompt rows (k_rows.hip)
 hipError_t launch_attn_rows(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s);
-// singles, several: the batch has sequences of one row, of several
-hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, bool singles, bool several, int max_kv_len, int head_dim,
-                            hipStream_t s);
+// *wgs: the workgroups that it launched
+hipError_t launch_attn_mass(const AttnMassArgs& a, int head_dim, int64_t* wgs, hipStream_t s);
 
 }  // namespace vsk

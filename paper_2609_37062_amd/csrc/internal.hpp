@@ -111,6 +111,7 @@ struct BatchDev {
   // prefill rows: causal work items, and the rows left to the decode kernel
   const int32_t* pre_items = nullptr;
   const int32_t* dec_rows = nullptr;
+  const int32_t* mass_tiles = nullptr;
   int32_t n_pre_items = 0, n_dec_rows = 0;
 };
 

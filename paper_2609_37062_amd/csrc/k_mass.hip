@@ -40,18 +40,19 @@ namespace vsk {
 
 constexpr int kMassWaves = 8;
 
-template <int D>
+// ROWS: of the listed rows, a sequence each; else of the listed tiles.
+template <int D, bool ROWS>
 __global__ __launch_bounds__(64 * kMassWaves) void k_attn_mass(AttnMassArgs a) {
   constexpr int KC = D / 32;
   __shared__ float s_sum[kMassWaves][32];
-  const int seq = blockIdx.y;
+  const int32_t* tile = a.tiles + 2 * (blockIdx.x / (kMassTile / 32));
+  const int seq = ROWS ? a.row_seq[a.rows[blockIdx.y]] : tile[0];
   const int kv_len = a.kv_len[seq];
-  const int t0 = 32 * blockIdx.x;
+  const int t0 = ROWS ? 32 * blockIdx.x : tile[1] + 32 * (blockIdx.x % (kMassTile / 32));
   if (t0 >= kv_len) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane & 15, quad = lane >> 4;
   const int r0 = a.cu_q[seq], n = a.cu_q[seq + 1] - r0;
-  if (n > 1 ? a.parts > 0 : a.scores != nullptr) return;  // k_mass_rows, k_mass_scores
   const int p0 = kv_len - n;  // position of the first row
   // the rows that see any of these keys: from position t0 on, and while the
   // window reaches back to key t0 + 31 (a sink key is seen by all of them)
@@ -208,12 +209,11 @@ __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
   __shared__ u32x4 s_q[kMassSlots][P / 4][kMassCols][4];
   __shared__ float2 s_ml[kMassSlots][4][kMassCols];  // (every wave its own)
   auto order = [](int c) { return c >> 2 & 3; };
-  const int seq = blockIdx.z;
+  // KV heads fastest: an XCD then keeps few heads' queries in its L2
+  const int hk = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv, part = blockIdx.y;
+  const int seq = a.tiles[2 * tile], t0 = a.tiles[2 * tile + 1];
   const int kv_len = a.kv_len[seq];
   const int r0 = a.cu_q[seq], n = a.cu_q[seq + 1] - r0;
-  // KV heads fastest: an XCD then keeps few heads' queries in its L2
-  const int hk = blockIdx.x % a.Hkv, t0 = kMassTile * static_cast<int>(blockIdx.x / a.Hkv), part = blockIdx.y;
-  if (t0 >= kv_len || n == 1) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lc = lane & 31, hi = lane >> 5, G = a.G;
   const int p0 = kv_len - n;  // position of the first row
@@ -352,18 +352,18 @@ __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
       y[r] = mine + shfl_xor(theirs, x);
     }
   y[0] += shfl_xor(y[0], 1);
-  if ((lane & 1) == 0)  // (part_len is a multiple of the tile)
-    a.part[(static_cast<size_t>(part * a.Hkv + hk) * gridDim.z + seq) * a.part_len + tw + 8 * hi + 16 * (lc >> 4) +
+  if ((lane & 1) == 0)  // (keys past the sequence's end have a place too)
+    a.part[(static_cast<size_t>(part * a.Hkv + hk) * a.n_tiles + tile) * kMassTile + 32 * w + 8 * hi + 16 * (lc >> 4) +
            (lane >> 1 & 7)] = y[0];
 }
 
-// mass = (or +=) the sum over KV heads and parts, of the sequences of several rows.
-__global__ __launch_bounds__(256) void k_mass_sum(AttnMassArgs a) {
-  const int seq = blockIdx.y, t = blockIdx.x * 256 + threadIdx.x;
-  if (a.cu_q[seq + 1] - a.cu_q[seq] == 1 || t >= a.kv_len[seq]) return;
+// mass = (or +=) the sum over KV heads and parts, a workgroup a tile.
+__global__ __launch_bounds__(kMassTile) void k_mass_sum(AttnMassArgs a) {
+  const int seq = a.tiles[2 * blockIdx.x], t = a.tiles[2 * blockIdx.x + 1] + threadIdx.x;
+  if (t >= a.kv_len[seq]) return;
   const int n = a.Hkv * a.parts;
-  const size_t next = static_cast<size_t>(gridDim.y) * a.part_len;
-  const float* p = a.part + static_cast<size_t>(seq) * a.part_len + t;
+  const size_t next = static_cast<size_t>(a.n_tiles) * kMassTile;
+  const float* p = a.part + static_cast<size_t>(blockIdx.x) * kMassTile + threadIdx.x;
   float* dst = a.mass + seq * a.stride + t;
   float y = 0.f;
   for (int i = 0; i < n; i += 8) {
@@ -377,26 +377,29 @@ __global__ __launch_bounds__(256) void k_mass_sum(AttnMassArgs a) {
 }
 
 template <int D>
-static hipError_t launch_mass_d(const AttnMassArgs& a, int n_seqs, bool singles, bool several, int max_kv_len,
-                                hipStream_t s) {
-  // (sequences of one row first: the scores lie where the others' parts go)
-  if (singles && a.scores != nullptr)
-    hipLaunchKernelGGL(k_mass_scores, dim3((max_kv_len + 255) / 256, a.n_rows), dim3(256), 0, s, a);
-  if ((singles && a.scores == nullptr) || (several && a.parts == 0))
-    hipLaunchKernelGGL((k_attn_mass<D>), dim3((max_kv_len + 31) / 32, n_seqs), dim3(64 * kMassWaves), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.parts == 0) return e;
-  hipLaunchKernelGGL((k_mass_rows<D>), dim3((max_kv_len + kMassTile - 1) / kMassTile * a.Hkv, a.parts, n_seqs), dim3(256),
-                     0, s, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(k_mass_sum, dim3((max_kv_len + 255) / 256, n_seqs), dim3(256), 0, s, a);
-  return hipGetLastError();
+static hipError_t launch_mass_d(const AttnMassArgs& a, int64_t* wgs, hipStream_t s) {
+  hipError_t e;
+  *wgs = 0;
+  auto launch = [&](auto kernel, dim3 grid, int threads) {
+    *wgs += static_cast<int64_t>(grid.x) * grid.y;
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
+    return hipGetLastError();
+  };
+  // sequences of one row first: the scores lie where the others' parts go
+  if (a.n_rows > 0) {
+    e = a.scores != nullptr ? launch(k_mass_scores, dim3((a.max_len + 255) / 256, a.n_rows), 256)
+                            : launch(k_attn_mass<D, true>, dim3((a.max_len + 31) / 32, a.n_rows), 64 * kMassWaves);
+    if (e != hipSuccess) return e;
+  }
+  if (a.n_tiles == 0) return hipSuccess;
+  if (a.parts == 0) return launch(k_attn_mass<D, false>, dim3(a.n_tiles * (kMassTile / 32)), 64 * kMassWaves);
+  if ((e = launch(k_mass_rows<D>, dim3(a.n_tiles * a.Hkv, a.parts), 256)) != hipSuccess) return e;
+  return launch(k_mass_sum, dim3(a.n_tiles), kMassTile);
 }
 
-hipError_t launch_attn_mass(const AttnMassArgs& a, int n_seqs, bool singles, bool several, int max_kv_len, int head_dim,
-                            hipStream_t s) {
-  if (head_dim == 128) return launch_mass_d<128>(a, n_seqs, singles, several, max_kv_len, s);
-  if (head_dim == 64) return launch_mass_d<64>(a, n_seqs, singles, several, max_kv_len, s);
+hipError_t launch_attn_mass(const AttnMassArgs& a, int head_dim, int64_t* wgs, hipStream_t s) {
+  if (head_dim == 128) return launch_mass_d<128>(a, wgs, s);
+  if (head_dim == 64) return launch_mass_d<64>(a, wgs, s);
   return hipErrorInvalidValue;
 }
 

@@ -464,3 +464,26 @@ def test_single_tokens_whose_weights_are_not_numbers_leave_other_keys_alone(whic
             assert (m[i, :n][~see] == (0.25 if add else 0.0)).all(), (i, np.flatnonzero(m[i, :n] != 0.25))
             assert np.isnan(m[i, :n][see]).all() and (m[i, n:] == 0.25).all()
     c.close()
+
+
+def test_weights_launch_what_there_is_to_sum():
+    """A short prompt beside long single tokens, and a long one beside short ones: a
+    tile of 128 keys a KV head and part for the prompts, 256 keys a workgroup for
+    the single tokens, and nothing for the others' lengths."""
+    def n_wgs(kv, group, lens, ql):
+        tiles = sum(-(-n // 128) for n, q in zip(lens, ql) if q > 1)
+        one = [n for n, q in zip(lens, ql) if q == 1]
+        rows = -(-max(ql) // (32 // group))
+        parts = min(16, max(1, 1024 // (tiles * kv)), rows)
+        return tiles * kv * parts + tiles + len(one) * -(-max(one) // 256)
+
+    for kv, group, lens, ql in [(4, 2, [100] + [3000 + 40 * i for i in range(24)], [20] + [1] * 24),
+                                (2, 3, [5000, 130] + [60 + i for i in range(20)], [3, 40] + [1] * 20)]:
+        c = Cache(kv, group, 128, lens, seed=25)
+        c.batch(range(len(lens)), ql)
+        mass = torch.zeros((len(lens), max(lens)), device="cuda")
+        for window, sinks in [(0, 0), (90, 5)]:
+            c.attend(window=window, sinks=sinks, mass=mass)
+            check(c, window, sinks, mass=mass)
+            assert c.eng.exec_counters()[6] == n_wgs(kv, group, lens, ql)
+        c.close()
