@@ -1449,7 +1449,9 @@ static hipError_t launch_mass(Handle& h, const AttnPlan& p, int layer, float* ma
   m.tiles = h.bd.mass_tiles;
   m.n_tiles = bh.n_mass_tiles();
   m.part = p.dec.part_o;
-  if (m.n_tiles > 0) {
+  // (rows attended one a work item have their scores from other products: taken
+  // again with those, and no parts)
+  if (m.n_tiles > 0 && p.prefill) {
     const int64_t wgs = static_cast<int64_t>(m.n_tiles) * m.Hkv;
     const int64_t room = (p.part_bytes / 4) / (wgs * kMassTile);
     const int row_tile = 32 / m.G;

@@ -119,6 +119,12 @@ typedef PTermsOf<kPTerms> PTerms;
 // without fmas); the others, which wait for memory, never do (8B at 37 rows of
 // 100-6,000 tokens 845, 850 and 846).
 constexpr float kRoundedScores = 0x1p23f;
+// The general walk of prompt rows and the weights per token, which take its
+// scores again, part at 2^14.  Each chooses by steps (tiles) of its own, so that a
+// weight may be taken with the one where the sum has the other: half an ulp
+// apart, there 2^-11 of an exponent and 2^-11.5 of a weight (at 2^23 it was up to
+// a fifth).  Above, both round alike, and what is below is all ordinary scores.
+constexpr float kSpanRounded = 0x1p14f;
 // S = K q of a step, the two groups of keys.
 template <int D>
 __device__ __forceinline__ void pair_qk(const u32x4 (&qf)[D / 32], const u32x4 (&kg)[2][D / 32], f32x4& s0, f32x4& s1) {

@@ -5,9 +5,10 @@
 //
 // with s the base-2 score and (m, 1 / l) what the attention of these rows left
 // for each (row, head).  Scores are taken again from K and q with the
-// attention's own products, so an exponent is exactly the one that the softmax
-// summed.  Every sum is taken in a fixed order: no atomics, so results do not
-// change from run to run.
+// attention's own products, or are its own, and exponents as it takes them: a
+// weight is the term that the softmax summed, to 2^-11 of it (kSpanRounded: an
+// exponent by a fma or rounded) and exactly at the largest scores.  Every sum is
+// taken in a fixed order: no atomics, so results do not change from run to run.
 //
 // k_attn_mass, for sequences of one row: a workgroup owns 32 keys of a sequence
 // and sums over every head and row, each wave a run of (KV head, 16-column tile)
@@ -305,7 +306,7 @@ __global__ __launch_bounds__(256, 3) void k_mass_rows(AttnMassArgs a) {
     scores(0);
     while (i < tiles) {
       // (a loop of its own, so that the sums stay where they are)
-      while (r_first + Rt * i >= f_from && r_first + Rt * i <= f_to && !__any(fabsf(ml.x) >= kRoundedScores)) {
+      while (r_first + Rt * i >= f_from && r_first + Rt * i <= f_to && !__any(fabsf(ml.x) >= kSpanRounded)) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[r] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[r], sc, -ml.x)), ml.y, acc[r]);
         if (++i == tiles) break;

@@ -314,7 +314,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
       l *= f;
 #pragma unroll
       for (int i = 0; i < OC; ++i) o[i] *= f;
-      big = __any(fabsf(m) >= kRoundedScores && m != -INFINITY);
+      big = __any(fabsf(m) >= kSpanRounded && m != -INFINITY);
     }
     next(step);
     rest(step, s, std::false_type{});

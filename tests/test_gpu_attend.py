@@ -487,3 +487,30 @@ def test_weights_launch_what_there_is_to_sum():
             check(c, window, sinks, mass=mass)
             assert c.eng.exec_counters()[6] == n_wgs(kv, group, lens, ql)
         c.close()
+
+
+@pytest.mark.parametrize("kind", ["one item a row", "few rows of a long cache", "chunk"])
+@pytest.mark.parametrize("scale", [2.0 ** 12, 2.0 ** 19, 2.0 ** 21, 2.0 ** 24])
+def test_weights_of_large_scores_come_to_one_a_head(kind, scale):
+    """Scores of four times the scale: from 2^23 on one rounding of a float32 score
+    is a factor of 2 or more in a weight.  The weights are terms of the attention's
+    own sums on every path: at most half an ulp of a score below 2^14 apart, 2^-11 in
+    the exponent, ln 2 of that in the weight (3.4e-4)."""
+    print(f"[gpu] large scores {kind} {scale}", flush=True)
+    if kind == "few rows of a long cache":
+        c = Cache(1, 1, 64, [16001, 15000, 16384, 16383], seed=26, scale=scale)
+        c.batch(range(4), [2, 1, 1, 1])
+    else:
+        c = Cache(2, 4, 128, [200, 90, 1000], seed=27, scale=scale)
+        if kind == "one item a row":
+            c.eng.set_tuning(6, 0)
+        c.batch([0, 1, 2], [40, 1, 30])
+    heads = c.kv * c.group
+    mass = torch.zeros((len(c.lens), max(c.lens)), device="cuda")
+    for window, sinks in [(0, 0), (30, 2), (700, 40)]:
+        c.attend(window=window, sinks=sinks, mass=mass)
+        assert np.isfinite(c.out()).all()
+        for i, ql in enumerate(c.q_lens):
+            m = mass[i, :c.lens[i]].double().cpu().numpy()
+            assert abs(m.sum() - ql * heads) < 5e-4 * ql * heads, (window, i, m.sum())
+    c.close()
