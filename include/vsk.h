@@ -519,7 +519,8 @@ int vsk_residual_copy(vsk_handle* h, void* dst_dev, int32_t n_rows, void* stream
  * splits (max per row), [4] workgroups per 16-column tile of the last down
  * projection, [5] 1 if the last pass ran as the persistent kernel, else 0,
  * [6] workgroups that the weights per token of the last layer, or vsk_attend,
- * that took them were launched as. */
+ * that took them were launched as, [7] attention plans of the last pass (one
+ * for each window and sinks of its layers; the persistent kernel makes none). */
 int vsk_exec_counters(const vsk_handle* h, int64_t* out, int32_t cap);
 
 /* Measurement: while buf_dev is set (NULL clears it), each persistent pass

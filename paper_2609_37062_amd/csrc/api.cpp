@@ -1153,6 +1153,7 @@ static hipError_t run_step(Handle& h, const PassArgs& pa, int n_wgs, hipStream_t
   h.counters[3] = a.max_splits;
   h.counters[4] = 1;
   h.counters[5] = 1;
+  h.counters[7] = 0;
   return hipSuccess;
 }
 
@@ -1526,10 +1527,15 @@ hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
   ga.out_Rg = Rg;
   ga.xcd_remap = h.xcd_remap;
 
-  // attention of layers that see every key, planned once; layers with a window
-  // have a plan of their own (the last one is kept, layers come in runs)
-  AttnPlan attn = plan_attn(h, q, fa, Rg, ws, wl, pa.logit_rows == nullptr, 0, 0, h.mass != nullptr);
-  Handle::Span attn_span;
+  // attention, planned once for every window and sinks of the pass's layers
+  std::vector<std::pair<Handle::Span, AttnPlan>> plans;
+  auto plan_of = [&](const Handle::Span& span) -> AttnPlan& {
+    for (auto& p : plans)
+      if (p.first.window == span.window && p.first.sinks == span.sinks) return p.second;
+    plans.emplace_back(span, plan_attn(h, q, fa, Rg, ws, wl, pa.logit_rows == nullptr, span.window, span.sinks,
+                                       h.mass != nullptr));
+    return plans.back().second;
+  };
 
   const int rt = h.resid_target;  // -1 no split, 0 the layout's default, else the target
   const GemmPlan p_qkv = plan_gemm(Nq + 2 * Nkv, H, R, EPI_QKV, h.gemm_shape, 0, h.row_tile);
@@ -1596,6 +1602,7 @@ hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
     return hipSuccess;
   };
   ga.X = reinterpret_cast<const u4*>(fb);
+  int max_splits = 1;
   for (int l = 0; l < n_run; ++l) {
     const uint8_t* L = P + h.pl.layer_bytes * l;
     const bool routed = l >= first_routed;
@@ -1620,11 +1627,8 @@ hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
     }
     // (a window that no row reaches the end of is none)
     const Handle::Span span = h.spans.empty() || h.spans[l].window >= b.max_kv_len ? Handle::Span{} : h.spans[l];
-    if (span.window != attn_span.window || span.sinks != attn_span.sinks) {
-      attn_span = span;
-      attn = plan_attn(h, q, fa, Rg, ws, wl, pa.logit_rows == nullptr, attn_span.window, attn_span.sinks,
-                       h.mass != nullptr);
-    }
+    AttnPlan& attn = plan_of(span);
+    max_splits = attn.dec.max_splits;
     TRY(launch_attn(h, attn, l, mask, true, s));
     if (h.mass != nullptr) TRY(launch_mass(h, attn, l, h.mass, h.mass_stride, true, s));
     // O projection: x += o Wo^T, then the MLP's RMSNorm
@@ -1726,9 +1730,10 @@ hipError_t run_pass(Handle& h, const PassArgs& pa, hipStream_t s) {
   h.counters[0] += 1;
   h.counters[1] += 4 * n_run + 1;
   h.counters[2] += n_run;
-  h.counters[3] = attn.dec.max_splits;
+  h.counters[3] = max_splits;
   h.counters[4] = p_d.n_groups;
   h.counters[5] = 0;
+  h.counters[7] = static_cast<int64_t>(plans.size());
   return hipSuccess;
 }
 

@@ -373,3 +373,27 @@ def test_probes_of_decode_attention_wait_for_a_decode_kernel(window):
     d.eng.set_probe(4, [], [])
     ev.destroy(b + e)
     d.release()
+
+
+@pytest.mark.parametrize("kind", ["decode", "mixed"])
+def test_alternating_windows_are_planned_once_each(kind, monkeypatch):
+    import dataclasses
+    m = dataclasses.replace(MID, name="bounded-5L", n_layers=5)
+    spans = [(30, 4), (0, 0), (30, 4), (0, 0), (100, 4)]
+    if kind == "decode":
+        w = decode_workload(m, [3, 40, 333], seed=33, name="alternate-decode")
+    else:
+        w = mixed_workload(m, 1, 70, [5, 200], seed=34, name="alternate-mixed")
+    d = _run(w)
+    for l, (window, sinks) in enumerate(spans):
+        d.eng.set_span(l, window, sinks)
+    d.step()
+    lg, ids = d.results()
+    assert d.eng.exec_counters()[7] == 3
+    monkeypatch.setattr(nm, "attend", Spanned(spans, w.n_rows * m.n_q_heads))
+    e2e_compare(w, lg, ids)
+    d.eng.set_span(-1, 30, 4)
+    d.step()
+    d.results()
+    assert d.eng.exec_counters()[7] == 1
+    d.release()
