@@ -261,7 +261,10 @@ int vsk_argmax_sample(const void* logits_dev, int32_t dtype, int32_t rows, int32
  * key t for query head h is w = exp(q_h . k_t / sqrt(head_dim)) over the sum
  * of that over the keys it sees; its output is sum w v_t.  What a row does not
  * see does not matter, NaN and infinities included; a value of a visible key
- * that is not finite makes the outputs that it enters not finite. */
+ * that is not finite makes the outputs that it enters not finite.  In the
+ * product with v, w is rounded to 16 bits (two bf16 terms) here, in a pass's
+ * layers that have a window, and in all of them while weights per token are
+ * set; to 24 in other passes. */
 
 /* Attention of the uploaded batch's rows (any q_lens) over one layer's cache,
  * for queries of the caller's: q_dev bf16 [n_rows][n_q_heads][head_dim], after

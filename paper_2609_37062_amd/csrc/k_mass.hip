@@ -17,6 +17,7 @@
 // key) beside 4 hd of K and V a (KV head, key), and k_mass_scores sums over
 // those instead: 32 sequences of 1,000-4,000 tokens (32/8 heads x 128) 32 us of
 // its own; with the scores the attention takes 60 instead of 54 and their sum 5.
+// (Prompt rows that are attended one a work item have theirs taken so too.)
 //
 // k_mass_rows, for sequences of several rows: a product of K with all the
 // queries that see it, 2 hd flops for each (row, head, key) where the attention
@@ -31,8 +32,11 @@
 // cached tokens (32/8 heads x 128): 196 us as k_attn_mass (every workgroup read
 // every query, 16 columns at a time), 41 with loads through registers and columns
 // that ran on over rows (139 vector operations a tile of 32 x 32, 48 of them the
-// exponentials), 33 so, and 4.5 for the sum.  64 keys a wave, which halve the
-// reads of LDS, took 36: two waves a SIMD hide less.
+// exponentials), 33 so, and 4.5 for the sum (30 and 4.6 among a thousand
+// calls).  64 keys a wave, which halve the reads of LDS, took 36: two waves a SIMD
+// hide less.  The grid is the list of the sequences' 128-key runs: as the longest
+// sequence times all of them, 20 rows of 100 tokens beside 64 single rows of up to
+// 16,000 launched a million workgroups for 128, 523 us a call against 445.
 #include <climits>
 
 #include "attn_core.hpp"

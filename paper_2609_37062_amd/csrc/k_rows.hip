@@ -32,7 +32,8 @@
 // scores in it, 103 with copies into LDS instead of loads and stores; 777 rows
 // after 2,300 tokens 92, 84 with the loop, 79, 72; 4 x 1,037 rows of 24/8 through
 // a window of 256, whose steps are mostly cut by a mask, 60, 45, 41, and 38 with
-// masks as bit inserts and finite V left as it is.  These MFMAs with the same
+// masks as bit inserts and finite V left as it is.  (Few calls at a time; among a
+// thousand 98, 63 and 37 now.)  These MFMAs with the same
 // vector operations between them and nothing else, no memory, would take 82 of
 // the 103: with all of them busy the chip runs 1.45 PFLOP/s.  One bf16 term a
 // weight would be a fifth faster, at errors of 2^-9 a weight.
@@ -434,10 +435,15 @@ __global__ __launch_bounds__(256) void k_rows_join(AttnPrefillArgs a) {
 }
 
 // Up to one work item a compute unit, eight waves each; beyond that two of four
-// waves, which wait for each other less often (2 x 2,000 fresh rows of 32/8
-// heads 133 and 120 us, 4 x 1,037 of 24/8 through a window of 256 58 and 41,
-// 3 x 1,500 of 8/8 42 and 49; 1,000 rows through 4,096 in 256 work items 117
-// and, one wave a SIMD, about twice that).
+// waves, which wait for each other less often.  Eight and four waves, us: 777
+// rows of 32/8 heads after 2,300 tokens (200 work items) 71 and 82, 1,000 through
+// a window of 4,096 (256) 116 and 129; 1,040 after 2,300 (264) 109 and 98, 1,500
+// (376) 128 and 122, 2,080 (520) 207 and 184, 2 x 2,000 fresh ones (1,008) 122 and
+// 101; through a window of 256 1,500 rows of 24/8 (288) 27 and 20, 4 x 1,037 (800)
+// 55 and 38; 34 prompts of 5 rows (272) 13 and 8.  Only fresh prompts without a
+// window, whose longest work items set the time, go the other way up to some 400
+// work items (3 x 1,500 of 8/8, 288: 40 and 46; 4 x 1,500, 384: 46 and 50; 480: 55
+// and 53): not told apart.
 template <int D>
 static void launch_rows_d(const AttnPrefillArgs& a, int n_items, hipStream_t s) {
   const int wgs = n_items * a.Hkv * a.splits;
