@@ -83,8 +83,8 @@ constexpr int kPTerms = 3;
 // The general walks (windows, sinks, weights per token) take two: 16 bits of a
 // probability, where the output that they end in keeps 8 (with three, single
 // tokens: 32 rows of 1,000-4,000 tokens with their weights 73 -> 77 us, 100 rows of
-// 64/8 heads through a window of 700 51 -> 59; prompt rows 8
-// MFMAs more a step of 24).
+// 64/8 heads through a window of 700 51 -> 59; prompt rows 8 MFMAs more a step of
+// 24).
 constexpr int kSpanPTerms = 2;
 template <int NT>
 struct PTermsOf {
