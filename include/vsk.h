@@ -21,8 +21,8 @@
  *    memory includes two pinned staging buffers for vsk_batch_upload.)
  *  - `stream` is a hipStream_t passed as void* (NULL = the null stream).
  *    Device work is enqueued asynchronously on it.  The calls that wait for
- *    the device are: vsk_weights_pack_head (setup; it waits for its rotary
- *    table copy), vsk_device_status (by definition), and vsk_batch_upload
+ *    the device are: vsk_weights_pack_head and vsk_rope_bind (setup; they wait
+ *    for their rotary table copies), vsk_device_status (by definition), and vsk_batch_upload
  *    only when the staging buffer it takes is still being read by the copy
  *    it issued two uploads earlier.  Nothing else synchronises.
  *  - bf16 tensors are IEEE bfloat16 bit patterns (uint16), row-major unless
@@ -49,6 +49,13 @@ enum {
   VSK_E_STATE = -5,        /* call out of order (unknown/duplicate sequence, nothing bound) */
   VSK_E_HIP = -6,          /* the HIP runtime reported an error */
   VSK_E_UNSUPPORTED = -7   /* shape the library has no kernel for */
+};
+
+/* Element types of the calls that take one. */
+enum {
+  VSK_BF16 = 0,
+  VSK_FP32 = 1,
+  VSK_MX4 = 2 /* a matrix in microscaled 4 bits (vsk_mx4_bytes) */
 };
 
 /* Model shape.  block_size must be 16; head_dim 64 or 128; n_q_heads a
@@ -315,6 +322,81 @@ int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host
                  int32_t sinks, int32_t recent, const float* mass_dev, int32_t mass_stride, float* mass_out_dev,
                  int32_t* kept_dev, int32_t* slots_dev, int32_t out_stride, void* meta_dev, size_t meta_bytes,
                  void* stream);
+
+/* ----------------------------------------------------------------- 4 bits
+ * Microscaled 4-bit floating point (the OCP format with e2m1 elements): 32
+ * consecutive values of a row share a power of two, 2^(floor(log2(largest
+ * magnitude)) - 2), at least 2^-127; each is rounded to the nearest of 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 times it, ties to the even code, beyond 6 to 6.  A row's last
+ * block may be shorter.  A block with a value that is not finite stands for NaNs.
+ *
+ * A matrix [rows][k] in that format ("MX4 matrix") is held in a layout of the
+ * library's own, in caller-owned device memory of vsk_mx4_bytes (0 for a bad
+ * shape), 256-byte aligned; rows and k from 1 to 2^30 (at most 2^31 tiles of 16 x
+ * 128).  It is either an activation (rows are the batch's) or a weight matrix
+ * [out][in].  These calls need no handle; VSK_E_ARG on a null pointer, a bad
+ * shape, type, stride (elements from row to row, at least a row) or alignment (to
+ * the element), or buffers that overlap.  Rows that are 16-byte aligned with k a
+ * multiple of 32 are taken with wide loads. */
+size_t vsk_mx4_bytes(int32_t rows, int32_t k);
+/* Quantise src_dev [rows][k] of VSK_BF16 or VSK_FP32. */
+int vsk_mx4_quantise(const void* src_dev, int32_t dtype, int64_t stride, int32_t rows, int32_t k, void* mx_dev,
+                     void* stream);
+/* From codes uint8 [rows][(k + 1) / 2] (sign, two exponent bits, one mantissa bit;
+ * the first value in the low half of a byte) and exponents uint8 [rows][(k + 31) /
+ * 32] (biased by 127, 255: NaN), as files hold them. */
+int vsk_mx4_pack(const uint8_t* codes_dev, const uint8_t* scales_dev, int32_t rows, int32_t k, void* mx_dev, void* stream);
+/* The values that a matrix stands for, VSK_BF16 (exact) or VSK_FP32. */
+int vsk_mx4_read(const void* mx_dev, int32_t rows, int32_t k, void* dst_dev, int32_t dtype, int64_t stride, void* stream);
+/* y[r][c] = (add[r][c] +) sum over i of x[r][i] w[c][i], for w an MX4 matrix [n][k]
+ * and x VSK_BF16 or VSK_FP32 [rows][k], which the call quantises first, or an MX4
+ * matrix (x_stride then counts for nothing).  Products are exact, sums float32, one
+ * rounding to y's type, VSK_BF16 or VSK_FP32.  add_dev (nullable) is of y's type
+ * and stride, and may be y_dev.  ws_dev: device scratch of at least
+ * vsk_mx4_product_bytes, 256-byte aligned (unused, and nullable, where x is MX4);
+ * concurrent calls need one each.  Can be captured. */
+size_t vsk_mx4_product_bytes(int32_t rows, int32_t n, int32_t k);
+int vsk_mx4_product(const void* x_dev, int32_t x_dtype, int64_t x_stride, const void* w_mx_dev, int32_t rows, int32_t n,
+                    int32_t k, void* y_dev, int32_t y_dtype, int64_t y_stride, const void* add_dev, void* ws_dev,
+                    size_t ws_bytes, void* stream);
+
+/* A KV cache in 4 bits: K and V of every token and head in that format, in blocks
+ * of 32 along the head's dims, 17/64 of the 16-bit cache's bytes.  It shares the
+ * handle's allocator: the same sequences, block tables, slots and batches, beside
+ * the 16-bit pool or instead of it (vsk_kv_init with a NULL pool).  The passes keep
+ * to the 16-bit pool, eviction (vsk_kv_evict) refuses a handle with a 4-bit one
+ * (VSK_E_UNSUPPORTED); the caller's own layers use it, with the calls below. */
+size_t vsk_kv4_pool_bytes(const vsk_model_cfg* cfg, int32_t n_blocks);
+/* Bind a pool, 256-byte aligned, for vsk_kv_init's n_blocks (NULL: none any more;
+ * vsk_kv_init unbinds it too). */
+int vsk_kv4_init(vsk_handle* h, void* pool_dev, size_t bytes);
+/* As vsk_kv_write and vsk_kv_read: logical bf16 k, v [n][n_kv_heads][head_dim] are
+ * quantised into their slots / the values that slots stand for. */
+int vsk_kv4_write(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_t n, const void* k_dev,
+                  const void* v_dev, void* stream);
+int vsk_kv4_read(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_t n, void* k_dev, void* v_dev,
+                 void* stream);
+/* vsk_attend over the 4-bit cache, without weights per token: K and V count as the
+ * values that they stand for (below 2^-126: maybe as zero). */
+int vsk_kv4_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev, int32_t window, int32_t sinks,
+                   void* ws_dev, size_t ws_bytes, void* stream);
+
+/* Rotary table of vsk_qkv_norm_rope, in caller-owned device memory (256-byte
+ * aligned, vsk_rope_bytes); waits for its copy, like vsk_weights_pack_head. */
+size_t vsk_rope_bytes(const vsk_handle* h);
+int vsk_rope_bind(vsk_handle* h, void* table_dev, size_t bytes, void* stream);
+/* From a QKV projection's rows to attention's inputs, for the rows of the uploaded
+ * batch: qkv_dev bf16 [n_rows] rows of n_q_heads query, n_kv_heads key and as many
+ * value heads (stride, a multiple of 8, from row to row).  Each query and key head
+ * x becomes x / sqrt(mean(x^2) + rms_eps) * gain (gains bf16 [head_dim]; NULL: no
+ * norm, no gain), then its dims j and j + head_dim/2 turn by pos * theta^(-2j /
+ * head_dim), pos the row's position.  Queries go to q_dev bf16
+ * [n_rows][n_q_heads][head_dim], keys and values to the rows' slots of `layer` in
+ * the 16-bit cache (cache_bits 16) or the 4-bit one (4).  One rounding each: to
+ * bf16, or from the exact key to 4 bits.  qkv and q are 16-byte aligned and must
+ * not overlap. */
+int vsk_qkv_norm_rope(vsk_handle* h, int32_t layer, const void* qkv_dev, int64_t stride, const void* q_gain_dev,
+                      const void* k_gain_dev, void* q_dev, int32_t cache_bits, void* stream);
 
 /* ----------------------------------------------------------------- routed mode
  * One routed layer per Algorithm 1 (Section 3.1, "Route-Guided Cohort

@@ -14,6 +14,7 @@
 #include "evict.hpp"
 #include "gemm.hpp"
 #include "internal.hpp"
+#include "kv4.hpp"
 #include "misc.hpp"
 #include "step.hpp"
 
@@ -278,6 +279,7 @@ int vsk_kv_init(vsk_handle* h, void* pool_dev, int32_t n_blocks) {
   if (n_blocks <= 0) return fail(h, VSK_E_ARG, "n_blocks must be positive");
   if (static_cast<int64_t>(n_blocks) * kBlock > INT32_MAX) return fail(h, VSK_E_ARG, "pool too large for int32 slots");
   h->pool = static_cast<uint16_t*>(pool_dev);
+  h->pool4 = nullptr;
   h->n_blocks = n_blocks;
   h->alloc = BlockAllocator(n_blocks, kBlock);
   h->alloc_ready = true;
@@ -793,10 +795,9 @@ int vsk_set_mass(vsk_handle* h, float* mass_dev, int32_t n_seqs, int32_t stride)
   return VSK_OK;
 }
 
-int vsk_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev, int32_t window, int32_t sinks,
-               float* mass_dev, int32_t mass_stride, int32_t mass_add, void* ws_dev, size_t ws_bytes, void* stream) {
-  if (!h) return VSK_E_ARG;
-  if (!h->pool) return fail(h, VSK_E_STATE, "no KV pool bound");
+// What a call of the caller's own queries over one layer's cache needs.
+static int attend_common(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev, int32_t window, int32_t sinks,
+                         void* ws_dev, size_t ws_bytes) {
   if (!h->batch_uploaded) return fail(h, VSK_E_STATE, "no batch uploaded");
   if (layer < 0 || layer >= h->cfg.n_layers) return fail(h, VSK_E_RANGE, "layer out of range");
   if (!q_dev || !o_dev || !ws_dev) return fail(h, VSK_E_ARG, "null buffer");
@@ -811,7 +812,24 @@ int vsk_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev, int
     return fail(h, VSK_E_ARG, "batch exceeds the workspace capacity");
   const size_t bytes = static_cast<size_t>(b.n_rows) * h->cfg.n_q_heads * h->cfg.head_dim * 2;
   if (overlap(q_dev, bytes, o_dev, bytes)) return fail(h, VSK_E_ARG, "q and o overlap");
+  return VSK_OK;
+}
+
+// A window that holds every cached token is none.
+static void span_clamp(const vsk_handle* h, int32_t& window, int32_t& sinks) {
+  if (window >= h->bd.max_kv_len) window = 0;  // every row sees every key before it
+  sinks = window == 0 ? 0 : std::min(sinks, h->bd.max_kv_len);
+}
+
+int vsk_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev, int32_t window, int32_t sinks,
+               float* mass_dev, int32_t mass_stride, int32_t mass_add, void* ws_dev, size_t ws_bytes, void* stream) {
+  if (!h) return VSK_E_ARG;
+  if (!h->pool) return fail(h, VSK_E_STATE, "no KV pool bound");
+  const int st = attend_common(h, layer, q_dev, o_dev, window, sinks, ws_dev, ws_bytes);
+  if (st != VSK_OK) return st;
+  const BatchDev& b = h->bd;
   if (mass_dev) {
+    const size_t bytes = static_cast<size_t>(b.n_rows) * h->cfg.n_q_heads * h->cfg.head_dim * 2;
     if (mass_stride < b.max_kv_len) return fail(h, VSK_E_ARG, "mass rows shorter than the longest sequence");
     if (mass_add != 0 && mass_add != 1) return fail(h, VSK_E_ARG, "mass_add must be 0 or 1");
     if (reinterpret_cast<uintptr_t>(mass_dev) % 4) return fail(h, VSK_E_ARG, "mass not 4-byte aligned");
@@ -819,11 +837,151 @@ int vsk_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev, int
     if (overlap(mass_dev, mass_bytes, q_dev, bytes) || overlap(mass_dev, mass_bytes, o_dev, bytes))
       return fail(h, VSK_E_ARG, "mass overlaps q or o");
   }
-  if (window >= b.max_kv_len) window = 0;  // every row sees every key before it
-  sinks = window == 0 ? 0 : std::min(sinks, b.max_kv_len);
+  span_clamp(h, window, sinks);
   return hip_check(h, run_attend(*h, layer, static_cast<const uint16_t*>(q_dev), static_cast<uint16_t*>(o_dev), window,
-                                 sinks, mass_dev, mass_stride, mass_add != 0, static_cast<hipStream_t>(stream)),
+                                 sinks, mass_dev, mass_stride, mass_add != 0, false, static_cast<hipStream_t>(stream)),
                    "attend");
+}
+
+// ------------------------------------------------------------------ 4-bit cache
+size_t vsk_kv4_pool_bytes(const vsk_model_cfg* cfg, int32_t n_blocks) {
+  std::string why;
+  if (!cfg_ok(cfg, why) || n_blocks <= 0) return 0;
+  return static_cast<size_t>(cfg->n_layers) * n_blocks * cfg->n_kv_heads * kv4_record(cfg->head_dim);
+}
+
+int vsk_kv4_init(vsk_handle* h, void* pool_dev, size_t bytes) {
+  NEED_ALLOC(h);
+  if (!pool_dev) {
+    h->pool4 = nullptr;
+    return VSK_OK;
+  }
+  if (reinterpret_cast<uintptr_t>(pool_dev) % kAlign) return fail(h, VSK_E_ARG, "4-bit pool not aligned");
+  if (bytes < vsk_kv4_pool_bytes(&h->cfg, h->n_blocks)) return fail(h, VSK_E_ARG, "4-bit pool smaller than vsk_kv4_pool_bytes()");
+  h->pool4 = static_cast<uint8_t*>(pool_dev);
+  return VSK_OK;
+}
+
+static int kv4_move(vsk_handle* h, bool write, int32_t layer, const int32_t* slots, int32_t n, const void* k,
+                    const void* v, void* stream) {
+  if (!h) return VSK_E_ARG;
+  if (!h->pool4) return fail(h, VSK_E_STATE, "no 4-bit KV pool bound");
+  if (layer < 0 || layer >= h->cfg.n_layers) return fail(h, VSK_E_RANGE, "layer out of range");
+  if (n < 0 || (n > 0 && (!slots || !k || !v))) return fail(h, VSK_E_ARG, "bad KV transfer arguments");
+  if (reinterpret_cast<uintptr_t>(slots) % 4 || reinterpret_cast<uintptr_t>(k) % 2 || reinterpret_cast<uintptr_t>(v) % 2)
+    return fail(h, VSK_E_ARG, "buffer not aligned to its elements");
+  const Kv4Pool p{h->pool4, layer, h->n_blocks, h->cfg.n_kv_heads};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e =
+      write ? launch_kv4_write(p, h->cfg.head_dim, slots, n, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), s)
+            : launch_kv4_read(p, h->cfg.head_dim, slots, n, static_cast<uint16_t*>(const_cast<void*>(k)),
+                              static_cast<uint16_t*>(const_cast<void*>(v)), s);
+  return hip_check(h, e, "4-bit kv transfer");
+}
+
+int vsk_kv4_write(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_t n, const void* k_dev,
+                  const void* v_dev, void* stream) {
+  return kv4_move(h, true, layer, slots_dev, n, k_dev, v_dev, stream);
+}
+
+int vsk_kv4_read(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_t n, void* k_dev, void* v_dev,
+                 void* stream) {
+  return kv4_move(h, false, layer, slots_dev, n, k_dev, v_dev, stream);
+}
+
+int vsk_kv4_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev, int32_t window, int32_t sinks,
+                   void* ws_dev, size_t ws_bytes, void* stream) {
+  if (!h) return VSK_E_ARG;
+  if (!h->pool4) return fail(h, VSK_E_STATE, "no 4-bit KV pool bound");
+  const int st = attend_common(h, layer, q_dev, o_dev, window, sinks, ws_dev, ws_bytes);
+  if (st != VSK_OK) return st;
+  span_clamp(h, window, sinks);
+  return hip_check(h, run_attend(*h, layer, static_cast<const uint16_t*>(q_dev), static_cast<uint16_t*>(o_dev), window,
+                                 sinks, nullptr, 0, false, true, static_cast<hipStream_t>(stream)),
+                   "attend");
+}
+
+// ------------------------------------------------------------------ QKV rows into a cache
+size_t vsk_rope_bytes(const vsk_handle* h) {
+  return h ? static_cast<size_t>(h->cfg.max_pos) * (h->cfg.head_dim / 2) * 2 * sizeof(float2) : 0;
+}
+
+int vsk_rope_bind(vsk_handle* h, void* table_dev, size_t bytes, void* stream) {
+  if (!h) return VSK_E_ARG;
+  if (!table_dev || bytes < vsk_rope_bytes(h)) return fail(h, VSK_E_ARG, "rotary table smaller than vsk_rope_bytes()");
+  if (reinterpret_cast<uintptr_t>(table_dev) % kAlign) return fail(h, VSK_E_ARG, "rotary table not aligned");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  int st = hip_check(h, hipStreamIsCapturing(s, &cap), "rotary table");
+  if (st != VSK_OK) return st;
+  if (cap != hipStreamCaptureStatusNone) return fail(h, VSK_E_STATE, "the rotary table cannot be bound in a capture");
+  const vsk_model_cfg& c = h->cfg;
+  const int half = c.head_dim / 2;
+  const size_t n = static_cast<size_t>(c.max_pos) * half;
+  std::vector<float2> tab;
+  try {
+    tab.resize(2 * n);
+  } catch (const std::bad_alloc&) {
+    return fail(h, VSK_E_ARG, "no host memory for the rotary table");
+  }
+  // (cos, sin) of pos * theta^(-2j/d) as float, and what the floats leave of the doubles
+  for (int j = 0; j < half; ++j) {
+    const double inv = std::pow(static_cast<double>(c.rope_theta), -2.0 * j / c.head_dim);
+    for (int p = 0; p < c.max_pos; ++p) {
+      const double x = std::cos(p * inv), y = std::sin(p * inv);
+      const float2 f = make_float2(static_cast<float>(x), static_cast<float>(y));
+      tab[static_cast<size_t>(p) * half + j] = f;
+      tab[n + static_cast<size_t>(p) * half + j] = make_float2(static_cast<float>(x - f.x), static_cast<float>(y - f.y));
+    }
+  }
+  st = hip_check(h, hipMemcpyAsync(table_dev, tab.data(), tab.size() * sizeof(float2), hipMemcpyHostToDevice, s), "copy rotary table");
+  if (st == VSK_OK) st = hip_check(h, hipStreamSynchronize(s), "sync");
+  if (st == VSK_OK) h->rope = static_cast<float2*>(table_dev);
+  return st;
+}
+
+int vsk_qkv_norm_rope(vsk_handle* h, int32_t layer, const void* qkv_dev, int64_t stride, const void* q_gain_dev,
+                      const void* k_gain_dev, void* q_dev, int32_t cache_bits, void* stream) {
+  if (!h) return VSK_E_ARG;
+  if (cache_bits != 16 && cache_bits != 4) return fail(h, VSK_E_ARG, "cache_bits must be 16 or 4");
+  if (cache_bits == 16 && !h->pool) return fail(h, VSK_E_STATE, "no KV pool bound");
+  if (cache_bits == 4 && !h->pool4) return fail(h, VSK_E_STATE, "no 4-bit KV pool bound");
+  if (!h->rope) return fail(h, VSK_E_STATE, "no rotary table bound");
+  if (!h->batch_uploaded) return fail(h, VSK_E_STATE, "no batch uploaded");
+  if (layer < 0 || layer >= h->cfg.n_layers) return fail(h, VSK_E_RANGE, "layer out of range");
+  if (!qkv_dev || !q_dev) return fail(h, VSK_E_ARG, "null buffer");
+  const vsk_model_cfg& c = h->cfg;
+  const BatchDev& b = h->bd;
+  const int64_t width = static_cast<int64_t>(c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim;
+  if (stride < width || stride % 8) return fail(h, VSK_E_ARG, "stride must be a multiple of 8, of a row at least");
+  if (stride > INT64_MAX / 4 / b.n_rows) return fail(h, VSK_E_ARG, "stride too large");
+  if (reinterpret_cast<uintptr_t>(qkv_dev) % 16 || reinterpret_cast<uintptr_t>(q_dev) % 16)
+    return fail(h, VSK_E_ARG, "qkv and q must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(q_gain_dev) % 2 || reinterpret_cast<uintptr_t>(k_gain_dev) % 2)
+    return fail(h, VSK_E_ARG, "gain not 2-byte aligned");
+  if (b.max_position >= c.max_pos) return fail(h, VSK_E_RANGE, "position beyond max_pos");
+  const size_t in = ((static_cast<size_t>(b.n_rows) - 1) * stride + width) * 2;
+  const size_t out = static_cast<size_t>(b.n_rows) * c.n_q_heads * c.head_dim * 2;
+  if (overlap(qkv_dev, in, q_dev, out)) return fail(h, VSK_E_ARG, "qkv and q overlap");
+  QkvArgs a{};
+  a.qkv = static_cast<const uint16_t*>(qkv_dev);
+  a.stride = stride;
+  a.R = b.n_rows;
+  a.Hq = c.n_q_heads;
+  a.Hkv = c.n_kv_heads;
+  a.q_gain = static_cast<const uint16_t*>(q_gain_dev);
+  a.k_gain = static_cast<const uint16_t*>(k_gain_dev);
+  a.eps = c.rms_eps;
+  a.rot = b.rot;
+  a.slot = b.slot;
+  a.rope = h->rope;
+  a.max_pos = c.max_pos;
+  a.q = static_cast<uint16_t*>(q_dev);
+  a.pool = cache_bits == 16 ? h->pool : nullptr;
+  a.pool4 = cache_bits == 4 ? h->pool4 : nullptr;
+  a.layer = layer;
+  a.n_blocks = h->n_blocks;
+  return hip_check(h, launch_qkv_norm_rope(a, c.head_dim, static_cast<hipStream_t>(stream)), "qkv norm and rotation");
 }
 
 // Device metadata of an eviction: [n][4] (length, kept, first source block,
@@ -856,6 +1014,7 @@ int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host
                  void* stream) {
   NEED_ALLOC(h);
   if (!h->pool) return fail(h, VSK_E_STATE, "no KV pool bound");
+  if (h->pool4) return fail(h, VSK_E_UNSUPPORTED, "the 4-bit cache has no eviction");
   if (!dst_host || !src_host || !keep_host || n < 1) return fail(h, VSK_E_ARG, "empty eviction");
   if (n > 65535) return fail(h, VSK_E_ARG, "at most 65535 sequences a call");
   if (!mass_dev || !kept_dev || !meta_dev) return fail(h, VSK_E_ARG, "null buffer");
@@ -1463,8 +1622,10 @@ static hipError_t launch_mass(Handle& h, const AttnPlan& p, int layer, float* ma
 }
 
 hipError_t run_attend(Handle& h, int layer, const uint16_t* q, uint16_t* out, int window, int sinks, float* mass,
-                      int64_t stride, bool add, hipStream_t s) {
-  AttnPlan p = plan_attn(h, q, out, 0, h.ws, h.wl, h.bd.max_q_len == 1, window, sinks, mass != nullptr);
+                      int64_t stride, bool add, bool four, hipStream_t s) {
+  // (the 4-bit cache has no walk of shared prefixes)
+  AttnPlan p = plan_attn(h, q, out, 0, h.ws, h.wl, !four && h.bd.max_q_len == 1, window, sinks, mass != nullptr);
+  if (four) p.dec.pool4 = p.pre.pool4 = h.pool4;
   hipError_t e = launch_attn(h, p, layer, nullptr, false, s);
   if (e == hipSuccess && mass != nullptr) e = launch_mass(h, p, layer, mass, stride, add, s);
   return e;

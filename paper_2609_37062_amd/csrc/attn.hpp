@@ -74,6 +74,7 @@ struct AttnArgs {
   // key of the row's SpanWalk list, -inf where the row does not see it
   float* scores;
   int64_t scores_len;
+  const uint8_t* pool4;  // general walks over the 4-bit cache (nullable: `pool`)
 };
 
 // Causal attention of prefill rows (see k_attn_prefill).
@@ -99,6 +100,7 @@ struct AttnPrefillArgs {
   int splits;
   float* part_o;
   float2* part_ml;
+  const uint8_t* pool4;  // as in AttnArgs
 };
 
 // Attention weight per key (see k_attn_mass).

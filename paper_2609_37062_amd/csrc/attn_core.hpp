@@ -26,7 +26,8 @@
 #include <type_traits>
 
 #include "attn.hpp"
-#include "dev.hpp"
+#include "kv4.hpp"
+#include "mx4_dev.hpp"
 
 namespace vsk {
 
@@ -284,6 +285,68 @@ __device__ __forceinline__ void pair_pv(u32x4 (&vt)[D / 16], int t0, int t_end, 
   pair_pv_add<D>(vt, pp, alpha, o);
 }
 
+// ---- the same steps over the 4-bit cache (kv4.hpp).  What a lane loads of a step's
+// two blocks: its tokens' K codes of both groups (a quarter of the dims, so that one
+// exponent a group does), and the V codes of its eight tokens with theirs.  K and V
+// become bf16 in registers (4-bit values are exact there), 64 conversions a step at
+// D = 128, and everything behind is the 16-bit walk's.
+template <int D>
+struct Kv4Pair {
+  u32x4 k[D / 64], v[D / 64], vs[D / 64];
+  uint32_t ks;
+};
+template <int D, bool NTKV>
+__device__ __forceinline__ void kv4_load(Kv4Pair<D>& x, const uint8_t* rec_k, const uint8_t* rec_v, int lane) {
+  const int quad = lane >> 4, i = lane & 15, th = quad & 1;
+  auto ld = [](const uint8_t* p) {
+    const u32x4* q = reinterpret_cast<const u32x4*>(p);
+    return NTKV ? __builtin_nontemporal_load(q) : *q;
+  };
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j) {
+    x.k[j] = ld(rec_k + 16 * ((i & 7) + D / 8 * quad + 8 * j));
+    x.v[j] = ld(rec_v + kv4_v_at(D) + 16 * (i + 16 * th + 32 * j));
+    x.vs[j] = *reinterpret_cast<const u32x4*>(rec_v + kv4_vs_at(D) + D / 4 * th + 16 * j);
+  }
+  x.ks = *reinterpret_cast<const uint16_t*>(rec_k + kv4_ks_at(D) + 2 * ((i & 7) + 8 * (D == 128 ? quad : quad >> 1)));
+}
+// The exponent in byte b of s as a scale: the conversions look at bits 30..23 only.
+__device__ __forceinline__ float kv4_scale(uint32_t s, int b) {
+  return __uint_as_float(b == 3 ? s >> 1 : s << (23 - 8 * b));
+}
+template <int D>
+__device__ __forceinline__ void kv4_expand_k(const Kv4Pair<D>& x, u32x4 (&kg)[2][D / 32]) {
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      const uint32_t codes = D == 128 ? x.k[g * (D / 64) / 2][c] : x.k[0][2 * g + (c & 1)];
+      kg[g][c] = mx4_decode8(codes, kv4_scale(x.ks, g));
+    }
+}
+// A token's byte b as two dims, 32 b + d and 32 b + 16 + d.
+template <int D>
+__device__ __forceinline__ uint32_t kv4_v_dims(const u32x4 (&v)[D / 64], const u32x4 (&vs)[D / 64], int t, int b) {
+  const uint32_t w = D == 128 ? v[t / 4 * (D / 128)][t & 3] : v[0][t >> 1];
+  const uint32_t s = D == 128 ? vs[t / 4 * (D / 128)][t & 3] : vs[0][t >> 1];
+  const int at = D == 128 ? b : 2 * (t & 1) + b;
+  const float sc = kv4_scale(s, at);
+  return at == 0 ? mx4_decode<0>(w, sc) : at == 1 ? mx4_decode<1>(w, sc) : at == 2 ? mx4_decode<2>(w, sc) : mx4_decode<3>(w, sc);
+}
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+template <int D>
+__device__ __forceinline__ void kv4_expand_v(const Kv4Pair<D>& x, u32x4 (&vt)[D / 16]) {
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t t0 = kv4_v_dims<D>(x.v, x.vs, 2 * j, b), t1 = kv4_v_dims<D>(x.v, x.vs, 2 * j + 1, b);
+      vt[2 * b][j] = low_halves(t0, t1);
+      vt[2 * b + 1][j] = high_halves(t0, t1);
+    }
+}
+
 // WT: the attention output is stored write-through (sc1), so that other
 // workgroups of the same launch read it from memory, not from a stale L2.
 // FOLD2: a wave loads two shared-prefix partials before folding either (one
@@ -292,8 +355,9 @@ __device__ __forceinline__ void pair_pv(u32x4 (&vt)[D / 16], int t0, int t_end, 
 // SPAN: the general walk (AttnArgs::window, sinks, ml, row-major output): the
 // wave's blocks are a run of the row's SpanWalk list, and a step is full
 // where both of its blocks are visible whole.
+// Q4: over the 4-bit cache (a general walk without scores or shared prefixes).
 // launch_row: the row's place in the launch, for its scores.
-template <int D, bool WT, int NW, bool FOLD2 = false, bool NTKV = true, bool SPAN = false>
+template <int D, bool WT, int NW, bool FOLD2 = false, bool NTKV = true, bool SPAN = false, bool Q4 = false>
 __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, int split, AttnLds<D, NW>& sm,
                                           int launch_row = 0) {
   constexpr int KC = D / 32;  // K chunks (1 KiB) per block
@@ -350,7 +414,8 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
     const uint16_t* qrow = a.q + static_cast<size_t>(row) * a.Nq + static_cast<size_t>(hk * G + h) * D;
 #pragma unroll
     for (int c = 0; c < KC; ++c)
-      qf[c] = (h < G) ? *reinterpret_cast<const u32x4*>(qrow + 32 * c + 8 * quad) : u32x4{0u, 0u, 0u, 0u};
+      qf[c] = (h < G) ? *reinterpret_cast<const u32x4*>(qrow + (Q4 ? D / 4 * quad + 8 * c : 32 * c + 8 * quad))
+                      : u32x4{0u, 0u, 0u, 0u};
   }
   const float sc = a.scale_log2;  // log2(e) / sqrt(D)
   float m = -INFINITY, l = 0.f;
@@ -396,6 +461,15 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
     for (int c = 0; c < VC; ++c) vt[c] = kv(vp + c * 32);
   };
 
+  Kv4Pair<D> raw;
+  auto load_raw = [&](int p, int cnt, int w_lo) {
+    size_t bA, bB;
+    pair_blocks(p, cnt, w_lo, bA, bB);
+    const uint8_t* base = a.pool4 + (static_cast<size_t>(a.layer) * a.n_blocks * a.Hkv + hk) * kv4_record(D);
+    auto rec = [&](bool second) { return base + (second ? bB : bA) * (a.Hkv * kv4_record(D)); };
+    kv4_load<D, NTKV>(raw, rec(pair_k_block(lane)), rec(pair_v_block(lane)), lane);
+  };
+
   __syncthreads();  // sm.tbl
   // this wave's blocks: a contiguous range of the split, taken two at a time.
   // One pair's K and V live in registers: the next pair's K is loaded as soon
@@ -411,8 +485,12 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   u32x4 kg[2][KC];
   u32x4 vt[VC], vt2[VC];  // V of the even and the odd pairs
   if (cnt > 0) {
-    load_k(kg, 0, cnt, w_lo);
-    load_v(vt, 0, cnt, w_lo);
+    if constexpr (Q4) {
+      load_raw(0, cnt, w_lo);
+    } else {
+      load_k(kg, 0, cnt, w_lo);
+      load_v(vt, 0, cnt, w_lo);
+    }
   }
   // the first split starts from the group's shared-prefix partials: wave w
   // folds in partials w, w + NW, ... (their loads wait behind the K/V loads
@@ -470,6 +548,10 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
                    ? span_bits(kBlock * (quad >> 1 ? bb : ba) + 8 * (quad & 1), kv_len, span.lo, a.sinks)
                    : 0u;
       f32x4 s0, s1;
+      if constexpr (Q4) {
+        kv4_expand_k<D>(raw, kg);
+        kv4_expand_v<D>(raw, vc);
+      }
       pair_qk<D>(qf, kg, s0, s1);
       if (!full) span_mask(bits, s0, s1);
       if (a.scores != nullptr && h < G && 2 * p + (quad >> 1) < cnt) {  // (16 bytes to 4 floats each)
@@ -481,8 +563,12 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
       PTermsOf<kSpanPTerms> pp;
       pair_softmax<false>(s0, s1, sc, m, l, pp, alpha);
       if constexpr (!LAST) {
-        load_k(kg, p + 1, cnt, w_lo);
-        load_v(vn, p + 1, cnt, w_lo);
+        if constexpr (Q4) {
+          load_raw(p + 1, cnt, w_lo);
+        } else {
+          load_k(kg, p + 1, cnt, w_lo);
+          load_v(vn, p + 1, cnt, w_lo);
+        }
       }
       if (!full) span_zero_v<D>(vc, bits);
       pair_pv_add<D>(vc, pp, alpha, o);

@@ -166,6 +166,8 @@ struct Handle {
   PackedLayout pl;
   // kv
   uint16_t* pool = nullptr;
+  uint8_t* pool4 = nullptr;  // the 4-bit one (kv4.hpp)
+  float2* rope = nullptr;    // rotary table of vsk_rope_bind
   int32_t n_blocks = 0;
   BlockAllocator alloc;
   bool alloc_ready = false;
@@ -265,9 +267,9 @@ struct PassArgs {
 };
 hipError_t run_pass(Handle& h, const PassArgs& a, hipStream_t s);
 // One layer's attention of the uploaded batch for given queries, row-major, with
-// the bound workspace (mass nullable).
+// the bound workspace (mass nullable).  four: over the 4-bit cache, without mass.
 hipError_t run_attend(Handle& h, int layer, const uint16_t* q, uint16_t* out, int window, int sinks, float* mass,
-                      int64_t stride, bool add, hipStream_t s);
+                      int64_t stride, bool add, bool four, hipStream_t s);
 // True when run_pass would take the persistent step kernel for this pass.
 bool step_eligible(Handle& h, const PassArgs& a);
 

@@ -38,7 +38,7 @@ constexpr int kPreTiles = kPreCols / 16;   // 16-column tiles (one wave each) of
 // General walks: grid (KV head, row, split), longest row first, with a row's
 // splits even; where all of them are at most one a compute unit, and the grid
 // would be more (rows of different lengths), packed: (KV head, split of any row).
-template <int D, bool FOLD2, bool NTKV, bool SPAN>
+template <int D, bool FOLD2, bool NTKV, bool SPAN, bool Q4>
 __global__ __launch_bounds__(64 * kAttnWaves) void k_attn_decode(AttnArgs a) {
   __shared__ AttnLds<D, kAttnWaves> sm;
   if constexpr (!SPAN) {
@@ -67,21 +67,24 @@ __global__ __launch_bounds__(64 * kAttnWaves) void k_attn_decode(AttnArgs a) {
       r = __builtin_ctzll(behind);
       split = blockIdx.y - __builtin_amdgcn_readlane(end - n, r);
     }
-    attn_unit<D, false, kAttnWaves, FOLD2, NTKV, SPAN>(a, a.rows != nullptr ? a.rows[r] : r, blockIdx.x, split, sm, r);
+    attn_unit<D, false, kAttnWaves, FOLD2, NTKV, SPAN, Q4>(a, a.rows != nullptr ? a.rows[r] : r, blockIdx.x, split, sm, r);
   }
 }
 
-template <int D, bool FOLD2, bool NTKV, bool SPAN>
+template <int D, bool FOLD2, bool NTKV, bool SPAN, bool Q4 = false>
 static void launch_decode_k(const AttnArgs& a, dim3 grid, hipStream_t s, const LaunchEvents& ev) {
   if (ev.start != nullptr || ev.stop != nullptr)  // events bound to this dispatch
-    hipExtLaunchKernelGGL((k_attn_decode<D, FOLD2, NTKV, SPAN>), grid, dim3(64 * kAttnWaves), 0u, s, ev.start, ev.stop, 0u, a);
+    hipExtLaunchKernelGGL((k_attn_decode<D, FOLD2, NTKV, SPAN, Q4>), grid, dim3(64 * kAttnWaves), 0u, s, ev.start, ev.stop, 0u, a);
   else
-    hipLaunchKernelGGL((k_attn_decode<D, FOLD2, NTKV, SPAN>), grid, dim3(64 * kAttnWaves), 0, s, a);
+    hipLaunchKernelGGL((k_attn_decode<D, FOLD2, NTKV, SPAN, Q4>), grid, dim3(64 * kAttnWaves), 0, s, a);
 }
 
 template <int D>
 static void launch_decode_d(const AttnArgs& a, dim3 grid, bool fold2, bool span, hipStream_t s, const LaunchEvents& ev) {
-  if (span) {
+  if (a.pool4 != nullptr) {
+    if (a.kv_once != 0) launch_decode_k<D, false, true, true, true>(a, grid, s, ev);
+    else launch_decode_k<D, false, false, true, true>(a, grid, s, ev);
+  } else if (span) {
     if (a.kv_once != 0) launch_decode_k<D, false, true, true>(a, grid, s, ev);
     else launch_decode_k<D, false, false, true>(a, grid, s, ev);
   } else if (a.kv_once != 0) {
@@ -95,7 +98,7 @@ static void launch_decode_d(const AttnArgs& a, dim3 grid, bool fold2, bool span,
 
 hipError_t launch_attn_decode(const AttnArgs& a, int n_rows, int grid_splits, int max_pfx_splits, hipStream_t s,
                               LaunchEvents ev, bool span) {
-  if (grid_splits < 1 || grid_splits > a.max_splits) return hipErrorInvalidValue;
+  if (grid_splits < 1 || grid_splits > a.max_splits || (a.pool4 != nullptr && !span)) return hipErrorInvalidValue;
   const dim3 grid = !span          ? dim3(a.Hkv, grid_splits, n_rows)
                     : a.packed > 0 ? dim3(a.Hkv, a.packed_items)
                                    : dim3(a.Hkv, n_rows, grid_splits);

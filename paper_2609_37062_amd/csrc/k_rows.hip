@@ -81,7 +81,11 @@ struct RowsLds {
   float m[kRowTiles][64], l[kRowTiles][64];  // the second half's, when the halves join
 };
 
-template <int D, int NH>
+// Q4: the 4-bit cache.  A wave's K or V block of a step is 1 KiB of codes there at D =
+// 128, 16 bytes a lane; they are loaded a step ahead of the slot's turn, turned into
+// bf16 once for the workgroup, and stored in the order of the 16-bit blocks, so the
+// walk is the same.
+template <int D, int NH, bool Q4>
 __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   constexpr int T = 256 * NH;
   constexpr int QC = D / 16;  // q and K operands of a step
@@ -146,6 +150,64 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   auto landed = [&](auto steps) __attribute__((always_inline)) {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(steps)::value * kCopies) : "memory");
   };
+  // (Q4) this lane's part of the wave's block: K of place p and a quarter of the dims
+  // (two lanes of a 16-byte piece at D = 64), V of four tokens' (t, d)
+  struct Codes {
+    u32x4 c, s;
+  };
+  const uint8_t* rec0 = a.pool4 + (static_cast<size_t>(a.layer) * a.n_blocks * a.Hkv + hk) * kv4_record(D);
+  const int piece = D == 128 ? lane : lane >> 1, part = D == 128 ? 0 : lane & 1;
+  const int kp = D == 128 ? piece & 15 : (piece & 7) + 8 * part, kq = D == 128 ? piece >> 4 : piece >> 3;
+  const int vd = piece & 15, vth = piece >> 4 & 1, vtq = D == 128 ? piece >> 5 : part;
+  auto fetch = [&](int step, Codes& x) __attribute__((always_inline)) {
+    const uint32_t blk = __builtin_amdgcn_readfirstlane(sm.tbl[min(2 * NH * step + my_blk, span.nv - 1)]);
+    const uint8_t* rec = rec0 + static_cast<size_t>(blk) * (a.Hkv * kv4_record(D));
+    const uint8_t* at = rec + (w & 1 ? kv4_v_at(D) : 0) + D / 8 * lane;
+    if constexpr (D == 128) {
+      x.c = *reinterpret_cast<const u32x4*>(at);
+    } else {
+      const u32x2 y = *reinterpret_cast<const u32x2*>(at);
+      x.c = u32x4{y[0], y[1], 0u, 0u};
+    }
+    if (w & 1) {
+      const uint8_t* sp = rec + kv4_vs_at(D) + (8 * vth + 4 * vtq) * (D / 32);
+      if constexpr (D == 128) {
+        x.s = *reinterpret_cast<const u32x4*>(sp);
+      } else {
+        const u32x2 y = *reinterpret_cast<const u32x2*>(sp);
+        x.s = u32x4{y[0], y[1], 0u, 0u};
+      }
+    } else {
+      x.s[0] = rec[kv4_ks_at(D) + kv4_ks_byte(kp, D == 128 ? kq : kq >> 1)];
+    }
+  };
+  auto expand = [&](int step, const Codes& x) __attribute__((always_inline)) {
+    u32x4* dst = &sm.kv[step % kRowSlots][w & 1][w >> 2][w >> 1 & 1][0];
+    if (w & 1) {
+      u32x2* half = reinterpret_cast<u32x2*>(dst);  // (four tokens of a dim)
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b) {
+        uint32_t y[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t cw = D == 128 ? x.c[t] : x.c[t >> 1], sw = D == 128 ? x.s[t] : x.s[t >> 1];
+          const int n = D == 128 ? b : 2 * (t & 1) + b;
+          const float sc = kv4_scale(sw, n);
+          y[t] = n == 0 ? mx4_decode<0>(cw, sc) : n == 1 ? mx4_decode<1>(cw, sc) : n == 2 ? mx4_decode<2>(cw, sc) : mx4_decode<3>(cw, sc);
+        }
+        half[2 * (32 * (2 * b) + vd + 16 * vth) + vtq] = u32x2{low_halves(y[0], y[1]), low_halves(y[2], y[3])};
+        half[2 * (32 * (2 * b + 1) + vd + 16 * vth) + vtq] = u32x2{high_halves(y[0], y[1]), high_halves(y[2], y[3])};
+      }
+    } else {
+      const float sc = mx4_scale(x.s[0]);
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {  // dims D / 4 * kq + 8 c ..
+        const int e = D / 4 * kq + 8 * c;
+        dst[64 * (e >> 5) + kp + 16 * (e >> 3 & 3)] = mx4_decode8(x.c[c], sc);
+      }
+    }
+  };
+  Codes raw;
   float m = -INFINITY, l = 0.f;
   f32x16 o[OC];
 #pragma unroll
@@ -258,15 +320,29 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     }
   };
 
+  if constexpr (Q4) {
 #pragma unroll
-  for (int j = 0; j < 3; ++j) copy(first + j);
+    for (int j = 0; j < 3; ++j) {
+      fetch(first + j, raw);
+      expand(first + j, raw);
+    }
+    fetch(first + 3, raw);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 3; ++j) copy(first + j);
+  }
   bool big = false;  // (uniform) scores so large that a fma's unrounded product would be off the maximum
   f32x16 s;          // s[r]: key 8 hi + r of the step's first block (r < 8), 8 hi + r - 8 of the second
   float mx;
   auto next = [&](int step) __attribute__((always_inline)) {
-    landed(std::integral_constant<int, 1>{});
+    if constexpr (!Q4) landed(std::integral_constant<int, 1>{});
     barrier_after_lds_reads();  // the next step's slot is whole, the one of the last step free
-    copy(step + 3);
+    if constexpr (Q4) {
+      expand(step + 3, raw);
+      fetch(step + 4, raw);
+    } else {
+      copy(step + 3);
+    }
   };
   auto qk = [&](int step, f32x16& s) __attribute__((always_inline)) {
     const u32x4* kp = &sm.kv[step % kRowSlots][0][hh][lc >> 4][(lane & 15) + 16 * hi];
@@ -282,7 +358,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     return max_xor32(x) * sc;
   };
   int step = first;
-  landed(std::integral_constant<int, 2>{});
+  if constexpr (!Q4) landed(std::integral_constant<int, 2>{});
   barrier_after_lds_reads();
   qk(step, s);
   mx = top(s);
@@ -325,7 +401,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     mx = top(s);
   }
   l = add_xor32(l);
-  landed(std::integral_constant<int, 0>{});  // (the steps past the list: before LDS is used again or ends)
+  if constexpr (!Q4) landed(std::integral_constant<int, 0>{});  // (the steps past the list: before LDS is used again or ends)
 
   if constexpr (NH == 2) {  // the second half's sums join the first's
     static_assert(sizeof(sm.kv) >= kRowTiles * OC * 16 * 64 * 4, "space for a half's sums");
@@ -444,19 +520,19 @@ __global__ __launch_bounds__(256) void k_rows_join(AttnPrefillArgs a) {
 // window, whose longest work items set the time, go the other way up to some 400
 // work items (3 x 1,500 of 8/8, 288: 40 and 46; 4 x 1,500, 384: 46 and 50; 480: 55
 // and 53): not told apart.
-template <int D>
+template <int D, bool Q4>
 static void launch_rows_d(const AttnPrefillArgs& a, int n_items, hipStream_t s) {
   const int wgs = n_items * a.Hkv * a.splits;
-  if (n_items * a.Hkv <= 256) hipLaunchKernelGGL((k_attn_rows<D, 2>), dim3(wgs), dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((k_attn_rows<D, 1>), dim3(wgs), dim3(256), 0, s, a);
+  if (n_items * a.Hkv <= 256) hipLaunchKernelGGL((k_attn_rows<D, 2, Q4>), dim3(wgs), dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((k_attn_rows<D, 1, Q4>), dim3(wgs), dim3(256), 0, s, a);
   if (a.splits > 1) hipLaunchKernelGGL((k_rows_join<D>), dim3(n_items * a.Hkv, kPreCols * D / 1024), dim3(256), 0, s, a);
 }
 
 hipError_t launch_attn_rows(const AttnPrefillArgs& a, int n_items, int head_dim, hipStream_t s) {
   if (n_items <= 0) return hipSuccess;
-  if (head_dim == 128) launch_rows_d<128>(a, n_items, s);
-  else if (head_dim == 64) launch_rows_d<64>(a, n_items, s);
-  else return hipErrorInvalidValue;
+  if (head_dim != 128 && head_dim != 64) return hipErrorInvalidValue;
+  if (a.pool4 != nullptr) head_dim == 128 ? launch_rows_d<128, true>(a, n_items, s) : launch_rows_d<64, true>(a, n_items, s);
+  else head_dim == 128 ? launch_rows_d<128, false>(a, n_items, s) : launch_rows_d<64, false>(a, n_items, s);
   return hipGetLastError();
 }
 

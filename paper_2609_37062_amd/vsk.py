@@ -17,6 +17,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libvsk.so")
 
 VSK_OK = 0
+BF16, FP32, MX4 = 0, 1, 2  # VSK_BF16, VSK_FP32, VSK_MX4
 SCRATCH_BYTES = 64 * 1024 * 1024  # VSK_SCRATCH_BYTES in vsk.h
 STATUS = {0: "OK", -1: "ARG", -2: "NOMEM", -3: "RANGE", -4: "SHARED_WRITE", -5: "STATE", -6: "HIP",
           -7: "UNSUPPORTED"}
@@ -92,6 +93,20 @@ SIGNATURES = [
     ("vsk_kv_evict_bytes", _SZ, [_VP, _PI64, _PI32, _I32]),
     ("vsk_kv_evict", C.c_int, [_VP, _PI64, _PI64, _PI32, _I32, _I32, _I32, _VP, _I32, _VP, _VP, _VP, _I32, _VP, _SZ,
                                _VP]),
+    ("vsk_mx4_bytes", _SZ, [_I32, _I32]),
+    ("vsk_mx4_quantise", C.c_int, [_VP, _I32, _I64, _I32, _I32, _VP, _VP]),
+    ("vsk_mx4_pack", C.c_int, [_VP, _VP, _I32, _I32, _VP, _VP]),
+    ("vsk_mx4_read", C.c_int, [_VP, _I32, _I32, _VP, _I32, _I64, _VP]),
+    ("vsk_mx4_product_bytes", _SZ, [_I32, _I32, _I32]),
+    ("vsk_mx4_product", C.c_int, [_VP, _I32, _I64, _VP, _I32, _I32, _I32, _VP, _I32, _I64, _VP, _VP, _SZ, _VP]),
+    ("vsk_kv4_pool_bytes", _SZ, [C.POINTER(ModelCfg), _I32]),
+    ("vsk_kv4_init", C.c_int, [_VP, _VP, _SZ]),
+    ("vsk_kv4_write", C.c_int, [_VP, _I32, _VP, _I32, _VP, _VP, _VP]),
+    ("vsk_kv4_read", C.c_int, [_VP, _I32, _VP, _I32, _VP, _VP, _VP]),
+    ("vsk_kv4_attend", C.c_int, [_VP, _I32, _VP, _VP, _I32, _I32, _VP, _SZ, _VP]),
+    ("vsk_rope_bytes", _SZ, [_VP]),
+    ("vsk_rope_bind", C.c_int, [_VP, _VP, _SZ, _VP]),
+    ("vsk_qkv_norm_rope", C.c_int, [_VP, _I32, _VP, _I64, _VP, _VP, _VP, _I32, _VP]),
     ("vsk_set_tuning", C.c_int, [_VP, _I32, _I32]),
     ("vsk_residual_copy", C.c_int, [_VP, _VP, _I32, _VP]),
     ("vsk_routed_weight_bytes", _SZ, [C.POINTER(ModelCfg), _I32, _I32]),
@@ -163,6 +178,45 @@ def stream_read(src_ptr, nbytes, out_ptr, workgroups, stream=None):
     st = lib().vsk_stream_read(src_ptr, nbytes, out_ptr, workgroups, stream)
     if st != VSK_OK:
         raise VskError(st, "stream_read")
+
+
+# ------------------------------------------------------------------ 4-bit matrices
+def mx4_bytes(rows, k) -> int:
+    return lib().vsk_mx4_bytes(rows, k)
+
+
+def mx4_quantise(src_ptr, dtype, stride, rows, k, mx_ptr, stream=None):
+    """[rows][k] of BF16 or FP32 (rows `stride` elements apart) as an MX4 matrix."""
+    st = lib().vsk_mx4_quantise(src_ptr, dtype, stride, rows, k, mx_ptr, stream)
+    if st != VSK_OK:
+        raise VskError(st, "mx4_quantise")
+
+
+def mx4_pack(codes_ptr, scales_ptr, rows, k, mx_ptr, stream=None):
+    """Codes and exponents as files hold them, as an MX4 matrix."""
+    st = lib().vsk_mx4_pack(codes_ptr, scales_ptr, rows, k, mx_ptr, stream)
+    if st != VSK_OK:
+        raise VskError(st, "mx4_pack")
+
+
+def mx4_read(mx_ptr, rows, k, dst_ptr, dtype, stride, stream=None):
+    """The values of an MX4 matrix, BF16 or FP32."""
+    st = lib().vsk_mx4_read(mx_ptr, rows, k, dst_ptr, dtype, stride, stream)
+    if st != VSK_OK:
+        raise VskError(st, "mx4_read")
+
+
+def mx4_product_bytes(rows, n, k) -> int:
+    return lib().vsk_mx4_product_bytes(rows, n, k)
+
+
+def mx4_product(x_ptr, x_dtype, x_stride, w_ptr, rows, n, k, y_ptr, y_dtype, y_stride, ws_ptr=None, ws_bytes=0,
+                add_ptr=None, stream=None):
+    """y [rows][n] = (add +) x [rows][k] w^T for an MX4 weight matrix [n][k]."""
+    st = lib().vsk_mx4_product(x_ptr, x_dtype, x_stride, w_ptr, rows, n, k, y_ptr, y_dtype, y_stride, add_ptr, ws_ptr,
+                               ws_bytes, stream)
+    if st != VSK_OK:
+        raise VskError(st, "mx4_product")
 
 
 # ------------------------------------------------------------------ mode switch
@@ -375,6 +429,34 @@ class Engine:
         self._ck(lib().vsk_kv_evict(self.h, _p64(d), _p64(s), _p32(k), len(s), sinks, recent, mass_ptr, mass_stride,
                                     mass_out_ptr, kept_ptr, slots_ptr, out_stride, meta_ptr, meta_bytes, stream),
                  "kv_evict")
+
+    # -- 4-bit cache
+    def kv4_pool_bytes(self, n_blocks):
+        return lib().vsk_kv4_pool_bytes(C.byref(self.cfg), n_blocks)
+
+    def kv4_init(self, pool_ptr, nbytes=0):
+        self._ck(lib().vsk_kv4_init(self.h, pool_ptr, nbytes), "kv4_init")
+
+    def kv4_write(self, layer, slots_ptr, n, k_ptr, v_ptr, stream=None):
+        self._ck(lib().vsk_kv4_write(self.h, layer, slots_ptr, n, k_ptr, v_ptr, stream), "kv4_write")
+
+    def kv4_read(self, layer, slots_ptr, n, k_ptr, v_ptr, stream=None):
+        self._ck(lib().vsk_kv4_read(self.h, layer, slots_ptr, n, k_ptr, v_ptr, stream), "kv4_read")
+
+    def kv4_attend(self, layer, q_ptr, o_ptr, ws_ptr, ws_bytes, window=0, sinks=0, stream=None):
+        """Attention of the batch's rows over one layer of the 4-bit cache."""
+        self._ck(lib().vsk_kv4_attend(self.h, layer, q_ptr, o_ptr, window, sinks, ws_ptr, ws_bytes, stream), "kv4_attend")
+
+    def rope_bytes(self):
+        return lib().vsk_rope_bytes(self.h)
+
+    def rope_bind(self, table_ptr, nbytes, stream=None):
+        self._ck(lib().vsk_rope_bind(self.h, table_ptr, nbytes, stream), "rope_bind")
+
+    def qkv_norm_rope(self, layer, qkv_ptr, stride, q_gain_ptr, k_gain_ptr, q_ptr, cache_bits, stream=None):
+        """Norms and rotation of a QKV projection's rows: queries out, keys and values into a cache."""
+        self._ck(lib().vsk_qkv_norm_rope(self.h, layer, qkv_ptr, stride, q_gain_ptr, k_gain_ptr, q_ptr, cache_bits, stream),
+                 "qkv_norm_rope")
 
     # -- routed mode
     def routed_weight_bytes(self, first_routed, proj_ffn):

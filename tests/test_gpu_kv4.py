@@ -1,0 +1,305 @@
+"""The 4-bit cache on the device: what slots hold, attention over it against float64
+over the values that it stands for, and the rows of a QKV projection into either
+cache."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import mx4_case as mx  # noqa: E402
+from cache_case import BLOCK, Cache, bf16, check  # noqa: E402
+from mx4_case import Cache4  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+SPANS = [(0, 0), (1, 0), (1, 5), (16, 4), (17, 16), (40, 33), (256, 4), (1000, 100)]
+
+
+@pytest.mark.parametrize("kv,hd", [(1, 64), (3, 64), (1, 128), (8, 128)])
+def test_slots_hold_what_was_written(kv, hd):
+    print(f"[gpu] kv4 slots kv={kv} hd={hd}", flush=True)
+    c = Cache4(kv, 2, hd, [1, 16, 17, 200, 45], layers=2, seed=kv + hd, scale=3.0)
+    for l in range(2):
+        for s in range(5):
+            k, v = c.read(l, s)
+            np.testing.assert_array_equal(k, c.K[l][s])
+            np.testing.assert_array_equal(v, c.V[l][s])
+    # a token written again changes no other, nor a slot outside the pool anything
+    before = [c.read(1, s) for s in range(5)]
+    slots = np.array([c.slots(3, 200)[77], -1, c.n_blocks * 16, c.slots(4, 45)[44]], np.int32)
+    k, v = bf16(c.rng.standard_normal((4, kv, hd))), bf16(c.rng.standard_normal((4, kv, hd)))
+    sd, kd, vd = torch.from_numpy(slots).cuda(), k.cuda(), v.cuda()
+    c.eng.kv4_write(1, sd.data_ptr(), 4, kd.data_ptr(), vd.data_ptr(), c.sp)
+    for (s, at), i in (((3, 77), 0), ((4, 44), 3)):
+        before[s][0][at], before[s][1][at] = mx.values(k.float().numpy()[i]), mx.values(v.float().numpy()[i])
+    for s in range(5):
+        for a, b in zip(c.read(1, s), before[s]):
+            np.testing.assert_array_equal(a, b)
+        np.testing.assert_array_equal(c.read(0, s)[0], c.K[0][s])
+    c.close()
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+def test_a_token_that_is_not_finite(bad):
+    """Its block of 32 dims reads as NaN; only rows that see it are not finite."""
+    for hd in (64, 128):
+        c = Cache4(2, 4, hd, [60, 90], seed=3)
+        for x in (c.K, c.V):
+            x[0][0][30, 1, 5] = bad
+            x[0][1][10, 0, hd - 1] = bad
+        for s in range(2):
+            c.write(0, s)
+            k, v = c.read(0, s)
+            np.testing.assert_array_equal(k, c.K[0][s])
+            np.testing.assert_array_equal(v, c.V[0][s])
+        assert np.isnan(c.K[0][0][30, 1, :32]).all() and not np.isnan(c.K[0][0][30, 0]).any()
+        c.batch([0, 1], [40, 1])
+        c.attend(window=20)
+        o = c.out().reshape(41, 2, 4, hd)
+        # row i of sequence 0 is at index 20 + i and sees 1 + i .. 20 + i
+        sees = np.array([1 + i <= 30 <= 20 + i for i in range(40)])
+        assert np.isnan(o[:40][sees][:, 1]).all() and np.isfinite(o[:40][~sees]).all() and np.isfinite(o[:40, 0]).all()
+        assert np.isfinite(o[40]).all()
+        c.close()
+
+
+@pytest.mark.parametrize("kv,group,hd", [(1, 1, 64), (2, 16, 64), (4, 3, 128), (8, 4, 128), (3, 7, 128), (1, 16, 128)])
+@pytest.mark.parametrize("window,sinks", SPANS)
+def test_single_tokens(kv, group, hd, window, sinks):
+    print(f"[gpu] kv4 decode kv={kv} group={group} hd={hd} window={window} sinks={sinks}", flush=True)
+    c = Cache4(kv, group, hd, [1, 2, 15, 16, 17, 31, 32, 33, 48, 63, 129, 300, 777], seed=kv * 100 + group)
+    c.batch(range(13), [1] * 13)
+    c.attend(window=window, sinks=sinks)
+    check(c, window, sinks)
+    c.close()
+
+
+@pytest.mark.parametrize("bps", [0, 8, 16, 512])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 4), (1500, 130)])
+def test_single_tokens_split_and_joined(bps, window, sinks):
+    print(f"[gpu] kv4 splits bps={bps} window={window} sinks={sinks}", flush=True)
+    c = Cache4(2, 4, 128, [2000, 5, 1023, 1537, 4099], seed=3)
+    c.eng.set_tuning(0, bps)
+    c.batch(range(5), [1] * 5)
+    for _ in range(2):
+        c.o.fill_(-7.0)
+        c.attend(window=window, sinks=sinks)
+        check(c, window, sinks)
+    c.close()
+
+
+@pytest.mark.parametrize("kv,group,hd", [(1, 1, 64), (2, 16, 64), (2, 3, 128), (4, 4, 128), (1, 7, 128)])
+@pytest.mark.parametrize("window,sinks", SPANS)
+def test_prompt_rows(kv, group, hd, window, sinks):
+    print(f"[gpu] kv4 prompt kv={kv} group={group} hd={hd} window={window} sinks={sinks}", flush=True)
+    c = Cache4(kv, group, hd, [2, 16, 37, 130, 411, 290], seed=kv * 10 + group)
+    c.batch(range(6), [2, 16, 37, 33, 200, 1])
+    c.attend(window=window, sinks=sinks)
+    check(c, window, sinks)
+    c.close()
+
+
+def test_prompt_rows_of_many_work_items():
+    """More work items than compute units (four waves each), and one a row."""
+    c = Cache4(4, 4, 64, [300, 513, 700, 90] * 5, seed=11)
+    c.batch(range(20), [300, 200, 333, 1] * 5)
+    for window, sinks in [(0, 0), (100, 7)]:
+        c.attend(window=window, sinks=sinks)
+        check(c, window, sinks)
+    c.close()
+    c = Cache4(2, 4, 128, [70, 300], seed=5)
+    c.eng.set_tuning(6, 0)
+    c.batch([0, 1], [70, 3])
+    for window, sinks in [(0, 0), (20, 3)]:
+        c.attend(window=window, sinks=sinks)
+        check(c, window, sinks)
+    c.close()
+
+
+def test_long_cache():
+    for hd in (64, 128):
+        c = Cache4(1, 2, hd, [16384, 16383], seed=6)
+        for q_lens in ([1, 1], [3, 40]):
+            c.batch([0, 1], q_lens)
+            for window, sinks in [(0, 0), (9000, 70)]:
+                c.attend(window=window, sinks=sinks)
+                check(c, window, sinks)
+        c.close()
+
+
+def test_a_shared_prefix_is_the_same_attention():
+    c = Cache4(2, 4, 128, [200, 150, 170], seed=7)
+    free = [b for b in range(c.n_blocks) if all(b not in t for t in c.blocks)]
+    for i, n in ((3, 160), (4, 149)):
+        own = -(-(n - 144) // BLOCK)
+        c.eng.seq_create(i)
+        c.eng.seq_set_blocks(i, np.concatenate([c.blocks[0][:9], free[:own]]).astype(np.int32), n)
+        free = free[own:]
+        for x in (c.K, c.V):
+            x[0].append(np.concatenate([x[0][0][:144], x[0][1][:n - 144]]))
+        c.write(0, i, 144)
+    c.batch([0, 1, 3, 2, 4], [1] * 5)
+    for window, sinks in [(0, 0), (30, 5)]:
+        c.attend(window=window, sinks=sinks)
+        check(c, window, sinks)
+    c.close()
+
+
+def test_slots_behind_a_sequence_do_not_matter():
+    """Codes and exponents of no token: the pool starts as exponents that say NaN."""
+    for hd in (64, 128):
+        c = Cache4(2, 4, hd, [5, 33, 100], seed=12)
+        for ql in ([1, 1, 1], [5, 20, 99]):
+            c.batch([0, 1, 2], ql)
+            c.attend()
+            check(c)
+        c.close()
+
+
+def test_large_scores():
+    c = Cache4(2, 4, 128, [300, 90], seed=8, scale=2.0 ** 20)
+    for ql in ([1, 1], [100, 90]):
+        c.batch([0, 1], ql)
+        c.attend()
+        assert np.isfinite(c.out()).all()
+    c.close()
+
+
+def test_replayed_beside_eager_calls():
+    c = Cache4(2, 4, 128, [300, 97, 1500], seed=9)
+    c.batch([0, 1, 2], [60, 1, 1])
+    c.attend()
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        c.attend(window=200, sinks=4, stream=torch.cuda.current_stream().cuda_stream)
+    for i in range(3):
+        c.q = bf16(c.rng.standard_normal(tuple(c.q.shape)))
+        c.qd.copy_(c.q)
+        c.o[:-1].fill_(0)
+        g.replay()
+        check(c, 200, 4)
+        c.attend()
+        check(c)
+    c.close()
+
+
+# ------------------------------------------------------------------ rows of a QKV projection
+def _rows(cls, kv, group, hd, lens, q_lens, seed, pad=0, max_pos=16384):
+    c = cls(kv, group, hd, lens, layers=2, seed=seed, max_pos=max_pos)
+    c.batch(range(len(lens)), q_lens)
+    rows, width = sum(q_lens), kv * (group + 2) * hd
+    x = bf16(c.rng.standard_normal((rows, width + pad)) * 2.0)
+    gains = bf16(1 + 0.3 * c.rng.standard_normal((2, hd)))
+    nb = c.eng.rope_bytes()
+    c._rope, at = c.buf(nb, "cuda")
+    c.eng.rope_bind(at, nb, c.sp)
+    return c, x, gains
+
+
+def _turned(x, pos, gain, theta, eps):
+    """[rows][heads][hd] in 64 bits; also the magnitudes of the terms."""
+    hd = x.shape[-1]
+    if gain is not None:
+        x = x / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps) * gain
+    a = (pos[:, None] * theta ** (-2.0 * np.arange(hd // 2) / hd))[:, None, :]
+    lo, hi = x[..., :hd // 2], x[..., hd // 2:]
+    y = np.concatenate([lo * np.cos(a) - hi * np.sin(a), hi * np.cos(a) + lo * np.sin(a)], axis=-1)
+    m = np.concatenate([np.abs(lo * np.cos(a)) + np.abs(hi * np.sin(a)), np.abs(hi * np.cos(a)) + np.abs(lo * np.sin(a))], axis=-1)
+    return y, m
+
+
+def _check_rows(c, x, gains, bits, norm, layer=1):
+    kv, heads, hd = c.kv, c.kv * c.group, c.hd
+    rows = x.shape[0]
+    xd, gd = x.cuda(), gains.cuda()
+    q = torch.full((rows + 1, heads, hd), -7.0, dtype=torch.bfloat16, device="cuda")
+    c.eng.qkv_norm_rope(layer, xd.data_ptr(), x.shape[1], gd[0].data_ptr() if norm else None,
+                        gd[1].data_ptr() if norm else None, q.data_ptr(), bits, c.sp)
+    h = c.eng.batch_host()
+    slots = torch.from_numpy(h["slot"]).cuda()
+    K = torch.zeros((rows, kv, hd), dtype=torch.bfloat16, device="cuda")
+    V = torch.zeros_like(K)
+    (c.eng.kv4_read if bits == 4 else c.eng.kv_read)(layer, slots.data_ptr(), rows, K.data_ptr(), V.data_ptr(), c.sp)
+    torch.cuda.synchronize()
+    assert (q[-1] == -7).all()
+    q, K, V = (t.float().cpu().numpy().astype(np.float64) for t in (q[:-1], K, V))
+    xs = x[:, :kv * (c.group + 2) * hd].float().numpy().astype(np.float64).reshape(rows, -1, hd)
+    pos = h["pos"].astype(np.float64)
+    g = gains.float().numpy().astype(np.float64)
+    eps, theta = float(np.float32(1e-5)), 500000.0
+    wq, mq = _turned(xs[:, :heads], pos, g[0] if norm else None, theta, eps)
+    wk, mk = _turned(xs[:, heads:heads + kv], pos, g[1] if norm else None, theta, eps)
+    # float32: a sum of squares (hd / 8 + 6 roundings), a root, a quotient, two products,
+    # cos and sin (one each) and the turn (two): at most 40 half steps; half a step of bf16
+    near = lambda got, want, mag: (np.abs(got - want) <= 40 * 2.0 ** -24 * mag + 2.0 ** -8 * np.abs(want) + 1e-38).all()
+    assert near(q, wq, mq)
+    wv = xs[:, heads + kv:]
+    if bits == 16:
+        assert near(K, wk, mk)
+        np.testing.assert_array_equal(V, wv)
+    else:
+        # (keys are taken in 64 bits: their codes are the exact values')
+        np.testing.assert_array_equal(K, mx.values(wk))
+        np.testing.assert_array_equal(V, mx.values(wv))
+    return h["slot"]
+
+
+@pytest.mark.parametrize("kv,group,hd", [(1, 1, 64), (3, 2, 64), (2, 16, 64), (8, 4, 128), (1, 3, 128), (5, 7, 128)])
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("norm", [True, False])
+def test_qkv_rows(kv, group, hd, bits, norm):
+    print(f"[gpu] qkv rows kv={kv} group={group} hd={hd} bits={bits} norm={norm}", flush=True)
+    c, x, gains = _rows(Cache4 if bits == 4 else Cache, kv, group, hd, [1, 40, 333, 2000], [1, 1, 47, 130], kv * 7 + hd, pad=24)
+    written = set(_check_rows(c, x, gains, bits, norm).tolist())
+    # nothing else of the cache has changed, in this layer or the other
+    for layer in range(2):
+        for s, n in enumerate(c.lens):
+            k, v = c.read(layer, s)
+            keep = np.array([layer == 0 or int(t) not in written for t in c.slots(s, n)])
+            np.testing.assert_array_equal(k[keep], c.K[layer][s][keep])
+            np.testing.assert_array_equal(v[keep], c.V[layer][s][keep])
+    c.close()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_qkv_rows_last_positions_and_evicted_ones(bits):
+    c, x, gains = _rows(Cache4 if bits == 4 else Cache, 2, 2, 128, [16384, 16383], [70, 1], 5)
+    _check_rows(c, x, gains, bits, True)
+    c.close()
+    if bits == 16:  # a shorter cache whose positions go on
+        c, _, gains = _rows(Cache, 2, 2, 64, [300], [1], 6)
+        mass = torch.rand((1, 300), device="cuda")
+        c.eng.seq_create(9)
+        nb = c.eng.kv_evict_bytes([0], [100])
+        meta, at = c.buf(nb, "cuda")
+        kept = torch.empty((1, 100), dtype=torch.int32, device="cuda")
+        c.eng.kv_evict([9], [0], [100], 4, 20, mass.data_ptr(), 300, at, nb, kept_ptr=kept.data_ptr(), out_stride=100, stream=c.sp)
+        c.eng.reserve(9, 3)
+        c.batch([9], [3])
+        assert c.eng.batch_host()["pos"].tolist() == [300, 301, 302]
+        _check_rows(c, bf16(c.rng.standard_normal((3, 2 * 4 * 64))), gains, 16, True)
+        c.close()
+
+
+def test_qkv_rows_refusals():
+    c, x, gains = _rows(Cache4, 2, 2, 64, [40, 30], [3, 1], 4, max_pos=64)
+    from paper_2609_37062_amd import vsk
+    xd = x.cuda()
+    q = torch.zeros((4, 4, 64), dtype=torch.bfloat16, device="cuda")
+    ok = dict(layer=0, qkv=xd.data_ptr(), stride=x.shape[1], q=q.data_ptr(), bits=4, gq=None)
+    for bad, code in ((dict(layer=2), "RANGE"), (dict(layer=-1), "RANGE"), (dict(qkv=None), "ARG"), (dict(q=None), "ARG"),
+                      (dict(stride=x.shape[1] - 8), "ARG"), (dict(stride=x.shape[1] + 4), "ARG"), (dict(stride=1 << 62), "ARG"),
+                      (dict(qkv=xd.data_ptr() + 8), "ARG"), (dict(q=q.data_ptr() + 8), "ARG"), (dict(bits=8), "ARG"),
+                      (dict(gq=gains.data_ptr() | 1), "ARG"), (dict(q=xd.data_ptr() + 64), "ARG")):
+        a = {**ok, **bad}
+        with pytest.raises(vsk.VskError) as e:
+            c.eng.qkv_norm_rope(a["layer"], a["qkv"], a["stride"], a["gq"], None, a["q"], a["bits"], c.sp)
+        assert e.value.code == code, bad
+    for bad, code in ((dict(q=c.qd.data_ptr() + 8), "ARG"), (dict(o=c.qd.data_ptr()), "ARG"), (dict(layer=2), "RANGE"),
+                      (dict(window=-1), "ARG"), (dict(sinks=-1), "ARG"), (dict(ws=c.ws + 256), "STATE"), (dict(q=None), "ARG")):
+        a = {**dict(layer=0, q=c.qd.data_ptr(), o=c.o.data_ptr(), window=0, sinks=0, ws=c.ws), **bad}
+        with pytest.raises(vsk.VskError) as e:
+            c.eng.kv4_attend(a["layer"], a["q"], a["o"], a["ws"], c.ws_bytes, a["window"], a["sinks"], c.sp)
+        assert e.value.code == code, bad
+    c.close()

@@ -1,0 +1,273 @@
+"""Microscaled 4-bit matrices on the device: codes and values equal to the format's
+definition, products equal where every sum is exact, and within the roundings of
+float32 sums elsewhere."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import mx4_case as mx  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def _vsk():
+    from paper_2609_37062_amd import vsk
+    return vsk
+
+
+def _buf(n, fill=0xff):
+    from paper_2609_37062_amd.runner import _dev_buffer
+    t, at = _dev_buffer(n, "cuda")
+    t.fill_(fill if t.dtype == torch.uint8 else -1)
+    return t, at
+
+
+def _sp():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _dev(x, dtype, stride=None, off=0):
+    """x [rows][k] on the device, rows `stride` elements apart from element `off`, the rest 77."""
+    rows, k = x.shape
+    stride = stride or k
+    t = torch.full((off + (rows - 1) * stride + k + 9,), 77.0, dtype=dtype, device="cuda")
+    v = t[off:].as_strided((rows, k), (stride, 1))
+    v.copy_(torch.from_numpy(np.ascontiguousarray(x, np.float32)).to(dtype))
+    return t, v
+
+
+def _matrix(x):
+    """An MX4 matrix from float64 values' codes, through the file form."""
+    vsk = _vsk()
+    c, e = torch.from_numpy(mx.in_file(mx.codes(x))).cuda(), torch.from_numpy(mx.exponents(x)).cuda()
+    t, at = _buf(vsk.mx4_bytes(*x.shape))
+    vsk.mx4_pack(c.data_ptr(), e.data_ptr(), *x.shape, at, _sp())
+    torch.cuda.synchronize()
+    return t, at
+
+
+def _read(at, rows, k, dtype=None, stride=None):
+    vsk = _vsk()
+    dtype = dtype or torch.float32
+    t = torch.full((rows * (stride or k) + 5,), 77.0, dtype=dtype, device="cuda")
+    vsk.mx4_read(at, rows, k, t.data_ptr(), vsk.FP32 if dtype == torch.float32 else vsk.BF16, stride or k, _sp())
+    torch.cuda.synchronize()
+    y = t[:rows * (stride or k)].view(rows, stride or k)
+    assert (y[:, k:] == 77).all() and (t[rows * (stride or k):] == 77).all(), "written beside the rows"
+    return y[:, :k].float().cpu().numpy().astype(np.float64)
+
+
+def _draw(rng, rows, k):
+    x = rng.standard_normal((rows, k)) * 2.0 ** rng.integers(-30, 30, (rows, 1))
+    x[rng.random((rows, k)) < 0.1] = 0
+    return torch.from_numpy(x.astype(np.float32)).to(torch.bfloat16).float().numpy()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,k,stride,off", [(1, 1, None, 0), (1, 31, None, 0), (3, 32, None, 0), (17, 33, 40, 3), (16, 128, None, 0),
+                                               (15, 500, 512, 8), (40, 512, None, 0), (33, 1100, 1101, 1), (2, 640, 648, 0)])
+def test_quantise_and_read(rows, k, stride, off, dtype):
+    print(f"[gpu] mx4 quantise {rows}x{k} stride={stride} off={off} {dtype}", flush=True)
+    vsk = _vsk()
+    rng = np.random.default_rng(rows * 1000 + k)
+    x = _draw(rng, rows, k)
+    if dtype == torch.float32:
+        x = x * np.float32(1.0 + 2.0 ** -20)
+    t, v = _dev(x, dtype, stride, off)
+    m, at = _buf(vsk.mx4_bytes(rows, k))
+    vsk.mx4_quantise(v.data_ptr(), vsk.FP32 if dtype == torch.float32 else vsk.BF16, stride or k, rows, k, at, _sp())
+    want = mx.values(x)
+    np.testing.assert_array_equal(_read(at, rows, k), want)
+    np.testing.assert_array_equal(_read(at, rows, k, torch.bfloat16, k + 3), want)
+    m2, at2 = _matrix(x.astype(np.float64))  # the file form gives the same matrix
+    np.testing.assert_array_equal(_read(at2, rows, k), want)
+
+
+def test_every_bf16_value_in_blocks_of_its_own_magnitude():
+    """All finite bf16 values, 32 of a magnitude a block, next to a largest value that
+    puts them on each part of the grid; ties and zeros of both signs."""
+    vsk = _vsk()
+    bits = np.arange(65536, dtype=np.uint32)
+    bits = bits[(bits & 0x7f80) != 0x7f80]
+    rows = []
+    for shift in (0, 1, 2, 3):  # the largest value's exponent above the others'
+        v = (bits << 16).view(np.float32)
+        order = np.argsort(np.abs(v), kind="stable")
+        v = v[order].reshape(-1, 30)
+        with np.errstate(over="ignore"):
+            top = np.abs(v).max(axis=1) * np.float32(2.0 ** shift)
+        top = np.where(np.isfinite(top), top, np.float32(2.0 ** 127))
+        rows.append(np.concatenate([v, top[:, None], -top[:, None] * 0], axis=1))
+    x = np.concatenate(rows).reshape(-1, 32)
+    n = len(x) // 16 * 16
+    x = torch.from_numpy(np.ascontiguousarray(x[:n].reshape(16, -1))).to(torch.bfloat16)
+    k = x.shape[1]
+    m, at = _buf(vsk.mx4_bytes(16, k))
+    xd = x.cuda()
+    vsk.mx4_quantise(xd.data_ptr(), vsk.BF16, k, 16, k, at, _sp())
+    np.testing.assert_array_equal(_read(at, 16, k), mx.values(x.float().numpy()))
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_block_that_is_not_finite_stands_for_nan(bad, dtype):
+    vsk = _vsk()
+    x = _draw(np.random.default_rng(1), 5, 200)
+    x[2, 70] = bad
+    t, v = _dev(x, dtype)
+    m, at = _buf(vsk.mx4_bytes(5, 200))
+    vsk.mx4_quantise(v.data_ptr(), vsk.FP32 if dtype == torch.float32 else vsk.BF16, 200, 5, 200, at, _sp())
+    got = _read(at, 5, 200)
+    np.testing.assert_array_equal(got, mx.values(x))
+    assert np.isnan(got[2, 64:96]).all() and np.isnan(got).sum() == 32
+    # and makes its row (a weight: its column) of a product NaN
+    w, wat = _matrix(_draw(np.random.default_rng(2), 20, 200).astype(np.float64))
+    y = torch.zeros((5, 20), device="cuda")
+    vsk.mx4_product(at, vsk.MX4, 0, wat, 5, 20, 200, y.data_ptr(), vsk.FP32, 20, stream=_sp())
+    assert torch.isnan(y[2]).all() and not torch.isnan(y[[0, 1, 3, 4]]).any()
+    y = torch.zeros((20, 5), device="cuda")
+    vsk.mx4_product(wat, vsk.MX4, 0, at, 20, 5, 200, y.data_ptr(), vsk.FP32, 5, stream=_sp())
+    assert torch.isnan(y[:, 2]).all() and not torch.isnan(y[:, [0, 1, 3, 4]]).any()
+
+
+def _product(x, wat, n, x_kind, y_dtype, add=None, y_stride=None, x_stride=None, off=0, inplace=False):
+    vsk = _vsk()
+    rows, k = x.shape
+    if x_kind == "mx4":
+        keep, ptr = _matrix(x.astype(np.float64))
+        kind, xs = vsk.MX4, 0
+    else:
+        dt = torch.float32 if x_kind == "fp32" else torch.bfloat16
+        keep, v = _dev(x, dt, x_stride, off)
+        ptr, kind, xs = v.data_ptr(), vsk.FP32 if x_kind == "fp32" else vsk.BF16, x_stride or k
+    ys = y_stride or n
+    y = torch.full((rows * ys + 7,), 77.0, dtype=y_dtype, device="cuda")
+    ad = None
+    if add is not None:
+        ad = torch.full((rows * ys + 7,), 77.0, dtype=y_dtype, device="cuda")
+        ad[:rows * ys].view(rows, ys)[:, :n] = torch.from_numpy(add.astype(np.float32)).to(y_dtype).cuda()
+        if inplace:
+            y.copy_(ad)
+            ad = y
+    nb = 0 if x_kind == "mx4" else vsk.mx4_product_bytes(rows, n, k)
+    ws, wsp = _buf(nb) if nb else (None, None)
+    vsk.mx4_product(ptr, kind, xs, wat, rows, n, k, y.data_ptr(), vsk.FP32 if y_dtype == torch.float32 else vsk.BF16, ys, wsp,
+                    nb, add_ptr=None if ad is None else ad.data_ptr(), stream=_sp())
+    torch.cuda.synchronize()
+    m = y[:rows * ys].view(rows, ys)
+    assert (m[:, n:] == 77).all() and (y[rows * ys:] == 77).all(), "written beside the rows"
+    return m[:, :n].float().cpu().numpy().astype(np.float64)
+
+
+# rows over every kernel's range and its borders, columns and K odd and even
+SIZES = [(1, 16, 32), (1, 1, 1), (1, 33, 500), (3, 100, 1000), (16, 64, 4096), (15, 48, 130), (17, 80, 512), (31, 40, 2052),
+         (32, 128, 640), (33, 256, 1024), (48, 20, 5000), (64, 300, 384), (65, 300, 384), (77, 130, 3000), (128, 512, 256),
+         (129, 257, 300), (200, 64, 96), (255, 255, 255), (256, 256, 512), (257, 513, 1030), (300, 1000, 700), (513, 300, 2100),
+         (1000, 700, 160), (70, 5000, 40)]
+
+
+@pytest.mark.parametrize("rows,n,k", SIZES)
+def test_products_of_small_whole_numbers_are_exact(rows, n, k):
+    """Multiples of 1/4 whose sums stay below 2^22: float32 holds every partial sum, so
+    the order of the sum changes nothing."""
+    print(f"[gpu] mx4 product {rows}x{n}x{k}", flush=True)
+    rng = np.random.default_rng(rows + 7 * n + 13 * k)
+    grid = np.concatenate([mx.GRID, -mx.GRID])
+    # (each block holds a 6: its exponent is the drawn one)
+    x, w = grid[rng.integers(0, 16, (rows, k))], grid[rng.integers(0, 16, (n, k))]
+    for m in (x, w):
+        m[:, ::32] = 6
+        e = np.repeat(rng.integers(0, 3, (m.shape[0], (k + 31) // 32)), 32, axis=1)[:, :k]
+        m *= 2.0 ** e
+    want = x @ w.T
+    wm, wat = _matrix(w)
+    assert np.abs(x).max() * np.abs(w).max() * k < 2 ** 22 * 4
+    for kind in ("mx4", "bf16", "fp32"):
+        np.testing.assert_array_equal(_product(x, wat, n, kind, torch.float32), want, err_msg=kind)
+    add = rng.integers(-1000, 1000, want.shape).astype(np.float64)
+    np.testing.assert_array_equal(_product(x, wat, n, "bf16", torch.float32, add, n + 3, k + 5, 1), want + add)
+    np.testing.assert_array_equal(_product(x, wat, n, "bf16", torch.float32, add, inplace=True), want + add)
+    as_bf16 = torch.from_numpy(want.astype(np.float32)).to(torch.bfloat16).float().numpy()
+    np.testing.assert_array_equal(_product(x, wat, n, "mx4", torch.bfloat16, None, n + 1), as_bf16)
+
+
+@pytest.mark.parametrize("rows,n,k", [(1, 130, 4096), (16, 64, 14336), (40, 100, 3000), (100, 96, 2048), (300, 300, 1500), (520, 260, 4100)])
+@pytest.mark.parametrize("y_dtype", [torch.float32, torch.bfloat16])
+def test_products_of_drawn_values(rows, n, k, y_dtype):
+    print(f"[gpu] mx4 drawn product {rows}x{n}x{k} {y_dtype}", flush=True)
+    rng = np.random.default_rng(rows + n + k)
+    x = torch.from_numpy(rng.standard_normal((rows, k)).astype(np.float32)).to(torch.bfloat16).float().numpy()
+    w = rng.standard_normal((n, k)) * 0.05
+    wm, wat = _matrix(w)
+    xv, wv = mx.values(x), mx.values(w)
+    add = torch.from_numpy(rng.standard_normal((rows, n)).astype(np.float32)).to(y_dtype).float().numpy().astype(np.float64)
+    got = _product(x, wat, n, "bf16", y_dtype, add)
+    want, mag = xv @ wv.T + add, np.abs(xv) @ np.abs(wv).T + np.abs(add)
+    # products are exact; a sum of 128 of them and what is there already is off by at
+    # most two steps of float32 of the magnitudes in it, a join of partial sums and the
+    # addend by one each (16 of them at most)
+    bound = (4 * ((k + 127) // 128) + 2 * 16) * U * mag
+    if y_dtype == torch.bfloat16:
+        bound = bound * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want)  # (half a step of 8 bits)
+    err = np.abs(got - want)
+    assert (err <= bound).all(), float((err / bound).max())
+
+
+def test_wide_exponents():
+    """Exponents at both ends of the format, and far apart within a row."""
+    rng = np.random.default_rng(9)
+    x, w = rng.standard_normal((20, 256)), rng.standard_normal((40, 256))
+    x[:, :32] *= 2.0 ** -100
+    w[:, :32] *= 2.0 ** 100
+    x[:, 64:96] *= 2.0 ** 90
+    w[:, 64:96] *= 2.0 ** -110
+    xv, wv = mx.values(x), mx.values(w)
+    wm, wat = _matrix(w)
+    got = _product(x, wat, 40, "mx4", torch.float32)
+    assert (np.abs(got - xv @ wv.T) <= 40 * U * (np.abs(xv) @ np.abs(wv).T)).all()
+    tiny = np.full((3, 32), 2.0 ** -126)
+    m, at = _matrix(tiny)
+    np.testing.assert_array_equal(_read(at, 3, 32), mx.values(tiny))
+
+
+def test_streams_and_graphs():
+    """The same call on another stream, and captured and replayed between eager ones with
+    other inputs in the same buffers."""
+    vsk = _vsk()
+    rng = np.random.default_rng(3)
+    for rows, n, k in ((5, 200, 1000), (40, 300, 512), (300, 520, 700)):
+        w = rng.standard_normal((n, k))
+        wm, wat = _matrix(w)
+        x = torch.randn((rows, k), device="cuda").to(torch.bfloat16)
+        y = torch.zeros((rows, n), device="cuda")
+        nb = vsk.mx4_product_bytes(rows, n, k)
+        ws, wsp = _buf(nb)
+
+        def call(stream):
+            vsk.mx4_product(x.data_ptr(), vsk.BF16, k, wat, rows, n, k, y.data_ptr(), vsk.FP32, n, wsp, nb, stream=stream)
+
+        call(_sp())
+        first = y.clone()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        y.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        call(side.cuda_stream)
+        torch.cuda.synchronize()
+        assert torch.equal(y, first)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(torch.cuda.current_stream().cuda_stream)
+        for i in range(3):
+            x.copy_(torch.randn((rows, k), device="cuda"))
+            y.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            replayed = y.clone()
+            y.zero_()
+            call(_sp())
+            torch.cuda.synchronize()
+            assert torch.equal(y, replayed), i
