@@ -20,7 +20,7 @@ LIB = os.path.join(HERE, "libvsk.so")
 ROOT = os.path.dirname(HERE)
 
 SOURCES = ["alloc.cpp", "api.cpp", "mode.cpp", "k_misc.hip", "k_gemm.hip", "k_gemm_tiled.hip", "k_attn.hip", "k_step.hip",
-           "k_rows.hip", "k_mass.hip", "k_evict.hip", "mx4.cpp", "k_mx4.hip", "k_kv4.hip"]
+           "k_rows.hip", "k_mass.hip", "k_evict.hip", "mx4.cpp", "k_mx4.hip", "k_mx4_tile.hip", "k_kv4.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

@@ -2,22 +2,9 @@
 // with a weight matrix on v_mfma_scale_f32_16x16x128_f8f6f4.
 #include <algorithm>
 
-#include "mx4.hpp"
-#include "mx4_dev.hpp"
+#include "mx4_mma.hpp"
 
 namespace vsk {
-
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-
-// D(16x16, f32) += A(16x128) * B(128x16) in 4 bits, one exponent a lane: lane l
-// feeds row (column) l % 16, columns (rows) 32 (l / 16) .. + 31; byte SA of sa and
-// SB of sb hold the exponents.
-template <int SA, int SB>
-__device__ __forceinline__ f32x4 mfma_mx4(u32x4 a, u32x4 b, f32x4 c, uint32_t sa, uint32_t sb) {
-  const i32x8 av = {static_cast<int>(a[0]), static_cast<int>(a[1]), static_cast<int>(a[2]), static_cast<int>(a[3]), 0, 0, 0, 0};
-  const i32x8 bv = {static_cast<int>(b[0]), static_cast<int>(b[1]), static_cast<int>(b[2]), static_cast<int>(b[3]), 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, c, 4, 4, SA, static_cast<int>(sa), SB, static_cast<int>(sb));
-}
 
 // ------------------------------------------------------------------ quantisation
 // A block (32 values of a row) a thread, a tile (16 rows x 4 blocks) a wave, so
@@ -200,18 +187,6 @@ hipError_t launch_mx4_read(const uint8_t* mx, int rows, int k, void* dst, int dt
 }
 
 // ------------------------------------------------------------------ product
-// y[r][c] (+ add) from a float32 sum, rounded once.
-__device__ __forceinline__ void mx4_store(const Mx4ProductArgs& a, int r, int c, float v) {
-  const int64_t at = r * a.y_stride + c;
-  if (a.y_fp32) {
-    if (a.add != nullptr) v += static_cast<const float*>(a.add)[at];
-    static_cast<float*>(a.y)[at] = v;
-  } else {
-    if (a.add != nullptr) v += bf2f(static_cast<const uint16_t*>(a.add)[at]);
-    static_cast<uint16_t*>(a.y)[at] = static_cast<uint16_t>(f2bf(v));
-  }
-}
-
 // Weights streamed: a workgroup takes 16 columns and up to 16 RG rows, its eight
 // waves an eighth of K each; their sums are added in wave order.
 constexpr int kMxWaves = 8;
@@ -261,15 +236,13 @@ __global__ __launch_bounds__(64 * kMxWaves) void k_mx4_stream(Mx4ProductArgs a) 
 #pragma unroll
     for (int i = 1; i < kMxWaves; ++i) y += part[i][g][lane];
     const int row = 16 * (g0 + g) + (lane & 15), c0 = 16 * nt + 4 * (lane >> 4);
-    if (row >= a.rows) continue;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (c0 + r < a.n) mx4_store(a, row, c0 + r, y[r]);
+    if (row < a.rows) mx4_store4(a, row, c0, y);
   }
 }
 
 hipError_t launch_mx4_product(const Mx4ProductArgs& a, hipStream_t s) {
   const int nt = (a.n + 15) / 16, rg = (a.rows + 15) / 16;
+  if (rg > 8) return launch_mx4_tile(a, s);
   if (rg <= 1) hipLaunchKernelGGL((k_mx4_stream<1>), dim3(nt, 1), dim3(64 * kMxWaves), 0, s, a);
   else hipLaunchKernelGGL((k_mx4_stream<4>), dim3(nt, (rg + 3) / 4), dim3(64 * kMxWaves), 0, s, a);
   return hipGetLastError();

@@ -99,6 +99,8 @@ int vsk_mx4_product(const void* x_dev, int32_t x_dtype, int64_t x_stride, const 
   a.y_fp32 = y_dtype == VSK_FP32;
   a.y_stride = y_stride;
   a.add = add_dev;
+  const size_t four = 4 * element(y_dtype);
+  a.wide = y_stride % 4 == 0 && aligned(y_dev, four) && aligned(add_dev, four);
   return launched(launch_mx4_product(a, s));
 }
 

@@ -42,7 +42,9 @@ struct Mx4ProductArgs {
   int y_fp32;
   int64_t y_stride;
   const void* add;  // nullable, as y
+  int wide;  // y, add and their rows allow vectors of four
 };
 hipError_t launch_mx4_product(const Mx4ProductArgs& a, hipStream_t s);
+hipError_t launch_mx4_tile(const Mx4ProductArgs& a, hipStream_t s);  // many rows (k_mx4_tile.hip)
 
 }  // namespace vsk

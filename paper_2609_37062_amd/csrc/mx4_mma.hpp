@@ -1,0 +1,53 @@
+// The scaled matrix instruction on 4-bit operands, and what a product leaves.
+#pragma once
+
+#include "mx4.hpp"
+#include "mx4_dev.hpp"
+
+namespace vsk {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// D(16x16, f32) += A(16x128) * B(128x16) in 4 bits, one exponent a lane: lane l
+// feeds row (column) l % 16, columns (rows) 32 (l / 16) .. + 31; byte SA of sa and
+// SB of sb hold the exponents.
+template <int SA, int SB>
+__device__ __forceinline__ f32x4 mfma_mx4(u32x4 a, u32x4 b, f32x4 c, uint32_t sa, uint32_t sb) {
+  const i32x8 av = {static_cast<int>(a[0]), static_cast<int>(a[1]), static_cast<int>(a[2]), static_cast<int>(a[3]), 0, 0, 0, 0};
+  const i32x8 bv = {static_cast<int>(b[0]), static_cast<int>(b[1]), static_cast<int>(b[2]), static_cast<int>(b[3]), 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, c, 4, 4, SA, static_cast<int>(sa), SB, static_cast<int>(sb));
+}
+
+// y[row][c0 .. c0 + 3] (+ add) from float32 sums, rounded once.  a.wide: rows and
+// their first elements allow stores of four.
+__device__ __forceinline__ void mx4_store4(const Mx4ProductArgs& a, int row, int c0, f32x4 v) {
+  const int64_t at = row * a.y_stride + c0;
+  if (a.wide && c0 + 3 < a.n) {
+    if (a.y_fp32) {
+      if (a.add != nullptr) v += *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.add) + at);
+      *reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + at) = v;
+    } else {
+      if (a.add != nullptr) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(a.add) + at);
+        v += f32x4{bf2f(x[0] & 0xffffu), __uint_as_float(x[0] & 0xffff0000u), bf2f(x[1] & 0xffffu), __uint_as_float(x[1] & 0xffff0000u)};
+      }
+      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.y) + at) = u32x2{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
+    }
+    return;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    if (c0 + r >= a.n) continue;
+    if (a.y_fp32) {
+      float x = v[r];
+      if (a.add != nullptr) x += static_cast<const float*>(a.add)[at + r];
+      static_cast<float*>(a.y)[at + r] = x;
+    } else {
+      float x = v[r];
+      if (a.add != nullptr) x += bf2f(static_cast<const uint16_t*>(a.add)[at + r]);
+      static_cast<uint16_t*>(a.y)[at + r] = static_cast<uint16_t>(f2bf(x));
+    }
+  }
+}
+
+}  // namespace vsk
