@@ -353,8 +353,8 @@ int vsk_mx4_read(const void* mx_dev, int32_t rows, int32_t k, void* dst_dev, int
  * matrix (x_stride then counts for nothing).  Products are exact, sums float32, one
  * rounding to y's type, VSK_BF16 or VSK_FP32.  add_dev (nullable) is of y's type
  * and stride, and may be y_dev.  ws_dev: device scratch of at least
- * vsk_mx4_product_bytes, 256-byte aligned (unused, and nullable, where x is MX4);
- * concurrent calls need one each.  Can be captured. */
+ * vsk_mx4_product_bytes, 256-byte aligned, whatever it holds; calls that may run
+ * at the same time (captured ones too) need one each.  Can be captured. */
 size_t vsk_mx4_product_bytes(int32_t rows, int32_t n, int32_t k);
 int vsk_mx4_product(const void* x_dev, int32_t x_dtype, int64_t x_stride, const void* w_mx_dev, int32_t rows, int32_t n,
                     int32_t k, void* y_dev, int32_t y_dtype, int64_t y_stride, const void* add_dev, void* ws_dev,

@@ -7,84 +7,93 @@
 namespace vsk {
 
 // ------------------------------------------------------------------ quantisation
-// A block (32 values of a row) a thread, a tile (16 rows x 4 blocks) a wave, so
-// that a tile's codes are one contiguous store.  VEC: rows are 16-byte aligned
-// and k a multiple of 32.  Bound by memory: 2 (4) bytes a value read, 17/32
-// written.
-template <bool FP32, bool VEC>
+// Eight values of a row in registers, a quarter of a block, four lanes a block: a
+// load of a wave then takes whole lines (4 rows x 256 bytes in bf16; with a block a
+// lane it touched 64 of them: 16 x 11008 by every workgroup of a product took 9 us).
+// WIDE: p is 16-byte aligned and cnt 8 or 0; cnt values count, the others as zero.
+__device__ __forceinline__ uint32_t max_of_quad(uint32_t v) {
+  v = max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0xb1, 0xf, 0xf, true)));  // lane ^ 1
+  return max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x4e, 0xf, 0xf, true)));  // lane ^ 2
+}
+template <bool FP32>
+using Mx4Elem = std::conditional_t<FP32, float, uint16_t>;
+template <bool FP32>
+struct Mx4Eight {
+  u32x4 v[FP32 ? 2 : 1];
+  template <bool WIDE>
+  __device__ __forceinline__ void load(const Mx4Elem<FP32>* p, int cnt) {
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int i = 0; i < (FP32 ? 2 : 1); ++i) v[i] = cnt > 0 ? reinterpret_cast<const u32x4*>(p)[i] : u32x4{0u, 0u, 0u, 0u};
+    } else if constexpr (FP32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = i < cnt ? __float_as_uint(p[i]) : 0u;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[0][i] = (2 * i < cnt ? p[2 * i] : 0u) | (2 * i + 1 < cnt ? static_cast<uint32_t>(p[2 * i + 1]) : 0u) << 16;
+    }
+  }
+  // the codes, and the block's exponent (on each of its four lanes)
+  __device__ __forceinline__ uint32_t encode(uint32_t& e) const {
+    uint32_t top = 0, c;
+    if constexpr (FP32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, v[i >> 2][i & 3] & 0x7fffffffu);
+    } else {
+      top = mx4_top(mx4_top2(mx4_top2(v[0][0] & 0x7fff7fffu, v[0][1] & 0x7fff7fffu),
+                             mx4_top2(v[0][2] & 0x7fff7fffu, v[0][3] & 0x7fff7fffu)));
+    }
+    e = mx4_exponent(max_of_quad(top));
+    const float sc = mx4_scale(e);
+    if constexpr (FP32) {
+      auto f = [&](int i) { return __uint_as_float(v[i >> 2][i & 3]); };
+      c = mx4_encode_f32<0>(0u, f(0), f(1), sc);
+      c = mx4_encode_f32<1>(c, f(2), f(3), sc);
+      c = mx4_encode_f32<2>(c, f(4), f(5), sc);
+      c = mx4_encode_f32<3>(c, f(6), f(7), sc);
+    } else {
+      c = mx4_encode_bf16<0>(0u, v[0][0], sc);
+      c = mx4_encode_bf16<1>(c, v[0][1], sc);
+      c = mx4_encode_bf16<2>(c, v[0][2], sc);
+      c = mx4_encode_bf16<3>(c, v[0][3], sc);
+    }
+    return e == 255u ? 0u : c;
+  }
+};
+
+// A tile (16 rows x 4 blocks) a wave, four rows at a time.  Bound by memory: 2 (4)
+// bytes a value read, 17/32 written.
+template <bool FP32, bool WIDE>
 __global__ __launch_bounds__(256) void k_mx4_quantise(const void* __restrict__ src, int64_t stride, int rows, int k,
-                                                      uint8_t* __restrict__ mx, int kt_n, int n_tiles, size_t scales_at) {
+                                                      uint8_t* __restrict__ mx, int kt_n, int n_tiles, size_t scales_at,
+                                                      int* __restrict__ counters, int n_counters) {
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n_counters; i += gridDim.x * 256) counters[i] = 0;
   const int lane = threadIdx.x & 63;
   const int tile = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (tile >= n_tiles) return;
   const int rt = tile / kt_n, kt = tile - rt * kt_n;
-  const int row = 16 * rt + (lane & 15), k0 = 128 * kt + 32 * (lane >> 4);
-  const int cnt = row < rows ? min(32, max(0, k - k0)) : 0;
-  u32x4 codes = u32x4{0u, 0u, 0u, 0u};
-  uint32_t e = 0;
-  const int64_t at = row * stride + k0;
-  if constexpr (FP32) {
-    float v[32];
-    uint32_t top = 0;
-    const float* p = static_cast<const float*>(src) + at;
+  const int r0 = lane >> 4, b = lane >> 2 & 3, k0 = 128 * kt + 8 * (lane & 15);
+  Mx4Eight<FP32> x[4];
 #pragma unroll
-    for (int i = 0; i < 32; i += 4) {
-      if constexpr (VEC) {
-        const f32x4 x = cnt > 0 ? *reinterpret_cast<const f32x4*>(p + i) : f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < 4; ++i) {
+    const int row = 16 * rt + 4 * i + r0;
+    x[i].template load<WIDE>(static_cast<const Mx4Elem<FP32>*>(src) + row * stride + k0, row < rows ? min(8, max(0, k - k0)) : 0);
+  }
+  uint32_t* codes = reinterpret_cast<uint32_t*>(mx + static_cast<size_t>(tile) * 1024) + (lane & 3);
+  uint8_t* expo = mx + scales_at + ((static_cast<size_t>(rt) * ((kt_n + 3) / 4) + kt / 4) * 64) * 4;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[i + j] = x[j];
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[i + j] = i + j < cnt ? p[i + j] : 0.f;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-    e = mx4_exponent(top);
-    const float sc = mx4_scale(e);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint32_t c = mx4_encode_f32<0>(0u, v[8 * j], v[8 * j + 1], sc);
-      c = mx4_encode_f32<1>(c, v[8 * j + 2], v[8 * j + 3], sc);
-      c = mx4_encode_f32<2>(c, v[8 * j + 4], v[8 * j + 5], sc);
-      codes[j] = mx4_encode_f32<3>(c, v[8 * j + 6], v[8 * j + 7], sc);
-    }
-  } else {
-    uint32_t v[16];
-    uint32_t top = 0;
-    const uint16_t* p = static_cast<const uint16_t*>(src) + at;
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      if constexpr (VEC) {
-        const u32x4 x = cnt > 0 ? *reinterpret_cast<const u32x4*>(p + 2 * i) : u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[i + j] = x[j];
-      } else {
-#pragma unroll
-        for (int j = i; j < i + 4; ++j)
-          v[j] = (2 * j < cnt ? p[2 * j] : 0u) | (2 * j + 1 < cnt ? static_cast<uint32_t>(p[2 * j + 1]) : 0u) << 16;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) top = mx4_top2(top, v[i] & 0x7fff7fffu);
-    e = mx4_exponent(mx4_top(top));
-    const float sc = mx4_scale(e);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint32_t c = mx4_encode_bf16<0>(0u, v[4 * j], sc);
-      c = mx4_encode_bf16<1>(c, v[4 * j + 1], sc);
-      c = mx4_encode_bf16<2>(c, v[4 * j + 2], sc);
-      codes[j] = mx4_encode_bf16<3>(c, v[4 * j + 3], sc);
+  for (int i = 0; i < 4; ++i) {
+    const int at = 4 * i + r0 + 16 * b;  // the block's place in the tile
+    uint32_t e;
+    codes[4 * at] = x[i].encode(e);
+    if ((lane & 3) == 0) {
+      expo[4 * at + (kt & 3)] = static_cast<uint8_t>(e);
+      // (the last tile of a row of tiles fills up its four)
+      if (kt == kt_n - 1)
+        for (int j = (kt & 3) + 1; j < 4; ++j) expo[4 * at + j] = 0;
     }
   }
-  if (e == 255u) codes = u32x4{0u, 0u, 0u, 0u};
-  *reinterpret_cast<u32x4*>(mx + (static_cast<size_t>(tile) * 64 + lane) * 16) = codes;
-  const int kq_n = (kt_n + 3) / 4;
-  uint8_t* sp = mx + scales_at + ((static_cast<size_t>(rt) * kq_n + kt / 4) * 64 + lane) * 4;
-  sp[kt & 3] = static_cast<uint8_t>(e);
-  // (the last tile of a row of tiles fills up its four)
-  if (kt == kt_n - 1)
-    for (int j = (kt & 3) + 1; j < 4; ++j) sp[j] = 0;
 }
 
 // Codes [rows][ceil(k / 2)] and exponents [rows][ceil(k / 32)] as files hold them.
@@ -153,16 +162,19 @@ __global__ __launch_bounds__(256) void k_mx4_read(const uint8_t* __restrict__ mx
   }
 }
 
+// Rows that wide loads and stores of eight values take.
 static bool rows_aligned(const void* p, int64_t stride, int k, int size) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0 && k % 32 == 0;
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0 && k % 8 == 0;
 }
 
-hipError_t launch_mx4_quantise(const void* src, int dtype, int64_t stride, int rows, int k, uint8_t* mx, hipStream_t s) {
+hipError_t launch_mx4_quantise(const void* src, int dtype, int64_t stride, int rows, int k, uint8_t* mx, int* counters,
+                               int n_counters, hipStream_t s) {
+  if (counters == nullptr) n_counters = 0;
   const Mx4Shape g(rows, k);
   const int n = static_cast<int>(g.rt * g.kt);
   const dim3 grid((n + 3) / 4), block(256);
   const bool fp32 = dtype == kMxFp32, vec = rows_aligned(src, stride, k, fp32 ? 4 : 2);
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, s, src, stride, rows, k, mx, static_cast<int>(g.kt), n, g.scales_at()); };
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, s, src, stride, rows, k, mx, static_cast<int>(g.kt), n, g.scales_at(), counters, n_counters); };
   if (fp32) vec ? go(k_mx4_quantise<true, true>) : go(k_mx4_quantise<true, false>);
   else vec ? go(k_mx4_quantise<false, true>) : go(k_mx4_quantise<false, false>);
   return hipGetLastError();
@@ -187,64 +199,231 @@ hipError_t launch_mx4_read(const uint8_t* mx, int rows, int k, void* dst, int dt
 }
 
 // ------------------------------------------------------------------ product
-// Weights streamed: a workgroup takes 16 columns and up to 16 RG rows, its eight
-// waves an eighth of K each; their sums are added in wave order.
+// Up to four rows as they are: weights streamed.  A workgroup takes 16 columns at a
+// time (tiles blockIdx.x, + gridDim.x, ..), its eight waves every eighth four of K's
+// steps of 128 columns each; their sums are added in wave order.  Each wave first
+// quantises its part of x into LDS, which it alone reads: a launch less.
+//
+// A four's weights are in flight while the four before is used: two sets of registers
+// in turn, loads without a branch around them (behind a branch, or copied from
+// register to register, the compiler waits for all of them).
 constexpr int kMxWaves = 8;
-template <int RG>
+constexpr int kMxRawRows = 4;    // (16 rows: 16 x 4096 x 4096 7.2 us, quantised by a launch of its own 7.1)
+constexpr int kMxResident = 48;  // most steps of K of x in LDS (with two workgroups a compute unit)
+template <bool FP32>
 __global__ __launch_bounds__(64 * kMxWaves) void k_mx4_stream(Mx4ProductArgs a) {
-  __shared__ f32x4 part[kMxWaves][RG][64];
-  const Mx4Shape gw(a.n, a.k), gx(a.rows, a.k);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int nt = blockIdx.x, g0 = blockIdx.y * RG;
+  __shared__ f32x4 s_part[2][kMxWaves][64];
+  extern __shared__ __align__(16) unsigned char s_x[];  // [kt][64] codes, [kt][64] exponents
+  const Mx4Shape gw(a.n, a.k);
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kt_n = static_cast<int>(gw.kt), kq_n = static_cast<int>(gw.kq);
-  const int groups = min(RG, static_cast<int>(gx.rt) - g0);
-  const u32x4* wp = reinterpret_cast<const u32x4*>(a.w) + static_cast<size_t>(nt) * kt_n * 64 + lane;
-  const uint32_t* ws = reinterpret_cast<const uint32_t*>(a.w + gw.scales_at()) + static_cast<size_t>(nt) * kq_n * 64 + lane;
-  const u32x4* xp = reinterpret_cast<const u32x4*>(a.x) + static_cast<size_t>(g0) * kt_n * 64 + lane;
-  const uint32_t* xs = reinterpret_cast<const uint32_t*>(a.x + gx.scales_at()) + static_cast<size_t>(g0) * kq_n * 64 + lane;
-  f32x4 acc[RG];
+  const int tiles = (static_cast<int>(gw.rt) - static_cast<int>(blockIdx.x) + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x);
+  const int fours = kq_n > w ? (kq_n - w + kMxWaves - 1) / kMxWaves : 0;  // this wave's, of a tile
+  u32x4* lx = reinterpret_cast<u32x4*>(s_x);
+  unsigned char* le = s_x + static_cast<size_t>(kt_n) * 1024;
+  struct Four {
+    u32x4 w[4];
+    uint32_t s;
+  };
+  int lt = blockIdx.x, lq = w;  // the next four to load
+  auto load = [&](Four& f) __attribute__((always_inline)) {
+    const u32x4* wp = reinterpret_cast<const u32x4*>(a.w) + static_cast<size_t>(lt) * kt_n * 64 + lane;
+    f.s = reinterpret_cast<const uint32_t*>(a.w + gw.scales_at())[(static_cast<size_t>(lt) * kq_n + lq) * 64 + lane];
 #pragma unroll
-  for (int g = 0; g < RG; ++g) acc[g] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int q = w; q < kq_n; q += kMxWaves) {
-    const int left = min(4, kt_n - 4 * q);
-    const uint32_t sw = ws[static_cast<size_t>(q) * 64];
-    uint32_t sx[RG];
+    for (int j = 0; j < 4; ++j) f.w[j] = __builtin_nontemporal_load(wp + static_cast<size_t>(min(4 * lq + j, kt_n - 1)) * 64);
+    lq += kMxWaves;
+    if (lq >= kq_n) {
+      lq = w;
+      lt += gridDim.x;
+    }
+  };
+  const int n = tiles * fours;
+  Four fa, fb;
+  if (n > 0) load(fa);
+  {
+    // (row lane / 16 of four, a quarter of a block)
+    const int row = lane >> 4, at = row + 16 * (lane >> 2 & 3), c = 8 * (lane & 15);
+    for (int q = w; q < kq_n; q += kMxWaves) {
+      Mx4Eight<FP32> v[4];
 #pragma unroll
-    for (int g = 0; g < RG; ++g) sx[g] = xs[(static_cast<size_t>(min(g, groups - 1)) * kq_n + q) * 64];
-    auto one = [&](auto jc) {
-      constexpr int J = decltype(jc)::value;
-      if (J >= left) return;
-      const size_t kt = 4 * static_cast<size_t>(q) + J;
-      const u32x4 wv = wp[kt * 64];
-#pragma unroll
-      for (int g = 0; g < RG; ++g) {
-        const u32x4 xv = xp[(static_cast<size_t>(min(g, groups - 1)) * kt_n + kt) * 64];
-        acc[g] = mfma_mx4<J, J>(wv, xv, acc[g], sw, sx[g]);
+      for (int j = 0; j < 4; ++j) {
+        const int kk = 128 * (4 * q + j) + c;
+        v[j].template load<true>(static_cast<const Mx4Elem<FP32>*>(a.x_raw) + row * a.x_stride + kk, row < a.rows && kk < a.k ? 8 : 0);
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int kt = 4 * q + j;
+        if (kt >= kt_n) break;
+        uint32_t e;
+        const uint32_t codes = v[j].encode(e);
+        uint32_t* to = reinterpret_cast<uint32_t*>(lx + static_cast<size_t>(kt) * 64 + at) + (lane & 3);
+        to[0] = codes;
+        to[16] = to[32] = to[48] = 0u;  // rows 4 .. 15 are none
+        if ((lane & 3) == 0) {
+          unsigned char* te = le + kt * 64 + at;
+          te[0] = static_cast<unsigned char>(e);
+          te[4] = te[8] = te[12] = 0;
+        }
+      }
+    }
+  }
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  int t = 0, cq = 0;  // the tile and four in use
+  auto finish = [&]() __attribute__((always_inline)) {
+    // (the lane holds columns 16 nt + 4 (lane / 16) + r of row lane % 16)
+    f32x4(&p)[kMxWaves][64] = s_part[t & 1];
+    p[w][lane] = acc;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    barrier_after_lds_reads();
+    if (w == t % kMxWaves) {
+      f32x4 y = p[0][lane];
+#pragma unroll
+      for (int i = 1; i < kMxWaves; ++i) y += p[i][lane];
+      if ((lane & 15) < a.rows) mx4_store4(a, lane & 15, 16 * static_cast<int>(blockIdx.x + t * gridDim.x) + 4 * (lane >> 4), y);
+    }
+    ++t;
+    cq = 0;
+  };
+  auto use = [&](const Four& f) __attribute__((always_inline)) {
+    const int q = w + cq * kMxWaves;
+    auto one = [&](auto jc) __attribute__((always_inline)) {
+      constexpr int J = decltype(jc)::value;
+      const int kt = 4 * q + J;
+      if (kt < kt_n) acc = mfma_mx4<J, 0>(f.w[J], lx[kt * 64 + lane], acc, f.s, le[kt * 64 + lane]);
     };
     one(std::integral_constant<int, 0>{});
     one(std::integral_constant<int, 1>{});
     one(std::integral_constant<int, 2>{});
     one(std::integral_constant<int, 3>{});
+    if (++cq == fours) finish();
+  };
+  int i = 0;
+  for (; i + 2 < n; i += 2) {
+    load(fb);
+    use(fa);
+    load(fa);
+    use(fb);
+  }
+  if (i + 1 < n) {
+    load(fb);
+    use(fa);
+    use(fb);
+  } else if (i < n) {
+    use(fa);
+  }
+  while (t < tiles) finish();  // (a wave without a four of K)
+}
+
+bool mx4_takes_rows(int dtype, const void* x, int64_t stride, int rows, int k) {
+  return rows <= kMxRawRows && k <= 128 * kMxResident && rows_aligned(x, stride, k, dtype == kMxFp32 ? 4 : 2);
+}
+
+hipError_t launch_mx4_stream(const Mx4ProductArgs& a, hipStream_t s) {
+  const Mx4Shape g(a.n, a.k);
+  // one workgroup a compute unit up to two tiles each, beyond that two
+  const int nt = static_cast<int>(g.rt), most = nt <= 512 ? 256 : 512, tiles = (nt + most - 1) / most;
+  const dim3 grid((nt + tiles - 1) / tiles), block(64 * kMxWaves);
+  const size_t lds = static_cast<size_t>(g.kt) * 1088;
+  if (a.x_fp32) hipLaunchKernelGGL(k_mx4_stream<true>, grid, block, lds, s, a);
+  else hipLaunchKernelGGL(k_mx4_stream<false>, grid, block, lds, s, a);
+  return hipGetLastError();
+}
+
+// Up to 128 rows: a workgroup takes 16 columns and 16 RG rows, its eight waves every
+// eighth two of K's steps each; x comes from the caches.  Two steps' tiles are in
+// flight while the two before are used (see k_mx4_stream).
+template <int RG>
+__global__ __launch_bounds__(64 * kMxWaves) void k_mx4_rows(Mx4ProductArgs a) {
+  __shared__ f32x4 part[kMxWaves][RG][64];
+  const Mx4Shape gw(a.n, a.k), gx(a.rows, a.k);
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int nt = blockIdx.x, g0 = blockIdx.y * RG;
+  const int kt_n = static_cast<int>(gw.kt), kq_n = static_cast<int>(gw.kq);
+  const u32x4* wp = reinterpret_cast<const u32x4*>(a.w) + static_cast<size_t>(nt) * kt_n * 64;
+  const uint32_t* ws = reinterpret_cast<const uint32_t*>(a.w + gw.scales_at()) + static_cast<size_t>(nt) * kq_n * 64;
+  const u32x4* xp[RG];
+  const uint32_t* xs[RG];
+#pragma unroll
+  for (int g = 0; g < RG; ++g) {  // (groups past the last one: it again, its sums are not stored)
+    const int64_t t = min(static_cast<int64_t>(g0 + g), gx.rt - 1);
+    xp[g] = reinterpret_cast<const u32x4*>(a.x) + t * kt_n * 64;
+    xs[g] = reinterpret_cast<const uint32_t*>(a.x + gx.scales_at()) + t * kq_n * 64;
+  }
+  f32x4 acc[RG];
+#pragma unroll
+  for (int g = 0; g < RG; ++g) acc[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+  struct Two {
+    u32x4 w[2], x[2][RG];
+    uint32_t sw, sx[RG];
+  };
+  auto load = [&](Two& s, int i) __attribute__((always_inline)) {
+    const int h = w + i * kMxWaves, q = h >> 1;
+    const size_t k0 = 2 * h, k1 = min(2 * h + 1, kt_n - 1);
+    s.sw = ws[static_cast<size_t>(q) * 64 + lane];
+    s.w[0] = __builtin_nontemporal_load(wp + k0 * 64 + lane);
+    s.w[1] = __builtin_nontemporal_load(wp + k1 * 64 + lane);
+#pragma unroll
+    for (int g = 0; g < RG; ++g) {
+      s.sx[g] = xs[g][static_cast<size_t>(q) * 64 + lane];
+      s.x[0][g] = xp[g][k0 * 64 + lane];
+      s.x[1][g] = xp[g][k1 * 64 + lane];
+    }
+  };
+  auto use = [&](const Two& s, int i) __attribute__((always_inline)) {
+    const int h = w + i * kMxWaves, sh = 16 * (h & 1);
+    const uint32_t sw = s.sw >> sh;
+#pragma unroll
+    for (int g = 0; g < RG; ++g) acc[g] = mfma_mx4<0, 0>(s.w[0], s.x[0][g], acc[g], sw, s.sx[g] >> sh);
+    if (2 * h + 1 < kt_n) {
+#pragma unroll
+      for (int g = 0; g < RG; ++g) acc[g] = mfma_mx4<1, 1>(s.w[1], s.x[1][g], acc[g], sw, s.sx[g] >> sh);
+    }
+  };
+  const int twos = (kt_n + 1) / 2, n = twos > w ? (twos - w + kMxWaves - 1) / kMxWaves : 0;
+  Two sa, sb;
+  if (n > 0) load(sa, 0);
+  int i = 0;
+  for (; i + 2 < n; i += 2) {
+    load(sb, i + 1);
+    use(sa, i);
+    load(sa, i + 2);
+    use(sb, i + 1);
+  }
+  if (i + 1 < n) {
+    load(sb, i + 1);
+    use(sa, i);
+    use(sb, i + 1);
+  } else if (i < n) {
+    use(sa, i);
   }
 #pragma unroll
   for (int g = 0; g < RG; ++g) part[w][g][lane] = acc[g];
   __syncthreads();
-  // (the lane holds columns 16 nt + 4 (lane / 16) + r of row lane % 16)
-  for (int g = w; g < groups; g += kMxWaves) {
+  for (int g = w; g < RG; g += kMxWaves) {
     f32x4 y = part[0][g][lane];
 #pragma unroll
-    for (int i = 1; i < kMxWaves; ++i) y += part[i][g][lane];
-    const int row = 16 * (g0 + g) + (lane & 15), c0 = 16 * nt + 4 * (lane >> 4);
-    if (row < a.rows) mx4_store4(a, row, c0, y);
+    for (int j = 1; j < kMxWaves; ++j) y += part[j][g][lane];
+    const int row = 16 * (g0 + g) + (lane & 15);
+    if (row < a.rows) mx4_store4(a, row, 16 * nt + 4 * (lane >> 4), y);
   }
 }
 
-hipError_t launch_mx4_product(const Mx4ProductArgs& a, hipStream_t s) {
+hipError_t launch_mx4_rows(const Mx4ProductArgs& a, hipStream_t s) {
   const int nt = (a.n + 15) / 16, rg = (a.rows + 15) / 16;
-  if (rg > 8) return launch_mx4_tile(a, s);
-  if (rg <= 1) hipLaunchKernelGGL((k_mx4_stream<1>), dim3(nt, 1), dim3(64 * kMxWaves), 0, s, a);
-  else hipLaunchKernelGGL((k_mx4_stream<4>), dim3(nt, (rg + 3) / 4), dim3(64 * kMxWaves), 0, s, a);
+  auto go = [&](auto c) {
+    constexpr int RG = decltype(c)::value;
+    hipLaunchKernelGGL((k_mx4_rows<RG>), dim3(nt, (rg + RG - 1) / RG), dim3(64 * kMxWaves), 0, s, a);
+  };
+  switch (rg) {
+    case 1: go(std::integral_constant<int, 1>{}); break;
+    case 2: go(std::integral_constant<int, 2>{}); break;
+    case 3: go(std::integral_constant<int, 3>{}); break;
+    case 4: go(std::integral_constant<int, 4>{}); break;
+    case 5: go(std::integral_constant<int, 5>{}); break;
+    case 6: go(std::integral_constant<int, 6>{}); break;
+    case 7: go(std::integral_constant<int, 7>{}); break;
+    default: go(std::integral_constant<int, 8>{}); break;
+  }
   return hipGetLastError();
 }
 

@@ -2,6 +2,7 @@
 #include "mx4.hpp"
 
 #include <climits>
+#include <cstdlib>
 #include <cstdint>
 
 #include "../../include/vsk.h"
@@ -39,7 +40,7 @@ int vsk_mx4_quantise(const void* src_dev, int32_t dtype, int64_t stride, int32_t
   if (!src_dev || !mx_dev || !shape_ok(rows, k) || (dtype != VSK_BF16 && dtype != VSK_FP32) || stride < k) return VSK_E_ARG;
   if (!aligned(mx_dev, kAlign) || !aligned(src_dev, element(dtype))) return VSK_E_ARG;
   if (overlap(src_dev, extent(rows, k, stride, element(dtype)), mx_dev, vsk_mx4_bytes(rows, k))) return VSK_E_ARG;
-  return launched(launch_mx4_quantise(src_dev, dtype, stride, rows, k, static_cast<uint8_t*>(mx_dev),
+  return launched(launch_mx4_quantise(src_dev, dtype, stride, rows, k, static_cast<uint8_t*>(mx_dev), nullptr, 0,
                                       static_cast<hipStream_t>(stream)));
 }
 
@@ -61,36 +62,45 @@ int vsk_mx4_read(const void* mx_dev, int32_t rows, int32_t k, void* dst_dev, int
                                   static_cast<hipStream_t>(stream)));
 }
 
+// A product's workspace: x as an MX4 matrix, the arrival counters, the split sums.
+namespace {
+struct ProductWs {
+  size_t counter, part, total;
+  Mx4Split sp;
+  ProductWs(int32_t rows, int32_t n, int32_t k) : sp{} {
+    counter = vsk_mx4_bytes(rows, k);
+    sp = mx4_split(rows, n, k);
+    part = counter + align_up(sp.counter_bytes());
+    total = part + align_up(sp.part_bytes());
+  }
+};
+}  // namespace
+
 size_t vsk_mx4_product_bytes(int32_t rows, int32_t n, int32_t k) {
-  return shape_ok(n, k) ? vsk_mx4_bytes(rows, k) : 0;
+  return shape_ok(rows, k) && shape_ok(n, k) ? ProductWs(rows, n, k).total : 0;
 }
 
 int vsk_mx4_product(const void* x_dev, int32_t x_dtype, int64_t x_stride, const void* w_mx_dev, int32_t rows, int32_t n,
                     int32_t k, void* y_dev, int32_t y_dtype, int64_t y_stride, const void* add_dev, void* ws_dev,
                     size_t ws_bytes, void* stream) {
-  if (!x_dev || !w_mx_dev || !y_dev || !shape_ok(rows, k) || !shape_ok(n, k)) return VSK_E_ARG;
+  if (!x_dev || !w_mx_dev || !y_dev || !ws_dev || !shape_ok(rows, k) || !shape_ok(n, k)) return VSK_E_ARG;
   if (x_dtype != VSK_BF16 && x_dtype != VSK_FP32 && x_dtype != VSK_MX4) return VSK_E_ARG;
   if ((y_dtype != VSK_BF16 && y_dtype != VSK_FP32) || y_stride < n) return VSK_E_ARG;
   const bool mx = x_dtype == VSK_MX4;
   if (mx ? !aligned(x_dev, kAlign) : x_stride < k || !aligned(x_dev, element(x_dtype))) return VSK_E_ARG;
   if (!aligned(w_mx_dev, kAlign) || !aligned(y_dev, element(y_dtype)) || !aligned(add_dev, element(y_dtype))) return VSK_E_ARG;
-  const size_t need = mx ? 0 : vsk_mx4_product_bytes(rows, n, k);
-  if (need > 0 && (!ws_dev || ws_bytes < need || !aligned(ws_dev, kAlign))) return VSK_E_ARG;
+  const ProductWs ws(rows, n, k);
+  if (ws_bytes < ws.total || !aligned(ws_dev, kAlign)) return VSK_E_ARG;
   const size_t xb = mx ? vsk_mx4_bytes(rows, k) : extent(rows, k, x_stride, element(x_dtype));
   const size_t wb = vsk_mx4_bytes(n, k), yb = extent(rows, n, y_stride, element(y_dtype));
   if (overlap(y_dev, yb, x_dev, xb) || overlap(y_dev, yb, w_mx_dev, wb)) return VSK_E_ARG;
   if (add_dev && add_dev != y_dev && overlap(y_dev, yb, add_dev, yb)) return VSK_E_ARG;
-  if (need > 0 && (overlap(ws_dev, need, x_dev, xb) || overlap(ws_dev, need, w_mx_dev, wb) ||
-                   overlap(ws_dev, need, y_dev, yb) || (add_dev && overlap(ws_dev, need, add_dev, yb))))
+  if (overlap(ws_dev, ws.total, x_dev, xb) || overlap(ws_dev, ws.total, w_mx_dev, wb) ||
+      overlap(ws_dev, ws.total, y_dev, yb) || (add_dev && overlap(ws_dev, ws.total, add_dev, yb)))
     return VSK_E_ARG;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  uint8_t* base = static_cast<uint8_t*>(ws_dev);
   Mx4ProductArgs a{};
-  a.x = static_cast<const uint8_t*>(x_dev);
-  if (!mx) {
-    const hipError_t e = launch_mx4_quantise(x_dev, x_dtype, x_stride, rows, k, static_cast<uint8_t*>(ws_dev), s);
-    if (e != hipSuccess) return VSK_E_HIP;
-    a.x = static_cast<const uint8_t*>(ws_dev);
-  }
   a.w = static_cast<const uint8_t*>(w_mx_dev);
   a.rows = rows;
   a.n = n;
@@ -100,8 +110,27 @@ int vsk_mx4_product(const void* x_dev, int32_t x_dtype, int64_t x_stride, const 
   a.y_stride = y_stride;
   a.add = add_dev;
   const size_t four = 4 * element(y_dtype);
-  a.wide = y_stride % 4 == 0 && aligned(y_dev, four) && aligned(add_dev, four);
-  return launched(launch_mx4_product(a, s));
+  a.wide = y_stride % 4 != 0 || !aligned(y_dev, four) || !aligned(add_dev, four) ? 0 : y_stride % 8 == 0 && aligned(y_dev, 16) ? 2 : 1;
+  Mx4Split sp = ws.sp;
+  int* counter = sp.splits > 1 ? reinterpret_cast<int*>(base + ws.counter) : nullptr;
+  sp.counter = counter;
+  sp.part = reinterpret_cast<decltype(sp.part)>(base + ws.part);
+  hipError_t e = hipSuccess;
+  if (mx) {
+    a.x = static_cast<const uint8_t*>(x_dev);
+    if (counter) e = launch_fill_zero(counter, sp.counter_bytes(), s);
+  } else if (mx4_takes_rows(x_dtype, x_dev, x_stride, rows, k)) {
+    a.x_raw = x_dev;
+    a.x_fp32 = x_dtype == VSK_FP32;
+    a.x_stride = x_stride;
+  } else {
+    a.x = base;
+    e = launch_mx4_quantise(x_dev, x_dtype, x_stride, rows, k, base, counter, sp.tiles(), s);
+  }
+  if (e != hipSuccess) return VSK_E_HIP;
+  if (a.x_raw) return launched(launch_mx4_stream(a, s));
+  static const int rowsmax = getenv("MXR") ? atoi(getenv("MXR")) : 128;
+  return launched(rows <= rowsmax ? launch_mx4_rows(a, s) : launch_mx4_tile(a, sp, s));
 }
 
 }  // extern "C"

@@ -30,21 +30,41 @@ struct Mx4Shape {
 
 enum Mx4Type { kMxBf16 = 0, kMxFp32 = 1, kMxMx4 = 2 };
 
-hipError_t launch_mx4_quantise(const void* src, int dtype, int64_t stride, int rows, int k, uint8_t* mx, hipStream_t s);
+// counters (nullable): so many ints set to zero by the launch, for the product
+// that follows.
+hipError_t launch_mx4_quantise(const void* src, int dtype, int64_t stride, int rows, int k, uint8_t* mx, int* counters,
+                               int n_counters, hipStream_t s);
 hipError_t launch_mx4_pack(const uint8_t* codes, const uint8_t* scales, int rows, int k, uint8_t* mx, hipStream_t s);
 hipError_t launch_mx4_read(const uint8_t* mx, int rows, int k, void* dst, int dtype, int64_t stride, hipStream_t s);
 
 struct Mx4ProductArgs {
-  const uint8_t* x;  // MX4 [rows][k]
+  const uint8_t* x;   // MX4 [rows][k], or
+  const void* x_raw;  // rows to quantise (mx4_takes_rows), bf16 or fp32, x_stride apart
+  int x_fp32;
+  int64_t x_stride;
   const uint8_t* w;  // MX4 [n][k]
   int rows, n, k;
   void* y;  // [rows][n], stride y_stride, bf16 or fp32
   int y_fp32;
   int64_t y_stride;
   const void* add;  // nullable, as y
-  int wide;  // y, add and their rows allow vectors of four
+  int wide;         // 1: y, add and their rows allow vectors of four, 2: y's also of eight
 };
-hipError_t launch_mx4_product(const Mx4ProductArgs& a, hipStream_t s);
-hipError_t launch_mx4_tile(const Mx4ProductArgs& a, hipStream_t s);  // many rows (k_mx4_tile.hip)
+// Whether launch_mx4_stream takes x as it is (few short rows).
+bool mx4_takes_rows(int dtype, const void* x, int64_t stride, int rows, int k);
+hipError_t launch_mx4_stream(const Mx4ProductArgs& a, hipStream_t s);
+hipError_t launch_mx4_rows(const Mx4ProductArgs& a, hipStream_t s);
+// The others (k_mx4_tile.hip): y in tiles of tm x tn 16ths, K in `splits` parts of
+// `steps` 128 columns, whose sums meet in `part`; `counter` an int a tile, zero.
+struct Mx4Split {
+  int tm, tn, tiles_m, tiles_n, splits, steps;
+  float __attribute__((ext_vector_type(4)))* part;
+  int* counter;
+  int tiles() const { return tiles_m * tiles_n; }
+  size_t counter_bytes() const { return splits > 1 ? static_cast<size_t>(tiles()) * 4 : 0; }
+  size_t part_bytes() const { return splits > 1 ? static_cast<size_t>(tiles()) * splits * tm * tn * 1024 : 0; }
+};
+Mx4Split mx4_split(int rows, int n, int k);
+hipError_t launch_mx4_tile(const Mx4ProductArgs& a, const Mx4Split& sp, hipStream_t s);
 
 }  // namespace vsk

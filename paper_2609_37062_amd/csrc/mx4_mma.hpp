@@ -18,6 +18,15 @@ __device__ __forceinline__ f32x4 mfma_mx4(u32x4 a, u32x4 b, f32x4 c, uint32_t sa
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, c, 4, 4, SA, static_cast<int>(sa), SB, static_cast<int>(sb));
 }
 
+// D(32x32, f32) += A(32x64) * B(64x32): lane l feeds row (column) l % 32, columns
+// (rows) 32 (l / 32) .. + 31, and holds D[8 (r / 4) + 4 (l / 32) + r % 4][l % 32] in r.
+template <int SA, int SB>
+__device__ __forceinline__ f32x16 mfma_mx4_32(u32x4 a, u32x4 b, f32x16 c, uint32_t sa, uint32_t sb) {
+  const i32x8 av = {static_cast<int>(a[0]), static_cast<int>(a[1]), static_cast<int>(a[2]), static_cast<int>(a[3]), 0, 0, 0, 0};
+  const i32x8 bv = {static_cast<int>(b[0]), static_cast<int>(b[1]), static_cast<int>(b[2]), static_cast<int>(b[3]), 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(av, bv, c, 4, 4, SA, static_cast<int>(sa), SB, static_cast<int>(sb));
+}
+
 // y[row][c0 .. c0 + 3] (+ add) from float32 sums, rounded once.  a.wide: rows and
 // their first elements allow stores of four.
 __device__ __forceinline__ void mx4_store4(const Mx4ProductArgs& a, int row, int c0, f32x4 v) {
@@ -48,6 +57,17 @@ __device__ __forceinline__ void mx4_store4(const Mx4ProductArgs& a, int row, int
       static_cast<uint16_t*>(a.y)[at + r] = static_cast<uint16_t>(f2bf(x));
     }
   }
+}
+
+// The same of eight columns.  a.wide 2: stores of eight bf16 values.
+__device__ __forceinline__ void mx4_store8(const Mx4ProductArgs& a, int row, int c0, f32x4 lo, f32x4 up) {
+  if (a.wide == 2 && a.add == nullptr && !a.y_fp32 && c0 + 7 < a.n) {
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.y) + row * a.y_stride + c0) =
+        u32x4{pack_bf2(lo[0], lo[1]), pack_bf2(lo[2], lo[3]), pack_bf2(up[0], up[1]), pack_bf2(up[2], up[3])};
+    return;
+  }
+  mx4_store4(a, row, c0, lo);
+  mx4_store4(a, row, c0 + 4, up);
 }
 
 }  // namespace vsk

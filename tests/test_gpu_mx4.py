@@ -125,11 +125,13 @@ def test_a_block_that_is_not_finite_stands_for_nan(bad, dtype):
     assert np.isnan(got[2, 64:96]).all() and np.isnan(got).sum() == 32
     # and makes its row (a weight: its column) of a product NaN
     w, wat = _matrix(_draw(np.random.default_rng(2), 20, 200).astype(np.float64))
+    nb = max(vsk.mx4_product_bytes(5, 20, 200), vsk.mx4_product_bytes(20, 5, 200))
+    ws, wsp = _buf(nb)
     y = torch.zeros((5, 20), device="cuda")
-    vsk.mx4_product(at, vsk.MX4, 0, wat, 5, 20, 200, y.data_ptr(), vsk.FP32, 20, stream=_sp())
+    vsk.mx4_product(at, vsk.MX4, 0, wat, 5, 20, 200, y.data_ptr(), vsk.FP32, 20, wsp, nb, stream=_sp())
     assert torch.isnan(y[2]).all() and not torch.isnan(y[[0, 1, 3, 4]]).any()
     y = torch.zeros((20, 5), device="cuda")
-    vsk.mx4_product(wat, vsk.MX4, 0, at, 20, 5, 200, y.data_ptr(), vsk.FP32, 5, stream=_sp())
+    vsk.mx4_product(wat, vsk.MX4, 0, at, 20, 5, 200, y.data_ptr(), vsk.FP32, 5, wsp, nb, stream=_sp())
     assert torch.isnan(y[:, 2]).all() and not torch.isnan(y[:, [0, 1, 3, 4]]).any()
 
 
@@ -152,8 +154,8 @@ def _product(x, wat, n, x_kind, y_dtype, add=None, y_stride=None, x_stride=None,
         if inplace:
             y.copy_(ad)
             ad = y
-    nb = 0 if x_kind == "mx4" else vsk.mx4_product_bytes(rows, n, k)
-    ws, wsp = _buf(nb) if nb else (None, None)
+    nb = vsk.mx4_product_bytes(rows, n, k)
+    ws, wsp = _buf(nb)
     vsk.mx4_product(ptr, kind, xs, wat, rows, n, k, y.data_ptr(), vsk.FP32 if y_dtype == torch.float32 else vsk.BF16, ys, wsp,
                     nb, add_ptr=None if ad is None else ad.data_ptr(), stream=_sp())
     torch.cuda.synchronize()
@@ -166,7 +168,8 @@ def _product(x, wat, n, x_kind, y_dtype, add=None, y_stride=None, x_stride=None,
 SIZES = [(1, 16, 32), (1, 1, 1), (1, 33, 500), (3, 100, 1000), (16, 64, 4096), (15, 48, 130), (17, 80, 512), (31, 40, 2052),
          (32, 128, 640), (33, 256, 1024), (48, 20, 5000), (64, 300, 384), (65, 300, 384), (77, 130, 3000), (128, 512, 256),
          (129, 257, 300), (200, 64, 96), (255, 255, 255), (256, 256, 512), (257, 513, 1030), (300, 1000, 700), (513, 300, 2100),
-         (1000, 700, 160), (70, 5000, 40)]
+         (1000, 700, 160), (70, 5000, 40), (2, 20, 12288), (16, 30, 12300), (7, 5000, 600), (90, 70, 12288), (112, 64, 9000),
+         (1500, 8200, 400)]
 
 
 @pytest.mark.parametrize("rows,n,k", SIZES)
