@@ -329,57 +329,76 @@ hipError_t launch_mx4_stream(const Mx4ProductArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Up to 128 rows: a workgroup takes 16 columns and 16 RG rows, its eight waves every
-// eighth two of K's steps each; x comes from the caches.  Two steps' tiles are in
-// flight while the two before are used (see k_mx4_stream).
-template <int RG>
-__global__ __launch_bounds__(64 * kMxWaves) void k_mx4_rows(Mx4ProductArgs a) {
-  __shared__ f32x4 part[kMxWaves][RG][64];
+// Up to 128 rows: a workgroup takes 16 NT columns and all rows, 16 RG, its eight waves
+// every eighth two of its K's steps each; x comes from the caches.  Two steps' tiles
+// are in flight while the two before are used (see k_mx4_stream).  What x is read for
+// each 16 columns sets the time of many rows (77 x 4096 x 14336: 143 MB), so NT is 2
+// there, and K cut over two workgroups where the columns are then too few; the one
+// that arrives last adds the sums, as in k_mx4_tile.
+template <int RG, int NT>
+__global__ __launch_bounds__(64 * kMxWaves, 2) void k_mx4_rows(Mx4ProductArgs a, Mx4Split sp) {
+  constexpr int U = RG * NT;
+  __shared__ f32x4 part[kMxWaves][U][64];
+  __shared__ int s_last;
   const Mx4Shape gw(a.n, a.k), gx(a.rows, a.k);
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int nt = blockIdx.x, g0 = blockIdx.y * RG;
+  const int bm = blockIdx.x / sp.splits, split = blockIdx.x % sp.splits;
   const int kt_n = static_cast<int>(gw.kt), kq_n = static_cast<int>(gw.kq);
-  const u32x4* wp = reinterpret_cast<const u32x4*>(a.w) + static_cast<size_t>(nt) * kt_n * 64;
-  const uint32_t* ws = reinterpret_cast<const uint32_t*>(a.w + gw.scales_at()) + static_cast<size_t>(nt) * kq_n * 64;
-  const u32x4* xp[RG];
-  const uint32_t* xs[RG];
+  const int k0 = min(kt_n, split * sp.steps), k1 = min(kt_n, k0 + sp.steps);  // (k0 a multiple of four)
+  const u32x4 *wp[NT], *xp[RG];
+  const uint32_t *ws[NT], *xs[RG];
+  // (rows of tiles past the last one: it again, the sums are not stored)
 #pragma unroll
-  for (int g = 0; g < RG; ++g) {  // (groups past the last one: it again, its sums are not stored)
-    const int64_t t = min(static_cast<int64_t>(g0 + g), gx.rt - 1);
+  for (int i = 0; i < NT; ++i) {
+    const int64_t t = min(static_cast<int64_t>(bm) * NT + i, gw.rt - 1);
+    wp[i] = reinterpret_cast<const u32x4*>(a.w) + t * kt_n * 64;
+    ws[i] = reinterpret_cast<const uint32_t*>(a.w + gw.scales_at()) + t * kq_n * 64;
+  }
+#pragma unroll
+  for (int g = 0; g < RG; ++g) {
+    const int64_t t = min(static_cast<int64_t>(g), gx.rt - 1);
     xp[g] = reinterpret_cast<const u32x4*>(a.x) + t * kt_n * 64;
     xs[g] = reinterpret_cast<const uint32_t*>(a.x + gx.scales_at()) + t * kq_n * 64;
   }
-  f32x4 acc[RG];
+  f32x4 acc[RG][NT];
 #pragma unroll
-  for (int g = 0; g < RG; ++g) acc[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int g = 0; g < RG; ++g)
+#pragma unroll
+    for (int i = 0; i < NT; ++i) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   struct Two {
-    u32x4 w[2], x[2][RG];
-    uint32_t sw, sx[RG];
+    u32x4 w[2][NT], x[2][RG];
+    uint32_t sw[NT], sx[RG];
   };
   auto load = [&](Two& s, int i) __attribute__((always_inline)) {
-    const int h = w + i * kMxWaves, q = h >> 1;
-    const size_t k0 = 2 * h, k1 = min(2 * h + 1, kt_n - 1);
-    s.sw = ws[static_cast<size_t>(q) * 64 + lane];
-    s.w[0] = __builtin_nontemporal_load(wp + k0 * 64 + lane);
-    s.w[1] = __builtin_nontemporal_load(wp + k1 * 64 + lane);
+    const int kt = k0 + 2 * (w + i * kMxWaves);
+    const size_t q = kt >> 2, ka = kt, kb = min(kt + 1, kt_n - 1);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      s.sw[j] = ws[j][q * 64 + lane];
+      s.w[0][j] = __builtin_nontemporal_load(wp[j] + ka * 64 + lane);
+      s.w[1][j] = __builtin_nontemporal_load(wp[j] + kb * 64 + lane);
+    }
 #pragma unroll
     for (int g = 0; g < RG; ++g) {
-      s.sx[g] = xs[g][static_cast<size_t>(q) * 64 + lane];
-      s.x[0][g] = xp[g][k0 * 64 + lane];
-      s.x[1][g] = xp[g][k1 * 64 + lane];
+      s.sx[g] = xs[g][q * 64 + lane];
+      s.x[0][g] = xp[g][ka * 64 + lane];
+      s.x[1][g] = xp[g][kb * 64 + lane];
     }
   };
   auto use = [&](const Two& s, int i) __attribute__((always_inline)) {
-    const int h = w + i * kMxWaves, sh = 16 * (h & 1);
-    const uint32_t sw = s.sw >> sh;
+    const int kt = k0 + 2 * (w + i * kMxWaves), sh = 8 * (kt & 3);
 #pragma unroll
-    for (int g = 0; g < RG; ++g) acc[g] = mfma_mx4<0, 0>(s.w[0], s.x[0][g], acc[g], sw, s.sx[g] >> sh);
-    if (2 * h + 1 < kt_n) {
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int g = 0; g < RG; ++g) acc[g] = mfma_mx4<1, 1>(s.w[1], s.x[1][g], acc[g], sw, s.sx[g] >> sh);
+      for (int g = 0; g < RG; ++g) acc[g][j] = mfma_mx4<0, 0>(s.w[0][j], s.x[0][g], acc[g][j], s.sw[j] >> sh, s.sx[g] >> sh);
+    if (kt + 1 < k1) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int g = 0; g < RG; ++g) acc[g][j] = mfma_mx4<1, 1>(s.w[1][j], s.x[1][g], acc[g][j], s.sw[j] >> sh, s.sx[g] >> sh);
     }
   };
-  const int twos = (kt_n + 1) / 2, n = twos > w ? (twos - w + kMxWaves - 1) / kMxWaves : 0;
+  const int twos = (k1 - k0 + 1) / 2, n = twos > w ? (twos - w + kMxWaves - 1) / kMxWaves : 0;
   Two sa, sb;
   if (n > 0) load(sa, 0);
   int i = 0;
@@ -397,24 +416,45 @@ __global__ __launch_bounds__(64 * kMxWaves) void k_mx4_rows(Mx4ProductArgs a) {
     use(sa, i);
   }
 #pragma unroll
-  for (int g = 0; g < RG; ++g) part[w][g][lane] = acc[g];
-  __syncthreads();
-  for (int g = w; g < RG; g += kMxWaves) {
-    f32x4 y = part[0][g][lane];
+  for (int g = 0; g < RG; ++g)
 #pragma unroll
-    for (int j = 1; j < kMxWaves; ++j) y += part[j][g][lane];
-    const int row = 16 * (g0 + g) + (lane & 15);
-    if (row < a.rows) mx4_store4(a, row, 16 * nt + 4 * (lane >> 4), y);
+    for (int j = 0; j < NT; ++j) part[w][g * NT + j][lane] = acc[g][j];
+  __syncthreads();
+  constexpr int kMine = (U + kMxWaves - 1) / kMxWaves;
+  f32x4 y[kMine];
+  auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int m = 0; m < kMine; ++m)
+      if (w + m * kMxWaves < U) f(m, w + m * kMxWaves);
+  };
+  each([&](int m, int u) __attribute__((always_inline)) {
+    y[m] = part[0][u][lane];
+#pragma unroll
+    for (int j = 1; j < kMxWaves; ++j) y[m] += part[j][u][lane];
+  });
+  if (sp.splits > 1) {
+    uint8_t* mem = reinterpret_cast<uint8_t*>(sp.part) + static_cast<size_t>(bm) * sp.splits * U * 1024;
+    each([&](int m, int u) __attribute__((always_inline)) { store_wt(mem + (split * U + u) * 1024 + 16 * lane, __builtin_bit_cast(u32x4, y[m])); });
+    if (!mx4_last_of(sp, bm, s_last)) return;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(mem, 0, sp.splits * U * 1024, 0x00020000);
+    each([&](int m, int) __attribute__((always_inline)) { y[m] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+    for (int s = 0; s < sp.splits; ++s)
+      each([&](int m, int u) __attribute__((always_inline)) { y[m] += load_agent4(rs, (s * U + u) * 1024 + 16 * lane); });
   }
+  each([&](int m, int u) __attribute__((always_inline)) {
+    const int row = 16 * (u / NT) + (lane & 15);
+    if (row < a.rows) mx4_store4(a, row, 16 * (bm * NT + u % NT) + 4 * (lane >> 4), y[m]);
+  });
 }
 
-hipError_t launch_mx4_rows(const Mx4ProductArgs& a, hipStream_t s) {
-  const int nt = (a.n + 15) / 16, rg = (a.rows + 15) / 16;
+hipError_t launch_mx4_rows(const Mx4ProductArgs& a, const Mx4Split& sp, hipStream_t s) {
   auto go = [&](auto c) {
     constexpr int RG = decltype(c)::value;
-    hipLaunchKernelGGL((k_mx4_rows<RG>), dim3(nt, (rg + RG - 1) / RG), dim3(64 * kMxWaves), 0, s, a);
+    const dim3 grid(sp.tiles() * sp.splits), block(64 * kMxWaves);
+    if (sp.tm == 2) hipLaunchKernelGGL((k_mx4_rows<RG, 2>), grid, block, 0, s, a, sp);
+    else hipLaunchKernelGGL((k_mx4_rows<RG, 1>), grid, block, 0, s, a, sp);
   };
-  switch (rg) {
+  switch (sp.tn) {
     case 1: go(std::integral_constant<int, 1>{}); break;
     case 2: go(std::integral_constant<int, 2>{}); break;
     case 3: go(std::integral_constant<int, 3>{}); break;

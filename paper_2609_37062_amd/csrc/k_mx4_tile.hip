@@ -13,15 +13,10 @@
 
 namespace vsk {
 
-// 16 bytes past this XCD's L2 (what other workgroups of the launch stored through).
-__device__ __forceinline__ f32x4 load_agent4(__amdgpu_buffer_rsrc_t r, uint32_t at) {
-  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 16 /* sc1 */));
-}
-
 // S: slots of LDS, a step of 128 columns each, S copied ahead; exponents of four
 // steps each in E slots of their own.
 template <int WM, int WN, int FM, int FN, int S, int E>
-__global__ __launch_bounds__(64 * WM * WN, WM * WN == 4 ? 2 : 2) void k_mx4_tile(Mx4ProductArgs a, Mx4Split sp) {
+__global__ __launch_bounds__(64 * WM * WN, FM * FN == 16 ? 1 : 2) void k_mx4_tile(Mx4ProductArgs a, Mx4Split sp) {
   constexpr int NW = WM * WN, TM = 2 * WM * FM, TN = 2 * WN * FN, T = TM + TN;  // waves; 16-row tiles of w and x
   constexpr int kCopies = (T + NW - 1) / NW;                                    // 1 KiB copies of a wave for a slot
   static_assert((S - 1) * kCopies + E * kCopies <= 63, "copies in flight");
@@ -30,7 +25,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 4 ? 2 : 2) void k_mx4_tile
   __shared__ int s_last;
 
   // an XCD's workgroups (every eighth) take neighbouring columns, all rows of each
-  const int total = sp.tiles_m * sp.tiles_n * sp.splits, per = (total + 7) / 8;
+  const int total = sp.tiles() * sp.splits, per = (total + 7) / 8;
   const int id = static_cast<int>(blockIdx.x % 8) * per + static_cast<int>(blockIdx.x / 8);
   if (static_cast<int>(blockIdx.x / 8) >= per || id >= total) return;
   const int split = id % sp.splits, tile = id / sp.splits;
@@ -58,17 +53,12 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 4 ? 2 : 2) void k_mx4_tile
     to_exp[c] = lds_address(&s_exp[0][i][0]);
   }
   const uint32_t lane16 = 16 * lane, lane4 = 4 * lane;
-  auto copy = [&](int kt) __attribute__((always_inline)) {  // (past the end: the last one again)
-    const size_t at = static_cast<size_t>(min(kt, kt_n - 1)) * 1024;
-#pragma unroll
-    for (int c = 0; c < kCopies; ++c)
-      lds_copy16<false>(code[c] + at, lane16, to_code[c] + (kt - k0) % S * static_cast<uint32_t>(sizeof(s_code[0])));
+  auto copy = [&](int kt, int c) __attribute__((always_inline)) {  // (past the end: the last one again)
+    lds_copy16<false>(code[c] + static_cast<size_t>(min(kt, kt_n - 1)) * 1024, lane16,
+                      to_code[c] + (kt - k0) % S * static_cast<uint32_t>(sizeof(s_code[0])));
   };
-  auto copy_exp = [&](int q) __attribute__((always_inline)) {
-    const size_t at = static_cast<size_t>(min(q, kq_n - 1)) * 256;
-#pragma unroll
-    for (int c = 0; c < kCopies; ++c)
-      lds_copy4(expo[c] + at, lane4, to_exp[c] + q % E * static_cast<uint32_t>(sizeof(s_exp[0])));
+  auto copy_exp = [&](int q, int c) __attribute__((always_inline)) {
+    lds_copy4(expo[c] + static_cast<size_t>(min(q, kq_n - 1)) * 256, lane4, to_exp[c] + q % E * static_cast<uint32_t>(sizeof(s_exp[0])));
   };
 
   f32x16 acc[FM][FN];
@@ -93,17 +83,25 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 4 ? 2 : 2) void k_mx4_tile
     for (int i = 0; i < FM; ++i) f.w[i] = s[2 * (wm * FM + i) * 64];
   };
   uint32_t sw[FM][2], sx[FN][2];
-  auto mma = [&](const Half& f, auto jc, auto hc) __attribute__((always_inline)) {
+  // between(m) is issued behind the m-th matrix instruction
+  auto mma = [&](const Half& f, auto jc, auto hc, auto between) __attribute__((always_inline)) {
     constexpr int J = decltype(jc)::value, H = decltype(hc)::value;
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = mfma_mx4_32<J, J>(f.w[i], f.x[j], acc[i][j], sw[i][H], sx[j][H]);
+      for (int j = 0; j < FN; ++j) {
+        acc[i][j] = mfma_mx4_32<J, J>(f.w[i], f.x[j], acc[i][j], sw[i][H], sx[j][H]);
+        between(i * FN + j);
+      }
   };
 #pragma unroll
-  for (int q = 0; q < E; ++q) copy_exp(k0 / 4 + q);
+  for (int q = 0; q < E; ++q)
 #pragma unroll
-  for (int i = 0; i < S; ++i) copy(k0 + i);
+    for (int c = 0; c < kCopies; ++c) copy_exp(k0 / 4 + q, c);
+#pragma unroll
+  for (int i = 0; i < S; ++i)
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) copy(k0 + i, c);
   // The first half of a step is read behind the middle of the step before it, the
   // second while the first is used.  In the middle all waves have read their step,
   // its slot is free, and this wave's copies for the next have landed once no more
@@ -126,14 +124,24 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 4 ? 2 : 2) void k_mx4_tile
       }
     }
     read(fb, kt, 1);
-    mma(fa, jc, std::integral_constant<int, 0>{});
+    __builtin_amdgcn_sched_barrier(0);  // (else the reads sink to where they are waited for)
+    mma(fa, jc, std::integral_constant<int, 0>{}, [](int) {});
     constexpr int kLater = (J == 3 ? (S - 2 < 4 * E - 2 ? S - 2 : 4 * E - 2) : S - 2) * kCopies;
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLater) : "memory");
     barrier_after_lds_reads();
-    copy(kt + S);
-    if constexpr (J == 0) copy_exp(kt / 4 + E);
     read(fa, kt + 1, 0);
-    mma(fb, jc, std::integral_constant<int, 1>{});
+    // the copies go between the matrix instructions: issued in a row, they hold up the
+    // wave (and all waves at once) until the ones before them have been taken
+    mma(fb, jc, std::integral_constant<int, 1>{}, [&](int m) __attribute__((always_inline)) {
+      constexpr int kM = FM * FN, kEach = (kCopies + kM - 1) / kM;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int c = m * kEach; c < (m + 1) * kEach && c < kCopies; ++c) {
+        copy(kt + S, c);
+        if constexpr (J == 0) copy_exp(kt / 4 + E, c);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
   };
   for (int kt = k0; kt < k1; kt += 4) {
     step(kt, std::integral_constant<int, 0>{});
@@ -144,8 +152,6 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 4 ? 2 : 2) void k_mx4_tile
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the copies past the end land before LDS is given back)
 
   if (sp.splits > 1) {
-    // Sums are written through to memory, the arrival counted once they are there
-    // (see attn_unit); nobody waits for another.
     constexpr uint32_t kWave = FM * FN * 4 * 1024, kSplit = NW * kWave;  // bytes
     uint8_t* part = reinterpret_cast<uint8_t*>(sp.part) + static_cast<size_t>(tile) * sp.splits * kSplit;
     const uint32_t mine = w * kWave + lane16;
@@ -157,13 +163,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 4 ? 2 : 2) void k_mx4_tile
         for (int g = 0; g < 4; ++g)
           store_wt(part + split * kSplit + mine + ((i * FN + j) * 4 + g) * 1024,
                    __builtin_bit_cast(u32x4, f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]}));
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (threadIdx.x == 0)
-      s_last = __hip_atomic_fetch_add(sp.counter + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == sp.splits - 1;
-    __syncthreads();
-    if (!s_last) return;
+    if (!mx4_last_of(sp, tile, s_last)) return;
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(part, 0, static_cast<int>(sp.splits * kSplit), 0x00020000);
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -207,14 +207,14 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 4 ? 2 : 2) void k_mx4_tile
 
 template <int WM, int WN, int FM, int FN, int S, int E>
 static void launch_tile(const Mx4ProductArgs& a, const Mx4Split& sp, hipStream_t s) {
-  const unsigned grid = (static_cast<unsigned>(sp.tiles_m) * sp.tiles_n * sp.splits + 7) / 8 * 8;
+  const unsigned grid = (static_cast<unsigned>(sp.tiles()) * sp.splits + 7) / 8 * 8;
   hipLaunchKernelGGL((k_mx4_tile<WM, WN, FM, FN, S, E>), dim3(grid), dim3(64 * WM * WN), 0, s, a, sp);
 }
 
+constexpr int kMxUnits = 256;  // compute units
+
 Mx4Split mx4_split(int rows, int n, int k) {
   const Mx4Shape gw(n, k), gx(rows, k);
-  const int rg = static_cast<int>(gx.rt);
-  static const int cfg = getenv("MXC") ? atoi(getenv("MXC")) : 0;
   Mx4Split sp{};
   auto tiles = [&](int tm, int tn) {
     sp.tm = tm;
@@ -224,15 +224,28 @@ Mx4Split mx4_split(int rows, int n, int k) {
     return static_cast<int64_t>(sp.tiles_m) * sp.tiles_n;
   };
   int64_t t;
-  if (rg <= 8) {
-    t = tiles(8, (rg + 1) / 2 * 2);
+  if (gx.rt <= 8) {
+    const int tn = static_cast<int>(gx.rt + 1) / 2 * 2;
+    t = tiles(8, tn);
+    // few columns: by rows (128 columns a workgroup and K cut in eight to fill the
+    // units, 32 x 6144 x 4096 10.6 us and 7.5, 128 x 4096 x 4096 14.5 and 9.5; enough of
+    // them, 64 x 14336 x 4096 13.8 and 18.3).  Two tiles of columns where that leaves
+    // workgroups for most units (48 x 6144 x 4096 9.5 us and 8.0) or K is long (77 x
+    // 4096 x 14336 17.1 and 16.3; 128 x 4096 x 4096 9.5 and 15.7).
+    if (t < 100) {
+      sp.rows = 1;
+      const bool two = gx.rt >= 2 && ((gw.rt >= 384 && gx.rt <= 6) || gw.kq >= 16);
+      t = tiles(two ? 2 : 1, static_cast<int>(gx.rt));
+    }
   } else {
-    t = cfg == 1 ? tiles(16, 8) : tiles(16, 16);
+    t = tiles(16, 16);
+    if (t > kMxUnits && t % kMxUnits <= kMxUnits / 2) t = tiles(16, 8);
     if (t < 192) t = tiles(8, 8);
   }
-  // K in fours of steps, two at least a split
-  const int fours = static_cast<int>(gw.kq);
-  int splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(256 / std::max<int64_t>(t, 1), fours / 2)));
+  // Fewer tiles than compute units: K is cut, in fours of steps, two at least a split
+  // (by rows, whose eight waves cut it already, eight).
+  const int fours = static_cast<int>(gw.kq), least = sp.rows ? 8 : 2;
+  const int splits = t >= kMxUnits ? 1 : std::max(1, std::min(static_cast<int>(kMxUnits / t), fours / least));
   const int each = (fours + splits - 1) / splits;
   sp.steps = 4 * each;
   sp.splits = (fours + each - 1) / each;
@@ -243,10 +256,12 @@ hipError_t launch_mx4_tile(const Mx4ProductArgs& a, const Mx4Split& sp, hipStrea
   if (sp.tm == 16 && sp.tn == 16) launch_tile<2, 4, 4, 2, 4, 1>(a, sp, s);
   else if (sp.tm == 16) launch_tile<2, 2, 4, 2, 3, 1>(a, sp, s);
   else if (sp.tn == 8 && sp.tiles_n > 1) launch_tile<2, 2, 2, 2, 4, 1>(a, sp, s);
-  else if (sp.tn == 2) launch_tile<4, 1, 1, 1, 6, 2>(a, sp, s);
-  else if (sp.tn == 4) launch_tile<4, 1, 1, 2, 6, 2>(a, sp, s);
-  else if (sp.tn == 6) launch_tile<4, 1, 1, 3, 5, 2>(a, sp, s);
-  else launch_tile<4, 1, 1, 4, 4, 2>(a, sp, s);
+  else {
+    if (sp.tn == 2) launch_tile<4, 1, 1, 1, 6, 2>(a, sp, s);
+    else if (sp.tn == 4) launch_tile<4, 1, 1, 2, 6, 2>(a, sp, s);
+    else if (sp.tn == 6) launch_tile<4, 1, 1, 3, 5, 2>(a, sp, s);
+    else launch_tile<4, 1, 1, 4, 4, 2>(a, sp, s);
+  }
   return hipGetLastError();
 }
 

@@ -70,7 +70,7 @@ struct ProductWs {
   ProductWs(int32_t rows, int32_t n, int32_t k) : sp{} {
     counter = vsk_mx4_bytes(rows, k);
     sp = mx4_split(rows, n, k);
-    part = counter + align_up(sp.counter_bytes());
+    part = counter + align_up(static_cast<size_t>(sp.counters()) * 4);
     total = part + align_up(sp.part_bytes());
   }
 };
@@ -112,25 +112,24 @@ int vsk_mx4_product(const void* x_dev, int32_t x_dtype, int64_t x_stride, const 
   const size_t four = 4 * element(y_dtype);
   a.wide = y_stride % 4 != 0 || !aligned(y_dev, four) || !aligned(add_dev, four) ? 0 : y_stride % 8 == 0 && aligned(y_dev, 16) ? 2 : 1;
   Mx4Split sp = ws.sp;
-  int* counter = sp.splits > 1 ? reinterpret_cast<int*>(base + ws.counter) : nullptr;
+  int* counter = sp.counters() > 0 ? reinterpret_cast<int*>(base + ws.counter) : nullptr;
   sp.counter = counter;
   sp.part = reinterpret_cast<decltype(sp.part)>(base + ws.part);
   hipError_t e = hipSuccess;
   if (mx) {
     a.x = static_cast<const uint8_t*>(x_dev);
-    if (counter) e = launch_fill_zero(counter, sp.counter_bytes(), s);
+    if (counter) e = launch_fill_zero(counter, static_cast<size_t>(sp.counters()) * 4, s);
   } else if (mx4_takes_rows(x_dtype, x_dev, x_stride, rows, k)) {
     a.x_raw = x_dev;
     a.x_fp32 = x_dtype == VSK_FP32;
     a.x_stride = x_stride;
   } else {
     a.x = base;
-    e = launch_mx4_quantise(x_dev, x_dtype, x_stride, rows, k, base, counter, sp.tiles(), s);
+    e = launch_mx4_quantise(x_dev, x_dtype, x_stride, rows, k, base, counter, sp.counters(), s);
   }
   if (e != hipSuccess) return VSK_E_HIP;
   if (a.x_raw) return launched(launch_mx4_stream(a, s));
-  static const int rowsmax = getenv("MXR") ? atoi(getenv("MXR")) : 128;
-  return launched(rows <= rowsmax ? launch_mx4_rows(a, s) : launch_mx4_tile(a, sp, s));
+  return launched(sp.rows ? launch_mx4_rows(a, sp, s) : launch_mx4_tile(a, sp, s));
 }
 
 }  // extern "C"

@@ -53,18 +53,19 @@ struct Mx4ProductArgs {
 // Whether launch_mx4_stream takes x as it is (few short rows).
 bool mx4_takes_rows(int dtype, const void* x, int64_t stride, int rows, int k);
 hipError_t launch_mx4_stream(const Mx4ProductArgs& a, hipStream_t s);
-hipError_t launch_mx4_rows(const Mx4ProductArgs& a, hipStream_t s);
 // The others (k_mx4_tile.hip): y in tiles of tm x tn 16ths, K in `splits` parts of
 // `steps` 128 columns, whose sums meet in `part`; `counter` an int a tile, zero.
 struct Mx4Split {
+  int rows;  // 1: taken by launch_mx4_rows
   int tm, tn, tiles_m, tiles_n, splits, steps;
   float __attribute__((ext_vector_type(4)))* part;
   int* counter;
-  int tiles() const { return tiles_m * tiles_n; }
-  size_t counter_bytes() const { return splits > 1 ? static_cast<size_t>(tiles()) * 4 : 0; }
-  size_t part_bytes() const { return splits > 1 ? static_cast<size_t>(tiles()) * splits * tm * tn * 1024 : 0; }
+  __host__ __device__ int tiles() const { return tiles_m * tiles_n; }
+  int counters() const { return splits > 1 ? tiles() : 0; }
+  size_t part_bytes() const { return static_cast<size_t>(counters()) * splits * tm * tn * 1024; }
 };
 Mx4Split mx4_split(int rows, int n, int k);
+hipError_t launch_mx4_rows(const Mx4ProductArgs& a, const Mx4Split& sp, hipStream_t s);
 hipError_t launch_mx4_tile(const Mx4ProductArgs& a, const Mx4Split& sp, hipStream_t s);
 
 }  // namespace vsk

@@ -27,6 +27,24 @@ __device__ __forceinline__ f32x16 mfma_mx4_32(u32x4 a, u32x4 b, f32x16 c, uint32
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(av, bv, c, 4, 4, SA, static_cast<int>(sa), SB, static_cast<int>(sb));
 }
 
+// 16 bytes past this XCD's L2 (what other workgroups of the launch stored through).
+__device__ __forceinline__ f32x4 load_agent4(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 16 /* sc1 */));
+}
+
+// Behind a workgroup's write-through stores of its part of K: whether it is the last
+// of its tile's to have come this far (the others' stores are in memory then; nobody
+// waits, see attn_unit).
+__device__ __forceinline__ bool mx4_last_of(const Mx4Split& sp, int tile, int& s_last) {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (threadIdx.x == 0)
+    s_last = __hip_atomic_fetch_add(sp.counter + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == sp.splits - 1;
+  __syncthreads();
+  return s_last != 0;
+}
+
 // y[row][c0 .. c0 + 3] (+ add) from float32 sums, rounded once.  a.wide: rows and
 // their first elements allow stores of four.
 __device__ __forceinline__ void mx4_store4(const Mx4ProductArgs& a, int row, int c0, f32x4 v) {
