@@ -93,6 +93,20 @@ struct PTermsOf {
 };
 typedef PTermsOf<kPTerms> PTerms;
 
+template <int NT>
+__device__ __forceinline__ void split_terms(const float (&p)[8], PTermsOf<NT>& pp) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float r0 = p[2 * j], r1 = p[2 * j + 1];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      pp.t[t][j] = pack_bf2(r0, r1);
+      r0 -= bf2f(pp.t[t][j]);
+      r1 -= __uint_as_float(pp.t[t][j] & 0xffff0000u);
+    }
+  }
+}
+
 // One step over the keys at positions t0 .. t0 + 31, in two phases so that a
 // caller streaming K and V through registers can reload K as soon as the
 // scores are taken and V as soon as P V is issued.
@@ -177,16 +191,7 @@ __device__ __forceinline__ void pair_softmax(const f32x4& s0, const f32x4& s1, f
   }
   l = fmaf(l, alpha, ps[0] + ps[1]);
   m = m_new;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    float r0 = p[2 * j], r1 = p[2 * j + 1];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      pp.t[t][j] = pack_bf2(r0, r1);
-      r0 -= bf2f(pp.t[t][j]);
-      r1 -= __uint_as_float(pp.t[t][j] & 0xffff0000u);
-    }
-  }
+  split_terms(p, pp);
 }
 
 template <int D, bool MASK, bool FULL>
@@ -287,14 +292,84 @@ __device__ __forceinline__ void pair_pv(u32x4 (&vt)[D / 16], int t0, int t_end, 
 
 // ---- the same steps over the 4-bit cache (kv4.hpp).  What a lane loads of a step's
 // two blocks: its tokens' K codes of both groups (a quarter of the dims, so that one
-// exponent a group does), and the V codes of its eight tokens with theirs.  K and V
-// become bf16 in registers (4-bit values are exact there), 64 conversions a step at
-// D = 128, and everything behind is the 16-bit walk's.
+// exponent a group does), and the V codes of its eight tokens with theirs.
+//
+// V becomes bf16 in registers (4-bit values are exact there), 32 conversions a step
+// at D = 128.  K does at D = 64; at D = 128 a quarter of a head's dims is a block of
+// the format, and S = K q runs on v_mfma_scale_f32_16x16x128_f8f6f4 with K's codes and
+// exponents as they are and q as two 8-bit terms (Kv4Query).  A step's vector
+// instructions pace this walk (4.7 cycles each, two waves a SIMD), not its bytes: 64
+// rows of 2,000-12,000 tokens 122 us with K converted too and masks in every step.
 template <int D>
 struct Kv4Pair {
   u32x4 k[D / 64], v[D / 64], vs[D / 64];
   uint32_t ks;
 };
+// A column's 128 dims of q as the sums of two terms of 4 significant bits (e4m3) with
+// exponents of their own for each 32: q = hi + lo exactly for values from 2^-13 of the
+// largest of the 32 on; below that lo ends at 2^-22 of it.  The instruction takes 8-bit
+// operands by 16 dims: lane quarter j feeds 16 j .. + 15 in bytes 0..15 and 64 + 16 j ..
+// in bytes 16..31, and the exponent of block j.
+struct Kv4Query {
+  i32x8 hi, lo;
+  uint32_t e;  // byte 0: hi's exponent, byte 1: lo's
+};
+__device__ __forceinline__ int kv4_query_dim(int quad, int c) { return 64 * (c >> 1) + 16 * quad + 8 * (c & 1); }  // of q[c]
+__device__ __forceinline__ Kv4Query kv4_query(const u32x4 (&q)[4], int quad) {
+  typedef short i16x2 __attribute__((ext_vector_type(2)));
+  Kv4Query r;
+  uint32_t own = 0;  // hi's exponents of this lane's two blocks
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int c = 2 * s; c < 2 * s + 2; ++c)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top = mx4_top2(top, q[c][j] & 0x7fff7fffu);
+    top = mx4_top(top);
+    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 16, 64)));  // the block's other half
+    // hi's largest value lies in 128 .. 256, what it leaves of a value below 8, 5 bits up
+    const uint32_t t = top >> 23, eh = t == 255u ? 255u : t > 7u ? t - 7u : 0u, el = eh == 255u ? 255u : eh > 5u ? eh - 5u : 0u;
+    const float sh = mx4_scale(eh), sl = mx4_scale(el);
+    own |= (eh | el << 8) << (16 * s);
+#pragma unroll
+    for (int c = 4 * s; c < 4 * s + 4; ++c) {  // four dims
+      float x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t u = q[c >> 1][2 * (c & 1) + (j >> 1)];
+        x[j] = __uint_as_float(j & 1 ? u & 0xffff0000u : u << 16);
+      }
+      i16x2 h = i16x2{0, 0}, l = i16x2{0, 0};
+      h = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(h, x[0], x[1], sh, false);
+      h = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(h, x[2], x[3], sh, true);
+      const uint32_t hw = __builtin_bit_cast(uint32_t, h);
+      const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hw, sh, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hw, sh, true);
+      l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, x[0] - a[0], x[1] - a[1], sl, false);
+      l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, x[2] - b[0], x[3] - b[1], sl, true);
+      r.hi[c] = static_cast<int>(hw);
+      r.lo[c] = __builtin_bit_cast(int, l);
+    }
+  }
+  // blocks 0 and 2 are those of quarters 0 and 1, 1 and 3 of quarters 2 and 3
+  const uint32_t other = static_cast<uint32_t>(__shfl_xor(static_cast<int>(own), 48, 64));
+  r.e = quad == 0 ? own : quad == 1 ? other : quad == 2 ? other >> 16 : own >> 16;
+  return r;
+}
+// S of 16 tokens (G: the exponent's byte) x 16 columns, all 128 dims.
+template <int G>
+__device__ __forceinline__ f32x4 kv4_scores(u32x4 k, uint32_t ks, const Kv4Query& q) {
+  const i32x8 a = {static_cast<int>(k[0]), static_cast<int>(k[1]), static_cast<int>(k[2]), static_cast<int>(k[3]), 0, 0, 0, 0};
+  f32x4 c = f32x4{0.f, 0.f, 0.f, 0.f};
+  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.hi, c, 4, 0, G, static_cast<int>(ks), 0, static_cast<int>(q.e));
+  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.lo, c, 4, 0, G, static_cast<int>(ks), 1, static_cast<int>(q.e));
+  // The operands stay until the sums are there: given registers of an operand that it
+  // takes as dead, the compiler let the sums overlap them partly, and the instruction,
+  // which reads an 8-bit operand in two passes, then took its own results (seen in a
+  // check of its lane layout).
+  asm("" : "+v"(c) : "v"(k), "v"(q.lo));
+  return c;
+}
 template <int D, bool NTKV>
 __device__ __forceinline__ void kv4_load(Kv4Pair<D>& x, const uint8_t* rec_k, const uint8_t* rec_v, int lane) {
   const int quad = lane >> 4, i = lane & 15, th = quad & 1;
@@ -414,7 +489,7 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
     const uint16_t* qrow = a.q + static_cast<size_t>(row) * a.Nq + static_cast<size_t>(hk * G + h) * D;
 #pragma unroll
     for (int c = 0; c < KC; ++c)
-      qf[c] = (h < G) ? *reinterpret_cast<const u32x4*>(qrow + (Q4 ? D / 4 * quad + 8 * c : 32 * c + 8 * quad))
+      qf[c] = (h < G) ? *reinterpret_cast<const u32x4*>(qrow + (!Q4 ? 32 * c + 8 * quad : D == 128 ? kv4_query_dim(quad, c) : D / 4 * quad + 8 * c))
                       : u32x4{0u, 0u, 0u, 0u};
   }
   const float sc = a.scale_log2;  // log2(e) / sqrt(D)
@@ -461,13 +536,17 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
     for (int c = 0; c < VC; ++c) vt[c] = kv(vp + c * 32);
   };
 
-  Kv4Pair<D> raw;
-  auto load_raw = [&](int p, int cnt, int w_lo) {
-    size_t bA, bB;
-    pair_blocks(p, cnt, w_lo, bA, bB);
-    const uint8_t* base = a.pool4 + (static_cast<size_t>(a.layer) * a.n_blocks * a.Hkv + hk) * kv4_record(D);
-    auto rec = [&](bool second) { return base + (second ? bB : bA) * (a.Hkv * kv4_record(D)); };
-    kv4_load<D, NTKV>(raw, rec(pair_k_block(lane)), rec(pair_v_block(lane)), lane);
+  Kv4Pair<D> raw_a, raw_b;  // (Q4) the even and the odd pairs' codes
+  Kv4Query q8;
+  if constexpr (Q4 && D == 128) q8 = kv4_query(qf, quad);
+  const uint8_t* base4 = Q4 ? a.pool4 + (static_cast<size_t>(a.layer) * a.n_blocks * a.Hkv + hk) * kv4_record(D) : nullptr;
+  const size_t stride4 = a.Hkv * kv4_record(D);
+  auto load_raw = [&](Kv4Pair<D>& raw, int p, int cnt, int w_lo) {
+    auto rec = [&](int i) {  // (uniform)
+      return base4 + static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(sm.tbl[w_lo + min(i, cnt - 1)])) * stride4;
+    };
+    const uint8_t *ra = rec(2 * p), *rb = rec(2 * p + 1);
+    kv4_load<D, NTKV>(raw, pair_k_block(lane) ? rb : ra, pair_v_block(lane) ? rb : ra, lane);
   };
 
   __syncthreads();  // sm.tbl
@@ -486,7 +565,8 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   u32x4 vt[VC], vt2[VC];  // V of the even and the odd pairs
   if (cnt > 0) {
     if constexpr (Q4) {
-      load_raw(0, cnt, w_lo);
+      load_raw(raw_a, 0, cnt, w_lo);
+      load_raw(raw_b, 1, cnt, w_lo);
     } else {
       load_k(kg, 0, cnt, w_lo);
       load_v(vt, 0, cnt, w_lo);
@@ -548,10 +628,6 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
                    ? span_bits(kBlock * (quad >> 1 ? bb : ba) + 8 * (quad & 1), kv_len, span.lo, a.sinks)
                    : 0u;
       f32x4 s0, s1;
-      if constexpr (Q4) {
-        kv4_expand_k<D>(raw, kg);
-        kv4_expand_v<D>(raw, vc);
-      }
       pair_qk<D>(qf, kg, s0, s1);
       if (!full) span_mask(bits, s0, s1);
       if (a.scores != nullptr && h < G && 2 * p + (quad >> 1) < cnt) {  // (16 bytes to 4 floats each)
@@ -563,12 +639,8 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
       PTermsOf<kSpanPTerms> pp;
       pair_softmax<false>(s0, s1, sc, m, l, pp, alpha);
       if constexpr (!LAST) {
-        if constexpr (Q4) {
-          load_raw(p + 1, cnt, w_lo);
-        } else {
-          load_k(kg, p + 1, cnt, w_lo);
-          load_v(vn, p + 1, cnt, w_lo);
-        }
+        load_k(kg, p + 1, cnt, w_lo);
+        load_v(vn, p + 1, cnt, w_lo);
       }
       if (!full) span_zero_v<D>(vc, bits);
       pair_pv_add<D>(vc, pp, alpha, o);
@@ -584,16 +656,90 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   };
   constexpr auto kMore = std::false_type{};
   constexpr auto kLast = std::true_type{};
+  // The 4-bit walk's step: the codes of the next pair are in registers already, those
+  // of the one after it are loaded once these are used, unless LAST.  Its maximum may
+  // lag by 2^kLag4, so that sums are rescaled in few steps (probabilities are then up
+  // to that, and the sums as exact); whole steps have no mask.
+  constexpr float kLag4 = 8.f;
+  auto step4 = [&](int p, auto last_c, Kv4Pair<D>& raw) {
+    const int va = __builtin_amdgcn_readfirstlane(b_lo + w_lo + 2 * p);
+    const int ba = span.block(va), bb = span.block(va + 1);
+    auto whole = [&](int b) { return kBlock * (b + 1) <= kv_len && (kBlock * b >= span.lo || kBlock * (b + 1) <= a.sinks); };
+    const bool full = 2 * p + 1 < cnt && whole(ba) && whole(bb);  // (uniform)
+    f32x4 s0, s1;
+    if constexpr (D == 128) {
+      s0 = kv4_scores<0>(raw.k[0], raw.ks, q8);
+      s1 = kv4_scores<1>(raw.k[D / 128], raw.ks, q8);
+    } else {
+      kv4_expand_k<D>(raw, kg);
+      pair_qk<D>(qf, kg, s0, s1);
+    }
+    kv4_expand_v<D>(raw, vt);
+    if constexpr (!decltype(last_c)::value) load_raw(raw, p + 2, cnt, w_lo);
+    if (__builtin_expect(!full, 0)) {
+      const uint32_t bits = 2 * p + (quad >> 1) < cnt
+                                ? span_bits(kBlock * (quad >> 1 ? bb : ba) + 8 * (quad & 1), kv_len, span.lo, a.sinks)
+                                : 0u;
+      span_mask(bits, s0, s1);
+      span_zero_v<D>(vt, bits);
+      asm volatile("" ::: "memory");  // (a branch, not a mask in every step)
+    }
+    float mx = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3]))) * sc;
+    if (__any(mx > m + kLag4)) {  // (-inf + 8 is -inf: first keys always are)
+      const float mn = fmaxf(m, max_xor32(max_xor16(mx)));
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < VC; ++c) o[c] *= f;
+    }
+    const float mb = m == -INFINITY ? 0.f : m;
+    float pr[8], ps[2] = {0.f, 0.f};
+    {
+      // both sides of the difference rounded alike, so the maximum's is 0
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float x = s0[r] * sc, y = s1[r] * sc;
+        pr[r] = __builtin_amdgcn_exp2f(x - mb);
+        pr[4 + r] = __builtin_amdgcn_exp2f(y - mb);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      ps[0] += pr[j];
+      ps[1] += pr[4 + j];
+    }
+    l += ps[0] + ps[1];
+    PTermsOf<kSpanPTerms> pp;
+    split_terms(pr, pp);
+    pair_pv_add<D>(vt, pp, 1.f, o);
+  };
   int p = 0;
-  for (; p + 2 < n_pairs; p += 2) {
-    step(vt, vt2, p, kMore);
-    step(vt2, vt, p + 1, kMore);
-  }
-  if (p + 1 < n_pairs) {
-    step(vt, vt2, p, kMore);
-    step(vt2, vt, p + 1, kLast);
-  } else if (p < n_pairs) {
-    step(vt, vt2, p, kLast);
+  if constexpr (Q4) {
+    for (; p + 3 < n_pairs; p += 2) {
+      step4(p, kMore, raw_a);
+      step4(p + 1, kMore, raw_b);
+    }
+    if (p + 2 < n_pairs) {
+      step4(p, kMore, raw_a);
+      step4(p + 1, kLast, raw_b);
+      step4(p + 2, kLast, raw_a);
+    } else {
+      if (p < n_pairs) step4(p, kLast, raw_a);
+      if (p + 1 < n_pairs) step4(p + 1, kLast, raw_b);
+    }
+  } else {
+    for (; p + 2 < n_pairs; p += 2) {
+      step(vt, vt2, p, kMore);
+      step(vt2, vt, p + 1, kMore);
+    }
+    if (p + 1 < n_pairs) {
+      step(vt, vt2, p, kMore);
+      step(vt2, vt, p + 1, kLast);
+    } else if (p < n_pairs) {
+      step(vt, vt2, p, kLast);
+    }
   }
   l = walk_sum(l);
 

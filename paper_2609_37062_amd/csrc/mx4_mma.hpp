@@ -6,8 +6,6 @@
 
 namespace vsk {
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-
 // D(16x16, f32) += A(16x128) * B(128x16) in 4 bits, one exponent a lane: lane l
 // feeds row (column) l % 16, columns (rows) 32 (l / 16) .. + 31; byte SA of sa and
 // SB of sb hold the exponents.
