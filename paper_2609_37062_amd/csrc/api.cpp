@@ -1340,9 +1340,10 @@ struct AttnPlan {
 // decode: a decode pass (every row one sequence's), whose shared prefixes are
 // read once.  Row r at index p sees keys 0..p, or with a window keys
 // p - window + 1 .. p and 0 .. sinks - 1.  general: the walk that takes
-// windows, row-major output and leaves (maximum, 1 / sum) per row and head.
+// windows, row-major output and leaves (maximum, 1 / sum) per row and head.  four:
+// over the 4-bit cache (a general walk, which reads no prefix once for a group).
 static AttnPlan plan_attn(Handle& h, const uint16_t* q, uint16_t* out, int out_Rg, uint8_t* ws, const WsLayout& wl,
-                          bool decode, int window, int sinks, bool general) {
+                          bool decode, int window, int sinks, bool general, bool four = false) {
   const vsk_model_cfg& c = h.cfg;
   const BatchDev& b = h.bd;
   const int R = b.n_rows, d = c.head_dim, Nq = c.n_q_heads * d;
@@ -1422,7 +1423,20 @@ static AttnPlan plan_attn(Handle& h, const uint16_t* q, uint16_t* out, int out_R
   if (h.attn_bps == 0 && n_dec > 0 && ((pairs >= 128 && pairs < 256 && 5 * blk_min >= 4 * blk_max) ||
                                        blk_sum * c.n_kv_heads >= static_cast<int64_t>(kAttnSlots) * blk_max))
     aa.bps = std::clamp((blk_max + 7) / 8 * 8, kAttnMinBps, kAttnMaxBps);
-  if (p.span && n_dec <= kPackedRows) {
+  // The 4-bit cache's walks read 17/64 of the bytes, so that what a split costs (its
+  // own start, and a part of the join) is more of them: no walk is cut that is no
+  // longer than 1.6 times what each compute unit has to walk in all, or than 64 blocks
+  // (64 rows of 2,000-12,000 tokens 101 us cut at 128 blocks, 89 uncut; 32 of
+  // 1,000-4,000 28 and 25; 16 of 512-1,024 12 and 10.6); few blocks in all are cut
+  // finer (one row of 2,000 tokens 9.9 us at 32 blocks, 8.9 at 16).
+  bool uncut = false;
+  if (four && h.attn_bps == 0 && n_dec > 0) {
+    const int64_t all = blk_sum * c.n_kv_heads;
+    uncut = blk_max <= 64 || 5 * kAttnUnits * static_cast<int64_t>(blk_max) <= 8 * all;
+    if (uncut) aa.bps = std::clamp((blk_max + 7) / 8 * 8, kAttnMinBps, kAttnMaxBps);
+    else if (all < kAttnMinBps * kAttnUnits) aa.bps = 16;
+  }
+  if (p.span && n_dec <= kPackedRows && !uncut) {
     auto items = [&](int bps) {
       int64_t n = 0;
       for (int i = 0; i < n_dec; ++i) {
@@ -1623,8 +1637,7 @@ static hipError_t launch_mass(Handle& h, const AttnPlan& p, int layer, float* ma
 
 hipError_t run_attend(Handle& h, int layer, const uint16_t* q, uint16_t* out, int window, int sinks, float* mass,
                       int64_t stride, bool add, bool four, hipStream_t s) {
-  // (the 4-bit cache has no walk of shared prefixes)
-  AttnPlan p = plan_attn(h, q, out, 0, h.ws, h.wl, !four && h.bd.max_q_len == 1, window, sinks, mass != nullptr);
+  AttnPlan p = plan_attn(h, q, out, 0, h.ws, h.wl, !four && h.bd.max_q_len == 1, window, sinks, mass != nullptr, four);
   if (four) p.dec.pool4 = p.pre.pool4 = h.pool4;
   hipError_t e = launch_attn(h, p, layer, nullptr, false, s);
   if (e == hipSuccess && mass != nullptr) e = launch_mass(h, p, layer, mass, stride, add, s);

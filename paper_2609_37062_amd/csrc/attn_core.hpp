@@ -422,6 +422,57 @@ __device__ __forceinline__ void kv4_expand_v(const Kv4Pair<D>& x, u32x4 (&vt)[D 
     }
 }
 
+// 16 and 8 bytes past this XCD's L2 (what other workgroups of the launch stored through).
+__device__ __forceinline__ f32x4 load_agent4(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 16 /* sc1 */));
+}
+__device__ __forceinline__ f32x2_t load_agent2(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+  return __builtin_bit_cast(f32x2_t, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 16 /* sc1 */));
+}
+
+// The splits of a (row, KV head), joined in their order and stored row-major: four
+// dims a thread, 16 bytes a load, kC splits in flight (one memory round trip for
+// each).  po, pml: their (O, [G][D]) and ((m, l), [G]).
+template <int D>
+__device__ __forceinline__ void join_splits(const AttnArgs& a, int row, int hk, int n, const uint8_t* po, const uint8_t* pml) {
+  constexpr int kC = 8;
+  const int G = a.G;
+  const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(po), 0, n * G * D * 4, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rm = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(pml), 0, n * G * 8, 0x00020000);
+  for (int i = threadIdx.x; i < G * D / 4; i += blockDim.x) {
+    const int hh = i / (D / 4), e = i % (D / 4) * 4;
+    float M = -INFINITY, L = 0.f;
+    f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < n; s0 += kC) {
+      f32x2_t ml[kC];
+      f32x4 x[kC];
+#pragma unroll
+      for (int j = 0; j < kC; ++j) {
+        const int at = min(s0 + j, n - 1) * G + hh;
+        ml[j] = load_agent2(rm, at * 8);
+        x[j] = load_agent4(ro, (at * D + e) * 4);
+      }
+      float Mn = M;
+#pragma unroll
+      for (int j = 0; j < kC; ++j) Mn = fmaxf(Mn, ml[j][0]);
+      const float f0 = M == -INFINITY ? 0.f : exp2f(M - Mn);
+      L *= f0;
+      y *= f0;
+#pragma unroll
+      for (int j = 0; j < kC; ++j) {
+        // (a split of which the row sees nothing: its maximum is -inf, its sums zero)
+        const float f = s0 + j < n && ml[j][0] != -INFINITY ? exp2f(ml[j][0] - Mn) : 0.f;
+        L += ml[j][1] * f;
+        y += x[j] * f;
+      }
+      M = Mn;
+    }
+    const float inv = 1.f / L;
+    *reinterpret_cast<u32x2*>(a.out + static_cast<size_t>(row) * a.Nq + (hk * G + hh) * D + e) =
+        u32x2{pack_bf2(y[0] * inv, y[1] * inv), pack_bf2(y[2] * inv, y[3] * inv)};
+  }
+}
+
 // WT: the attention output is stored write-through (sc1), so that other
 // workgroups of the same launch read it from memory, not from a stale L2.
 // FOLD2: a wave loads two shared-prefix partials before folding either (one
@@ -536,16 +587,14 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
     for (int c = 0; c < VC; ++c) vt[c] = kv(vp + c * 32);
   };
 
-  Kv4Pair<D> raw_a, raw_b;  // (Q4) the even and the odd pairs' codes
+  Kv4Pair<D> raw;  // (Q4) the next pair's codes
   Kv4Query q8;
   if constexpr (Q4 && D == 128) q8 = kv4_query(qf, quad);
   const uint8_t* base4 = Q4 ? a.pool4 + (static_cast<size_t>(a.layer) * a.n_blocks * a.Hkv + hk) * kv4_record(D) : nullptr;
   const size_t stride4 = a.Hkv * kv4_record(D);
-  auto load_raw = [&](Kv4Pair<D>& raw, int p, int cnt, int w_lo) {
-    auto rec = [&](int i) {  // (uniform)
-      return base4 + static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(sm.tbl[w_lo + min(i, cnt - 1)])) * stride4;
-    };
-    const uint8_t *ra = rec(2 * p), *rb = rec(2 * p + 1);
+  auto load_raw = [&](int id_a, int id_b) {
+    auto rec = [&](int id) { return base4 + static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(id)) * stride4; };
+    const uint8_t *ra = rec(id_a), *rb = rec(id_b);
     kv4_load<D, NTKV>(raw, pair_k_block(lane) ? rb : ra, pair_v_block(lane) ? rb : ra, lane);
   };
 
@@ -565,8 +614,7 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   u32x4 vt[VC], vt2[VC];  // V of the even and the odd pairs
   if (cnt > 0) {
     if constexpr (Q4) {
-      load_raw(raw_a, 0, cnt, w_lo);
-      load_raw(raw_b, 1, cnt, w_lo);
+      load_raw(sm.tbl[w_lo], sm.tbl[w_lo + min(1, cnt - 1)]);
     } else {
       load_k(kg, 0, cnt, w_lo);
       load_v(vt, 0, cnt, w_lo);
@@ -656,12 +704,12 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   };
   constexpr auto kMore = std::false_type{};
   constexpr auto kLast = std::true_type{};
-  // The 4-bit walk's step: the codes of the next pair are in registers already, those
-  // of the one after it are loaded once these are used, unless LAST.  Its maximum may
-  // lag by 2^kLag4, so that sums are rescaled in few steps (probabilities are then up
+  // The 4-bit walk's step: the next pair's codes are loaded (unless LAST) as soon as
+  // this one's have become scores and bf16.  Its maximum may lag by 2^kLag4, so that sums are rescaled in few steps (probabilities are then up
   // to that, and the sums as exact); whole steps have no mask.
   constexpr float kLag4 = 8.f;
-  auto step4 = [&](int p, auto last_c, Kv4Pair<D>& raw) {
+  auto step4 = [&](int p, auto last_c) {
+    const int id_a = sm.tbl[w_lo + min(2 * p + 2, cnt - 1)], id_b = sm.tbl[w_lo + min(2 * p + 3, cnt - 1)];
     const int va = __builtin_amdgcn_readfirstlane(b_lo + w_lo + 2 * p);
     const int ba = span.block(va), bb = span.block(va + 1);
     auto whole = [&](int b) { return kBlock * (b + 1) <= kv_len && (kBlock * b >= span.lo || kBlock * (b + 1) <= a.sinks); };
@@ -675,7 +723,7 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
       pair_qk<D>(qf, kg, s0, s1);
     }
     kv4_expand_v<D>(raw, vt);
-    if constexpr (!decltype(last_c)::value) load_raw(raw, p + 2, cnt, w_lo);
+    if constexpr (!decltype(last_c)::value) load_raw(id_a, id_b);
     if (__builtin_expect(!full, 0)) {
       const uint32_t bits = 2 * p + (quad >> 1) < cnt
                                 ? span_bits(kBlock * (quad >> 1 ? bb : ba) + 8 * (quad & 1), kv_len, span.lo, a.sinks)
@@ -717,18 +765,8 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   };
   int p = 0;
   if constexpr (Q4) {
-    for (; p + 3 < n_pairs; p += 2) {
-      step4(p, kMore, raw_a);
-      step4(p + 1, kMore, raw_b);
-    }
-    if (p + 2 < n_pairs) {
-      step4(p, kMore, raw_a);
-      step4(p + 1, kLast, raw_b);
-      step4(p + 2, kLast, raw_a);
-    } else {
-      if (p < n_pairs) step4(p, kLast, raw_a);
-      if (p + 1 < n_pairs) step4(p + 1, kLast, raw_b);
-    }
+    for (; p + 1 < n_pairs; ++p) step4(p, kMore);
+    if (p < n_pairs) step4(p, kLast);
   } else {
     for (; p + 2 < n_pairs; p += 2) {
       step(vt, vt2, p, kMore);
@@ -817,6 +855,13 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   }
   __syncthreads();
   if (!sm.last) return;
+
+  if constexpr (Q4) {
+    join_splits<D>(a, row, hk, n_splits, reinterpret_cast<const uint8_t*>(a.part_o + rh * a.split_stride * G * D),
+                   reinterpret_cast<const uint8_t*>(a.part_ml + rh * a.split_stride * G));
+    if (threadIdx.x == 0) __hip_atomic_store(a.counter + rh, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return;
+  }
 
   // merge: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, in split order
   // (this row's own splits, which follow its group's prefix partials).  A
