@@ -78,13 +78,21 @@ template <int D, int NH>
 struct RowsLds {
   u32x4 kv[kRowSlots][2][NH][2][2 * D];  // [slot][K, V][half][block][16-byte piece]
   int32_t tbl[kMaxSpanBlocks];
+  int32_t wide[kRowSlots][NH][2];  // (4-bit cache) the step's V blocks that are bf16, the others fp16
   float m[kRowTiles][64], l[kRowTiles][64];  // the second half's, when the halves join
 };
 
-// Q4: the 4-bit cache.  A wave's K or V block of a step is 1 KiB of codes there at D =
-// 128, 16 bytes a lane; they are loaded a step ahead of the slot's turn, turned into
-// bf16 once for the workgroup, and stored in the order of the 16-bit blocks, so the
-// walk is the same.
+// Q4: the 4-bit cache.  A step's blocks are turned into 16 bits once for the workgroup
+// and stored in the order of the 16-bit ones, so that the walk is the same: two waves a
+// block, each half of its K and half of its V (with a wave for K and one for V the V
+// waves, 82 vector instructions a step against 30, held up the others at the barrier:
+// 1,000 rows after 7,000 tokens 180 us, 165).  A block's codes are loaded a step ahead
+// of its slot's turn.
+//
+// V becomes fp16 where that holds it exactly, which any block of ordinary size is, and
+// a weight then goes in with its first 11 bits: one matrix instruction instead of two
+// (2 x 1,000 rows through a window of 4,096 199 -> 177 us); a block with other
+// exponents becomes bf16 and takes weights of two terms.
 template <int D, int NH, bool Q4>
 __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   constexpr int T = 256 * NH;
@@ -150,62 +158,71 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   auto landed = [&](auto steps) __attribute__((always_inline)) {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(steps)::value * kCopies) : "memory");
   };
-  // (Q4) this lane's part of the wave's block: K of place p and a quarter of the dims
-  // (two lanes of a 16-byte piece at D = 64), V of four tokens' (t, d)
+  // (Q4) of block w / 2 of the step this lane turns K of place kp, dims D / 4 kq + D / 8
+  // hf .. (hf: the wave's half), and V of tokens 8 vth + 4 vtq + 2 hf, + 1 of its d; it
+  // also looks at the exponents of one token (two at D = 64).
   struct Codes {
-    u32x4 c, s;
+    uint32_t k[D / 64], v[D / 64], vs[D / 64], ks, all;
   };
   const uint8_t* rec0 = a.pool4 + (static_cast<size_t>(a.layer) * a.n_blocks * a.Hkv + hk) * kv4_record(D);
-  const int piece = D == 128 ? lane : lane >> 1, part = D == 128 ? 0 : lane & 1;
+  const int hf = w & 1, piece = D == 128 ? lane : lane >> 1, part = D == 128 ? 0 : lane & 1;
   const int kp = D == 128 ? piece & 15 : (piece & 7) + 8 * part, kq = D == 128 ? piece >> 4 : piece >> 3;
   const int vd = piece & 15, vth = piece >> 4 & 1, vtq = D == 128 ? piece >> 5 : part;
+  auto words = [](uint32_t (&to)[D / 64], const uint8_t* p) __attribute__((always_inline)) {
+    if constexpr (D == 128) {
+      const u32x2 y = *reinterpret_cast<const u32x2*>(p);
+      to[0] = y[0];
+      to[D / 64 - 1] = y[1];
+    } else {
+      to[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+  };
   auto fetch = [&](int step, Codes& x) __attribute__((always_inline)) {
     const uint32_t blk = __builtin_amdgcn_readfirstlane(sm.tbl[min(2 * NH * step + my_blk, span.nv - 1)]);
     const uint8_t* rec = rec0 + static_cast<size_t>(blk) * (a.Hkv * kv4_record(D));
-    const uint8_t* at = rec + (w & 1 ? kv4_v_at(D) : 0) + D / 8 * lane;
-    if constexpr (D == 128) {
-      x.c = *reinterpret_cast<const u32x4*>(at);
-    } else {
-      const u32x2 y = *reinterpret_cast<const u32x2*>(at);
-      x.c = u32x4{y[0], y[1], 0u, 0u};
-    }
-    if (w & 1) {
-      const uint8_t* sp = rec + kv4_vs_at(D) + (8 * vth + 4 * vtq) * (D / 32);
-      if constexpr (D == 128) {
-        x.s = *reinterpret_cast<const u32x4*>(sp);
-      } else {
-        const u32x2 y = *reinterpret_cast<const u32x2*>(sp);
-        x.s = u32x4{y[0], y[1], 0u, 0u};
-      }
-    } else {
-      x.s[0] = rec[kv4_ks_at(D) + kv4_ks_byte(kp, D == 128 ? kq : kq >> 1)];
-    }
+    words(x.k, rec + D / 8 * lane + D / 16 * hf);
+    words(x.v, rec + kv4_v_at(D) + D / 8 * lane + D / 16 * hf);
+    words(x.vs, rec + kv4_vs_at(D) + (8 * vth + 4 * vtq + 2 * hf) * (D / 32));
+    x.ks = rec[kv4_ks_at(D) + kv4_ks_byte(kp, D == 128 ? kq : kq >> 1)];
+    x.all = *reinterpret_cast<const uint32_t*>(rec + kv4_vs_at(D) + 4 * (lane & (D / 8 - 1)));
   };
   auto expand = [&](int step, const Codes& x) __attribute__((always_inline)) {
-    u32x4* dst = &sm.kv[step % kRowSlots][w & 1][w >> 2][w >> 1 & 1][0];
-    if (w & 1) {
-      u32x2* half = reinterpret_cast<u32x2*>(dst);  // (four tokens of a dim)
+    const float ksc = mx4_scale(x.ks);
+    u32x4* kt = &sm.kv[step % kRowSlots][0][w >> 2][w >> 1 & 1][0];
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {  // eight dims
+      const int e = D / 4 * kq + D / 8 * hf + 8 * c;
+      kt[64 * (e >> 5) + kp + 16 * (e >> 3 & 3)] = mx4_decode8(x.k[c], ksc);
+    }
+    // fp16 holds every value of a block exactly whose exponent is 104 .. 140
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const u16x2 even = __builtin_bit_cast(u16x2, x.all & 0x00ff00ffu) - u16x2{104, 104};
+    const u16x2 odd = __builtin_bit_cast(u16x2, x.all >> 8 & 0x00ff00ffu) - u16x2{104, 104};
+    const u16x2 off = __builtin_elementwise_max(even, odd);
+    const bool wide = __any(off[0] > 36 || off[1] > 36);  // (the same for both waves of the block)
+    if (lane == 0) sm.wide[step % kRowSlots][w >> 2][w >> 1 & 1] = wide;
+    uint32_t* vt = reinterpret_cast<uint32_t*>(&sm.kv[step % kRowSlots][1][w >> 2][w >> 1 & 1][0]) + 2 * vtq + hf;
+    auto put = [&](auto half_c) __attribute__((always_inline)) {
+      constexpr bool HALF = decltype(half_c)::value;
 #pragma unroll
       for (int b = 0; b < D / 32; ++b) {
-        uint32_t y[4];
+        uint32_t y[2];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const uint32_t cw = D == 128 ? x.c[t] : x.c[t >> 1], sw = D == 128 ? x.s[t] : x.s[t >> 1];
-          const int n = D == 128 ? b : 2 * (t & 1) + b;
+        for (int t = 0; t < 2; ++t) {
+          const uint32_t cw = x.v[t * (D / 64) / 2], sw = x.vs[t * (D / 64) / 2];
+          const int n = D == 128 ? b : 2 * t + b;
           const float sc = kv4_scale(sw, n);
-          y[t] = n == 0 ? mx4_decode<0>(cw, sc) : n == 1 ? mx4_decode<1>(cw, sc) : n == 2 ? mx4_decode<2>(cw, sc) : mx4_decode<3>(cw, sc);
+          if constexpr (HALF)
+            y[t] = n == 0 ? mx4_decode_half<0>(cw, sc) : n == 1 ? mx4_decode_half<1>(cw, sc) : n == 2 ? mx4_decode_half<2>(cw, sc) : mx4_decode_half<3>(cw, sc);
+          else
+            y[t] = n == 0 ? mx4_decode<0>(cw, sc) : n == 1 ? mx4_decode<1>(cw, sc) : n == 2 ? mx4_decode<2>(cw, sc) : mx4_decode<3>(cw, sc);
         }
-        half[2 * (32 * (2 * b) + vd + 16 * vth) + vtq] = u32x2{low_halves(y[0], y[1]), low_halves(y[2], y[3])};
-        half[2 * (32 * (2 * b + 1) + vd + 16 * vth) + vtq] = u32x2{high_halves(y[0], y[1]), high_halves(y[2], y[3])};
+        vt[4 * (32 * (2 * b) + vd + 16 * vth)] = low_halves(y[0], y[1]);
+        vt[4 * (32 * (2 * b + 1) + vd + 16 * vth)] = high_halves(y[0], y[1]);
       }
-    } else {
-      const float sc = mx4_scale(x.s[0]);
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) {  // dims D / 4 * kq + 8 c ..
-        const int e = D / 4 * kq + 8 * c;
-        dst[64 * (e >> 5) + kp + 16 * (e >> 3 & 3)] = mx4_decode8(x.c[c], sc);
-      }
-    }
+    };
+    if (__builtin_expect(wide, 0)) put(std::false_type{});
+    else put(std::true_type{});
   };
   Codes raw;
   float m = -INFINITY, l = 0.f;
@@ -278,10 +295,14 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   // maximum has not moved and no score is huge -- no branch and no change of a
   // register on a condition, which the compiler would pay for with copies of
   // all the sums in every step.
-  auto rest = [&](int step, const f32x16& s, auto fast_c) __attribute__((always_inline)) {
+  // (Q4: FAST steps' V is fp16, and so is that of the blocks whose bit in `wide` is
+  // clear: a weight goes in with its first 11 bits, one instruction instead of two.)
+  auto rest = [&](int step, const f32x16& s, auto fast_c, int wide = 0) __attribute__((always_inline)) {
     constexpr bool FAST = decltype(fast_c)::value;
     const u32x4* vp = &sm.kv[step % kRowSlots][1][hh][0][32 * (lc >> 4) + (lane & 15) + 16 * hi];
-    const float mb = !FAST && m == -INFINITY ? 0.f : m;
+    // (Q4: weights times 2^7, with the lag at most 2^15: an fp16's smallest step is then
+    // 2^-32 of the largest weight's and more, and many small weights keep their sum)
+    const float mb = (!FAST && m == -INFINITY ? 0.f : m) - (Q4 ? 7.f : 0.f);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       u32x4 vt[OC];
@@ -301,6 +322,14 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
         }
       }
       l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      if (Q4 && (FAST || !(wide >> b & 1))) {  // (uniform)
+        u32x4 ph;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ph[j] = pack_half2(p[2 * j], p[2 * j + 1]);
+#pragma unroll
+        for (int i = 0; i < OC; ++i) o[i] = mfma_32x32x16_f16(vt[i], ph, o[i]);
+        continue;
+      }
       u32x4 pt[kSpanPTerms];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -351,6 +380,11 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
 #pragma unroll
     for (int i = 0; i < QC; ++i) s = mfma_32x32x16(kp[32 * i], qf[i], s);
   };
+  auto wide_of = [&](int step) __attribute__((always_inline)) {  // (uniform)
+    if constexpr (!Q4) return 0;
+    const int32_t* f = sm.wide[step % kRowSlots][hh];
+    return __builtin_amdgcn_readfirstlane(f[0] | f[1] << 1);
+  };
   auto top = [&](const f32x16& s) __attribute__((always_inline)) {
     float x = s[0];
 #pragma unroll
@@ -362,12 +396,14 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   barrier_after_lds_reads();
   qk(step, s);
   mx = top(s);
+  int wide = wide_of(step);
   while (step < n_steps) {
     // (a loop of its own, so that the sums stay where they are)
-    while (is_full(step) && !big && !__any(mx > m + kRowsLag)) {  // (-inf + 8 is -inf: first keys always are)
+    while (is_full(step) && !big && !wide && !__any(mx > m + kRowsLag)) {  // (-inf + 8 is -inf: first keys always are)
       next(step);
       f32x16 sn;
       qk(step + 1, sn);
+      wide = wide_of(step + 1);
       rest(step, s, std::true_type{});
       s = sn;
       mx = top(s);
@@ -394,11 +430,12 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
       big = __any(fabsf(m) >= kSpanRounded && m != -INFINITY);
     }
     next(step);
-    rest(step, s, std::false_type{});
+    rest(step, s, std::false_type{}, wide);
     if (__builtin_expect(poisoned, 0)) poison(step);
     if (++step == n_steps) break;
     qk(step, s);
     mx = top(s);
+    wide = wide_of(step);
   }
   l = add_xor32(l);
   if constexpr (!Q4) landed(std::integral_constant<int, 0>{});  // (the steps past the list: before LDS is used again or ends)

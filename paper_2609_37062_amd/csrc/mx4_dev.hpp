@@ -32,6 +32,11 @@ template <int SEL>
 __device__ __forceinline__ uint32_t mx4_decode(uint32_t codes, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL));
 }
+// The same as two fp16 values.
+template <int SEL>
+__device__ __forceinline__ uint32_t mx4_decode_half(uint32_t codes, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, SEL));
+}
 // Eight codes as eight bf16 values.
 __device__ __forceinline__ u32x4 mx4_decode8(uint32_t codes, float scale) {
   return u32x4{mx4_decode<0>(codes, scale), mx4_decode<1>(codes, scale), mx4_decode<2>(codes, scale),

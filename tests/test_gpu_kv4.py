@@ -7,10 +7,34 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import mx4_case as mx  # noqa: E402
-from cache_case import BLOCK, Cache, bf16, check  # noqa: E402
+from cache_case import BLOCK, Cache, attend_ref, bf16, check  # noqa: E402
 from mx4_case import Cache4  # noqa: E402
 
 pytestmark = pytest.mark.gpu
+
+
+
+def check_rows(c, window=0, sinks=0, layer=0):
+    """As check, of prompt rows.  Beyond what that counts, a weight w_i, taken with 11
+    bits, is off by at most 2^-11 w_i (half a step of fp16), or by half of fp16's
+    smallest step where it is below 2^-14.  Weights go in as 2^7 times their ratio to a
+    maximum that the row's largest ratio exceeds by 1 to 2^8, and their sum is at least
+    2^7; so the second is at most 2^-25 / 2^7 of the sum, a key."""
+    got, r0 = c.out(), 0
+    for i, (s, ql) in enumerate(zip(c.seqs, c.q_lens)):
+        q, K, V = c.q[r0:r0 + ql].float().numpy(), c.K[layer][s], c.V[layer][s]
+        n = len(K)
+        o, ob, _, _ = attend_ref(q, K, V, n - ql, window, sinks)
+        oa, _, _, _ = attend_ref(q, K, np.abs(V), n - ql, window, sinks)
+        # (a key that a row does not see gives it nothing: the largest of those that it may)
+        see = n if window == 0 else min(n, window + sinks)
+        top = np.stack([np.abs(V[np.r_[:min(t + 1, sinks), max(0, t + 1 - window) if window else 0:t + 1]]).max(axis=0) for t in range(n - ql, n)])
+        top = np.repeat(top, c.group, axis=1).reshape(o.shape)
+        b = ob + 2.0 ** -11 * oa.reshape(o.shape) + see * 2.0 ** -32 * top
+        err = np.abs(got[r0:r0 + ql] - o)
+        assert (err <= b).all(), (i, n, ql, float(np.nanmax(err / b)), np.argwhere(~(err <= b))[:4].tolist())
+        r0 += ql
+
 
 SPANS = [(0, 0), (1, 0), (1, 5), (16, 4), (17, 16), (40, 33), (256, 4), (1000, 100)]
 
@@ -95,7 +119,7 @@ def test_prompt_rows(kv, group, hd, window, sinks):
     c = Cache4(kv, group, hd, [2, 16, 37, 130, 411, 290], seed=kv * 10 + group)
     c.batch(range(6), [2, 16, 37, 33, 200, 1])
     c.attend(window=window, sinks=sinks)
-    check(c, window, sinks)
+    check_rows(c, window, sinks)
     c.close()
 
 
@@ -105,14 +129,55 @@ def test_prompt_rows_of_many_work_items():
     c.batch(range(20), [300, 200, 333, 1] * 5)
     for window, sinks in [(0, 0), (100, 7)]:
         c.attend(window=window, sinks=sinks)
-        check(c, window, sinks)
+        check_rows(c, window, sinks)
     c.close()
     c = Cache4(2, 4, 128, [70, 300], seed=5)
     c.eng.set_tuning(6, 0)
     c.batch([0, 1], [70, 3])
     for window, sinks in [(0, 0), (20, 3)]:
         c.attend(window=window, sinks=sinks)
-        check(c, window, sinks)
+        check_rows(c, window, sinks)
+    c.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("e", [-126, -90, -40, -25, -24, -23, 10, 11, 12, 30, 100])
+def test_values_of_any_exponent(hd, e):
+    """Values of 2^e and near it, in every block, in some, and beside ordinary ones."""
+    print(f"[gpu] kv4 exponents hd={hd} e={e}", flush=True)
+    c = Cache4(2, 4, hd, [37, 130, 400], seed=hd + e + 200)
+    v = c.V[0]
+    v[0] = v[0] * 2.0 ** e
+    v[1][:, 1] = v[1][:, 1] * 2.0 ** e
+    v[1][20:90:7, 0, :32] = 0
+    v[2][64:170] = v[2][64:170] * 2.0 ** e
+    for s in range(3):
+        v[s] = bf16(v[s]).float().numpy()  # (the smallest bf16 has no bits to spare)
+        c.write(0, s)
+    for q_lens in ([37, 130, 400], [20, 33, 300], [1, 1, 1]):
+        for window, sinks in [(0, 0), (12, 0), (100, 3)]:
+            c.batch(range(3), q_lens)
+            c.attend(window=window, sinks=sinks)
+            check_rows(c, window, sinks)
+    c.close()
+
+
+def test_many_small_weights_keep_their_sum():
+    """One key of a score 14 to 19 above all others, of 16,000: they weigh 2^-20 to 2^-27
+    each, which a plain fp16 would round to one side or lose."""
+    c = Cache4(1, 1, 128, [16000], seed=2)
+    c.K[0][0][:] = 0
+    c.K[0][0][4000, 0, 0] = 4.0
+    c.V[0][0] = np.abs(c.V[0][0])
+    c.V[0][0][4000] = 0
+    c.write(0, 0)
+    c.batch([0], [64])
+    c.q[:] = 0
+    # scores are divided by sqrt(128)
+    c.q[:, 0, 0] = torch.linspace(14, 19, 64).to(c.q.dtype) * 128 ** 0.5 / 4
+    c.qd.copy_(c.q)
+    c.attend()
+    check_rows(c)
     c.close()
 
 
@@ -123,7 +188,7 @@ def test_long_cache():
             c.batch([0, 1], q_lens)
             for window, sinks in [(0, 0), (9000, 70)]:
                 c.attend(window=window, sinks=sinks)
-                check(c, window, sinks)
+                check_rows(c, window, sinks)
         c.close()
 
 
@@ -152,7 +217,7 @@ def test_slots_behind_a_sequence_do_not_matter():
         for ql in ([1, 1, 1], [5, 20, 99]):
             c.batch([0, 1, 2], ql)
             c.attend()
-            check(c)
+            check_rows(c)
         c.close()
 
 
@@ -178,9 +243,9 @@ def test_replayed_beside_eager_calls():
         c.qd.copy_(c.q)
         c.o[:-1].fill_(0)
         g.replay()
-        check(c, 200, 4)
+        check_rows(c, 200, 4)
         c.attend()
-        check(c)
+        check_rows(c)
     c.close()
 
 
