@@ -903,7 +903,7 @@ int vsk_kv4_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev,
 
 // ------------------------------------------------------------------ QKV rows into a cache
 size_t vsk_rope_bytes(const vsk_handle* h) {
-  return h ? static_cast<size_t>(h->cfg.max_pos) * (h->cfg.head_dim / 2) * 2 * sizeof(float2) : 0;
+  return h ? static_cast<size_t>(h->cfg.max_pos) * (h->cfg.head_dim / 2) * (sizeof(float2) + sizeof(double2)) : 0;
 }
 
 int vsk_rope_bind(vsk_handle* h, void* table_dev, size_t bytes, void* stream) {
@@ -920,18 +920,19 @@ int vsk_rope_bind(vsk_handle* h, void* table_dev, size_t bytes, void* stream) {
   const size_t n = static_cast<size_t>(c.max_pos) * half;
   std::vector<float2> tab;
   try {
-    tab.resize(2 * n);
+    tab.resize(3 * n);
   } catch (const std::bad_alloc&) {
     return fail(h, VSK_E_ARG, "no host memory for the rotary table");
   }
-  // (cos, sin) of pos * theta^(-2j/d) as float, and what the floats leave of the doubles
+  // (cos, sin) of pos * theta^(-2j/d) as float, and as doubles
   for (int j = 0; j < half; ++j) {
     const double inv = std::pow(static_cast<double>(c.rope_theta), -2.0 * j / c.head_dim);
     for (int p = 0; p < c.max_pos; ++p) {
       const double x = std::cos(p * inv), y = std::sin(p * inv);
-      const float2 f = make_float2(static_cast<float>(x), static_cast<float>(y));
-      tab[static_cast<size_t>(p) * half + j] = f;
-      tab[n + static_cast<size_t>(p) * half + j] = make_float2(static_cast<float>(x - f.x), static_cast<float>(y - f.y));
+      const size_t at = static_cast<size_t>(p) * half + j;
+      tab[at] = make_float2(static_cast<float>(x), static_cast<float>(y));
+      const double exact[2] = {x, y};
+      std::memcpy(&tab[n + 2 * at], exact, sizeof(exact));
     }
   }
   st = hip_check(h, hipMemcpyAsync(table_dev, tab.data(), tab.size() * sizeof(float2), hipMemcpyHostToDevice, s), "copy rotary table");

@@ -11,17 +11,34 @@ namespace vsk {
 
 constexpr int kHeadThreads = 256;
 
+// A value of another lane: ^ 1, ^ 2, ^ 7, ^ 15, which a reduction over 2, 4, 8 and 16
+// lanes takes in turn.
+template <int CTRL>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v) {
+  return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), CTRL, 0xf, 0xf, true));
+}
+constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kXor7 = 0x141, kXor15 = 0x140;
 // The largest over the eight lanes of a block.
 __device__ __forceinline__ uint32_t max8(uint32_t v) {
-#pragma unroll
-  for (int m = 1; m < 8; m <<= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), m, 64)));
-  return v;
+  v = max(v, from_lane<kXor1>(v));
+  v = max(v, from_lane<kXor2>(v));
+  return max(v, from_lane<kXor7>(v));
 }
 // Sum over the G lanes of a head.
+template <int CTRL, class T>
+__device__ __forceinline__ T add_lane(T v) {
+  if constexpr (sizeof(T) == 8) {
+    const u32x2 u = __builtin_bit_cast(u32x2, v);
+    return v + __builtin_bit_cast(T, u32x2{from_lane<CTRL>(u[0]), from_lane<CTRL>(u[1])});
+  } else {
+    return v + __builtin_bit_cast(T, from_lane<CTRL>(__builtin_bit_cast(uint32_t, v)));
+  }
+}
 template <int G, class T>
 __device__ __forceinline__ T sum_head(T v) {
-#pragma unroll
-  for (int m = 1; m < G; m <<= 1) v += __shfl_xor(v, m, 64);
+  static_assert(G == 8 || G == 16);
+  v = add_lane<kXor7>(add_lane<kXor2>(add_lane<kXor1>(v)));
+  if constexpr (G == 16) v = add_lane<kXor15>(v);
   return v;
 }
 
@@ -114,93 +131,138 @@ __global__ __launch_bounds__(kHeadThreads) void k_kv4_write(Kv4Pool p, const int
   put_v<D>(rec, sl & 15, i, encode_head(load(v + at), load(v + at + D / 2)), on);
 }
 
-// The values that slots hold, two dims a thread.
-template <int D>
-__global__ __launch_bounds__(256) void k_kv4_read(Kv4Pool p, const int32_t* __restrict__ slots, int n,
-                                                  uint16_t* __restrict__ k, uint16_t* __restrict__ v) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  const int64_t unit = i / (D / 2);
-  if (unit >= static_cast<int64_t>(n) * p.Hkv) return;
-  const int j = static_cast<int>(i % (D / 2));
+// The values that slots hold, eight dims of K and of V a lane.  VEC: k and v are
+// 16-byte aligned.
+template <int D, bool VEC>
+__global__ __launch_bounds__(kHeadThreads) void k_kv4_read(Kv4Pool p, const int32_t* __restrict__ slots, int n,
+                                                           uint16_t* __restrict__ k, uint16_t* __restrict__ v) {
+  constexpr int G = D / 8;
+  const int64_t unit = (static_cast<int64_t>(blockIdx.x) * kHeadThreads + threadIdx.x) / G;
+  const int i = threadIdx.x % G, first = (threadIdx.x & 63) - i;
+  if (unit >= static_cast<int64_t>(n) * p.Hkv) return;  // (whole heads of lanes, here and below)
   const int tok = static_cast<int>(unit / p.Hkv), hk = static_cast<int>(unit % p.Hkv);
   const int sl = slots[tok];
   if (sl < 0 || sl >= p.n_blocks * kBlock) return;
   const uint8_t* rec = kv4_rec<D>(p, sl, hk);
-  const int t = sl & 15, pl = kv4_p(t);
-  const size_t at = static_cast<size_t>(unit) * D;
-  const uint32_t kc = mx4_decode<0>(rec[kv4_k_byte(D, pl, 2 * j)], mx4_scale(rec[kv4_ks_at(D) + kv4_ks_byte(pl, j >> 4)]));
-  k[at + 2 * j] = static_cast<uint16_t>(kc);
-  k[at + 2 * j + 1] = static_cast<uint16_t>(kc >> 16);
-  const int b = j >> 4, d = j & 15;
-  const uint32_t vc = mx4_decode<0>(rec[kv4_v_at(D) + kv4_v_byte(D, t, d) + b], mx4_scale(rec[kv4_vs_at(D) + t * (D / 32) + b]));
-  v[at + 32 * b + d] = static_cast<uint16_t>(vc);
-  v[at + 32 * b + 16 + d] = static_cast<uint16_t>(vc >> 16);
+  const int t = sl & 15, pl = kv4_p(t), b = i >> 2;
+  const uint32_t kc = *reinterpret_cast<const uint32_t*>(rec + kv4_k_byte(D, pl, 8 * i));
+  const uint8_t* vp = rec + kv4_v_at(D);
+  uint32_t own;  // what (t, d) holds, d = i; D = 64: and d = i + 8 above it
+  if constexpr (D == 128)
+    own = *reinterpret_cast<const uint32_t*>(vp + kv4_v_byte(D, t, i));
+  else
+    own = *reinterpret_cast<const uint16_t*>(vp + kv4_v_byte(D, t, i)) |
+          static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(vp + kv4_v_byte(D, t, i + 8))) << 16;
+  const float ks = mx4_scale(rec[kv4_ks_at(D) + kv4_ks_byte(pl, b)]), vs = mx4_scale(rec[kv4_vs_at(D) + t * (D / 32) + b]);
+  uint32_t vc = 0;  // dims 8 i ..: nibble i / 2 of d = 8 (i % 2) ..
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int from = D == 128 ? 8 * (i & 1) + j : j, bit = 4 * (i >> 1) + (D == 128 ? 0 : 16 * (i & 1));
+    vc |= (static_cast<uint32_t>(__shfl(static_cast<int>(own), first + from, 64)) >> bit & 15u) << (4 * j);
+  }
+  const u32x4 ko = mx4_decode8(kc, ks), vo = mx4_decode8(vc, vs);
+  const size_t at = static_cast<size_t>(unit) * D + 8 * i;
+  if constexpr (VEC) {
+    *reinterpret_cast<u32x4*>(k + at) = ko;
+    *reinterpret_cast<u32x4*>(v + at) = vo;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      k[at + j] = static_cast<uint16_t>(ko[j >> 1] >> (16 * (j & 1)));
+      v[at + j] = static_cast<uint16_t>(vo[j >> 1] >> (16 * (j & 1)));
+    }
+  }
 }
 
-// A float that rounds to 4 bits (or to bf16) as the double does: where the double
-// lies beside the float, the neighbour with an odd last bit, which no border is.
+// A float that rounds to 4 bits as the double does: its first 23 bits behind the
+// point, the last one set where more follow.  (Every border between codes has fewer.)
 __device__ __forceinline__ float odd_float(double d) {
-  const float f = static_cast<float>(d);
-  const double r = d - static_cast<double>(f);
-  uint32_t u = __float_as_uint(f);
-  if (r != 0.0 && (u & 1u) == 0u && (u & 0x7f800000u) != 0x7f800000u) u += (r > 0.0) == (u >> 31 == 0u) ? 1u : -1u;
-  return __uint_as_float(u);
+  u32x2 u = __builtin_bit_cast(u32x2, d);
+  u[0] = (u[0] & 0xe0000000u) | ((u[0] & 0x1fffffffu) != 0u ? 0x20000000u : 0u);
+  return static_cast<float>(__builtin_bit_cast(double, u));
 }
 
-// One (row, head) for D / 8 lanes.  T: what norm and rotation are computed in; keys
-// of the 4-bit cache take doubles, with the rotary table's remainders, so that their
-// codes are those of the exact values: an error of float32 at a border between two
-// codes is a whole step there.
+__device__ __forceinline__ float inv_sqrt(float v) { return rsqrtf(v); }
+__device__ __forceinline__ double inv_sqrt(double v) {  // two Newton steps from the instruction's 2^-14 and better
+  double y = __builtin_amdgcn_rsq(v);
+  if (v < static_cast<double>(INFINITY) && v > 0.0) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) y = fma(y, 0.5 * fma(-v * y, y, 1.0), y);
+  }
+  return y;
+}
+
+// Norm and rotation of a head, D / 8 lanes.  T: what they are computed in; keys of
+// the 4-bit cache take doubles, and the rotary table's, so that their codes are those
+// of the exact values: an error of float32 at a border between two codes is a whole
+// step there.
 template <int D, class T>
-__device__ __forceinline__ void norm_rope(const QkvArgs& a, int row, int i, u32x2 lo, u32x2 hi, const uint16_t* gain,
-                                          T (&x)[4], T (&y)[4]) {
+__device__ __forceinline__ void norm_rope(float eps, int i, u32x2 lo, u32x2 hi, const uint16_t* gain, const T (&c)[4],
+                                          const T (&s)[4], T (&x)[4], T (&y)[4]) {
   constexpr int G = D / 8;
+  float fx[4], fy[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    x[j] = static_cast<T>(bf2f(lo[j >> 1] >> (16 * (j & 1)) & 0xffffu));
-    y[j] = static_cast<T>(bf2f(hi[j >> 1] >> (16 * (j & 1)) & 0xffffu));
+    fx[j] = bf2f(lo[j >> 1] >> (16 * (j & 1)) & 0xffffu);
+    fy[j] = bf2f(hi[j >> 1] >> (16 * (j & 1)) & 0xffffu);
   }
+  T r = 1;
+  typedef u32x2 __attribute__((aligned(2))) Four;  // (one load, whatever the gain's alignment)
+  u32x2 gl{}, gh{};
   if (gain != nullptr) {
+    gl = *reinterpret_cast<const Four*>(gain + 4 * i);
+    gh = *reinterpret_cast<const Four*>(gain + D / 2 + 4 * i);
     T ss = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) ss += x[j] * x[j] + y[j] * y[j];
-    ss = sum_head<G>(ss);
-    const T r = static_cast<T>(1) / sqrt(ss / D + static_cast<T>(a.eps));
-#pragma unroll
     for (int j = 0; j < 4; ++j) {
-      x[j] *= r * static_cast<T>(bf2f(gain[4 * i + j]));
-      y[j] *= r * static_cast<T>(bf2f(gain[D / 2 + 4 * i + j]));
+      ss = fma(static_cast<T>(fx[j]), static_cast<T>(fx[j]), ss);
+      ss = fma(static_cast<T>(fy[j]), static_cast<T>(fy[j]), ss);
     }
+    r = inv_sqrt(fma(sum_head<G>(ss), static_cast<T>(1.0 / D), static_cast<T>(eps)));
   }
-  const size_t at = static_cast<size_t>(a.rot[row]) * (D / 2) + 4 * i, more = static_cast<size_t>(a.max_pos) * (D / 2);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float2 cs = a.rope[at + j];
-    T c = static_cast<T>(cs.x), s = static_cast<T>(cs.y);
-    if constexpr (sizeof(T) == 8) {
-      const float2 rest = a.rope[more + at + j];
-      c += static_cast<T>(rest.x);
-      s += static_cast<T>(rest.y);
+    T u = static_cast<T>(fx[j]), v = static_cast<T>(fy[j]);
+    if (gain != nullptr) {
+      u *= r * static_cast<T>(bf2f(gl[j >> 1] >> (16 * (j & 1)) & 0xffffu));
+      v *= r * static_cast<T>(bf2f(gh[j >> 1] >> (16 * (j & 1)) & 0xffffu));
     }
-    const T u = x[j] * c - y[j] * s, v = y[j] * c + x[j] * s;
-    x[j] = u;
-    y[j] = v;
+    x[j] = u * c[j] - v * s[j];
+    y[j] = v * c[j] + u * s[j];
   }
 }
 
+// A wave takes one head of consecutive rows, D / 8 lanes each: the rows of a run are
+// neighbours in a block's record, where their small stores share lines.  Bound by
+// memory and, for few rows, by the launch: 1,833 rows of 32/8 heads x 128 into 4 bits,
+// 41 MB, 13.2 us; 16 into 16 bits 3.4.  (Lanes along the heads of a row 14.8; two or
+// four heads a wave, a row's angles loaded once for them, 14.9 and 14.5; gains as
+// single loads 17.3.)
 template <int D, bool FOUR>
 __global__ __launch_bounds__(kHeadThreads) void k_qkv_norm_rope(QkvArgs a) {
-  constexpr int G = D / 8;
+  constexpr int G = D / 8, kRows = 64 / G;
   const int heads = a.Hq + 2 * a.Hkv;
-  const int64_t unit = (static_cast<int64_t>(blockIdx.x) * kHeadThreads + threadIdx.x) / G;
-  const int i = threadIdx.x % G;
-  if (unit >= static_cast<int64_t>(a.R) * heads) return;  // (whole heads of lanes)
-  const int row = static_cast<int>(unit / heads), head = static_cast<int>(unit % heads);
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * (kHeadThreads / 64) + (threadIdx.x >> 6));
+  const int i = threadIdx.x % G, row0 = static_cast<int>(wave / heads) * kRows, head = static_cast<int>(wave % heads);
+  const int row = row0 + (threadIdx.x & 63) / G;
+  if (row >= a.R) return;  // (whole heads of lanes)
   const uint16_t* src = a.qkv + row * a.stride + static_cast<size_t>(head) * D + 4 * i;
   const u32x2 lo = *reinterpret_cast<const u32x2*>(src), hi = *reinterpret_cast<const u32x2*>(src + D / 2);
+  const size_t turn = static_cast<size_t>(a.rot[row]) * (D / 2) + 4 * i;
+  float c[4] = {}, s[4] = {};
+  if (head < (FOUR ? a.Hq : a.Hq + a.Hkv)) {
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+      const f32x4 cs = *reinterpret_cast<const f32x4*>(a.rope + turn + j);
+      c[j] = cs[0];
+      s[j] = cs[1];
+      c[j + 1] = cs[2];
+      s[j + 1] = cs[3];
+    }
+  }
   if (head < a.Hq) {
     float x[4], y[4];
-    norm_rope<D>(a, row, i, lo, hi, a.q_gain, x, y);
+    norm_rope<D>(a.eps, i, lo, hi, a.q_gain, c, s, x, y);
     uint16_t* dst = a.q + (static_cast<size_t>(row) * a.Hq + head) * D + 4 * i;
     *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf2(x[0], x[1]), pack_bf2(x[2], x[3])};
     *reinterpret_cast<u32x2*>(dst + D / 2) = u32x2{pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3])};
@@ -210,14 +272,19 @@ __global__ __launch_bounds__(kHeadThreads) void k_qkv_norm_rope(QkvArgs a) {
   const bool is_k = head < a.Hq + a.Hkv;
   const int hk = head - a.Hq - (is_k ? 0 : a.Hkv);
   if constexpr (FOUR) {
-    const Kv4Pool p{a.pool4, a.layer, a.n_blocks, a.Hkv};
-    uint8_t* rec = kv4_rec<D>(p, sl, hk);
+    uint8_t* rec = kv4_rec<D>(Kv4Pool{a.pool4, a.layer, a.n_blocks, a.Hkv}, sl, hk);
     if (!is_k) {
       put_v<D>(rec, t, i, encode_head(lo, hi), true);
       return;
     }
-    double x[4], y[4];
-    norm_rope<D>(a, row, i, lo, hi, a.k_gain, x, y);
+    double dc[4], ds[4], x[4], y[4];
+    const double2* exact = reinterpret_cast<const double2*>(a.rope + static_cast<size_t>(a.max_pos) * (D / 2)) + turn;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      dc[j] = exact[j].x;
+      ds[j] = exact[j].y;
+    }
+    norm_rope<D>(a.eps, i, lo, hi, a.k_gain, dc, ds, x, y);
     float fx[4], fy[4];
     uint32_t tl = 0, th = 0;
 #pragma unroll
@@ -227,22 +294,22 @@ __global__ __launch_bounds__(kHeadThreads) void k_qkv_norm_rope(QkvArgs a) {
       tl = max(tl, __float_as_uint(fx[j]) & 0x7fffffffu);
       th = max(th, __float_as_uint(fy[j]) & 0x7fffffffu);
     }
-    HeadCodes h;
-    h.lo = mx4_exponent(max8(tl));
-    h.hi = mx4_exponent(max8(th));
-    const float s0 = mx4_scale(h.lo), s1 = mx4_scale(h.hi);
-    uint32_t c = mx4_encode_f32<0>(0u, fx[0], fx[1], s0), d = mx4_encode_f32<0>(0u, fy[0], fy[1], s1);
-    c = mx4_encode_f32<1>(c, fx[2], fx[3], s0);
-    d = mx4_encode_f32<1>(d, fy[2], fy[3], s1);
-    h.codes = (h.lo == 255u ? 0u : c & 0xffffu) | (h.hi == 255u ? 0u : d << 16);
-    put_k<D>(rec, t, i, h, true);
+    HeadCodes hc;
+    hc.lo = mx4_exponent(max8(tl));
+    hc.hi = mx4_exponent(max8(th));
+    const float s0 = mx4_scale(hc.lo), s1 = mx4_scale(hc.hi);
+    uint32_t cl = mx4_encode_f32<0>(0u, fx[0], fx[1], s0), ch = mx4_encode_f32<0>(0u, fy[0], fy[1], s1);
+    cl = mx4_encode_f32<1>(cl, fx[2], fx[3], s0);
+    ch = mx4_encode_f32<1>(ch, fy[2], fy[3], s1);
+    hc.codes = (hc.lo == 255u ? 0u : cl & 0xffffu) | (hc.hi == 255u ? 0u : ch << 16);
+    put_k<D>(rec, t, i, hc, true);
   } else {
     const size_t head_elems = static_cast<size_t>(kBlock) * D;
     uint16_t* blk = a.pool + ((static_cast<size_t>(a.layer) * 2 + (is_k ? 0 : 1)) * a.n_blocks + (sl >> 4)) * a.Hkv * head_elems +
                     hk * head_elems;
     if (is_k) {
       float x[4], y[4];
-      norm_rope<D>(a, row, i, lo, hi, a.k_gain, x, y);
+      norm_rope<D>(a.eps, i, lo, hi, a.k_gain, c, s, x, y);
       *reinterpret_cast<u32x2*>(blk + kv_k_index(t, 4 * i)) = u32x2{pack_bf2(x[0], x[1]), pack_bf2(x[2], x[3])};
       *reinterpret_cast<u32x2*>(blk + kv_k_index(t, D / 2 + 4 * i)) = u32x2{pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3])};
     } else {
@@ -268,14 +335,18 @@ hipError_t launch_kv4_write(const Kv4Pool& p, int hd, const int32_t* slots, int 
 
 hipError_t launch_kv4_read(const Kv4Pool& p, int hd, const int32_t* slots, int n, uint16_t* k, uint16_t* v, hipStream_t s) {
   if (n == 0) return hipSuccess;
-  const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(n) * p.Hkv * (hd / 2) + 255) / 256)), block(256);
-  if (hd == 128) hipLaunchKernelGGL(k_kv4_read<128>, grid, block, 0, s, p, slots, n, k, v);
-  else hipLaunchKernelGGL(k_kv4_read<64>, grid, block, 0, s, p, slots, n, k, v);
+  const dim3 grid(head_blocks(static_cast<int64_t>(n) * p.Hkv, hd)), block(kHeadThreads);
+  const bool vec = (reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % 16 == 0;
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, s, p, slots, n, k, v); };
+  if (hd == 128) vec ? go(k_kv4_read<128, true>) : go(k_kv4_read<128, false>);
+  else vec ? go(k_kv4_read<64, true>) : go(k_kv4_read<64, false>);
   return hipGetLastError();
 }
 
 hipError_t launch_qkv_norm_rope(const QkvArgs& a, int hd, hipStream_t s) {
-  const dim3 grid(head_blocks(static_cast<int64_t>(a.R) * (a.Hq + 2 * a.Hkv), hd)), block(kHeadThreads);
+  const int rows = 64 / (hd / 8);  // a wave's
+  const int64_t waves = static_cast<int64_t>((a.R + rows - 1) / rows) * (a.Hq + 2 * a.Hkv);
+  const dim3 grid(static_cast<unsigned>((waves + kHeadThreads / 64 - 1) / (kHeadThreads / 64))), block(kHeadThreads);
   const bool four = a.pool4 != nullptr;
   auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, s, a); };
   if (hd == 128) four ? go(k_qkv_norm_rope<128, true>) : go(k_qkv_norm_rope<128, false>);

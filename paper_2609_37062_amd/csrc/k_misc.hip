@@ -769,7 +769,9 @@ hipError_t launch_kv_move(bool write, uint16_t* pool, int layer, int n_blocks, i
   const unsigned blocks = static_cast<unsigned>((total + 255) / 256);
   if (write)
     hipLaunchKernelGGL(k_kv_move<true>, dim3(blocks), dim3(256), 0, s, pool, layer, n_blocks, Hkv, hd, slots, n, k, v);
-  else if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % 16 != 0)
+  else if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % 16 != 0 || total <= (1u << 18))
+    // (a read of few values is latency, which a value a thread has less of: 16 slots of 8
+    // heads x 128 2.1 us, by tiles 2.6 to 3.5; 256 of them 2.6, 2.7 to 3.7; 512 3.5, 2.9 to 4.0)
     hipLaunchKernelGGL(k_kv_move<false>, dim3(blocks), dim3(256), 0, s, pool, layer, n_blocks, Hkv, hd, slots, n, k,
                        v);
   else if (hd == 128)

@@ -53,7 +53,7 @@ struct QkvArgs {
   const uint16_t *q_gain, *k_gain;  // nullable: no norm
   float eps;
   const int32_t *rot, *slot;  // [R]
-  const float2* rope;         // [max_pos][hd / 2] (cos, sin), and behind it what float32 leaves of them
+  const float2* rope;         // [max_pos][hd / 2] (cos, sin), and behind it the same in doubles
   int max_pos;
   uint16_t* q;     // [R][Hq][hd]
   uint16_t* pool;  // the 16-bit cache, or
