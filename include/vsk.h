@@ -21,8 +21,8 @@
  *    memory includes two pinned staging buffers for vsk_batch_upload.)
  *  - `stream` is a hipStream_t passed as void* (NULL = the null stream).
  *    Device work is enqueued asynchronously on it.  The calls that wait for
- *    the device are: vsk_weights_pack_head and vsk_rope_bind (setup; they wait
- *    for their rotary table copies), vsk_device_status (by definition), and vsk_batch_upload
+ *    the device are: vsk_weights_pack_head (setup; it waits for its rotary
+ *    table copy), vsk_device_status (by definition), and vsk_batch_upload
  *    only when the staging buffer it takes is still being read by the copy
  *    it issued two uploads earlier.  Nothing else synchronises.
  *  - bf16 tensors are IEEE bfloat16 bit patterns (uint16), row-major unless
@@ -385,7 +385,7 @@ int vsk_kv4_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev,
                    void* ws_dev, size_t ws_bytes, void* stream);
 
 /* Rotary table of vsk_qkv_norm_rope, in caller-owned device memory (256-byte
- * aligned, vsk_rope_bytes); waits for its copy, like vsk_weights_pack_head. */
+ * aligned, vsk_rope_bytes), filled by a launch on the stream. */
 size_t vsk_rope_bytes(const vsk_handle* h);
 int vsk_rope_bind(vsk_handle* h, void* table_dev, size_t bytes, void* stream);
 /* From a QKV projection's rows to attention's inputs, for the rows of the uploaded

@@ -910,34 +910,10 @@ int vsk_rope_bind(vsk_handle* h, void* table_dev, size_t bytes, void* stream) {
   if (!h) return VSK_E_ARG;
   if (!table_dev || bytes < vsk_rope_bytes(h)) return fail(h, VSK_E_ARG, "rotary table smaller than vsk_rope_bytes()");
   if (reinterpret_cast<uintptr_t>(table_dev) % kAlign) return fail(h, VSK_E_ARG, "rotary table not aligned");
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-  int st = hip_check(h, hipStreamIsCapturing(s, &cap), "rotary table");
-  if (st != VSK_OK) return st;
-  if (cap != hipStreamCaptureStatusNone) return fail(h, VSK_E_STATE, "the rotary table cannot be bound in a capture");
-  const vsk_model_cfg& c = h->cfg;
-  const int half = c.head_dim / 2;
-  const size_t n = static_cast<size_t>(c.max_pos) * half;
-  std::vector<float2> tab;
-  try {
-    tab.resize(3 * n);
-  } catch (const std::bad_alloc&) {
-    return fail(h, VSK_E_ARG, "no host memory for the rotary table");
-  }
-  // (cos, sin) of pos * theta^(-2j/d) as float, and as doubles
-  for (int j = 0; j < half; ++j) {
-    const double inv = std::pow(static_cast<double>(c.rope_theta), -2.0 * j / c.head_dim);
-    for (int p = 0; p < c.max_pos; ++p) {
-      const double x = std::cos(p * inv), y = std::sin(p * inv);
-      const size_t at = static_cast<size_t>(p) * half + j;
-      tab[at] = make_float2(static_cast<float>(x), static_cast<float>(y));
-      const double exact[2] = {x, y};
-      std::memcpy(&tab[n + 2 * at], exact, sizeof(exact));
-    }
-  }
-  st = hip_check(h, hipMemcpyAsync(table_dev, tab.data(), tab.size() * sizeof(float2), hipMemcpyHostToDevice, s), "copy rotary table");
-  if (st == VSK_OK) st = hip_check(h, hipStreamSynchronize(s), "sync");
-  if (st == VSK_OK) h->rope = static_cast<float2*>(table_dev);
+  float2* table = static_cast<float2*>(table_dev);
+  const int st = hip_check(h, launch_rope_table(table, h->cfg.max_pos, h->cfg.head_dim, h->cfg.rope_theta, static_cast<hipStream_t>(stream)),
+                           "rotary table");
+  if (st == VSK_OK) h->rope = table;
   return st;
 }
 

@@ -60,6 +60,8 @@ struct QkvArgs {
   uint8_t* pool4;  // the 4-bit one
   int layer, n_blocks;
 };
+// The table of QkvArgs::rope.
+hipError_t launch_rope_table(float2* table, int max_pos, int hd, double theta, hipStream_t s);
 hipError_t launch_qkv_norm_rope(const QkvArgs& a, int hd, hipStream_t s);
 
 }  // namespace vsk

@@ -4,7 +4,7 @@ from __future__ import annotations
 
 import numpy as np
 
-from cache_case import BLOCK, Cache, bf16
+from cache_case import BLOCK, Cache, attend_ref, bf16
 
 GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 
@@ -87,6 +87,40 @@ class Cache4(Cache):
     def attend(self, layer=0, window=0, sinks=0, stream=None):
         self.eng.kv4_attend(layer, self.qd.data_ptr(), self.o.data_ptr(), self.ws, self.ws_bytes, window=window,
                             sinks=sinks, stream=self.sp if stream is None else stream)
+
+
+def check_rows(c, window=0, sinks=0, layer=0):
+    """As check, of prompt rows.  Beyond what that counts, a weight w_i, taken with 11
+    bits, is off by at most 2^-11 w_i (half a step of fp16), or by half of fp16's
+    smallest step where it is below 2^-14.  Weights go in as 2^7 times their ratio to a
+    maximum that the row's largest ratio exceeds by 1 to 2^8, and their sum is at least
+    2^7; so the second is at most 2^-25 / 2^7 of the sum, a key."""
+    got, r0 = c.out(), 0
+    for i, (s, ql) in enumerate(zip(c.seqs, c.q_lens)):
+        q, K, V = c.q[r0:r0 + ql].float().numpy(), c.K[layer][s], c.V[layer][s]
+        n = len(K)
+        o, ob, _, _ = attend_ref(q, K, V, n - ql, window, sinks)
+        oa, _, _, _ = attend_ref(q, K, np.abs(V), n - ql, window, sinks)
+        # (a key that a row does not see gives it nothing: the largest of those that it may)
+        see = n if window == 0 else min(n, window + sinks)
+        top = np.stack([np.abs(V[np.r_[:min(t + 1, sinks), max(0, t + 1 - window) if window else 0:t + 1]]).max(axis=0) for t in range(n - ql, n)])
+        top = np.repeat(top, c.group, axis=1).reshape(o.shape)
+        b = ob + 2.0 ** -11 * oa.reshape(o.shape) + see * 2.0 ** -32 * top
+        err = np.abs(got[r0:r0 + ql] - o)
+        assert (err <= b).all(), (i, n, ql, float(np.nanmax(err / b)), np.argwhere(~(err <= b))[:4].tolist())
+        r0 += ql
+
+
+def turned(x, pos, gain, theta, eps):
+    """[rows][heads][hd] in 64 bits; also the magnitudes of the terms."""
+    hd = x.shape[-1]
+    if gain is not None:
+        x = x / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps) * gain
+    a = (pos[:, None] * theta ** (-2.0 * np.arange(hd // 2) / hd))[:, None, :]
+    lo, hi = x[..., :hd // 2], x[..., hd // 2:]
+    y = np.concatenate([lo * np.cos(a) - hi * np.sin(a), hi * np.cos(a) + lo * np.sin(a)], axis=-1)
+    m = np.concatenate([np.abs(lo * np.cos(a)) + np.abs(hi * np.sin(a)), np.abs(hi * np.cos(a)) + np.abs(lo * np.sin(a))], axis=-1)
+    return y, m
 
 
 assert BLOCK == 16

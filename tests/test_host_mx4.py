@@ -101,7 +101,7 @@ def test_cache_bytes_and_binding():
     e.kv4_init(A, e.kv4_pool_bytes(10))
     e.kv_init(None, 20)  # another pool size: bound again
     assert _code(e.kv4_read, 0, B, 1, W, Y) == "STATE"
-    assert e.rope_bytes() == 512 * 32 * 16
+    assert e.rope_bytes() == 512 * 32 * 24
     e.close()
 
 
