@@ -377,7 +377,8 @@ int vsk_kv4_write(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_
 int vsk_kv4_read(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_t n, void* k_dev, void* v_dev,
                  void* stream);
 /* vsk_attend over the 4-bit cache, without weights per token: K and V count as the
- * values that they stand for (below 2^-126: maybe as zero).  In the product with v a
+ * values that they stand for (below 2^-126: maybe as zero), of q what lies below 2^-22
+ * of the largest of its 32 dims may not.  In the product with v a
  * weight is rounded to 16 bits for single tokens; for the rows of longer runs to the
  * 11 bits of fp16 where that holds all values of a block of 16 tokens exactly (the
  * exponents of 32 values between 2^-23 and 2^13), to 16 bits elsewhere. */

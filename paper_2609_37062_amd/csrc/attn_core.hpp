@@ -315,10 +315,13 @@ struct Kv4Query {
   uint32_t e;  // byte 0: hi's exponent, byte 1: lo's
 };
 __device__ __forceinline__ int kv4_query_dim(int quad, int c) { return 64 * (c >> 1) + 16 * quad + 8 * (c & 1); }  // of q[c]
-__device__ __forceinline__ Kv4Query kv4_query(const u32x4 (&q)[4], int quad) {
+// PARTNER: lane ^ PARTNER holds the rest of this lane's two blocks; own: their
+// exponents, block by block 16 bits.
+template <int PARTNER>
+__device__ __forceinline__ Kv4Query kv4_query_terms(const u32x4 (&q)[4], uint32_t& own) {
   typedef short i16x2 __attribute__((ext_vector_type(2)));
   Kv4Query r;
-  uint32_t own = 0;  // hi's exponents of this lane's two blocks
+  own = 0;
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     uint32_t top = 0;
@@ -327,7 +330,7 @@ __device__ __forceinline__ Kv4Query kv4_query(const u32x4 (&q)[4], int quad) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) top = mx4_top2(top, q[c][j] & 0x7fff7fffu);
     top = mx4_top(top);
-    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 16, 64)));  // the block's other half
+    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), PARTNER, 64)));
     // hi's largest value lies in 128 .. 256, what it leaves of a value below 8, 5 bits up
     const uint32_t t = top >> 23, eh = t == 255u ? 255u : t > 7u ? t - 7u : 0u, el = eh == 255u ? 255u : eh > 5u ? eh - 5u : 0u;
     const float sh = mx4_scale(eh), sl = mx4_scale(el);
@@ -351,9 +354,22 @@ __device__ __forceinline__ Kv4Query kv4_query(const u32x4 (&q)[4], int quad) {
       r.lo[c] = __builtin_bit_cast(int, l);
     }
   }
+  return r;
+}
+__device__ __forceinline__ Kv4Query kv4_query(const u32x4 (&q)[4], int quad) {
+  uint32_t own;
+  Kv4Query r = kv4_query_terms<16>(q, own);
   // blocks 0 and 2 are those of quarters 0 and 1, 1 and 3 of quarters 2 and 3
   const uint32_t other = static_cast<uint32_t>(__shfl_xor(static_cast<int>(own), 48, 64));
   r.e = quad == 0 ? own : quad == 1 ? other : quad == 2 ? other >> 16 : own >> 16;
+  return r;
+}
+// Of 64 dims for v_mfma_scale_f32_32x32x64: lane half h feeds dims 16 h .. + 15 in bytes
+// 0..15 and 32 + 16 h .. in bytes 16..31, and the exponents of block h.
+__device__ __forceinline__ Kv4Query kv4_query_32(const u32x4 (&q)[4], int half) {
+  uint32_t own;
+  Kv4Query r = kv4_query_terms<32>(q, own);
+  r.e = own >> (16 * half);
   return r;
 }
 // S of 16 tokens (G: the exponent's byte) x 16 columns, all 128 dims.

@@ -82,17 +82,25 @@ struct RowsLds {
   float m[kRowTiles][64], l[kRowTiles][64];  // the second half's, when the halves join
 };
 
-// Q4: the 4-bit cache.  A step's blocks are turned into 16 bits once for the workgroup
-// and stored in the order of the 16-bit ones, so that the walk is the same: two waves a
-// block, each half of its K and half of its V (with a wave for K and one for V the V
-// waves, 82 vector instructions a step against 30, held up the others at the barrier:
-// 1,000 rows after 7,000 tokens 180 us, 165).  A block's codes are loaded a step ahead
-// of its slot's turn.
+// Q4: the 4-bit cache.  Scores are taken on v_mfma_scale_f32_32x32x64 from K's codes and
+// exponents as they are, which go through LDS in a quarter of the bytes, and from q as
+// two 8-bit terms (Kv4Query).  V is turned into 16 bits once for the workgroup and
+// stored in the 16-bit walk's order.  Two waves move a block, half of its K and half of
+// its V each (with a wave for K and one for V the V waves held up the others at the
+// barrier: 1,000 rows after 7,000 tokens 180 us, 165).  A block's codes are loaded a step
+// ahead of its slot's turn, its id a step before that, and a step's slot is filled
+// behind the next scores' matrix instructions, not in front of them.
 //
 // V becomes fp16 where that holds it exactly, which any block of ordinary size is, and
-// a weight then goes in with its first 11 bits: one matrix instruction instead of two
-// (2 x 1,000 rows through a window of 4,096 199 -> 177 us); a block with other
-// exponents becomes bf16 and takes weights of two terms.
+// a weight then goes in with its first 11 bits: one matrix instruction instead of two.
+// A block with other exponents becomes bf16 and takes weights of two terms.
+//
+// 2 x 1,000 rows through a window of 4,096 took 199 us with K and V turned into bf16,
+// 177 with V in fp16, 169 with K as codes, 159 with slots filled behind the scores (165
+// behind the whole step; priorities for the wave that has matrix instructions: none).
+// What bounds it is not one unit: of a step's 3,000 cycles on a SIMD its two waves'
+// matrix instructions take 1,020, their vector instructions about 1,500, the compute
+// unit's LDS about 1,000; two waves overlap them only in part.
 template <int D, int NH, bool Q4>
 __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   constexpr int T = 256 * NH;
@@ -122,12 +130,22 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   const int end = on ? min(kv_end, pos0 + row + 1) : 0;
   auto first_key = [&](int n) { return a.window > 0 && n > a.window ? n - a.window : 0; };  // of a row with n keys
   const int lo = first_key(pos0 + row + 1);
-  u32x4 qf[QC];
+  u32x4 qf[Q4 ? 1 : QC];
+  Kv4Query q4[Q4 ? D / 64 : 1];
   {
-    const uint16_t* qrow = a.q + static_cast<size_t>(row0 + row) * a.Nq + static_cast<size_t>(hk * G + qh) * D + 8 * hi;
+    const uint16_t* qrow = a.q + static_cast<size_t>(row0 + row) * a.Nq + static_cast<size_t>(hk * G + qh) * D;
+    auto q8 = [&](int e) __attribute__((always_inline)) { return on ? *reinterpret_cast<const u32x4*>(qrow + e) : u32x4{0u, 0u, 0u, 0u}; };
+    if constexpr (Q4) {
 #pragma unroll
-    for (int s = 0; s < QC; ++s)
-      qf[s] = on ? *reinterpret_cast<const u32x4*>(qrow + 16 * s) : u32x4{0u, 0u, 0u, 0u};
+      for (int i = 0; i < D / 64; ++i) {
+        const int e = 64 * i + 16 * hi;
+        const u32x4 x[4] = {q8(e), q8(e + 8), q8(e + 32), q8(e + 40)};
+        q4[i] = kv4_query_32(x, hi);
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < QC; ++s) qf[s] = q8(16 * s + 8 * hi);
+    }
   }
   // the wave's part of the list (none without a column), and from where to
   // where a key counts for all its columns
@@ -158,15 +176,18 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   auto landed = [&](auto steps) __attribute__((always_inline)) {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(steps)::value * kCopies) : "memory");
   };
-  // (Q4) of block w / 2 of the step this lane turns K of place kp, dims D / 4 kq + D / 8
-  // hf .. (hf: the wave's half), and V of tokens 8 vth + 4 vtq + 2 hf, + 1 of its d; it
-  // also looks at the exponents of one token (two at D = 64).
+  // (Q4) of block w / 2 of the step this lane moves K's codes of place kp, 4 (D = 64: 2)
+  // dims of K's quarter kq from D / 8 hf on (hf: the wave's half), and the exponent of
+  // (place ep, block eb); turns V of tokens 8 vth + 4 vtq + 2 hf, + 1 of its d; and looks
+  // at V's exponents of one token (two at D = 64).  K in LDS: for each block of 32 dims
+  // the codes of 32 places, then a place's exponents, four bytes each.
   struct Codes {
     uint32_t k[D / 64], v[D / 64], vs[D / 64], ks, all;
   };
   const uint8_t* rec0 = a.pool4 + (static_cast<size_t>(a.layer) * a.n_blocks * a.Hkv + hk) * kv4_record(D);
   const int hf = w & 1, piece = D == 128 ? lane : lane >> 1, part = D == 128 ? 0 : lane & 1;
   const int kp = D == 128 ? piece & 15 : (piece & 7) + 8 * part, kq = D == 128 ? piece >> 4 : piece >> 3;
+  const int ep = lane & 15, eb = lane >> 4 & (D / 32 - 1);
   const int vd = piece & 15, vth = piece >> 4 & 1, vtq = D == 128 ? piece >> 5 : part;
   auto words = [](uint32_t (&to)[D / 64], const uint8_t* p) __attribute__((always_inline)) {
     if constexpr (D == 128) {
@@ -177,23 +198,24 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
       to[0] = *reinterpret_cast<const uint32_t*>(p);
     }
   };
+  auto id_of = [&](int step) __attribute__((always_inline)) { return sm.tbl[min(2 * NH * step + my_blk, span.nv - 1)]; };
+  int32_t id = 0;  // of the next step to fetch
   auto fetch = [&](int step, Codes& x) __attribute__((always_inline)) {
-    const uint32_t blk = __builtin_amdgcn_readfirstlane(sm.tbl[min(2 * NH * step + my_blk, span.nv - 1)]);
+    const uint32_t blk = __builtin_amdgcn_readfirstlane(id);
+    id = id_of(step + 1);
     const uint8_t* rec = rec0 + static_cast<size_t>(blk) * (a.Hkv * kv4_record(D));
     words(x.k, rec + D / 8 * lane + D / 16 * hf);
     words(x.v, rec + kv4_v_at(D) + D / 8 * lane + D / 16 * hf);
     words(x.vs, rec + kv4_vs_at(D) + (8 * vth + 4 * vtq + 2 * hf) * (D / 32));
-    x.ks = rec[kv4_ks_at(D) + kv4_ks_byte(kp, D == 128 ? kq : kq >> 1)];
+    x.ks = rec[kv4_ks_at(D) + kv4_ks_byte(ep, eb)];
     x.all = *reinterpret_cast<const uint32_t*>(rec + kv4_vs_at(D) + 4 * (lane & (D / 8 - 1)));
   };
   auto expand = [&](int step, const Codes& x) __attribute__((always_inline)) {
-    const float ksc = mx4_scale(x.ks);
-    u32x4* kt = &sm.kv[step % kRowSlots][0][w >> 2][w >> 1 & 1][0];
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) {  // eight dims
-      const int e = D / 4 * kq + D / 8 * hf + 8 * c;
-      kt[64 * (e >> 5) + kp + 16 * (e >> 3 & 3)] = mx4_decode8(x.k[c], ksc);
-    }
+    u32x4* kt = &sm.kv[step % kRowSlots][0][w >> 2][0][0];
+    const int blk = 16 * (w >> 1 & 1);
+    if constexpr (D == 128) reinterpret_cast<u32x2*>(kt + 32 * kq + blk + kp)[hf] = u32x2{x.k[0], x.k[D / 64 - 1]};
+    else reinterpret_cast<uint32_t*>(kt + 32 * (kq >> 1) + blk + kp)[2 * (kq & 1) + hf] = x.k[0];
+    reinterpret_cast<uint8_t*>(kt + D + (blk + ep) / 4)[4 * (ep & 3) + eb] = static_cast<uint8_t>(x.ks);
     // fp16 holds every value of a block exactly whose exponent is 104 .. 140
     typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     const u16x2 even = __builtin_bit_cast(u16x2, x.all & 0x00ff00ffu) - u16x2{104, 104};
@@ -350,6 +372,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   };
 
   if constexpr (Q4) {
+    id = id_of(first);
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
       fetch(first + j, raw);
@@ -366,19 +389,41 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   auto next = [&](int step) __attribute__((always_inline)) {
     if constexpr (!Q4) landed(std::integral_constant<int, 1>{});
     barrier_after_lds_reads();  // the next step's slot is whole, the one of the last step free
+    if constexpr (!Q4) copy(step + 3);
+  };
+  auto refill = [&](int step) __attribute__((always_inline)) {  // (Q4: the slot that the barrier freed)
     if constexpr (Q4) {
       expand(step + 3, raw);
       fetch(step + 4, raw);
-    } else {
-      copy(step + 3);
     }
   };
   auto qk = [&](int step, f32x16& s) __attribute__((always_inline)) {
-    const u32x4* kp = &sm.kv[step % kRowSlots][0][hh][lc >> 4][(lane & 15) + 16 * hi];
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    if constexpr (Q4) {
+      const u32x4* kp = &sm.kv[step % kRowSlots][0][hh][0][lc];
+      const int ks = static_cast<int>(reinterpret_cast<const uint32_t*>(kp - lc + D)[lc] >> (8 * hi));
+      u32x4 k[D / 64];
 #pragma unroll
-    for (int i = 0; i < QC; ++i) s = mfma_32x32x16(kp[32 * i], qf[i], s);
+      for (int i = 0; i < D / 64; ++i) k[i] = kp[32 * (2 * i + hi)];
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const i32x8 x = {static_cast<int>(k[i][0]), static_cast<int>(k[i][1]), static_cast<int>(k[i][2]), static_cast<int>(k[i][3]), 0, 0, 0, 0};
+        const int e = static_cast<int>(q4[i].e);
+        if (i == 0) {  // (the exponent's byte is part of the instruction)
+          s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, q4[i].hi, s, 4, 0, 0, ks, 0, e);
+          s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, q4[i].lo, s, 4, 0, 0, ks, 1, e);
+        } else {
+          s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, q4[i].hi, s, 4, 0, 2, ks, 0, e);
+          s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, q4[i].lo, s, 4, 0, 2, ks, 1, e);
+        }
+        asm("" : "+v"(s) : "v"(k[i]));  // (see kv4_scores)
+      }
+    } else {
+      const u32x4* kp = &sm.kv[step % kRowSlots][0][hh][lc >> 4][(lane & 15) + 16 * hi];
+#pragma unroll
+      for (int i = 0; i < QC; ++i) s = mfma_32x32x16(kp[32 * i], qf[i], s);
+    }
   };
   auto wide_of = [&](int step) __attribute__((always_inline)) {  // (uniform)
     if constexpr (!Q4) return 0;
@@ -404,6 +449,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
       f32x16 sn;
       qk(step + 1, sn);
       wide = wide_of(step + 1);
+      refill(step);
       rest(step, s, std::true_type{});
       s = sn;
       mx = top(s);
@@ -430,6 +476,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
       big = __any(fabsf(m) >= kSpanRounded && m != -INFINITY);
     }
     next(step);
+    refill(step);
     rest(step, s, std::false_type{}, wide);
     if (__builtin_expect(poisoned, 0)) poison(step);
     if (++step == n_steps) break;
