@@ -438,14 +438,6 @@ __device__ __forceinline__ void kv4_expand_v(const Kv4Pair<D>& x, u32x4 (&vt)[D 
     }
 }
 
-// 16 and 8 bytes past this XCD's L2 (what other workgroups of the launch stored through).
-__device__ __forceinline__ f32x4 load_agent4(__amdgpu_buffer_rsrc_t r, uint32_t at) {
-  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 16 /* sc1 */));
-}
-__device__ __forceinline__ f32x2_t load_agent2(__amdgpu_buffer_rsrc_t r, uint32_t at) {
-  return __builtin_bit_cast(f32x2_t, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 16 /* sc1 */));
-}
-
 // The splits of a (row, KV head), joined in their order and stored row-major: four
 // dims a thread, 16 bytes a load, kC splits in flight (one memory round trip for
 // each).  po, pml: their (O, [G][D]) and ((m, l), [G]).

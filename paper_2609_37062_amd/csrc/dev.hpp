@@ -83,6 +83,14 @@ __device__ __forceinline__ void store_wt16(void* p, uint32_t v) {
   asm volatile("global_store_short %0, %1, off sc1" : : "v"(p), "v"(v) : "memory");
 }
 
+// 16 and 8 bytes past this XCD's L2 (what other workgroups of the launch stored through).
+__device__ __forceinline__ f32x4 load_agent4(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 16 /* sc1 */));
+}
+__device__ __forceinline__ f32x2_t load_agent2(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+  return __builtin_bit_cast(f32x2_t, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 16 /* sc1 */));
+}
+
 // 16 bytes per lane from global memory straight into LDS: lane l's bytes land
 // at lds + 16 l (the LDS address must be the same for the whole wave).  The
 // load counts in the wave's vector-memory counter until its bytes are in LDS.

@@ -16,7 +16,7 @@ namespace vsk {
 // S: slots of LDS, a step of 128 columns each, S copied ahead; exponents of four
 // steps each in E slots of their own.
 template <int WM, int WN, int FM, int FN, int S, int E>
-__global__ __launch_bounds__(64 * WM * WN, FM * FN == 16 ? 1 : 2) void k_mx4_tile(Mx4ProductArgs a, Mx4Split sp) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4ProductArgs a, Mx4Split sp) {
   constexpr int NW = WM * WN, TM = 2 * WM * FM, TN = 2 * WN * FN, T = TM + TN;  // waves; 16-row tiles of w and x
   constexpr int kCopies = (T + NW - 1) / NW;                                    // 1 KiB copies of a wave for a slot
   static_assert((S - 1) * kCopies + E * kCopies <= 63, "copies in flight");

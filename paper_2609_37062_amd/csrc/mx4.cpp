@@ -2,7 +2,6 @@
 #include "mx4.hpp"
 
 #include <climits>
-#include <cstdlib>
 #include <cstdint>
 
 #include "../../include/vsk.h"
@@ -23,6 +22,8 @@ int element(int32_t dtype) { return dtype == VSK_FP32 ? 4 : 2; }
 size_t extent(int32_t rows, int32_t k, int64_t stride, int size) {
   return (static_cast<size_t>(rows - 1) * stride + k) * size;
 }
+// rows whose extent in bytes 63 bits hold
+bool stride_ok(int64_t stride, int32_t rows, int32_t k) { return stride >= k && stride <= INT64_MAX / 8 / rows; }
 bool overlap(const void* a, size_t an, const void* b, size_t bn) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + bn && y < x + an;
@@ -37,7 +38,7 @@ size_t vsk_mx4_bytes(int32_t rows, int32_t k) { return shape_ok(rows, k) ? align
 
 int vsk_mx4_quantise(const void* src_dev, int32_t dtype, int64_t stride, int32_t rows, int32_t k, void* mx_dev,
                      void* stream) {
-  if (!src_dev || !mx_dev || !shape_ok(rows, k) || (dtype != VSK_BF16 && dtype != VSK_FP32) || stride < k) return VSK_E_ARG;
+  if (!src_dev || !mx_dev || !shape_ok(rows, k) || (dtype != VSK_BF16 && dtype != VSK_FP32) || !stride_ok(stride, rows, k)) return VSK_E_ARG;
   if (!aligned(mx_dev, kAlign) || !aligned(src_dev, element(dtype))) return VSK_E_ARG;
   if (overlap(src_dev, extent(rows, k, stride, element(dtype)), mx_dev, vsk_mx4_bytes(rows, k))) return VSK_E_ARG;
   return launched(launch_mx4_quantise(src_dev, dtype, stride, rows, k, static_cast<uint8_t*>(mx_dev), nullptr, 0,
@@ -55,7 +56,7 @@ int vsk_mx4_pack(const uint8_t* codes_dev, const uint8_t* scales_dev, int32_t ro
 }
 
 int vsk_mx4_read(const void* mx_dev, int32_t rows, int32_t k, void* dst_dev, int32_t dtype, int64_t stride, void* stream) {
-  if (!dst_dev || !mx_dev || !shape_ok(rows, k) || (dtype != VSK_BF16 && dtype != VSK_FP32) || stride < k) return VSK_E_ARG;
+  if (!dst_dev || !mx_dev || !shape_ok(rows, k) || (dtype != VSK_BF16 && dtype != VSK_FP32) || !stride_ok(stride, rows, k)) return VSK_E_ARG;
   if (!aligned(mx_dev, kAlign) || !aligned(dst_dev, element(dtype))) return VSK_E_ARG;
   if (overlap(dst_dev, extent(rows, k, stride, element(dtype)), mx_dev, vsk_mx4_bytes(rows, k))) return VSK_E_ARG;
   return launched(launch_mx4_read(static_cast<const uint8_t*>(mx_dev), rows, k, dst_dev, dtype, stride,
@@ -85,9 +86,9 @@ int vsk_mx4_product(const void* x_dev, int32_t x_dtype, int64_t x_stride, const 
                     size_t ws_bytes, void* stream) {
   if (!x_dev || !w_mx_dev || !y_dev || !ws_dev || !shape_ok(rows, k) || !shape_ok(n, k)) return VSK_E_ARG;
   if (x_dtype != VSK_BF16 && x_dtype != VSK_FP32 && x_dtype != VSK_MX4) return VSK_E_ARG;
-  if ((y_dtype != VSK_BF16 && y_dtype != VSK_FP32) || y_stride < n) return VSK_E_ARG;
+  if ((y_dtype != VSK_BF16 && y_dtype != VSK_FP32) || !stride_ok(y_stride, rows, n)) return VSK_E_ARG;
   const bool mx = x_dtype == VSK_MX4;
-  if (mx ? !aligned(x_dev, kAlign) : x_stride < k || !aligned(x_dev, element(x_dtype))) return VSK_E_ARG;
+  if (mx ? !aligned(x_dev, kAlign) : !stride_ok(x_stride, rows, k) || !aligned(x_dev, element(x_dtype))) return VSK_E_ARG;
   if (!aligned(w_mx_dev, kAlign) || !aligned(y_dev, element(y_dtype)) || !aligned(add_dev, element(y_dtype))) return VSK_E_ARG;
   const ProductWs ws(rows, n, k);
   if (ws_bytes < ws.total || !aligned(ws_dev, kAlign)) return VSK_E_ARG;

@@ -25,11 +25,6 @@ __device__ __forceinline__ f32x16 mfma_mx4_32(u32x4 a, u32x4 b, f32x16 c, uint32
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(av, bv, c, 4, 4, SA, static_cast<int>(sa), SB, static_cast<int>(sb));
 }
 
-// 16 bytes past this XCD's L2 (what other workgroups of the launch stored through).
-__device__ __forceinline__ f32x4 load_agent4(__amdgpu_buffer_rsrc_t r, uint32_t at) {
-  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 16 /* sc1 */));
-}
-
 // Behind a workgroup's write-through stores of its part of K: whether it is the last
 // of its tile's to have come this far (the others' stores are in memory then; nobody
 // waits, see attn_unit).

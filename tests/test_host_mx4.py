@@ -55,9 +55,9 @@ def test_matrix_refusals():
     for f, bads in (
         (q, (dict(src=None), dict(dst=None), dict(dtype=vsk.MX4), dict(dtype=-1), dict(stride=99), dict(rows=0), dict(k=0),
              dict(dst=B + 128), dict(src=A + 1), dict(src=A + 2, dtype=vsk.FP32), dict(dst=A), dict(src=B + 1024),
-             dict(rows=1 << 30, k=1 << 30, stride=1 << 30))),
+             dict(rows=1 << 30, k=1 << 30, stride=1 << 30), dict(stride=1 << 62))),
         (r, (dict(src=None), dict(dst=None), dict(dtype=vsk.MX4), dict(stride=99), dict(rows=-1), dict(src=A + 16),
-             dict(dst=B + 1), dict(dst=B + 2, dtype=vsk.FP32), dict(dst=A + 1024))),
+             dict(dst=B + 1), dict(dst=B + 2, dtype=vsk.FP32), dict(dst=A + 1024), dict(stride=1 << 62))),
         (p, (dict(codes=None), dict(scales=None), dict(dst=None), dict(rows=0), dict(dst=D + 64), dict(codes=D), dict(scales=D)))):
         for bad in bads:
             assert _code(f, **bad) == "ARG", bad
@@ -70,7 +70,7 @@ def test_product_refusals():
                 dict(n=0), dict(k=0), dict(x=A + 1), dict(x=A + 2, xt=vsk.FP32), dict(w=W + 128), dict(y=Y + 1),
                 dict(y=Y + 2, yt=vsk.FP32), dict(ws=None), dict(ws=D + 16), dict(nbytes=vsk.mx4_product_bytes(5, 40, 256) - 1),
                 dict(x=A + 16, xt=vsk.MX4), dict(y=A), dict(y=W + 64), dict(add=Y + 2), dict(add=Y + 1), dict(ws=A), dict(ws=W),
-                dict(ws=Y), dict(add=D), dict(n=1 << 30, k=1 << 30)):
+                dict(ws=Y), dict(add=D), dict(n=1 << 30, k=1 << 30), dict(xs=1 << 62), dict(ys=1 << 62)):
         assert _code(f, **bad) == "ARG", bad
 
 
