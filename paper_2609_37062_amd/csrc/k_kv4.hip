@@ -10,6 +10,7 @@
 namespace vsk {
 
 constexpr int kHeadThreads = 256;
+typedef u32x2 __attribute__((aligned(2))) Bf16x4;  // one load, whatever its alignment
 
 // A value of another lane: ^ 1, ^ 2, ^ 7, ^ 15, which a reduction over 2, 4, 8 and 16
 // lanes takes in turn.
@@ -108,25 +109,21 @@ __device__ __forceinline__ uint8_t* kv4_rec(const Kv4Pool& p, int slot, int hk) 
 }
 
 // Logical k, v [n][Hkv][D] into their slots (slots outside the pool are ignored).
+// A wave takes one head of consecutive tokens, which share lines of a record: 448,000
+// tokens of 8 heads x 128 658 us (a wave four heads of a token 741).
 template <int D>
 __global__ __launch_bounds__(kHeadThreads) void k_kv4_write(Kv4Pool p, const int32_t* __restrict__ slots, int n,
                                                             const uint16_t* __restrict__ k, const uint16_t* __restrict__ v) {
   constexpr int G = D / 8;
-  const int64_t unit = (static_cast<int64_t>(blockIdx.x) * kHeadThreads + threadIdx.x) / G;
-  const int i = threadIdx.x % G;
-  const bool in = unit < static_cast<int64_t>(n) * p.Hkv;
-  const int tok = in ? static_cast<int>(unit / p.Hkv) : 0, hk = in ? static_cast<int>(unit % p.Hkv) : 0;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * (kHeadThreads / 64) + (threadIdx.x >> 6));
+  const int i = threadIdx.x % G, hk = static_cast<int>(wave % p.Hkv);
+  const int64_t tok = static_cast<int64_t>(wave / p.Hkv) * (64 / G) + (threadIdx.x & 63) / G;
+  const bool in = tok < n;
   const int sl = in ? slots[tok] : -1;
   const bool on = sl >= 0 && sl < p.n_blocks * kBlock;
   uint8_t* rec = kv4_rec<D>(p, on ? sl : 0, hk);
-  const size_t at = (static_cast<size_t>(tok) * p.Hkv + hk) * D + 4 * i;
-  auto load = [&](const uint16_t* x) {
-    u32x2 r = u32x2{0u, 0u};
-    if (!on) return r;
-    r[0] = x[0] | static_cast<uint32_t>(x[1]) << 16;
-    r[1] = x[2] | static_cast<uint32_t>(x[3]) << 16;
-    return r;
-  };
+  const size_t at = static_cast<size_t>(tok * p.Hkv + hk) * D + 4 * i;
+  auto load = [&](const uint16_t* x) { return on ? *reinterpret_cast<const Bf16x4*>(x) : u32x2{0u, 0u}; };
   put_k<D>(rec, sl & 15, i, encode_head(load(k + at), load(k + at + D / 2)), on);
   put_v<D>(rec, sl & 15, i, encode_head(load(v + at), load(v + at + D / 2)), on);
 }
@@ -207,11 +204,10 @@ __device__ __forceinline__ void norm_rope(float eps, int i, u32x2 lo, u32x2 hi, 
     fy[j] = bf2f(hi[j >> 1] >> (16 * (j & 1)) & 0xffffu);
   }
   T r = 1;
-  typedef u32x2 __attribute__((aligned(2))) Four;  // (one load, whatever the gain's alignment)
   u32x2 gl{}, gh{};
   if (gain != nullptr) {
-    gl = *reinterpret_cast<const Four*>(gain + 4 * i);
-    gh = *reinterpret_cast<const Four*>(gain + D / 2 + 4 * i);
+    gl = *reinterpret_cast<const Bf16x4*>(gain + 4 * i);
+    gh = *reinterpret_cast<const Bf16x4*>(gain + D / 2 + 4 * i);
     T ss = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -324,10 +320,17 @@ __global__ __launch_bounds__(kHeadThreads) void k_qkv_norm_rope(QkvArgs a) {
 
 static unsigned head_blocks(int64_t units, int hd) { return static_cast<unsigned>((units * (hd / 8) + kHeadThreads - 1) / kHeadThreads); }
 
+// Workgroups of waves that take one head of 64 / (hd / 8) rows each.
+static unsigned wave_blocks(int rows, int heads, int hd) {
+  const int per = 64 / (hd / 8);
+  const int64_t waves = (static_cast<int64_t>(rows) + per - 1) / per * heads;
+  return static_cast<unsigned>((waves + kHeadThreads / 64 - 1) / (kHeadThreads / 64));
+}
+
 hipError_t launch_kv4_write(const Kv4Pool& p, int hd, const int32_t* slots, int n, const uint16_t* k, const uint16_t* v,
                             hipStream_t s) {
   if (n == 0) return hipSuccess;
-  const dim3 grid(head_blocks(static_cast<int64_t>(n) * p.Hkv, hd)), block(kHeadThreads);
+  const dim3 grid(wave_blocks(n, p.Hkv, hd)), block(kHeadThreads);
   if (hd == 128) hipLaunchKernelGGL(k_kv4_write<128>, grid, block, 0, s, p, slots, n, k, v);
   else hipLaunchKernelGGL(k_kv4_write<64>, grid, block, 0, s, p, slots, n, k, v);
   return hipGetLastError();
@@ -365,9 +368,7 @@ hipError_t launch_rope_table(float2* table, int max_pos, int hd, double theta, h
 }
 
 hipError_t launch_qkv_norm_rope(const QkvArgs& a, int hd, hipStream_t s) {
-  const int rows = 64 / (hd / 8);  // a wave's
-  const int64_t waves = static_cast<int64_t>((a.R + rows - 1) / rows) * (a.Hq + 2 * a.Hkv);
-  const dim3 grid(static_cast<unsigned>((waves + kHeadThreads / 64 - 1) / (kHeadThreads / 64))), block(kHeadThreads);
+  const dim3 grid(wave_blocks(a.R, a.Hq + 2 * a.Hkv, hd)), block(kHeadThreads);
   const bool four = a.pool4 != nullptr;
   auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, s, a); };
   if (hd == 128) four ? go(k_qkv_norm_rope<128, true>) : go(k_qkv_norm_rope<128, false>);
