@@ -98,9 +98,9 @@ struct RowsLds {
 // 2 x 1,000 rows through a window of 4,096 took 199 us with K and V turned into bf16,
 // 177 with V in fp16, 169 with K as codes, 159 with slots filled behind the scores (165
 // behind the whole step; priorities for the wave that has matrix instructions: none).
-// What bounds it is not one unit: of a step's 3,000 cycles on a SIMD its two waves'
-// matrix instructions take 1,020, their vector instructions about 1,500, the compute
-// unit's LDS about 1,000; two waves overlap them only in part.
+// What bounds it is not one unit: the matrix cores are busy 38% of the cycles, LDS 21%,
+// the vector units about half, and a wave waits 28% of its time, for the barrier of a
+// step and the operands behind it; two waves a SIMD overlap the rest only in part.
 template <int D, int NH, bool Q4>
 __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   constexpr int T = 256 * NH;
@@ -176,26 +176,33 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   auto landed = [&](auto steps) __attribute__((always_inline)) {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(steps)::value * kCopies) : "memory");
   };
-  // (Q4) of block w / 2 of the step this lane moves K's codes of place kp, 4 (D = 64: 2)
-  // dims of K's quarter kq from D / 8 hf on (hf: the wave's half), and the exponent of
-  // (place ep, block eb); turns V of tokens 8 vth + 4 vtq + 2 hf, + 1 of its d; and looks
-  // at V's exponents of one token (two at D = 64).  K in LDS: for each block of 32 dims
-  // the codes of 32 places, then a place's exponents, four bytes each.
+  // (Q4) of block w / 2 of the step this lane moves K's codes of place kp, 16 (D = 64: 8)
+  // dims of K's quarter kq of which half kh, and the exponent of (place ep, block eb);
+  // turns V of tokens 8 vth + 4 vtq + 2 vt2, + 1 of its d; and looks at V's exponents of
+  // one token (two at D = 64).  Lanes in the order of LDS: neighbours store neighbouring
+  // words (a wave's V stores four words apart: LDS busy 37% of the time, now 21%, and a
+  // hundredth of the call).  K in LDS: for each block of 32 dims the codes of 32 places,
+  // then a place's exponents, four bytes each.
   struct Codes {
     uint32_t k[D / 64], v[D / 64], vs[D / 64], ks, all;
   };
   const uint8_t* rec0 = a.pool4 + (static_cast<size_t>(a.layer) * a.n_blocks * a.Hkv + hk) * kv4_record(D);
-  const int hf = w & 1, piece = D == 128 ? lane : lane >> 1, part = D == 128 ? 0 : lane & 1;
-  const int kp = D == 128 ? piece & 15 : (piece & 7) + 8 * part, kq = D == 128 ? piece >> 4 : piece >> 3;
-  const int ep = lane & 15, eb = lane >> 4 & (D / 32 - 1);
-  const int vd = piece & 15, vth = piece >> 4 & 1, vtq = D == 128 ? piece >> 5 : part;
-  auto words = [](uint32_t (&to)[D / 64], const uint8_t* p) __attribute__((always_inline)) {
+  const int half = w & 1, ep = lane & 15, eb = lane >> 4 & (D / 32 - 1);
+  const int kh = lane & 1, piece = 16 * half + (lane >> 2);  // (D = 64: of 16 bytes)
+  const int kp = D == 128 ? lane >> 1 & 15 : (piece & 7) + 8 * (lane >> 1 & 1), kq = D == 128 ? 2 * half + (lane >> 5) : piece >> 3;
+  const int vt2 = lane & 1, vtq = lane >> 1 & 1, vd = lane >> 2, vth = half;
+  // (of a record, which the loads take as a buffer: a lane's place is 32 bits then)
+  const uint32_t k_at = 4 * D * half + D / 16 * lane;
+  const uint32_t v_at = kv4_v_at(D) + (D == 128 ? 16 * (vd + 16 * vth + 32 * vtq) + 8 * vt2 : 256 * half + 4 * lane);
+  const uint32_t vs_at = kv4_vs_at(D) + (8 * vth + 4 * vtq + 2 * vt2) * (D / 32);
+  const uint32_t ks_at = kv4_ks_at(D) + kv4_ks_byte(ep, eb), all_at = kv4_vs_at(D) + 4 * (lane & (D / 8 - 1));
+  auto words = [](uint32_t (&to)[D / 64], __amdgpu_buffer_rsrc_t rs, uint32_t at) __attribute__((always_inline)) {
     if constexpr (D == 128) {
-      const u32x2 y = *reinterpret_cast<const u32x2*>(p);
+      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, 0));
       to[0] = y[0];
       to[D / 64 - 1] = y[1];
     } else {
-      to[0] = *reinterpret_cast<const uint32_t*>(p);
+      to[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, at, 0, 0);
     }
   };
   auto id_of = [&](int step) __attribute__((always_inline)) { return sm.tbl[min(2 * NH * step + my_blk, span.nv - 1)]; };
@@ -203,18 +210,19 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   auto fetch = [&](int step, Codes& x) __attribute__((always_inline)) {
     const uint32_t blk = __builtin_amdgcn_readfirstlane(id);
     id = id_of(step + 1);
-    const uint8_t* rec = rec0 + static_cast<size_t>(blk) * (a.Hkv * kv4_record(D));
-    words(x.k, rec + D / 8 * lane + D / 16 * hf);
-    words(x.v, rec + kv4_v_at(D) + D / 8 * lane + D / 16 * hf);
-    words(x.vs, rec + kv4_vs_at(D) + (8 * vth + 4 * vtq + 2 * hf) * (D / 32));
-    x.ks = rec[kv4_ks_at(D) + kv4_ks_byte(ep, eb)];
-    x.all = *reinterpret_cast<const uint32_t*>(rec + kv4_vs_at(D) + 4 * (lane & (D / 8 - 1)));
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(rec0 + static_cast<size_t>(blk) * (a.Hkv * kv4_record(D))), 0, kv4_record(D), 0x00020000);
+    words(x.k, rs, k_at);
+    words(x.v, rs, v_at);
+    words(x.vs, rs, vs_at);
+    x.ks = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_at, 0, 0);
+    x.all = __builtin_amdgcn_raw_buffer_load_b32(rs, all_at, 0, 0);
   };
   auto expand = [&](int step, const Codes& x) __attribute__((always_inline)) {
     u32x4* kt = &sm.kv[step % kRowSlots][0][w >> 2][0][0];
     const int blk = 16 * (w >> 1 & 1);
-    if constexpr (D == 128) reinterpret_cast<u32x2*>(kt + 32 * kq + blk + kp)[hf] = u32x2{x.k[0], x.k[D / 64 - 1]};
-    else reinterpret_cast<uint32_t*>(kt + 32 * (kq >> 1) + blk + kp)[2 * (kq & 1) + hf] = x.k[0];
+    if constexpr (D == 128) reinterpret_cast<u32x2*>(kt + 32 * kq + blk + kp)[kh] = u32x2{x.k[0], x.k[D / 64 - 1]};
+    else reinterpret_cast<uint32_t*>(kt + 32 * (kq >> 1) + blk + kp)[2 * (kq & 1) + kh] = x.k[0];
     reinterpret_cast<uint8_t*>(kt + D + (blk + ep) / 4)[4 * (ep & 3) + eb] = static_cast<uint8_t>(x.ks);
     // fp16 holds every value of a block exactly whose exponent is 104 .. 140
     typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -223,7 +231,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     const u16x2 off = __builtin_elementwise_max(even, odd);
     const bool wide = __any(off[0] > 36 || off[1] > 36);  // (the same for both waves of the block)
     if (lane == 0) sm.wide[step % kRowSlots][w >> 2][w >> 1 & 1] = wide;
-    uint32_t* vt = reinterpret_cast<uint32_t*>(&sm.kv[step % kRowSlots][1][w >> 2][w >> 1 & 1][0]) + 2 * vtq + hf;
+    uint32_t* vt = reinterpret_cast<uint32_t*>(&sm.kv[step % kRowSlots][1][w >> 2][w >> 1 & 1][0]) + 2 * vtq + vt2;
     auto put = [&](auto half_c) __attribute__((always_inline)) {
       constexpr bool HALF = decltype(half_c)::value;
 #pragma unroll
