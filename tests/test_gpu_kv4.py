@@ -168,6 +168,28 @@ def test_long_cache():
         c.close()
 
 
+def test_blocks_behind_four_gigabytes():
+    lens, spare = [100, 40, 700], 260000
+    need = [-(-n // BLOCK) for n in lens]
+    last = sum(need) + spare
+    tables, at = [], last
+    for n in need:
+        tables.append(np.arange(at - n, at)[::-1])
+        at -= n
+    c = Cache4(8, 2, 128, lens, seed=13, spare=spare, tables=tables)
+    assert c._pool4.numel() > 2 ** 32
+    for s in range(3):
+        K, V = c.read(0, s)
+        np.testing.assert_array_equal(K, c.K[0][s])
+        np.testing.assert_array_equal(V, c.V[0][s])
+    for q_lens in ([1, 1, 1], [60, 1, 37]):
+        c.batch([0, 1, 2], q_lens)
+        for window, sinks in [(0, 0), (64, 4)]:
+            c.attend(window=window, sinks=sinks)
+            check_rows(c, window, sinks)
+    c.close()
+
+
 def test_a_shared_prefix_is_the_same_attention():
     c = Cache4(2, 4, 128, [200, 150, 170], seed=7)
     free = [b for b in range(c.n_blocks) if all(b not in t for t in c.blocks)]
@@ -243,8 +265,8 @@ def _check_rows(c, x, gains, bits, norm, layer=1):
     rows = x.shape[0]
     xd, gd = x.cuda(), gains.cuda()
     q = torch.full((rows + 1, heads, hd), -7.0, dtype=torch.bfloat16, device="cuda")
-    c.eng.qkv_norm_rope(layer, xd.data_ptr(), x.shape[1], gd[0].data_ptr() if norm else None,
-                        gd[1].data_ptr() if norm else None, q.data_ptr(), bits, c.sp)
+    c.eng.qkv_norm_rope(layer, xd.data_ptr(), x.shape[1], gd[0].data_ptr() if norm[0] else None,
+                        gd[1].data_ptr() if norm[1] else None, q.data_ptr(), bits, c.sp)
     h = c.eng.batch_host()
     slots = torch.from_numpy(h["slot"]).cuda()
     K = torch.zeros((rows, kv, hd), dtype=torch.bfloat16, device="cuda")
@@ -257,8 +279,8 @@ def _check_rows(c, x, gains, bits, norm, layer=1):
     pos = h["pos"].astype(np.float64)
     g = gains.float().numpy().astype(np.float64)
     eps, theta = float(np.float32(1e-5)), 500000.0
-    wq, mq = turned(xs[:, :heads], pos, g[0] if norm else None, theta, eps)
-    wk, mk = turned(xs[:, heads:heads + kv], pos, g[1] if norm else None, theta, eps)
+    wq, mq = turned(xs[:, :heads], pos, g[0] if norm[0] else None, theta, eps)
+    wk, mk = turned(xs[:, heads:heads + kv], pos, g[1] if norm[1] else None, theta, eps)
     # float32: a sum of squares (hd / 8 + 6 roundings), a root, a quotient, two products,
     # cos and sin (one each) and the turn (two): at most 40 half steps; half a step of bf16
     near = lambda got, want, mag: (np.abs(got - want) <= 40 * 2.0 ** -24 * mag + 2.0 ** -8 * np.abs(want) + 1e-38).all()
@@ -276,7 +298,7 @@ def _check_rows(c, x, gains, bits, norm, layer=1):
 
 @pytest.mark.parametrize("kv,group,hd", [(1, 1, 64), (3, 2, 64), (2, 16, 64), (8, 4, 128), (1, 3, 128), (5, 7, 128)])
 @pytest.mark.parametrize("bits", [16, 4])
-@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("norm", [(True, True), (False, False), (False, True), (True, False)])
 def test_qkv_rows(kv, group, hd, bits, norm):
     print(f"[gpu] qkv rows kv={kv} group={group} hd={hd} bits={bits} norm={norm}", flush=True)
     c, x, gains = _rows(Cache4 if bits == 4 else Cache, kv, group, hd, [1, 40, 333, 2000], [1, 1, 47, 130], kv * 7 + hd, pad=24)
@@ -294,7 +316,7 @@ def test_qkv_rows(kv, group, hd, bits, norm):
 @pytest.mark.parametrize("bits", [16, 4])
 def test_qkv_rows_last_positions_and_evicted_ones(bits):
     c, x, gains = _rows(Cache4 if bits == 4 else Cache, 2, 2, 128, [16384, 16383], [70, 1], 5)
-    _check_rows(c, x, gains, bits, True)
+    _check_rows(c, x, gains, bits, (True, True))
     c.close()
     if bits == 16:  # a shorter cache whose positions go on
         c, _, gains = _rows(Cache, 2, 2, 64, [300], [1], 6)
@@ -307,7 +329,7 @@ def test_qkv_rows_last_positions_and_evicted_ones(bits):
         c.eng.reserve(9, 3)
         c.batch([9], [3])
         assert c.eng.batch_host()["pos"].tolist() == [300, 301, 302]
-        _check_rows(c, bf16(c.rng.standard_normal((3, 2 * 4 * 64))), gains, 16, True)
+        _check_rows(c, bf16(c.rng.standard_normal((3, 2 * 4 * 64))), gains, 16, (True, True))
         c.close()
 
 

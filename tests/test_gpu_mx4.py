@@ -274,3 +274,31 @@ def test_streams_and_graphs():
             call(_sp())
             torch.cuda.synchronize()
             assert torch.equal(y, replayed), i
+
+
+def test_a_matrix_and_strides_behind_four_gigabytes():
+    """Weights of 4.9 GB, and rows of x so far apart that their offsets pass 32 bits."""
+    vsk = _vsk()
+    n, k = 140000, 65536
+    big = torch.empty((n, k), dtype=torch.bfloat16, device="cuda").normal_()
+    keep, at = _buf(vsk.mx4_bytes(n, k))
+    vsk.mx4_quantise(big.data_ptr(), vsk.BF16, k, n, k, at, _sp())
+    cols = np.r_[0:5, n - 60:n]
+    w = mx.values(big[torch.from_numpy(cols).cuda()].float().cpu().numpy())
+    for rows in (3, 40, 190):
+        print(f"[gpu] mx4 product {rows}x{n}x{k}", flush=True)
+        far = n // rows  # rows of x: every far-th of them
+        x = mx.values(big[::far][:rows].float().cpu().numpy())
+        y = torch.zeros((rows, n), device="cuda")
+        nb = vsk.mx4_product_bytes(rows, n, k)
+        ws, wsp = _buf(nb)
+        vsk.mx4_product(big.data_ptr(), vsk.BF16, far * k, at, rows, n, k, y.data_ptr(), vsk.FP32, n, wsp, nb, stream=_sp())
+        torch.cuda.synchronize()
+        got = y[:, torch.from_numpy(cols).cuda()].cpu().numpy().astype(np.float64)
+        # (as in test_products_of_drawn_values)
+        bound = (4 * ((k + 127) // 128) + 2 * 16) * U * (np.abs(x) @ np.abs(w).T)
+        assert (np.abs(got - x @ w.T) <= bound).all()
+    full = torch.empty((n, k), dtype=torch.bfloat16, device="cuda")
+    vsk.mx4_read(at, n, k, full.data_ptr(), vsk.BF16, k, _sp())
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(full[n - 60:].float().cpu().numpy(), w[5:])
