@@ -93,6 +93,7 @@ struct PTermsOf {
 };
 typedef PTermsOf<kPTerms> PTerms;
 
+// Eight probabilities as sums of NT bf16 terms.
 template <int NT>
 __device__ __forceinline__ void split_terms(const float (&p)[8], PTermsOf<NT>& pp) {
 #pragma unroll
@@ -713,8 +714,9 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, int row, int hk, in
   constexpr auto kMore = std::false_type{};
   constexpr auto kLast = std::true_type{};
   // The 4-bit walk's step: the next pair's codes are loaded (unless LAST) as soon as
-  // this one's have become scores and bf16.  Its maximum may lag by 2^kLag4, so that sums are rescaled in few steps (probabilities are then up
-  // to that, and the sums as exact); whole steps have no mask.
+  // this one's have become scores and bf16.  Its maximum may lag by kLag4 (base 2), so
+  // that sums are rescaled in few steps (probabilities are then up to 2^kLag4, and the
+  // sums as exact); whole steps have no mask.
   constexpr float kLag4 = 8.f;
   auto step4 = [&](int p, auto last_c) {
     const int id_a = sm.tbl[w_lo + min(2 * p + 2, cnt - 1)], id_b = sm.tbl[w_lo + min(2 * p + 3, cnt - 1)];

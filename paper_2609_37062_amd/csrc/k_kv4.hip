@@ -10,7 +10,9 @@
 namespace vsk {
 
 constexpr int kHeadThreads = 256;
-typedef u32x2 __attribute__((aligned(2))) Bf16x4;  // one load, whatever its alignment
+// (one load or store, whatever its alignment)
+typedef u32x2 __attribute__((aligned(2))) Bf16x4;
+typedef u32x4 __attribute__((aligned(2))) Bf16x8;
 
 // A value of another lane: ^ 1, ^ 2, ^ 7, ^ 15, which a reduction over 2, 4, 8 and 16
 // lanes takes in turn.
@@ -128,9 +130,8 @@ __global__ __launch_bounds__(kHeadThreads) void k_kv4_write(Kv4Pool p, const int
   put_v<D>(rec, sl & 15, i, encode_head(load(v + at), load(v + at + D / 2)), on);
 }
 
-// The values that slots hold, eight dims of K and of V a lane.  VEC: k and v are
-// 16-byte aligned.
-template <int D, bool VEC>
+// The values that slots hold, eight dims of K and of V a lane.
+template <int D>
 __global__ __launch_bounds__(kHeadThreads) void k_kv4_read(Kv4Pool p, const int32_t* __restrict__ slots, int n,
                                                            uint16_t* __restrict__ k, uint16_t* __restrict__ v) {
   constexpr int G = D / 8;
@@ -159,16 +160,8 @@ __global__ __launch_bounds__(kHeadThreads) void k_kv4_read(Kv4Pool p, const int3
   }
   const u32x4 ko = mx4_decode8(kc, ks), vo = mx4_decode8(vc, vs);
   const size_t at = static_cast<size_t>(unit) * D + 8 * i;
-  if constexpr (VEC) {
-    *reinterpret_cast<u32x4*>(k + at) = ko;
-    *reinterpret_cast<u32x4*>(v + at) = vo;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      k[at + j] = static_cast<uint16_t>(ko[j >> 1] >> (16 * (j & 1)));
-      v[at + j] = static_cast<uint16_t>(vo[j >> 1] >> (16 * (j & 1)));
-    }
-  }
+  *reinterpret_cast<Bf16x8*>(k + at) = ko;
+  *reinterpret_cast<Bf16x8*>(v + at) = vo;
 }
 
 // A float that rounds to 4 bits as the double does: its first 23 bits behind the
@@ -339,10 +332,8 @@ hipError_t launch_kv4_write(const Kv4Pool& p, int hd, const int32_t* slots, int 
 hipError_t launch_kv4_read(const Kv4Pool& p, int hd, const int32_t* slots, int n, uint16_t* k, uint16_t* v, hipStream_t s) {
   if (n == 0) return hipSuccess;
   const dim3 grid(head_blocks(static_cast<int64_t>(n) * p.Hkv, hd)), block(kHeadThreads);
-  const bool vec = (reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % 16 == 0;
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, s, p, slots, n, k, v); };
-  if (hd == 128) vec ? go(k_kv4_read<128, true>) : go(k_kv4_read<128, false>);
-  else vec ? go(k_kv4_read<64, true>) : go(k_kv4_read<64, false>);
+  if (hd == 128) hipLaunchKernelGGL(k_kv4_read<128>, grid, block, 0, s, p, slots, n, k, v);
+  else hipLaunchKernelGGL(k_kv4_read<64>, grid, block, 0, s, p, slots, n, k, v);
   return hipGetLastError();
 }
 

@@ -25,6 +25,13 @@ struct Mx4Eight {
     if constexpr (WIDE) {
 #pragma unroll
       for (int i = 0; i < (FP32 ? 2 : 1); ++i) v[i] = cnt > 0 ? reinterpret_cast<const u32x4*>(p)[i] : u32x4{0u, 0u, 0u, 0u};
+    } else if (cnt == 8) {  // (in vectors of no more than the elements' alignment)
+      if constexpr (FP32) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v[i] = __builtin_bit_cast(u32x4, static_cast<f32x4>(reinterpret_cast<const Fp32x4*>(p)[i]));
+      } else {
+        v[0] = *reinterpret_cast<const Bf16x8*>(p);
+      }
     } else if constexpr (FP32) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = i < cnt ? __float_as_uint(p[i]) : 0u;
@@ -129,7 +136,7 @@ __global__ __launch_bounds__(256) void k_mx4_pack(const uint8_t* __restrict__ co
 // The values a matrix stands for (exact in bf16), a tile a wave as in k_mx4_quantise: a
 // store takes whole lines (with a block a lane 2049 x 14336 in bf16 took 22.5 us,
 // so 12.4).
-template <bool FP32, bool VEC>
+template <bool FP32>
 __global__ __launch_bounds__(256) void k_mx4_read(const uint8_t* __restrict__ mx, int rows, int k, void* __restrict__ dst,
                                                   int64_t stride, int kt_n, int n_tiles, size_t scales_at) {
   const int lane = threadIdx.x & 63;
@@ -153,22 +160,22 @@ __global__ __launch_bounds__(256) void k_mx4_read(const uint8_t* __restrict__ mx
     if (row >= rows || cnt == 0) continue;
     const u32x4 v = mx4_decode8(c[i], mx4_scale(e[i]));
     Mx4Elem<FP32>* p = static_cast<Mx4Elem<FP32>*>(dst) + row * stride + k0;
-    if constexpr (FP32) {
-      auto f = [&](int j) { return v[j >> 1] << (j & 1 ? 0 : 16) & 0xffff0000u; };
-      if constexpr (VEC) {
-        reinterpret_cast<u32x4*>(p)[0] = u32x4{f(0), f(1), f(2), f(3)};
-        reinterpret_cast<u32x4*>(p)[1] = u32x4{f(4), f(5), f(6), f(7)};
+    auto f = [&](int j) { return v[j >> 1] << (j & 1 ? 0 : 16) & 0xffff0000u; };
+    if (cnt == 8) {  // (in vectors of no more than the elements' alignment)
+      if constexpr (FP32) {
+#pragma unroll
+        for (int j = 0; j < 8; j += 4)
+          *reinterpret_cast<Fp32x4*>(p + j) = __builtin_bit_cast(f32x4, u32x4{f(j), f(j + 1), f(j + 2), f(j + 3)});
       } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < cnt) p[j] = __uint_as_float(f(j));
+        *reinterpret_cast<Bf16x8*>(p) = v;
       }
-    } else if constexpr (VEC) {
-      *reinterpret_cast<u32x4*>(p) = v;
-    } else {
+      continue;
+    }
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < cnt) p[j] = static_cast<uint16_t>(v[j >> 1] >> (16 * (j & 1)));
+    for (int j = 0; j < 8; ++j) {
+      if (j >= cnt) continue;
+      if constexpr (FP32) p[j] = __uint_as_float(f(j));
+      else p[j] = static_cast<uint16_t>(f(j) >> 16);
     }
   }
 }
@@ -202,10 +209,8 @@ hipError_t launch_mx4_pack(const uint8_t* codes, const uint8_t* scales, int rows
 hipError_t launch_mx4_read(const uint8_t* mx, int rows, int k, void* dst, int dtype, int64_t stride, hipStream_t s) {
   const Mx4Shape g(rows, k);
   const int n = static_cast<int>(g.rt * g.kt);
-  const bool fp32 = dtype == kMxFp32, vec = rows_aligned(dst, stride, k, fp32 ? 4 : 2);
   auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((n + 3) / 4), dim3(256), 0, s, mx, rows, k, dst, stride, static_cast<int>(g.kt), n, g.scales_at()); };
-  if (fp32) vec ? go(k_mx4_read<true, true>) : go(k_mx4_read<true, false>);
-  else vec ? go(k_mx4_read<false, true>) : go(k_mx4_read<false, false>);
+  dtype == kMxFp32 ? go(k_mx4_read<true>) : go(k_mx4_read<false>);
   return hipGetLastError();
 }
 
@@ -462,8 +467,12 @@ hipError_t launch_mx4_rows(const Mx4ProductArgs& a, const Mx4Split& sp, hipStrea
   auto go = [&](auto c) {
     constexpr int RG = decltype(c)::value;
     const dim3 grid(sp.tiles() * sp.splits), block(64 * kMxWaves);
-    if (sp.tm == 2) hipLaunchKernelGGL((k_mx4_rows<RG, 2>), grid, block, 0, s, a, sp);
-    else hipLaunchKernelGGL((k_mx4_rows<RG, 1>), grid, block, 0, s, a, sp);
+    if constexpr (RG >= 2)  // (as mx4_split does)
+      if (sp.tm == 2) {
+        hipLaunchKernelGGL((k_mx4_rows<RG, 2>), grid, block, 0, s, a, sp);
+        return;
+      }
+    hipLaunchKernelGGL((k_mx4_rows<RG, 1>), grid, block, 0, s, a, sp);
   };
   switch (sp.tn) {
     case 1: go(std::integral_constant<int, 1>{}); break;

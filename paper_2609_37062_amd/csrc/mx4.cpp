@@ -110,8 +110,6 @@ int vsk_mx4_product(const void* x_dev, int32_t x_dtype, int64_t x_stride, const 
   a.y_fp32 = y_dtype == VSK_FP32;
   a.y_stride = y_stride;
   a.add = add_dev;
-  const size_t four = 4 * element(y_dtype);
-  a.wide = y_stride % 4 != 0 || !aligned(y_dev, four) || !aligned(add_dev, four) ? 0 : y_stride % 8 == 0 && aligned(y_dev, 16) ? 2 : 1;
   Mx4Split sp = ws.sp;
   int* counter = sp.counters() > 0 ? reinterpret_cast<int*>(base + ws.counter) : nullptr;
   sp.counter = counter;

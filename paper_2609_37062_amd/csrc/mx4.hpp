@@ -48,7 +48,6 @@ struct Mx4ProductArgs {
   int y_fp32;
   int64_t y_stride;
   const void* add;  // nullable, as y
-  int wide;         // 1: y, add and their rows allow vectors of four, 2: y's also of eight
 };
 // Whether launch_mx4_stream takes x as it is (few short rows).
 bool mx4_takes_rows(int dtype, const void* x, int64_t stride, int rows, int k);
