@@ -228,6 +228,29 @@ def test_large_scores():
     c.close()
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_a_query_that_is_not_finite(hd, bad):
+    """Only its own row and head are not finite."""
+    c = Cache4(2, 4, hd, [90, 300, 1500], seed=31)
+    for q_lens in ([60, 33, 1], [1, 1, 1]):
+        c.batch([0, 1, 2], q_lens)
+        c.attend(window=200, sinks=4)
+        finite = c.out()
+        rows = [0, sum(q_lens) - 1, sum(q_lens) // 2]
+        for r in rows:
+            c.qd[r, 5, 40] = bad
+        c.attend(window=200, sinks=4)
+        got = c.out()
+        for r in rows:
+            assert not np.isfinite(got[r, 5]).any()
+            got[r, 5] = finite[r, 5]
+        c.out = lambda: got
+        check_rows(c, 200, 4)
+        del c.out
+    c.close()
+
+
 def test_replayed_beside_eager_calls():
     c = Cache4(2, 4, 128, [300, 97, 1500], seed=9)
     c.batch([0, 1, 2], [60, 1, 1])
