@@ -331,8 +331,11 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     constexpr bool FAST = decltype(fast_c)::value;
     const u32x4* vp = &sm.kv[step % kRowSlots][1][hh][0][32 * (lc >> 4) + (lane & 15) + 16 * hi];
     // (Q4: weights times 2^7, with the lag at most 2^15: an fp16's smallest step is then
-    // 2^-32 of the largest weight's and more, and many small weights keep their sum)
-    const float mb = (!FAST && m == -INFINITY ? 0.f : m) - (Q4 ? 7.f : 0.f);
+    // 2^-32 of the largest weight's and more, and many small weights keep their sum.  The 7
+    // joins the maximum where that is below 2^14, so that a weight is one fma, and the
+    // difference elsewhere: from 2^24 on a float32 maximum less 7 is off by 1 and more)
+    constexpr float kUp = Q4 ? 7.f : 0.f;
+    const float mb = FAST ? m - kUp : m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       u32x4 vt[OC];
@@ -348,7 +351,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
           const float x = s[8 * b + r] * sc;
-          p[r] = __builtin_amdgcn_exp2f(x - mb);
+          p[r] = __builtin_amdgcn_exp2f(Q4 ? x - mb + kUp : x - mb);
         }
       }
       l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));

@@ -377,3 +377,41 @@ def test_qkv_rows_refusals():
             c.eng.kv4_attend(a["layer"], a["q"], a["o"], a["ws"], c.ws_bytes, a["window"], a["sinks"], c.sp)
         assert e.value.code == code, bad
     c.close()
+
+
+@pytest.mark.parametrize("cls", [Cache, Cache4])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n,q_len", [(700, 5), (700, 1), (16000, 3), (16000, 1), (16000, 200)])
+def test_equal_scores_weigh_the_same_at_any_size(cls, hd, n, q_len):
+    """Scores of 2^12 to 2^29.  Two keys A and B have the same one, some units in its last
+    place above a third's, L, and every other key's is zero (no weight at all).  What L
+    weighs is the arithmetic's; A and B weigh the same, and V is 2 at L, 3 at A, 1 at B
+    (all exact in 4 bits): 2 throughout, wherever the three stand and whichever is the
+    first to set a walk's maximum."""
+    print(f"[gpu] equal scores {cls.__name__} hd={hd} n={n} q_len={q_len}", flush=True)
+    kv, group = 4, 4
+    c = cls(kv, group, hd, [n], seed=17)
+    K, V = c.K[0][0], c.V[0][0]
+    K[:] = 0
+    far = n // 700
+    # (L and one of A and B in the same steps' part of a prompt row's walk, or in none)
+    for h, (l, a, b) in enumerate(((3, 197, 360 * far), (40, 70 * far, 104), (2, 600 * far, 600 * far + 1), (97 * far, 10, 97 * far + 64))):
+        K[[l, a, b], h, 0] = 2.0 ** 14
+        K[[a, b], h, 32] = 1.0
+        V[[l, a, b], h] = np.array([2.0, 3.0, 1.0])[:, None]
+    c.write(0, 0)
+    np.testing.assert_array_equal(c.read(0, 0)[0], K)
+    c.batch([0], [q_len])
+    c.q[:] = 0
+    for e in range(-2, 16):
+        for units in (1, 2, 3, 4, 6):
+            # a score of 2^(14 + e), whose last place is 2^(e - 9)
+            c.q[:, :, 0] = 2.0 ** e
+            c.q[:, :, 32] = units * 2.0 ** (e - 9)
+            c.qd.copy_(c.q)
+            c.attend()
+            # a weight is off by at most 2^-11 of itself (half a step of fp16) and some
+            # steps of float32, of values up to 3; half a step of bf16 of 2
+            err = np.abs(c.out() - 2.0)
+            assert (err <= 2.0 ** -7 + 3 * 2.0 ** -11 + 3 * 2.0 ** -16).all(), (e, units, float(err.max()), np.argwhere(~(err <= 2.0 ** -6))[:4].tolist())
+    c.close()
