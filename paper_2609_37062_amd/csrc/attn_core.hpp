@@ -380,13 +380,15 @@ __device__ __forceinline__ f32x4 kv4_scores(u32x4 k, uint32_t ks, const Kv4Query
   f32x4 c = f32x4{0.f, 0.f, 0.f, 0.f};
   c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.hi, c, 4, 0, G, static_cast<int>(ks), 0, static_cast<int>(q.e));
   c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.lo, c, 4, 0, G, static_cast<int>(ks), 1, static_cast<int>(q.e));
-  // The operands stay until the sums are there: given registers of an operand that it
-  // takes as dead, the compiler let the sums overlap them partly, and the instruction,
-  // which reads an 8-bit operand in two passes, then took its own results (seen in a
-  // check of its lane layout).
-  asm("" : "+v"(c) : "v"(k), "v"(q.lo));
+  // The operands of both stay until the sums are there: given registers of an operand
+  // that it takes as dead, the compiler let the sums overlap them partly, and the
+  // instruction, which reads an 8-bit operand in two passes, then took its own results
+  // (seen in a check of its lane layout).
+  asm("" : "+v"(c) : "v"(k), "v"(ks), "v"(q.hi), "v"(q.lo), "v"(q.e));
   return c;
 }
+// The terms stay up to here.
+__device__ __forceinline__ void kv4_keep(const Kv4Query& q) { asm volatile("" : : "v"(q.hi), "v"(q.lo), "v"(q.e)); }
 template <int D, bool NTKV>
 __device__ __forceinline__ void kv4_load(Kv4Pair<D>& x, const uint8_t* rec_k, const uint8_t* rec_v, int lane) {
   const int quad = lane >> 4, i = lane & 15, th = quad & 1;

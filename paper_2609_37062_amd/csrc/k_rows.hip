@@ -428,7 +428,7 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
           s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, q4[i].hi, s, 4, 0, 2, ks, 0, e);
           s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, q4[i].lo, s, 4, 0, 2, ks, 1, e);
         }
-        asm("" : "+v"(s) : "v"(k[i]));  // (see kv4_scores)
+        asm("" : "+v"(s) : "v"(k[i]), "v"(ks));  // (see kv4_scores; q stays to the end of the walk)
       }
     } else {
       const u32x4* kp = &sm.kv[step % kRowSlots][0][hh][lc >> 4][(lane & 15) + 16 * hi];
@@ -494,6 +494,10 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     qk(step, s);
     mx = top(s);
     wide = wide_of(step);
+  }
+  if constexpr (Q4) {
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) kv4_keep(q4[i]);
   }
   l = add_xor32(l);
   if constexpr (!Q4) landed(std::integral_constant<int, 0>{});  // (the steps past the list: before LDS is used again or ends)
