@@ -591,9 +591,11 @@ __global__ __launch_bounds__(256) void k_rows_join(AttnPrefillArgs a) {
     }
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      if (s0 + u >= a.splits || ml[u].x == -INFINITY) continue;  // (a split of which the row sees nothing)
+      if (s0 + u >= a.splits) continue;
+      // (a maximum of -inf: a split of which the row sees nothing, whose sums are zero, or
+      // only scores that are NaN, whose sums are)
       const float mn = fmaxf(M, ml[u].x);
-      const float f0 = M == -INFINITY ? 0.f : exp2f(M - mn), f1 = exp2f(ml[u].x - mn);
+      const float f0 = M == -INFINITY ? 0.f : exp2f(M - mn), f1 = ml[u].x == -INFINITY ? 0.f : exp2f(ml[u].x - mn);
       L = L * f0 + ml[u].y * f1;
       y = y * f0 + x[u] * f1;
       M = mn;

@@ -415,3 +415,23 @@ def test_equal_scores_weigh_the_same_at_any_size(cls, hd, n, q_len):
             err = np.abs(c.out() - 2.0)
             assert (err <= 2.0 ** -7 + 3 * 2.0 ** -11 + 3 * 2.0 ** -16).all(), (e, units, float(err.max()), np.argwhere(~(err <= 2.0 ** -6))[:4].tolist())
     c.close()
+
+
+@pytest.mark.parametrize("cls", [Cache, Cache4])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("q_len", [1, 3, 70])
+def test_keys_that_are_not_finite_fill_a_split(cls, hd, q_len):
+    """3,840 keys in a row that are NaN: whole splits of one (of 256, 320, 384, 640 or 768
+    keys).  Every row sees them, so every output of their head is NaN, and no other."""
+    print(f"[gpu] a split of NaN {cls.__name__} hd={hd} q_len={q_len}", flush=True)
+    c = cls(2, 4, hd, [16000], seed=23)
+    c.K[0][0][:3840, 1] = np.nan
+    c.write(0, 0)
+    c.batch([0], [q_len])
+    c.attend()
+    o = c.out().reshape(q_len, 2, 4, hd)
+    assert np.isnan(o[:, 1]).all()
+    assert np.isfinite(o[:, 0]).all()
+    c.attend(window=9000)  # (none of them is seen)
+    assert np.isfinite(c.out()).all()
+    c.close()
