@@ -37,6 +37,8 @@
 // vector operations between them and nothing else, no memory, would take 82 of
 // the 103: with all of them busy the chip runs 1.45 PFLOP/s.  One bf16 term a
 // weight would be a fifth faster, at errors of 2^-9 a weight.
+#include <climits>
+
 #include "attn_core.hpp"
 
 namespace vsk {
@@ -218,21 +220,47 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
     x.ks = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_at, 0, 0);
     x.all = __builtin_amdgcn_raw_buffer_load_b32(rs, all_at, 0, 0);
   };
+  // Slots behind the rows' last key (of the list's last block, and what stands in for those
+  // past it) become values of zero with an exponent that fp16 holds.
+  const int last_keys = min(kv_end, pos0 + n_rows) % kBlock;
+  const int cut_from = last_keys > 0 ? (span.nv - 1 - my_blk + 2 * NH - 1) / (2 * NH) : INT_MAX;  // steps
+  auto cut = [&](Codes& x) __attribute__((always_inline)) {
+    const uint32_t kNone = 0x78787878u;
+    const int t = 8 * vth + 4 * vtq + 2 * vt2, n = last_keys;
+    if constexpr (D == 128) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        x.v[j * (D / 128)] = t + j < n ? x.v[j * (D / 128)] : 0u;
+        x.vs[j * (D / 128)] = t + j < n ? x.vs[j * (D / 128)] : kNone;
+      }
+      x.all = (lane & 15) < n ? x.all : kNone;
+    } else {
+      auto some = [&](int first, uint32_t y, uint32_t none) {  // of two tokens, 16 bits each
+        const uint32_t keep = (first < n ? 0xffffu : 0u) | (first + 1 < n ? 0xffff0000u : 0u);
+        return (y & keep) | (none & ~keep);
+      };
+      x.v[0] = some(t, x.v[0], 0u);
+      x.vs[0] = some(t, x.vs[0], kNone);
+      x.all = some(2 * (lane & 7), x.all, kNone);
+    }
+  };
+  // fp16 holds every value of a block exactly whose exponents are 104 .. 140 (the same
+  // for both waves of the block)
+  auto is_wide = [](uint32_t all) __attribute__((always_inline)) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const u16x2 even = __builtin_bit_cast(u16x2, all & 0x00ff00ffu) - u16x2{104, 104};
+    const u16x2 odd = __builtin_bit_cast(u16x2, all >> 8 & 0x00ff00ffu) - u16x2{104, 104};
+    const u16x2 off = __builtin_elementwise_max(even, odd);
+    return static_cast<bool>(__any(off[0] > 36 || off[1] > 36));
+  };
   auto expand = [&](int step, const Codes& x) __attribute__((always_inline)) {
     u32x4* kt = &sm.kv[step % kRowSlots][0][w >> 2][0][0];
     const int blk = 16 * (w >> 1 & 1);
     if constexpr (D == 128) reinterpret_cast<u32x2*>(kt + 32 * kq + blk + kp)[kh] = u32x2{x.k[0], x.k[D / 64 - 1]};
     else reinterpret_cast<uint32_t*>(kt + 32 * (kq >> 1) + blk + kp)[2 * (kq & 1) + kh] = x.k[0];
     reinterpret_cast<uint8_t*>(kt + D + (blk + ep) / 4)[4 * (ep & 3) + eb] = static_cast<uint8_t>(x.ks);
-    // fp16 holds every value of a block exactly whose exponent is 104 .. 140
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-    const u16x2 even = __builtin_bit_cast(u16x2, x.all & 0x00ff00ffu) - u16x2{104, 104};
-    const u16x2 odd = __builtin_bit_cast(u16x2, x.all >> 8 & 0x00ff00ffu) - u16x2{104, 104};
-    const u16x2 off = __builtin_elementwise_max(even, odd);
-    const bool wide = __any(off[0] > 36 || off[1] > 36);  // (the same for both waves of the block)
-    if (lane == 0) sm.wide[step % kRowSlots][w >> 2][w >> 1 & 1] = wide;
     uint32_t* vt = reinterpret_cast<uint32_t*>(&sm.kv[step % kRowSlots][1][w >> 2][w >> 1 & 1][0]) + 2 * vtq + vt2;
-    auto put = [&](auto half_c) __attribute__((always_inline)) {
+    auto put = [&](const Codes& x, auto half_c) __attribute__((always_inline)) {
       constexpr bool HALF = decltype(half_c)::value;
 #pragma unroll
       for (int b = 0; b < D / 32; ++b) {
@@ -251,8 +279,21 @@ __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
         vt[4 * (32 * (2 * b + 1) + vd + 16 * vth)] = high_halves(y[0], y[1]);
       }
     };
-    if (__builtin_expect(wide, 0)) put(std::false_type{});
-    else put(std::true_type{});
+    bool wide = is_wide(x.all);
+    if (__builtin_expect(wide, 0)) {
+      // (slots of no token decide nothing: where what an earlier owner left in them is all
+      // that fp16 does not hold, it goes, and where it is not, weights of zero leave it out)
+      Codes y = x;
+      if (step >= cut_from) {
+        cut(y);
+        wide = is_wide(y.all);
+      }
+      if (wide) put(y, std::false_type{});
+      else put(y, std::true_type{});
+    } else {
+      put(x, std::true_type{});
+    }
+    if (lane == 0) sm.wide[step % kRowSlots][w >> 2][w >> 1 & 1] = wide;
   };
   Codes raw;
   float m = -INFINITY, l = 0.f;

@@ -435,3 +435,28 @@ def test_keys_that_are_not_finite_fill_a_split(cls, hd, q_len):
     c.attend(window=9000)  # (none of them is seen)
     assert np.isfinite(c.out()).all()
     c.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("q_lens", [[1, 1, 1], [5, 20, 99], [2, 33, 40]])
+def test_slots_of_no_token_leave_no_bit(hd, q_lens):
+    """The same tokens in a pool that held other things before: the same bits."""
+    print(f"[gpu] unused slots hd={hd} q_lens={q_lens}", flush=True)
+    c = Cache4(2, 4, hd, [5, 33, 100], seed=12)
+    c.batch([0, 1, 2], q_lens)
+    outs = []
+    for fill in (0x7f, 0xff, 0x00, 0x97, None):  # exponents 0, NaN, -127, 24, drawn ones
+        if fill is None:
+            c._pool4.view(torch.uint8).copy_(torch.from_numpy(np.random.default_rng(5).integers(0, 256, c._pool4.view(torch.uint8).numel(), np.uint8)))
+        else:
+            c._pool4.view(torch.uint8).fill_(fill)
+        for s in range(3):
+            c.write(0, s)
+        for window, sinks in [(0, 0), (12, 3)]:
+            c.o[:-1].fill_(0)
+            c.attend(window=window, sinks=sinks)
+            check_rows(c, window, sinks)
+            outs.append(c.out())
+    for i in range(2, len(outs)):
+        np.testing.assert_array_equal(outs[i], outs[i % 2])
+    c.close()
