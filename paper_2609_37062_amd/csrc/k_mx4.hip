@@ -345,9 +345,21 @@ hipError_t launch_mx4_stream(const Mx4ProductArgs& a, hipStream_t s) {
   // one workgroup a compute unit up to two tiles each, beyond that two
   const int nt = static_cast<int>(g.rt), most = nt <= 512 ? 256 : 512, tiles = (nt + most - 1) / most;
   const dim3 grid((nt + tiles - 1) / tiles), block(64 * kMxWaves);
-  const size_t lds = static_cast<size_t>(g.kt) * 1088;
-  if (a.x_fp32) hipLaunchKernelGGL(k_mx4_stream<true>, grid, block, lds, s, a);
-  else hipLaunchKernelGGL(k_mx4_stream<false>, grid, block, lds, s, a);
+  constexpr size_t kStep = 1024 + 64;  // bytes of LDS for a step's codes and exponents
+  const size_t lds = static_cast<size_t>(g.kt) * kStep;
+  // with the static arrays this can be more than 64 KiB of LDS: allow it once
+  auto allow = [](auto kern) {
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMxResident * kStep));
+  };
+  if (a.x_fp32) {
+    static const hipError_t attr = allow(&k_mx4_stream<true>);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL(k_mx4_stream<true>, grid, block, lds, s, a);
+  } else {
+    static const hipError_t attr = allow(&k_mx4_stream<false>);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL(k_mx4_stream<false>, grid, block, lds, s, a);
+  }
   return hipGetLastError();
 }
 

@@ -302,3 +302,34 @@ def test_a_matrix_and_strides_behind_four_gigabytes():
     vsk.mx4_read(at, n, k, full.data_ptr(), vsk.BF16, k, _sp())
     torch.cuda.synchronize()
     np.testing.assert_array_equal(full[n - 60:].float().cpu().numpy(), w[5:])
+
+
+@pytest.mark.parametrize("rows", [1, 4])
+@pytest.mark.parametrize("k", [5760, 5888, 6144, 6152, 6272])
+def test_few_rows_of_the_most_columns_held_in_lds(rows, k):
+    """Up to four rows are quantised into LDS, up to 48 steps of 128 columns: more than
+    64 KiB from 45 steps on.  Exact, as in test_products_of_small_whole_numbers_are_exact;
+    the same captured, as the first call of a size may be."""
+    print(f"[gpu] mx4 product {rows}x{k} in lds", flush=True)
+    rng = np.random.default_rng(rows + k)
+    grid = np.concatenate([mx.GRID, -mx.GRID])
+    n = 530
+    x, w = grid[rng.integers(0, 16, (rows, k))], grid[rng.integers(0, 16, (n, k))]
+    x[:, ::32] = w[:, ::32] = 6
+    wm, wat = _matrix(w)
+    for kind in ("bf16", "fp32"):
+        np.testing.assert_array_equal(_product(x, wat, n, kind, torch.float32), x @ w.T, err_msg=kind)
+    vsk = _vsk()
+    xd = torch.from_numpy(x).to("cuda", torch.bfloat16)
+    y = torch.zeros((rows, n), device="cuda")
+    nb = vsk.mx4_product_bytes(rows, n, k)
+    ws, wsp = _buf(nb)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        vsk.mx4_product(xd.data_ptr(), vsk.BF16, k, wat, rows, n, k, y.data_ptr(), vsk.FP32, n, wsp, nb,
+                        stream=torch.cuda.current_stream().cuda_stream)
+    for _ in range(3):
+        y.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(y.cpu().numpy().astype(np.float64), x @ w.T)
