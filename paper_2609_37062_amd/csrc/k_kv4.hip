@@ -196,28 +196,42 @@ __device__ __forceinline__ void norm_rope(float eps, int i, u32x2 lo, u32x2 hi, 
     fx[j] = bf2f(lo[j >> 1] >> (16 * (j & 1)) & 0xffffu);
     fy[j] = bf2f(hi[j >> 1] >> (16 * (j & 1)) & 0xffffu);
   }
-  T r = 1;
-  u32x2 gl{}, gh{};
-  if (gain != nullptr) {
-    gl = *reinterpret_cast<const Bf16x4*>(gain + 4 * i);
-    gh = *reinterpret_cast<const Bf16x4*>(gain + D / 2 + 4 * i);
-    T ss = 0;
+  T u[4], v[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      ss = fma(static_cast<T>(fx[j]), static_cast<T>(fx[j]), ss);
-      ss = fma(static_cast<T>(fy[j]), static_cast<T>(fy[j]), ss);
-    }
-    r = inv_sqrt(fma(sum_head<G>(ss), static_cast<T>(1.0 / D), static_cast<T>(eps)));
+  for (int j = 0; j < 4; ++j) {
+    u[j] = static_cast<T>(fx[j]);
+    v[j] = static_cast<T>(fy[j]);
+  }
+  if (gain != nullptr) {
+    const u32x2 gl = *reinterpret_cast<const Bf16x4*>(gain + 4 * i), gh = *reinterpret_cast<const Bf16x4*>(gain + D / 2 + 4 * i);
+    auto mean = [&](auto zero) {  // of the squares, and eps
+      using S = decltype(zero);
+      S ss = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        ss = fma(static_cast<S>(fx[j]), static_cast<S>(fx[j]), ss);
+        ss = fma(static_cast<S>(fy[j]), static_cast<S>(fy[j]), ss);
+      }
+      return fma(sum_head<G>(ss), static_cast<S>(1.0 / D), static_cast<S>(eps));
+    };
+    auto scaled = [&](auto r) {
+      using S = decltype(r);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        u[j] = static_cast<T>(static_cast<S>(fx[j]) * (r * static_cast<S>(bf2f(gl[j >> 1] >> (16 * (j & 1)) & 0xffffu))));
+        v[j] = static_cast<T>(static_cast<S>(fy[j]) * (r * static_cast<S>(bf2f(gh[j >> 1] >> (16 * (j & 1)) & 0xffffu))));
+      }
+    };
+    const T m = mean(T(0));
+    scaled(inv_sqrt(m));
+    // squares that a float32 does not hold, or not to its last bit (the lanes of a head agree)
+    if constexpr (sizeof(T) == 4)
+      if (__builtin_expect(!(m >= 0x1p-90f && m <= 0x1p120f), 0)) scaled(inv_sqrt(mean(0.0)));
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    T u = static_cast<T>(fx[j]), v = static_cast<T>(fy[j]);
-    if (gain != nullptr) {
-      u *= r * static_cast<T>(bf2f(gl[j >> 1] >> (16 * (j & 1)) & 0xffffu));
-      v *= r * static_cast<T>(bf2f(gh[j >> 1] >> (16 * (j & 1)) & 0xffffu));
-    }
-    x[j] = u * c[j] - v * s[j];
-    y[j] = v * c[j] + u * s[j];
+    x[j] = u[j] * c[j] - v[j] * s[j];
+    y[j] = v[j] * c[j] + u[j] * s[j];
   }
 }
 

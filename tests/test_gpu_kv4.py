@@ -460,3 +460,55 @@ def test_slots_of_no_token_leave_no_bit(hd, q_lens):
     for i in range(2, len(outs)):
         np.testing.assert_array_equal(outs[i], outs[i % 2])
     c.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("norm", [(True, True), (False, False)])
+def test_qkv_rows_of_any_magnitude(hd, bits, norm):
+    """Heads whose squares a float32 does not hold, and tiny ones."""
+    print(f"[gpu] qkv rows of any magnitude hd={hd} bits={bits} norm={norm}", flush=True)
+    c, x, gains = _rows(Cache4 if bits == 4 else Cache, 2, 3, hd, [40, 333], [33, 20], 77)
+    e = torch.from_numpy(c.rng.choice([-126, -80, -64, 0, 50, 62, 64, 66, 90, 120, 124], (53, 10)))
+    # (heads of mixed size too: half of the dims 2^-30 of the others)
+    f = torch.ones(hd, dtype=torch.float64)
+    f[::2] = 2.0 ** -30
+    v = x.reshape(53, 10, hd).double() * 2.0 ** e.double()[:, :, None]
+    v[::3] *= f
+    x = v.to(torch.bfloat16).reshape(53, -1)
+    assert torch.isfinite(x).all()
+    _check_rows(c, x, gains, bits, norm)
+    c.close()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_qkv_rows_without_an_epsilon(bits, monkeypatch):
+    """Tiny heads are normed as they are where nothing is added to their squares."""
+    import cache_case
+    model = cache_case.model
+
+    def no_eps(*a, **k):
+        m = model(*a, **k)
+        m.rms_eps = 0.0
+        return m
+
+    monkeypatch.setattr(cache_case, "model", no_eps)
+    c, x, gains = _rows(Cache4 if bits == 4 else Cache, 2, 3, 128, [40], [40], 78)
+    e = torch.from_numpy(c.rng.choice([-100, -75, -60, -44, 0, 70], (40, 10)))
+    x = (x.reshape(40, 10, 128).double() * 2.0 ** e.double()[:, :, None]).to(torch.bfloat16).reshape(40, -1)
+    xd, gd = x.cuda(), gains.cuda()
+    q = torch.zeros((40, 6, 128), dtype=torch.bfloat16, device="cuda")
+    c.eng.qkv_norm_rope(1, xd.data_ptr(), x.shape[1], gd[0].data_ptr(), gd[1].data_ptr(), q.data_ptr(), bits, c.sp)
+    K, _ = c.read(1, 0)
+    xs, g = x.double().numpy().reshape(40, -1, 128), gains.double().numpy()
+    pos = c.eng.batch_host()["pos"].astype(np.float64)
+    wq, mq = turned(xs[:, :6], pos, g[0], 500000.0, 0.0)
+    wk, mk = turned(xs[:, 6:8], pos, g[1], 500000.0, 0.0)
+    # (as in _check_rows)
+    near = lambda got, want, mag: (np.abs(got - want) <= 40 * 2.0 ** -24 * mag + 2.0 ** -8 * np.abs(want)).all()
+    assert near(q.double().cpu().numpy(), wq, mq)
+    if bits == 16:
+        assert near(K.astype(np.float64), wk, mk)
+    else:
+        np.testing.assert_array_equal(K, mx.values(wk))
+    c.close()
