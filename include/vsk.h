@@ -332,8 +332,8 @@ int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host
  *
  * A matrix [rows][k] in that format ("MX4 matrix") is held in a layout of the
  * library's own, in caller-owned device memory of vsk_mx4_bytes (0 for a bad
- * shape), 256-byte aligned; rows and k from 1 to 2^30 (at most 2^31 tiles of 16 x
- * 128).  It is either an activation (rows are the batch's) or a weight matrix
+ * shape), 256-byte aligned; rows and k from 1 to 2^30 (at most 2^26 - 4 tiles of
+ * 16 x 128).  It is either an activation (rows are the batch's) or a weight matrix
  * [out][in].  These calls need no handle; VSK_E_ARG on a null pointer, a bad
  * shape, type, stride (elements from row to row, at least a row) or alignment (to
  * the element), or buffers that overlap.  Rows that are 16-byte aligned with k a
@@ -371,7 +371,8 @@ size_t vsk_kv4_pool_bytes(const vsk_model_cfg* cfg, int32_t n_blocks);
  * vsk_kv_init unbinds it too). */
 int vsk_kv4_init(vsk_handle* h, void* pool_dev, size_t bytes);
 /* As vsk_kv_write and vsk_kv_read: logical bf16 k, v [n][n_kv_heads][head_dim] are
- * quantised into their slots / the values that slots stand for. */
+ * quantised into their slots / the values that slots stand for.  (n + 8) * n_kv_heads *
+ * head_dim is at most 2^35 - 4096 (VSK_E_ARG); vsk_qkv_norm_rope's rows and heads too. */
 int vsk_kv4_write(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_t n, const void* k_dev,
                   const void* v_dev, void* stream);
 int vsk_kv4_read(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_t n, void* k_dev, void* v_dev,

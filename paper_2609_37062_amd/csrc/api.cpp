@@ -870,6 +870,7 @@ static int kv4_move(vsk_handle* h, bool write, int32_t layer, const int32_t* slo
   if (n < 0 || (n > 0 && (!slots || !k || !v))) return fail(h, VSK_E_ARG, "bad KV transfer arguments");
   if (reinterpret_cast<uintptr_t>(slots) % 4 || reinterpret_cast<uintptr_t>(k) % 2 || reinterpret_cast<uintptr_t>(v) % 2)
     return fail(h, VSK_E_ARG, "buffer not aligned to its elements");
+  if (!kv4_launches(n, h->cfg.n_kv_heads, h->cfg.head_dim)) return fail(h, VSK_E_ARG, "too many tokens for one call");
   const Kv4Pool p{h->pool4, layer, h->n_blocks, h->cfg.n_kv_heads};
   hipStream_t s = static_cast<hipStream_t>(stream);
   const hipError_t e =
@@ -932,6 +933,7 @@ int vsk_qkv_norm_rope(vsk_handle* h, int32_t layer, const void* qkv_dev, int64_t
   const int64_t width = static_cast<int64_t>(c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim;
   if (stride < width || stride % 8) return fail(h, VSK_E_ARG, "stride must be a multiple of 8, of a row at least");
   if (stride > INT64_MAX / 4 / b.n_rows) return fail(h, VSK_E_ARG, "stride too large");
+  if (!kv4_launches(b.n_rows, c.n_q_heads + 2 * c.n_kv_heads, c.head_dim)) return fail(h, VSK_E_ARG, "too many rows for one call");
   if (reinterpret_cast<uintptr_t>(qkv_dev) % 16 || reinterpret_cast<uintptr_t>(q_dev) % 16)
     return fail(h, VSK_E_ARG, "qkv and q must be 16-byte aligned");
   if (reinterpret_cast<uintptr_t>(q_gain_dev) % 2 || reinterpret_cast<uintptr_t>(k_gain_dev) % 2)

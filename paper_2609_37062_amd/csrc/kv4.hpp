@@ -36,6 +36,10 @@ __host__ __device__ inline int kv4_v_byte(int D, int t, int d) {
   return D == 128 ? 16 * (d + 16 * (t >> 3) + 32 * (t >> 2 & 1)) + 4 * (t & 3) : 16 * (d + 16 * (t >> 3)) + 2 * (t & 7);
 }
 
+// Whether a launch takes so many heads of rows (eight values a thread, less than 2^32
+// of them with what fills up a wave and a workgroup).
+inline bool kv4_launches(int64_t rows, int heads, int hd) { return (rows + 8) * heads * hd <= (INT64_C(1) << 35) - 4096; }
+
 struct Kv4Pool {
   uint8_t* pool;
   int layer, n_blocks, Hkv;

@@ -11,10 +11,12 @@ using namespace vsk;
 
 namespace {
 
+// (a launch takes a wave a tile, and less than 2^32 threads)
+constexpr int64_t kMxMostTiles = (1 << 26) - 4;
 bool shape_ok(int32_t rows, int32_t k) {
   if (rows < 1 || k < 1 || rows > (1 << 30) || k > (1 << 30)) return false;
   const Mx4Shape g(rows, k);
-  return g.rt * g.kt <= INT32_MAX && g.rt * g.kq <= INT32_MAX;
+  return g.rt * g.kt <= kMxMostTiles;
 }
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 int element(int32_t dtype) { return dtype == VSK_FP32 ? 4 : 2; }

@@ -133,3 +133,20 @@ def test_eviction_refuses_a_four_bit_cache():
     assert _code(e.kv_evict, [7], [0], [20], 2, 4, W, 100, Y, 1 << 16, kept_ptr=D, out_stride=32) == "UNSUPPORTED"
     assert e.free_blocks() == free
     e.close()
+
+
+def test_sizes_that_no_launch_takes_are_refused():
+    """A wave a tile, eight values of a head a thread, less than 2^32 threads a launch."""
+    most = (1 << 26) - 4
+    assert vsk.mx4_bytes(16 * most, 1) == most * (1024 + 256)
+    assert vsk.mx4_bytes(1, 1 << 30) == (1 << 23) * 1024 + (1 << 21) * 256
+    for rows, k in ((16 * most + 1, 1), (1 << 30, 1), (8192 * 16, 8192 * 128)):
+        assert vsk.mx4_bytes(rows, k) == 0, (rows, k)
+        assert _code(vsk.mx4_read, A, rows, k, 1 << 50, vsk.BF16, k) == "ARG"
+        assert _code(vsk.mx4_pack, A, B, rows, k, 1 << 50) == "ARG"
+        assert vsk.mx4_product_bytes(rows, 5, k) == 0 and vsk.mx4_product_bytes(5, rows, k) == 0
+    e = _engine()
+    for f in (e.kv4_write, e.kv4_read):
+        for n in ((1 << 28) - 8, (1 << 31) - 1):
+            assert _code(f, 0, B, n, W, Y) == "ARG", n
+    e.close()
