@@ -336,8 +336,9 @@ int vsk_kv_evict(vsk_handle* h, const int64_t* dst_host, const int64_t* src_host
  * 16 x 128).  It is either an activation (rows are the batch's) or a weight matrix
  * [out][in].  These calls need no handle; VSK_E_ARG on a null pointer, a bad
  * shape, type, stride (elements from row to row, at least a row) or alignment (to
- * the element), or buffers that overlap.  Rows that are 16-byte aligned with k a
- * multiple of 32 are taken with wide loads. */
+ * the element), or buffers that overlap.  Rows whose base and stride are multiples of
+ * 16 bytes, with k a multiple of 8, are the fastest (up to four such rows of up to
+ * 6,144 columns are quantised and multiplied in one launch). */
 size_t vsk_mx4_bytes(int32_t rows, int32_t k);
 /* Quantise src_dev [rows][k] of VSK_BF16 or VSK_FP32. */
 int vsk_mx4_quantise(const void* src_dev, int32_t dtype, int64_t stride, int32_t rows, int32_t k, void* mx_dev,
@@ -371,8 +372,10 @@ size_t vsk_kv4_pool_bytes(const vsk_model_cfg* cfg, int32_t n_blocks);
  * vsk_kv_init unbinds it too). */
 int vsk_kv4_init(vsk_handle* h, void* pool_dev, size_t bytes);
 /* As vsk_kv_write and vsk_kv_read: logical bf16 k, v [n][n_kv_heads][head_dim] are
- * quantised into their slots / the values that slots stand for.  (n + 8) * n_kv_heads *
- * head_dim is at most 2^35 - 4096 (VSK_E_ARG); vsk_qkv_norm_rope's rows and heads too. */
+ * quantised into their slots / the values that slots stand for.  Slots of one write are
+ * different ones (of a slot given twice, codes and exponents may be from either).  (n +
+ * 8) * n_kv_heads * head_dim is at most 2^35 - 4096 (VSK_E_ARG); vsk_qkv_norm_rope's
+ * rows and heads too. */
 int vsk_kv4_write(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_t n, const void* k_dev,
                   const void* v_dev, void* stream);
 int vsk_kv4_read(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_t n, void* k_dev, void* v_dev,
@@ -382,12 +385,14 @@ int vsk_kv4_read(vsk_handle* h, int32_t layer, const int32_t* slots_dev, int32_t
  * of the largest of its 32 dims may not.  In the product with v a
  * weight is rounded to 16 bits for single tokens; for the rows of longer runs to the
  * 11 bits of fp16 where that holds all values of a block of 16 tokens exactly (the
- * exponents of 32 values between 2^-23 and 2^13), to 16 bits elsewhere. */
+ * exponents of 32 values between 2^-23 and 2^13; 32 zeros have 2^-127), to 16 bits
+ * elsewhere.  Slots behind the last of the rows count for neither. */
 int vsk_kv4_attend(vsk_handle* h, int32_t layer, const void* q_dev, void* o_dev, int32_t window, int32_t sinks,
                    void* ws_dev, size_t ws_bytes, void* stream);
 
 /* Rotary table of vsk_qkv_norm_rope, in caller-owned device memory (256-byte
- * aligned, vsk_rope_bytes), filled by a launch on the stream. */
+ * aligned, vsk_rope_bytes), filled by a launch on the stream, for which the call does
+ * not wait: vsk_qkv_norm_rope on another stream is the caller's to order behind it. */
 size_t vsk_rope_bytes(const vsk_handle* h);
 int vsk_rope_bind(vsk_handle* h, void* table_dev, size_t bytes, void* stream);
 /* From a QKV projection's rows to attention's inputs, for the rows of the uploaded

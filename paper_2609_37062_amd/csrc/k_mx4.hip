@@ -367,8 +367,9 @@ hipError_t launch_mx4_stream(const Mx4ProductArgs& a, hipStream_t s) {
 // every eighth two of its K's steps each; x comes from the caches.  Two steps' tiles
 // are in flight while the two before are used (see k_mx4_stream).  What x is read for
 // each 16 columns sets the time of many rows (77 x 4096 x 14336: 143 MB), so NT is 2
-// there, and K cut over two workgroups where the columns are then too few; the one
-// that arrives last adds the sums, as in k_mx4_tile.
+// there, and K cut over workgroups where the columns are then too few (mx4_split); the
+// one that arrives last adds the sums, as in k_mx4_tile.  (Eight row groups of two tiles
+// do not fit the registers: of 63 spilled ones some are in the loop.)
 template <int RG, int NT>
 __global__ __launch_bounds__(64 * kMxWaves, 2) void k_mx4_rows(Mx4ProductArgs a, Mx4Split sp) {
   constexpr int U = RG * NT;

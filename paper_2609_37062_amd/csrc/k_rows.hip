@@ -102,7 +102,10 @@ struct RowsLds {
 // behind the whole step; priorities for the wave that has matrix instructions: none).
 // What bounds it is not one unit: the matrix cores are busy 38% of the cycles, LDS 21%,
 // the vector units about half, and a wave waits 28% of its time, for the barrier of a
-// step and the operands behind it; two waves a SIMD overlap the rest only in part.
+// step and the operands behind it; two waves a SIMD overlap the rest only in part.  At
+// head_dim 128 some 20 registers are in scratch, which the masked and the rescaled steps
+// reload (a window of a few hundred keys is mostly those); the loop of whole steps does
+// not.
 template <int D, int NH, bool Q4>
 __global__ __launch_bounds__(256 * NH, 2) void k_attn_rows(AttnPrefillArgs a) {
   constexpr int T = 256 * NH;
